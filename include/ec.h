@@ -13,7 +13,9 @@
  *
  * plus variants of each (importance on top of cached rows or from a known log-sum-exp,
  * shared populations and eviction-only compaction, a native multi-step decode loop, the
- * retention-ratio policy, host-resident tensors, a decode step with built-in scratch).
+ * retention-ratio policy, host-resident tensors, a decode step with built-in scratch), and a
+ * paged cache with grouped query heads whose eviction goes by the attention weight that every
+ * row has gathered (ec_paged_*).
  *
  * Conventions shared by every call
  *  - Pointers named "dev" are CUDA device pointers of the current device; "host" pointers
@@ -53,7 +55,8 @@ typedef enum {
     EC_ERR_WORKSPACE = 5, /* workspace missing or smaller than the query reports         */
     EC_ERR_CUDA = 6,      /* a CUDA runtime call failed (launch error, no device, ...)   */
     EC_ERR_TIMEOUT = 7,   /* a bounded device-side wait expired (see ec_device_status)   */
-    EC_ERR_TOO_LARGE = 8  /* the problem does not fit the library's built-in scratch      */
+    EC_ERR_TOO_LARGE = 8, /* the problem does not fit the library's built-in scratch      */
+    EC_ERR_PAGE = 9       /* a page-table entry or a length is out of range               */
 } ec_status;
 
 /* Static description of a status code; never NULL. */
@@ -168,7 +171,8 @@ int ec_prefill_attention(const void *Q_dev, const void *K_dev, const void *V_dev
 /*
  * Synchronises `stream` and reports what the kernels recorded in the workspace's status
  * word: EC_OK, or EC_ERR_TIMEOUT if a bounded wait inside a kernel gave up (outputs are
- * then undefined but no out-of-bounds access happened). EC_ERR_CUDA on a runtime error.
+ * then undefined but no out-of-bounds access happened). The same for the state block of a
+ * paged cache, whose kernels report EC_ERR_PAGE. EC_ERR_CUDA on a runtime error.
  */
 int ec_device_status(void *ws_dev, void *stream);
 
@@ -462,6 +466,126 @@ size_t ec_decode_noalloc_capacity(void);
 int ec_decode_step_noalloc(const void *q_dev, const void *k_new_dev, const void *v_new_dev,
                            ec_cache *c, float scale, void *out_dev,
                            int *evicted_slot_host, int *slot_written_host, void *stream);
+
+/* ---------------------------------------------------------------- paged cache -------- */
+
+/*
+ * A cache in pages: the rows of N independent problems (sequences x layers folded), H key / value
+ * heads each, with a length of its own per problem, in fixed-size pages of a shared pool. Beside K
+ * and V, every row of every head carries the attention weight it has gathered so far and the
+ * position of the token it came from. Rows of a problem have no order (attention needs none):
+ * eviction fills holes, and "first" and "newest" go by position.
+ *
+ *   problem n's row j (0 <= j < lens[n]) of every head lies in page table[n][j / page_size], slot
+ *   j % page_size. Different heads may hold different tokens at the same row.
+ *
+ * The struct is plain host data; the arrays are the caller's, on the device. Lengths live on the
+ * device too, so that a captured step can be replayed. A negative length marks an empty place of a
+ * padded batch: its outputs are zero and nothing of it is changed. Entries of the table that no row
+ * reaches are not read.
+ *
+ * A table entry outside [0, n_pages) or a length beyond max_pages * page_size is never followed:
+ * the row counts as absent, and the status word at the head of `state` says EC_ERR_PAGE from then on
+ * (ec_device_status(state, stream); ec_paged_init clears it). ec_paged_check looks a host copy over
+ * before that happens.
+ *
+ * Calls that change a cache (append, attention that gathers weights, steps) are ordered by the
+ * caller: one stream, or events. Pages may be shared between problems only while nothing appends to
+ * or gathers weights in them.
+ */
+typedef enum { EC_BF16 = 0, EC_FP16 = 1 } ec_dtype;
+
+typedef struct {
+    void *Kp, *Vp;       /* device, 2-byte elements of `dtype`: [n_pages, H, page_size, D] by strides  */
+    float *weight;       /* device fp32 [n_pages, H, page_size]: attention weight gathered per row     */
+    int32_t *pos;        /* device int32 [n_pages, H, page_size]: position of the row's token          */
+    int32_t *table;      /* device int32 [N, max_pages]                                                */
+    int32_t *lens;       /* device int32 [N]: rows held, < 0 = empty place                             */
+    int32_t *seen;       /* device int32 [N]: tokens seen so far = position of the next token          */
+    void *state;         /* device, ec_paged_state_bytes(N), 256-byte aligned                          */
+    int N, H, D;         /* D is 64 or 128                                                             */
+    int page_size, n_pages, max_pages;
+    int dtype;           /* ec_dtype                                                                   */
+    int64_t page_stride, head_stride, row_stride;   /* of Kp and Vp, in elements, multiples of 8       */
+} ec_paged;
+
+/* Bytes of the device block `state` for N problems (0 when N < 1). */
+size_t ec_paged_state_bytes(int N);
+
+/*
+ * Fills *c after validating, and enqueues the clearing of `state` on `stream`. Limits: N*H < 2^24,
+ * n_pages*H*page_size < 2^31, N*max_pages < 2^31, max_pages*page_size < 2^30, and each pool's last row
+ * less than 64 GiB from its base. Strides are positive and keep rows apart (row_stride >= D).
+ */
+int ec_paged_init(ec_paged *c, void *Kp_dev, void *Vp_dev, float *weight_dev, int32_t *pos_dev, int32_t *table_dev,
+                  int32_t *lens_dev, int32_t *seen_dev, void *state_dev, int N, int H, int D, int page_size, int n_pages,
+                  int max_pages, int dtype, int64_t page_stride, int64_t head_stride, int64_t row_stride, void *stream);
+
+/*
+ * Looks over a host copy of the table and the lengths, for a cache that may grow to `rows` rows per
+ * problem (0: only what the lengths say): EC_ERR_PAGE when a length or an entry that rows reach is out
+ * of range or a page serves two places. Host arithmetic only; empty places (length < 0) are skipped.
+ */
+int ec_paged_check(const ec_paged *c, const int32_t *table_host, const int32_t *lens_host, int rows);
+
+/*
+ * Attention of one new token per problem over its cached rows and, when k_new is given, its own row:
+ *   x[g][j] = scale * <q_g, k_j>,  p[g] = softmax_j x[g],  out_g = sum_j p[g][j] * v_j
+ * for the Hq / H query heads g of every key / value head (query head i reads key / value head
+ * i / (Hq / H)). With accumulate != 0 every cached row's weight takes part in the decision what to
+ * evict later: weight_j <- decay * weight_j + sum over the group's heads of p[g][j] (decay = 1: the sum
+ * of all attention received; smaller: a moving average up to a factor). Nothing else of the cache
+ * changes: the new row joins with ec_paged_append.
+ *   q_dev                 [N, Hq, D], elements of c->dtype                                  (in)
+ *   k_new_dev, v_new_dev  [N, H, D]; both NULL: the cached rows alone                       (in)
+ *   out_dev               [N, Hq, D]; fp32 accumulation, probabilities rounded to the element type
+ *                         before they meet V, one rounding of the result. Zero where no row is
+ *                         left (an empty place, length 0 without a new row, all scores -inf)  (out)
+ *   lse_dev               fp32 [N, Hq], natural log-sum-exp (-inf where no row is left); nullable
+ *   w_new_dev             fp32 [N, H], the new row's share of the group's probability; required
+ *                         with accumulate and k_new, else NULL                               (out)
+ *   decay                 0 < decay <= 1, read with accumulate
+ * Limits: Hq a multiple of H, Hq / H <= 128, N*Hq < 2^24. Workspace: ec_paged_attention_workspace
+ * bytes (0 on invalid arguments); its contents need not survive between calls. Deterministic.
+ */
+size_t ec_paged_attention_workspace(const ec_paged *c, int Hq, int accumulate);
+int ec_paged_attention(const void *q_dev, const void *k_new_dev, const void *v_new_dev, const ec_paged *c, int Hq,
+                       float scale, int accumulate, float decay, void *out_dev, float *lse_dev, float *w_new_dev,
+                       void *ws_dev, size_t ws_bytes, void *stream);
+
+/*
+ * New rows join the cache, and eviction by gathered weight keeps every problem within `budget` rows.
+ * Candidates of a head are its cached rows, in row order, then the problem's new rows; F =
+ * min(lens[n] + new, budget) of them stay: rows at positions below `sinks` or among the newest
+ * `recent` ones first, then by weight (equal weights: the lower candidate stays; NaN counts as
+ * largest). Cached rows that stay below row F do not move; the holes below F take, in ascending order, the
+ * staying rows from behind F and then the staying new rows. lens[n] becomes F, seen[n] grows by the new
+ * rows. What the merging cache does by position (fixed truncation location), this does by weight.
+ *   K_new_dev, V_new_dev  [N, H, T, D], elements of c->dtype; NULL when T = 0 (eviction alone)  (in)
+ *   w_new_dev             fp32 [N, H, T] weights of the new rows (for a prompt: the scores of
+ *                         ec_importance / ec_prefill_attention); NULL: zero                     (in)
+ *   pos_new_dev           int32 [N, H, T] positions of the new rows; NULL: seen[n] + t          (in)
+ *   counts_dev            int32 [N] new rows of every problem, 0..T (clamped); NULL: T          (in)
+ *   fresh                 != 0: the problems start anew, their lengths and tokens seen count as 0
+ *   budget                1 .. max_pages*page_size;  recent, sinks >= 0, recent + sinks <= budget
+ * Pages need room for `budget` rows. Inputs must not overlap the pool. Workspace:
+ * ec_paged_append_workspace(c, T, budget) bytes (0 on invalid arguments). Deterministic.
+ */
+size_t ec_paged_append_workspace(const ec_paged *c, int T, int budget);
+int ec_paged_append(const void *K_new_dev, const void *V_new_dev, const float *w_new_dev, const int32_t *pos_new_dev,
+                    const int32_t *counts_dev, const ec_paged *c, int T, int fresh, int budget, int recent, int sinks,
+                    void *ws_dev, size_t ws_bytes, void *stream);
+
+/*
+ * One generation step on a paged cache: ec_paged_attention with the weights gathered, then
+ * ec_paged_append of the step's own row with the weight it received. recent >= 1 keeps the new row.
+ * Nothing is read back to the host, so the call can be captured once and replayed for every token.
+ * Arguments as in those two calls; lse_dev nullable. Workspace: ec_paged_step_workspace.
+ */
+size_t ec_paged_step_workspace(const ec_paged *c, int Hq, int budget);
+int ec_paged_decode_step(const void *q_dev, const void *k_new_dev, const void *v_new_dev, const ec_paged *c, int Hq,
+                         float scale, float decay, int budget, int recent, int sinks, void *out_dev, float *lse_dev,
+                         void *ws_dev, size_t ws_bytes, void *stream);
 
 #ifdef __cplusplus
 }

@@ -17,7 +17,8 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libec.so")
 
 EC_OK, EC_ERR_NULL, EC_ERR_SHAPE, EC_ERR_ALIGN, EC_ERR_ARG = 0, 1, 2, 3, 4
-EC_ERR_WORKSPACE, EC_ERR_CUDA, EC_ERR_TIMEOUT, EC_ERR_TOO_LARGE = 5, 6, 7, 8
+EC_ERR_WORKSPACE, EC_ERR_CUDA, EC_ERR_TIMEOUT, EC_ERR_TOO_LARGE, EC_ERR_PAGE = 5, 6, 7, 8, 9
+EC_BF16, EC_FP16 = 0, 1
 EC_PER_HEAD = 0
 EC_STAT_SUM, EC_STAT_MEAN, EC_STAT_MAX, EC_STAT_MOVING_AVERAGE = 0, 1, 2, 3
 EC_LAYER_SHARED = 1
@@ -29,6 +30,8 @@ EXPORTS = (
     "ec_cache_init", "ec_cache_init_ratio", "ec_cache_track_order", "ec_cache_concat", "ec_decode_workspace", "ec_decode_step", "ec_decode_steps",
     "ec_decode_noalloc_capacity", "ec_decode_step_noalloc", "ec_compress_host", "ec_decode_steps_host",
     "ec_probe_read_stream", "ec_probe_mixed_stream", "ec_decode_splits",
+    "ec_paged_state_bytes", "ec_paged_init", "ec_paged_check", "ec_paged_attention_workspace", "ec_paged_attention",
+    "ec_paged_append_workspace", "ec_paged_append", "ec_paged_step_workspace", "ec_paged_decode_step",
 )
 
 
@@ -47,6 +50,15 @@ class ec_cache(C.Structure):
                 ("policy", C.c_int), ("recent_head", C.c_int), ("keep_ratio", C.c_double),
                 ("n_tot", C.c_int64), ("recent_slots_host", C.POINTER(C.c_int)),
                 ("queue_slots_host", C.POINTER(C.c_int))]
+
+
+class ec_paged(C.Structure):
+    """Mirror of the C struct ec_paged (host-side plain data; the arrays are device tensors)."""
+    _fields_ = [("Kp", C.c_void_p), ("Vp", C.c_void_p), ("weight", C.c_void_p), ("pos", C.c_void_p),
+                ("table", C.c_void_p), ("lens", C.c_void_p), ("seen", C.c_void_p), ("state", C.c_void_p),
+                ("N", C.c_int), ("H", C.c_int), ("D", C.c_int),
+                ("page_size", C.c_int), ("n_pages", C.c_int), ("max_pages", C.c_int), ("dtype", C.c_int),
+                ("page_stride", C.c_int64), ("head_stride", C.c_int64), ("row_stride", C.c_int64)]
 
 
 _lib = None
@@ -119,6 +131,25 @@ def lib() -> C.CDLL:
     L.ec_probe_mixed_stream.argtypes = [vp, sz, vp, i, vp, vp]
     L.ec_decode_splits.restype = i
     L.ec_decode_splits.argtypes = [C.POINTER(ec_cache)]
+    pc, i64 = C.POINTER(ec_paged), C.c_int64
+    L.ec_paged_state_bytes.restype = sz
+    L.ec_paged_state_bytes.argtypes = [i]
+    L.ec_paged_init.restype = i
+    L.ec_paged_init.argtypes = [pc] + [vp] * 8 + [i] * 7 + [i64] * 3 + [vp]
+    L.ec_paged_check.restype = i
+    L.ec_paged_check.argtypes = [pc, vp, vp, i]
+    L.ec_paged_attention_workspace.restype = sz
+    L.ec_paged_attention_workspace.argtypes = [pc, i, i]
+    L.ec_paged_attention.restype = i
+    L.ec_paged_attention.argtypes = [vp, vp, vp, pc, i, f, i, f, vp, vp, vp, vp, sz, vp]
+    L.ec_paged_append_workspace.restype = sz
+    L.ec_paged_append_workspace.argtypes = [pc, i, i]
+    L.ec_paged_append.restype = i
+    L.ec_paged_append.argtypes = [vp, vp, vp, vp, vp, pc, i, i, i, i, i, vp, sz, vp]
+    L.ec_paged_step_workspace.restype = sz
+    L.ec_paged_step_workspace.argtypes = [pc, i, i]
+    L.ec_paged_decode_step.restype = i
+    L.ec_paged_decode_step.argtypes = [vp, vp, vp, pc, i, f, f, i, i, i, vp, vp, vp, sz, vp]
     _lib = L
     return L
 
@@ -387,3 +418,132 @@ def ec_probe_mixed_stream(buf: torch.Tensor, dst: torch.Tensor, write_every: int
 
 def ec_decode_splits(cache: ec_cache) -> int:
     return int(lib().ec_decode_splits(C.byref(cache)))
+
+
+# ---- paged cache -------------------------------------------------------------------------
+
+_ELEM = {torch.bfloat16: EC_BF16, torch.float16: EC_FP16}
+
+
+def _want(t: Optional[torch.Tensor], name: str, dtype: torch.dtype, shape, device: int) -> Optional[int]:
+    """Device pointer of an argument after checking type, shape, layout and device (None stays None)."""
+    if t is None:
+        return None
+    if t.dtype != dtype or tuple(t.shape) != shape:
+        raise ValueError(f"{name} must be {dtype} {list(shape)}, got {t.dtype} {list(t.shape)}")
+    if not t.is_cuda or t.device.index != device:
+        raise ValueError(f"{name} must be on the cache's device")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+def _paged_stream(cache: ec_paged) -> int:
+    """The current stream; the cache's device has to be the current one, as the kernels launch there."""
+    if torch.cuda.current_device() != cache._device:
+        raise ValueError("the cache's device is not the current CUDA device")
+    return torch.cuda.current_stream().cuda_stream
+
+
+def ec_paged_state_bytes(N: int) -> int:
+    return int(lib().ec_paged_state_bytes(int(N)))
+
+
+def ec_paged_init(Kp: torch.Tensor, Vp: torch.Tensor, weight: torch.Tensor, pos: torch.Tensor, table: torch.Tensor,
+                  lens: torch.Tensor, seen: torch.Tensor, state: torch.Tensor) -> ec_paged:
+    """Describe a paged cache. Kp, Vp: bf16 or fp16 [n_pages,H,page_size,D], any strides with D contiguous, the same
+    for both; weight fp32, pos int32 [n_pages,H,page_size]; table int32 [N,max_pages]; lens, seen int32 [N];
+    state: uint8 [ec_paged_state_bytes(N)], cleared here. The returned object keeps the tensors alive."""
+    if Kp.dim() != 4 or Kp.shape != Vp.shape or Kp.dtype != Vp.dtype or Kp.stride() != Vp.stride() or Kp.dtype not in _ELEM:
+        raise ValueError("Kp and Vp must be bf16 or fp16 [n_pages, H, page_size, D] of one layout")
+    if Kp.stride(3) != 1 or not Kp.is_cuda or Kp.device != Vp.device or table.dim() != 2:
+        raise ValueError("rows must be contiguous along D, on one CUDA device; table must be [N, max_pages]")
+    n_pages, H, page_size, D = Kp.shape
+    N, max_pages = table.shape
+    dev = Kp.device.index
+    c = ec_paged()
+    c._device = dev
+    c._tensors = (Kp, Vp, weight, pos, table, lens, seen, state)
+    c._dtype = Kp.dtype
+    rows = (n_pages, H, page_size)
+    if state.numel() * state.element_size() < ec_paged_state_bytes(N) or not state.is_contiguous() or state.device != Kp.device:
+        raise ValueError("state must hold ec_paged_state_bytes(N) bytes on the cache's device")
+    # a stride along an axis of extent 1 is never used: a dense one stands in for whatever the view says
+    ps, hs, rs = Kp.stride(0), Kp.stride(1), Kp.stride(2)
+    rs = rs if page_size > 1 else D
+    hs = hs if H > 1 else D
+    ps = ps if n_pages > 1 else D
+    st = lib().ec_paged_init(C.byref(c), Kp.data_ptr(), Vp.data_ptr(), _want(weight, "weight", torch.float32, rows, dev),
+                             _want(pos, "pos", torch.int32, rows, dev), _want(table, "table", torch.int32, (N, max_pages), dev),
+                             _want(lens, "lens", torch.int32, (N,), dev), _want(seen, "seen", torch.int32, (N,), dev),
+                             state.data_ptr(), N, H, D, page_size, n_pages, max_pages, _ELEM[Kp.dtype], ps, hs, rs,
+                             _paged_stream(c))
+    _check(st, "ec_paged_init")
+    return c
+
+
+def ec_paged_check(cache: ec_paged, table_host: torch.Tensor, lens_host: torch.Tensor, rows: int = 0) -> None:
+    """Raises EcError (EC_ERR_PAGE) when a host copy of the table and the lengths points outside the pool or uses a
+    page twice, for problems of up to `rows` rows (0: the lengths as they are)."""
+    if table_host.dtype != torch.int32 or lens_host.dtype != torch.int32 or tuple(table_host.shape) != (cache.N, cache.max_pages) \
+            or tuple(lens_host.shape) != (cache.N,):
+        raise ValueError("table must be int32 [N, max_pages] and lens int32 [N]")
+    _check(lib().ec_paged_check(C.byref(cache), _host_ptr(table_host), _host_ptr(lens_host), int(rows)), "ec_paged_check")
+
+
+def ec_paged_attention_workspace(cache: ec_paged, Hq: int, accumulate: bool) -> int:
+    return int(lib().ec_paged_attention_workspace(C.byref(cache), int(Hq), int(bool(accumulate))))
+
+
+def ec_paged_attention(q: torch.Tensor, k_new: Optional[torch.Tensor], v_new: Optional[torch.Tensor], cache: ec_paged,
+                       scale: float, accumulate: bool, decay: float, out: torch.Tensor, lse: Optional[torch.Tensor],
+                       w_new: Optional[torch.Tensor], ws: torch.Tensor) -> None:
+    """Attention of one new token per problem over its paged rows and its own row. q, out (out): [N,Hq,D]; k_new,
+    v_new: [N,H,D], both None for the cached rows alone; lse (out, optional): fp32 [N,Hq]. accumulate: every cached
+    row's weight becomes decay * weight + the group's probability, and w_new (out) fp32 [N,H] is the new row's."""
+    N, H, D, dt, dev = cache.N, cache.H, cache.D, cache._dtype, cache._device
+    Hq = q.shape[1]
+    st = lib().ec_paged_attention(_want(q, "q", dt, (N, Hq, D), dev), _want(k_new, "k_new", dt, (N, H, D), dev),
+                                  _want(v_new, "v_new", dt, (N, H, D), dev), C.byref(cache), Hq, scale, int(bool(accumulate)),
+                                  decay, _want(out, "out", dt, (N, Hq, D), dev), _want(lse, "lse", torch.float32, (N, Hq), dev),
+                                  _want(w_new, "w_new", torch.float32, (N, H), dev), _ptr(ws),
+                                  ws.numel() * ws.element_size(), _paged_stream(cache))
+    _check(st, "ec_paged_attention")
+
+
+def ec_paged_append_workspace(cache: ec_paged, T: int, budget: int) -> int:
+    return int(lib().ec_paged_append_workspace(C.byref(cache), int(T), int(budget)))
+
+
+def ec_paged_append(K_new: Optional[torch.Tensor], V_new: Optional[torch.Tensor], w_new: Optional[torch.Tensor],
+                    pos_new: Optional[torch.Tensor], counts: Optional[torch.Tensor], cache: ec_paged, fresh: bool,
+                    budget: int, recent: int, sinks: int, ws: torch.Tensor) -> None:
+    """T new rows per problem join the cache, each head then keeps its `budget` rows of largest weight. K_new, V_new:
+    [N,H,T,D] (None: eviction alone); w_new fp32, pos_new int32 [N,H,T] and counts int32 [N] are optional."""
+    N, H, D, dt, dev = cache.N, cache.H, cache.D, cache._dtype, cache._device
+    T = 0 if K_new is None else K_new.shape[2]
+    st = lib().ec_paged_append(_want(K_new, "K_new", dt, (N, H, T, D), dev), _want(V_new, "V_new", dt, (N, H, T, D), dev),
+                               _want(w_new, "w_new", torch.float32, (N, H, T), dev),
+                               _want(pos_new, "pos_new", torch.int32, (N, H, T), dev),
+                               _want(counts, "counts", torch.int32, (N,), dev), C.byref(cache), T, int(bool(fresh)), int(budget),
+                               int(recent), int(sinks), _ptr(ws), ws.numel() * ws.element_size(), _paged_stream(cache))
+    _check(st, "ec_paged_append")
+
+
+def ec_paged_step_workspace(cache: ec_paged, Hq: int, budget: int) -> int:
+    return int(lib().ec_paged_step_workspace(C.byref(cache), int(Hq), int(budget)))
+
+
+def ec_paged_decode_step(q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor, cache: ec_paged, scale: float, decay: float,
+                         budget: int, recent: int, sinks: int, out: torch.Tensor, lse: Optional[torch.Tensor],
+                         ws: torch.Tensor) -> None:
+    """One generation step on a paged cache: attention with the weights gathered, then the step's row joins and the
+    heads above `budget` rows evict by weight. Nothing comes back to the host: the call can be captured and replayed."""
+    N, H, D, dt, dev = cache.N, cache.H, cache.D, cache._dtype, cache._device
+    Hq = q.shape[1]
+    st = lib().ec_paged_decode_step(_want(q, "q", dt, (N, Hq, D), dev), _want(k_new, "k_new", dt, (N, H, D), dev),
+                                    _want(v_new, "v_new", dt, (N, H, D), dev), C.byref(cache), Hq, scale, decay, int(budget),
+                                    int(recent), int(sinks), _want(out, "out", dt, (N, Hq, D), dev),
+                                    _want(lse, "lse", torch.float32, (N, Hq), dev), _ptr(ws),
+                                    ws.numel() * ws.element_size(), _paged_stream(cache))
+    _check(st, "ec_paged_decode_step")

@@ -99,6 +99,7 @@ const char *ec_status_string(int status)
     case EC_ERR_CUDA: return "CUDA runtime error";
     case EC_ERR_TIMEOUT: return "device-side wait timed out";
     case EC_ERR_TOO_LARGE: return "problem too large for the built-in scratch";
+    case EC_ERR_PAGE: return "page-table entry or length out of range";
     default: return "unknown status";
     }
 }
@@ -209,7 +210,7 @@ int ec_device_status(void *ws, void *stream)
     cudaError_t e = cudaMemcpyAsync(&word, ws, sizeof word, cudaMemcpyDeviceToHost, (cudaStream_t)stream);
     if (e == cudaSuccess) e = cudaStreamSynchronize((cudaStream_t)stream);
     if (e != cudaSuccess) return EC_ERR_CUDA;
-    return word == 0 ? EC_OK : EC_ERR_TIMEOUT;
+    return word == 0 ? EC_OK : word == ec::kStatusPage ? EC_ERR_PAGE : EC_ERR_TIMEOUT;
 }
 
 size_t ec_select_compact_workspace(int N, int H, int T, int D, int n_keep, int share)

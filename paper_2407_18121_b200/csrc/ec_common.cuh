@@ -21,6 +21,7 @@ struct NvtxRange {
 };
 
 constexpr int kStatusBytes = 256;   // status block at the head of an importance workspace
+constexpr int kStatusPage = 2;      // status word of a paged cache: a length or page-table entry is out of range
 
 __device__ __forceinline__ float bf16lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }

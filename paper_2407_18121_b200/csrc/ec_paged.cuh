@@ -1,0 +1,106 @@
+// What the kernels of the paged cache share: the cache as a kernel argument, the address arithmetic of its
+// pages and the packed element types.
+#pragma once
+
+#include "ec_common.cuh"
+
+#include <cuda_fp16.h>
+
+namespace ec {
+
+namespace {
+
+constexpr uint32_t kRowNone = 0xFFFFFFFFu;   // no row here: not read, no weight
+constexpr uint32_t kRowNew = 0xFFFFFFFEu;    // the step's own row, read from the call's inputs
+
+__device__ __forceinline__ void grid_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void grid_release() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
+// Kernel launch that may be placed while the previous kernel of the stream drains; every kernel launched
+// this way waits (grid_wait) before its first access to memory that an earlier kernel may write.
+template <typename... KArgs, typename... Args>
+cudaError_t launch_chained(void (*kernel)(KArgs...), dim3 grid, unsigned block, size_t smem, cudaStream_t stream, Args... args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(block);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
+}
+
+}  // namespace
+
+// The cache as the kernels take it. Offsets of rows are counted in 16-byte units, in 32 bits: the host refuses
+// pools that reach past 2^32 - 2 of them (64 GiB for K and as much for V).
+struct PagedView {
+    uint4 *K, *V;
+    float *weight;
+    int *pos;
+    const int *table;
+    int *lens, *seen;
+    int *state;                                  // [0]: status word; from int 64 on: arrival counters, one per problem
+    int N, H, page_size, n_pages, max_pages;
+    uint32_t page_step, head_step, row_step;     // strides in 16-byte units
+};
+
+namespace {
+
+struct Slot {
+    int page, slot;        // page < 0: the table has no valid page here
+};
+
+__device__ __forceinline__ Slot find_slot(const PagedView &c, int n, int row)
+{
+    const int p = row / c.page_size;
+    Slot s;
+    s.slot = row - p * c.page_size;
+    s.page = c.table[(size_t)n * c.max_pages + p];
+    if ((unsigned)s.page >= (unsigned)c.n_pages) {
+        s.page = -1;
+        atomicExch(c.state, kStatusPage);
+    }
+    return s;
+}
+
+// Index of a row's weight and position; fits 32 bits (checked by the host).
+__device__ __forceinline__ uint32_t meta_index(const PagedView &c, int h, const Slot &s)
+{
+    return ((uint32_t)s.page * (uint32_t)c.H + (uint32_t)h) * (uint32_t)c.page_size + (uint32_t)s.slot;
+}
+
+// Offset of a row of head 0 in the pools, in 16-byte units.
+__device__ __forceinline__ uint32_t row_offset(const PagedView &c, const Slot &s)
+{
+    return (uint32_t)s.page * c.page_step + (uint32_t)s.slot * c.row_step;
+}
+
+// Valid rows of problem n: negative for an empty place; a length past the table's reach is cut and reported.
+__device__ __forceinline__ int read_len(const PagedView &c, int n)
+{
+    const int len = c.lens[n];
+    const long long cap = (long long)c.max_pages * c.page_size;
+    if (len > cap) {
+        atomicExch(c.state, kStatusPage);
+        return (int)cap;
+    }
+    return len;
+}
+
+}  // namespace
+
+size_t paged_attention_workspace_bytes(const ec_paged *c, int Hq, int accumulate);
+cudaError_t launch_paged_attention(const PagedView &c, int D, int dtype, const void *q, const void *k_new, const void *v_new,
+                                   int Hq, float scale, int accumulate, float decay, void *out, float *lse, float *w_new,
+                                   void *ws, cudaStream_t stream);
+size_t paged_append_workspace_bytes(const ec_paged *c, int T, int budget);
+cudaError_t launch_paged_append(const PagedView &c, int D, const void *K_new, const void *V_new, const float *w_new,
+                                const int *pos_new, const int *counts, int T, int fresh, int budget, int recent, int sinks,
+                                void *ws, cudaStream_t stream);
+
+}  // namespace ec

@@ -1,0 +1,338 @@
+"""The paged cache on the GPU against plain 64-bit forms: attention of one token with gathered weights, append with
+eviction by weight, whole steps."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paged_reference import PagedMirror, attention_bounds
+from paper_2407_18121_b200 import binding as ec
+
+pytestmark = pytest.mark.gpu
+BF, HF = torch.bfloat16, torch.float16
+
+
+def scratch(n):
+    return torch.full((max(int(n), 256),), 0xA5, dtype=torch.uint8, device="cuda")
+
+
+def rand(shape, dtype, seed):
+    return torch.randn(shape, generator=torch.Generator().manual_seed(seed)).to(dtype)
+
+
+def check_attention(m, G, new=True, accumulate=False, decay=1.0, scale=None, seed=1, q=None, drop=(), twice=True):
+    N, H, D, dt = m.N, m.H, m.D, m.dtype
+    scale = scale or 1.0 / math.sqrt(D)
+    q = rand((N, H * G, D), dt, seed) if q is None else q
+    k, v = (rand((N, H, D), dt, seed + 1), rand((N, H, D), dt, seed + 2)) if new else (None, None)
+    cache = m.cache(ec)
+    before = m.dev["weight"].clone()
+    m.weight = before.cpu().double()             # a call before this one left fp32 weights: the definition starts from those
+    old = m.weight.clone()
+    ref, mass, dx = m.attention(q, k, v, scale, accumulate, decay, drop)
+    up = lambda t: None if t is None else t.cuda()  # noqa: E731
+    ws = scratch(ec.ec_paged_attention_workspace(cache, H * G, accumulate))
+    results = []
+    for _ in range(2 if twice else 1):
+        m.dev["weight"].copy_(before)
+        out = torch.full((N, H * G, D), float("nan"), dtype=dt, device="cuda")
+        lse = torch.full((N, H * G), float("nan"), device="cuda")
+        w_new = torch.full((N, H), float("nan"), device="cuda") if accumulate and new else None
+        ec.ec_paged_attention(up(q), up(k), up(v), cache, scale, accumulate, decay, out, lse, w_new, ws)
+        torch.cuda.synchronize()
+        results.append([t.clone() for t in (out, lse, w_new, m.dev["weight"]) if t is not None])
+    if twice:
+        for a, b in zip(*results):
+            assert torch.equal(a.nan_to_num(77.0), b.nan_to_num(77.0)), "two runs differ"
+    out_tol, lse_tol, w_tol = attention_bounds(ref, mass, dx, dt, G)
+    got = out.cpu().double()
+    assert torch.isfinite(got).all()
+    over = (got - ref[0]).abs() - out_tol
+    assert (over <= 0).all(), f"out: {float(over.max()):.3g} over its tolerance"
+    got = lse.cpu().double()
+    empty = torch.isinf(ref[1])
+    assert torch.equal(torch.isinf(got), empty)
+    assert ((got - ref[1]).abs()[~empty] <= lse_tol[~empty]).all()
+    if accumulate:
+        # the row's old weight, its decay and the sum are rounded once each
+        held = torch.isfinite(old)
+        atol = w_tol + float(old[held].abs().max() if held.any() else 0.0) * 2.0 ** -22
+        m.assert_same_rows(atol, "weights")
+        if new:
+            assert ((w_new.cpu().double() - ref[2]).abs() <= w_tol).all()
+    else:
+        m.assert_same_rows(0.0, "cache")
+    if not drop:
+        assert ec.ec_device_status(state_of(cache)) == ec.EC_OK
+    return cache
+
+
+def state_of(cache):
+    return cache._tensors[-1]
+
+
+EDGE = [0, 1, 15, 16, 17, 63, 64, 65, 127, 128, 129, -1, 200]
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("dt", [BF, HF])
+@pytest.mark.parametrize("G", [1, 3, 8, 9, 16, 20])
+def test_attention_edges_of_length_and_group(G, dt, D):
+    check_attention(PagedMirror(EDGE, 2, D, 16, 208, dt, G=G), G, accumulate=True)
+
+
+@pytest.mark.parametrize("page", [1, 5, 16, 24, 64, 300])
+@pytest.mark.parametrize("rows", ["heads", "tokens"])
+def test_attention_pages_and_strides(page, rows):
+    check_attention(PagedMirror([257, 3, 100], 3, 128, page, 300, rows=rows), 4, accumulate=True)
+
+
+@pytest.mark.parametrize("new", [True, False])
+@pytest.mark.parametrize("accumulate", [True, False])
+@pytest.mark.parametrize("lens", [[0], [1], [0, 5, -1], [-1, -1], [700], [40, 3000, 9, 1500]])
+def test_attention_with_and_without_the_own_row(lens, accumulate, new):
+    check_attention(PagedMirror(lens, 2, 64, 32, 3008), 5, new=new, accumulate=accumulate)
+
+
+@pytest.mark.parametrize("N,H,G,L", [(64, 16, 1, 130), (300, 4, 2, 70), (1, 1, 4, 20000), (3, 40, 1, 1000)])
+def test_attention_many_units_and_long_rows(N, H, G, L):
+    lens = [max(1, (L * (n % 7 + 1)) // 7) for n in range(N)]
+    check_attention(PagedMirror(lens, H, 64, 64, L), G, accumulate=True, decay=0.75)
+
+
+def test_attention_weights_decay():
+    check_attention(PagedMirror([90, 400], 2, 128, 16, 400), 3, accumulate=True, decay=0.5)
+
+
+def test_attention_rows_whose_score_is_minus_infinity():
+    m = PagedMirror([100, 40], 2, 64, 16, 112)
+    q = rand((2, 4, 64), BF, 3).abs() + 0.1
+    p, s = m.where(0, 100)
+    for pool in (m.K, m.dev["K"]):
+        pool[p[10:90], :, s[10:90]] = -math.inf                       # every query sees -inf there
+    check_attention(m, 2, q=q, accumulate=True)
+    p, s = m.where(1, 40)
+    for pool in (m.K, m.dev["K"]):
+        pool[p, :, s] = -math.inf                                     # nothing but the own row is left of problem 1
+    check_attention(m, 2, q=q, accumulate=True)
+    check_attention(m, 2, q=q, new=False)                             # and here nothing at all
+
+
+def test_attention_peaked_rows_and_large_scores():
+    m = PagedMirror([900], 1, 128, 64, 960)
+    for pool in (m.K, m.dev["K"]):
+        for r, f in ((5, 4.0), (700, 9.0), (899, 16.0)):              # the running maximum rises late
+            p, s = m.where(0, 900)
+            pool[p[r], 0, s[r]] *= f
+    check_attention(m, 4, scale=0.5, accumulate=True)
+
+
+def test_attention_refuses_bad_pages_in_the_kernel():
+    m = PagedMirror([100, 60], 2, 64, 16, 112)
+    m.dev["table"][0, 2] = -1                                         # rows 32..47 of problem 0
+    m.dev["table"][1, 3] = 1 << 30                                    # rows 48..59 of problem 1
+    drop = {(0, j) for j in range(32, 48)} | {(1, j) for j in range(48, 60)}
+    cache = check_attention(m, 2, accumulate=True, drop=drop)
+    assert ec.ec_device_status(state_of(cache)) == ec.EC_ERR_PAGE
+    assert ec.ec_device_status(state_of(m.cache(ec))) == ec.EC_OK   # a new description starts clean
+
+
+# ---------------------------------------------------------------------------------------- append
+
+def check_append(m, T, budget, recent=0, sinks=0, w=None, pos=None, counts=None, fresh=False, seed=4):
+    N, H, D, dt = m.N, m.H, m.D, m.dtype
+    K, V = (rand((N, H, T, D), dt, seed), rand((N, H, T, D), dt, seed + 1)) if T else (None, None)
+    m.append(K, V, w, pos, counts, T, fresh, budget, recent, sinks)
+    cache = m.cache(ec)
+    up = lambda t: None if t is None else t.cuda()  # noqa: E731
+    ws = scratch(ec.ec_paged_append_workspace(cache, T, budget))
+    ec.ec_paged_append(up(K), up(V), up(w), up(pos), up(counts), cache, fresh, budget, recent, sinks, ws)
+    torch.cuda.synchronize()
+    m.assert_same_rows(0.0, "append")
+    assert ec.ec_device_status(state_of(cache)) == ec.EC_OK
+
+
+@pytest.mark.parametrize("T", [1, 3, 16, 17, 100])
+@pytest.mark.parametrize("dt,D,rows", [(BF, 128, "heads"), (HF, 64, "tokens")])
+def test_append_evicts_by_weight(T, dt, D, rows):
+    N, H = 6, 3
+    m = PagedMirror([120, 119, 60, 0, -1, 5], H, D, 16, 120, dt, rows)
+    w = torch.rand(N, H, T, generator=torch.Generator().manual_seed(9))
+    check_append(m, T, 120, recent=8, sinks=2, w=w)
+    check_append(m, T, 120, recent=min(T, 100), sinks=4, w=w, counts=torch.tensor([T, 0, T // 2, 1, T, T + 9], dtype=torch.int32))
+
+
+@pytest.mark.parametrize("kind", ["equal", "none", "coarse", "special"])
+@pytest.mark.parametrize("T", [2, 40])
+def test_append_equal_weights_and_special_values(kind, T):
+    N, H, L = 2, 2, 300
+    m = PagedMirror([L, L - 7], H, 64, 24, L)
+    g = torch.Generator().manual_seed(5)
+    w = None if kind == "none" else torch.randint(0, 3, (N, H, T), generator=g).float()
+    if kind == "equal":
+        w = torch.zeros(N, H, T)
+    if kind == "special":
+        w[:, :, 0], w[:, :, 1] = math.nan, -0.0
+    for n in range(N):
+        p, s = m.where(n, int(m.lens[n]))
+        fill = torch.randint(0, 3, (len(p), H), generator=g).float()
+        if kind == "equal":
+            fill.zero_()
+        if kind == "special":
+            fill[::5], fill[1::5], fill[2::7], fill[3::7] = math.inf, -math.inf, math.nan, -0.0
+        m.weight[p, :, s] = fill.double()
+        m.dev["weight"][p.cuda(), :, s.cuda()] = fill.cuda()
+    check_append(m, T, L - 50 if T == 40 else L, recent=2, w=w)
+
+
+@pytest.mark.parametrize("T", [0, 1, 30])
+def test_append_shrinks_to_a_smaller_budget(T):
+    m = PagedMirror([500, 64, 63, 10, 0], 2, 64, 16, 512)
+    check_append(m, T, 64, recent=10, sinks=3, w=torch.rand(5, 2, T) if T else None)
+
+
+@pytest.mark.parametrize("T,budget", [(640, 320), (1, 1), (7, 64), (1000, 1000), (5000, 100)])
+def test_append_fresh_prompts(T, budget):
+    N, H = 3, 2
+    m = PagedMirror([17, 0, -1], H, 64, 16, budget if budget > 32 else 32)
+    g = torch.Generator().manual_seed(T)
+    w = torch.exp(2 * torch.randn(N, H, T, generator=g))
+    w[w < 0.2] = 0.0
+    counts = torch.tensor([T, max(1, T // 3), T], dtype=torch.int32)
+    check_append(m, T, budget, recent=min(budget // 2, 16), sinks=min(budget // 4, 4), w=w, counts=counts, fresh=True)
+
+
+def test_append_given_positions_decide_what_is_protected():
+    N, H, T = 2, 2, 40
+    m = PagedMirror([90, 50], H, 64, 16, 96)
+    pos = torch.randint(0, 400, (N, H, T), generator=torch.Generator().manual_seed(3)).to(torch.int32)
+    check_append(m, T, 96, recent=20, sinks=30, w=torch.rand(N, H, T), pos=pos)
+
+
+def test_append_does_not_follow_bad_pages():
+    m = PagedMirror([40, 40], 1, 64, 16, 48)
+    good = {k: v.clone() for k, v in m.dev.items()}
+    m.dev["table"][1, 2] = 12345                                       # rows 32.. of problem 1
+    cache = m.cache(ec)
+    K = rand((2, 1, 4, 64), BF, 1).cuda()
+    ws = scratch(ec.ec_paged_append_workspace(cache, 4, 48))
+    ec.ec_paged_append(K, K, None, None, None, cache, False, 48, 4, 0, ws)
+    torch.cuda.synchronize()
+    assert ec.ec_device_status(state_of(cache)) == ec.EC_ERR_PAGE
+    p = m.table[1].long()
+    assert torch.equal(m.dev["K"][p].view(torch.int16), good["K"][p].view(torch.int16))   # nothing of problem 1 was written
+    assert m.dev["lens"].tolist() == [44, 44]
+
+
+# ---------------------------------------------------------------------------------------- whole steps
+
+def run_steps(m, G, steps, budget, recent, sinks, use_graph=False, stream=None):
+    N, H, D, dt = m.N, m.H, m.D, m.dtype
+    scale, Hq = 1.0 / math.sqrt(D), H * G
+    cache = m.cache(ec)
+    ws = scratch(ec.ec_paged_step_workspace(cache, Hq, budget))
+    q, k, v = (torch.empty(N, h, D, dtype=dt, device="cuda") for h in (Hq, H, H))
+    out = torch.empty(N, Hq, D, dtype=dt, device="cuda")
+    lse = torch.empty(N, Hq, device="cuda")
+    ctx = torch.cuda.stream(stream) if stream is not None else torch.cuda.stream(torch.cuda.current_stream())
+
+    def step():
+        ec.ec_paged_decode_step(q, k, v, cache, scale, 1.0, budget, recent, sinks, out, lse, ws)
+    torch.cuda.synchronize()
+    graph = None
+    with ctx:
+        for i in range(steps):
+            hq, hk, hv = rand((N, Hq, D), dt, 100 + i), rand((N, H, D), dt, 200 + i), rand((N, H, D), dt, 300 + i)
+            for dst, src in ((q, hq), (k, hk), (v, hv)):
+                dst.copy_(src)
+            out.fill_(float("nan"))
+            if use_graph:
+                if graph is None:
+                    torch.cuda.synchronize()
+                    graph = torch.cuda.CUDAGraph()
+                    with torch.cuda.graph(graph):
+                        step()
+                graph.replay()
+            else:
+                step()
+            torch.cuda.current_stream().synchronize()
+            ref, mass, dx = m.attention(hq, hk, hv, scale, True, 1.0)
+            out_tol, lse_tol, w_tol = attention_bounds(ref, mass, dx, dt, G)
+            m.append(hk[:, :, None], hv[:, :, None], ref[2][:, :, None], None, None, 1, False, budget, recent, sinks)
+            assert ((out.cpu().double() - ref[0]).abs() <= out_tol).all(), f"step {i}"
+            held = m.weight[torch.isfinite(m.weight)]
+            m.assert_same_rows((i + 1) * (w_tol + float(held.max()) * 2.0 ** -22), f"step {i}")
+    assert ec.ec_device_status(state_of(cache)) == ec.EC_OK
+
+
+@pytest.mark.parametrize("G,dt,D", [(1, BF, 128), (4, HF, 64), (12, BF, 64)])
+def test_steps_follow_the_definition(G, dt, D):
+    run_steps(PagedMirror([40, 37, 0, -1, 12], 2, D, 16, 40, dt, G=G, ranked=True), G, 12, 40, 14, 2)
+
+
+def test_steps_captured_once_and_replayed():
+    run_steps(PagedMirror([100, 97, -1], 2, 64, 16, 100, ranked=True, G=2), 2, 8, 100, 10, 1, use_graph=True)
+
+
+def test_steps_on_another_stream():
+    run_steps(PagedMirror([64, 20], 2, 64, 32, 64, ranked=True), 1, 4, 64, 8, 0, stream=torch.cuda.Stream())
+
+
+def test_two_caches_share_a_workspace_in_one_stream():
+    """Two captured steps of different caches over one workspace, replayed in turn, give what separate ones give."""
+    outs = []
+    for shared in (True, False):
+        ms = [PagedMirror([50, 33], 2, 64, 16, 64, seed=s) for s in (1, 2)]
+        caches = [m.cache(ec) for m in ms]
+        need = ec.ec_paged_step_workspace(caches[0], 4, 64)
+        one = scratch(need)
+        graphs, got = [], []
+        for i, c in enumerate(caches):
+            q, k, v = rand((2, 4, 64), BF, i).cuda(), rand((2, 2, 64), BF, 5 + i).cuda(), rand((2, 2, 64), BF, 7 + i).cuda()
+            out = torch.zeros(2, 4, 64, dtype=BF, device="cuda")
+            ws = one if shared else scratch(need)
+            torch.cuda.synchronize()
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g):
+                ec.ec_paged_decode_step(q, k, v, c, 0.125, 1.0, 64, 4, 0, out, None, ws)
+            graphs.append((g, q, k, v, ws))
+            got.append(out)
+        for _ in range(20):
+            for g, *_rest in graphs:
+                g.replay()
+        torch.cuda.synchronize()
+        outs.append([o.clone() for o in got] + [m.dev[x].clone() for m in ms for x in ("K", "weight", "pos", "lens")])
+    for a, b in zip(*outs):
+        assert torch.equal(a.nan_to_num(7.0) if a.is_floating_point() else a, b.nan_to_num(7.0) if b.is_floating_point() else b)
+
+
+def test_offsets_past_32_bits():
+    """Rows more than 2^32 bytes and 2^31 elements into the pool."""
+    H, D, page, n_pages = 4, 128, 128, 36000                           # 36000 * 4 * 128 * 128 elements = 4.7 GB a pool
+    K = torch.empty((n_pages, H, page, D), dtype=BF, device="cuda")
+    V = torch.empty_like(K)
+    table = torch.tensor([[n_pages - 1, 0, n_pages - 2]], dtype=torch.int32)
+    m = PagedMirror([300], H, D, page, 384)
+    for pool, small in ((K, m.dev["K"]), (V, m.dev["V"])):
+        pool[table[0].long().cuda()] = small[m.table[0].long().cuda()]
+    weight = torch.zeros((n_pages, H, page), device="cuda")
+    pos = torch.zeros((n_pages, H, page), dtype=torch.int32, device="cuda")
+    state = torch.empty(ec.ec_paged_state_bytes(1), dtype=torch.uint8, device="cuda")
+    big = ec.ec_paged_init(K, V, weight, pos, table.cuda(), m.dev["lens"], m.dev["seen"], state)
+    small = m.cache(ec)
+    q = rand((1, 8, D), BF, 1).cuda()
+    outs = []
+    for c in (small, big):
+        out = torch.empty_like(q)
+        ws = scratch(ec.ec_paged_attention_workspace(c, 8, False))
+        ec.ec_paged_attention(q, None, None, c, 0.1, False, 1.0, out, None, None, ws)
+        outs.append(out.clone())
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], outs[1])
+    one = rand((1, H, 1, D), BF, 4).cuda()
+    ws = scratch(ec.ec_paged_append_workspace(big, 1, 384))
+    ec.ec_paged_append(one, one, None, None, None, big, False, 384, 1, 0, ws)
+    torch.cuda.synchronize()
+    assert torch.equal(K[n_pages - 2, :, 300 - 256], one[0, :, 0]) and int(m.dev["lens"][0]) == 301
+    assert ec.ec_device_status(state) == ec.EC_OK
