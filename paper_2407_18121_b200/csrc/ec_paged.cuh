@@ -36,6 +36,12 @@ cudaError_t launch_chained(void (*kernel)(KArgs...), dim3 grid, unsigned block, 
 
 }  // namespace
 
+// CTAs of an attention launch at most, and where the arrival counters lie in the state block (in ints behind the
+// status word). Every counter is zero between launches: whoever arrives last puts it back.
+constexpr int kPagedMaxCtas = 148 * 2;
+constexpr int kStateAttention = 64;
+constexpr int kStateAppend = kStateAttention + kPagedMaxCtas;      // one per problem
+
 // The cache as the kernels take it. Offsets of rows are counted in 16-byte units, in 32 bits: the host refuses
 // pools that reach past 2^32 - 2 of them (64 GiB for K and as much for V).
 struct PagedView {
@@ -44,7 +50,7 @@ struct PagedView {
     int *pos;
     const int *table;
     int *lens, *seen;
-    int *state;                                  // [0]: status word; from int 64 on: arrival counters, one per problem
+    int *state;                                  // status word and arrival counters, see kState*
     int N, H, page_size, n_pages, max_pages;
     uint32_t page_step, head_step, row_step;     // strides in 16-byte units
 };

@@ -97,7 +97,7 @@ int check_ws(const void *ws, size_t have, size_t need)
 
 extern "C" {
 
-size_t ec_paged_state_bytes(int N) { return N < 1 ? 0 : ec::kStatusBytes + round256((size_t)N * sizeof(int)); }
+size_t ec_paged_state_bytes(int N) { return N < 1 ? 0 : round256((ec::kStateAppend + (size_t)N) * sizeof(int)); }
 
 int ec_paged_init(ec_paged *c, void *Kp, void *Vp, float *weight, int32_t *pos, int32_t *table, int32_t *lens, int32_t *seen,
                   void *state, int N, int H, int D, int page_size, int n_pages, int max_pages, int dtype, int64_t page_stride,
