@@ -538,14 +538,14 @@ int ec_paged_check(const ec_paged *c, const int32_t *table_host, const int32_t *
  * changes: the new row joins with ec_paged_append.
  *   q_dev                 [N, Hq, D], elements of c->dtype                                  (in)
  *   k_new_dev, v_new_dev  [N, H, D]; both NULL: the cached rows alone                       (in)
- *   out_dev               [N, Hq, D]; fp32 accumulation, probabilities rounded to the element type
- *                         before they meet V, one rounding of the result. Zero where no row is
- *                         left (an empty place, length 0 without a new row, all scores -inf)  (out)
+ *   out_dev               [N, Hq, D]; fp32 accumulation, one rounding of the result. Zero where no row
+ *                         is left (an empty place, length 0 without a new row, all scores -inf) (out)
  *   lse_dev               fp32 [N, Hq], natural log-sum-exp (-inf where no row is left); nullable
  *   w_new_dev             fp32 [N, H], the new row's share of the group's probability; required
  *                         with accumulate and k_new, else NULL                               (out)
  *   decay                 0 < decay <= 1, read with accumulate
- * Limits: Hq a multiple of H, Hq / H <= 128, N*Hq < 2^24. Workspace: ec_paged_attention_workspace
+ * Limits: Hq a multiple of H, Hq / H <= 128, N*Hq < 2^24, and N*H*ceil(Hq/H/8) times
+ * (max_pages*page_size/64 + 2) below 2^31. Workspace: ec_paged_attention_workspace
  * bytes (0 on invalid arguments); its contents need not survive between calls. Deterministic.
  */
 size_t ec_paged_attention_workspace(const ec_paged *c, int Hq, int accumulate);

@@ -425,13 +425,13 @@ def ec_decode_splits(cache: ec_cache) -> int:
 _ELEM = {torch.bfloat16: EC_BF16, torch.float16: EC_FP16}
 
 
-def _want(t: Optional[torch.Tensor], name: str, dtype: torch.dtype, shape, device: int) -> Optional[int]:
+def _want(t: Optional[torch.Tensor], name: str, dtype: torch.dtype, shape: tuple, device: int) -> Optional[int]:
     """Device pointer of an argument after checking type, shape, layout and device (None stays None)."""
     if t is None:
         return None
-    if t.dtype != dtype or tuple(t.shape) != shape:
+    if t.dtype != dtype or t.shape != shape:
         raise ValueError(f"{name} must be {dtype} {list(shape)}, got {t.dtype} {list(t.shape)}")
-    if not t.is_cuda or t.device.index != device:
+    if t.get_device() != device:
         raise ValueError(f"{name} must be on the cache's device")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
@@ -442,7 +442,7 @@ def _paged_stream(cache: ec_paged) -> int:
     """The current stream; the cache's device has to be the current one, as the kernels launch there."""
     if torch.cuda.current_device() != cache._device:
         raise ValueError("the cache's device is not the current CUDA device")
-    return torch.cuda.current_stream().cuda_stream
+    return torch._C._cuda_getCurrentRawStream(cache._device)
 
 
 def ec_paged_state_bytes(N: int) -> int:

@@ -53,9 +53,35 @@ struct PagedView {
     int *state;                                  // status word and arrival counters, see kState*
     int N, H, page_size, n_pages, max_pages;
     uint32_t page_step, head_step, row_step;     // strides in 16-byte units
+    uint32_t div_mul, div_shift;                 // row / page_size, see page_of
 };
 
+// row / page_size for 0 <= row < 2^31 as a multiplication: with 2^(l-1) < d <= 2^l and mul = ceil(2^(31+l) / d), mul * d
+// exceeds 2^(31+l) by less than d <= 2^l, so the quotient is off by less than row * 2^l / (2^(31+l) d) < 1 / d: never
+// enough to reach the next whole number.
+inline void set_page_division(PagedView &c)
+{
+    uint32_t l = 0;
+    while ((1u << l) < (uint32_t)c.page_size) ++l;
+    c.div_shift = 31 + l;
+    c.div_mul = (uint32_t)(((1ull << c.div_shift) + (uint32_t)c.page_size - 1) / (uint32_t)c.page_size);
+}
+
 namespace {
+
+// Counts the CTA in at a counter (to be called by one thread, behind a block barrier): what the CTA wrote before is visible
+// to whoever arrives later, what the others wrote before is visible to this CTA behind the next block barrier.
+__device__ __forceinline__ int arrive(int *counter)
+{
+    int before;
+    asm volatile("atom.acq_rel.gpu.global.add.s32 %0, [%1], 1;" : "=r"(before) : "l"(counter) : "memory");
+    return before;
+}
+
+__device__ __forceinline__ int page_of(const PagedView &c, int row)
+{
+    return (int)(((unsigned long long)(uint32_t)row * c.div_mul) >> c.div_shift);
+}
 
 struct Slot {
     int page, slot;        // page < 0: the table has no valid page here
@@ -63,7 +89,7 @@ struct Slot {
 
 __device__ __forceinline__ Slot find_slot(const PagedView &c, int n, int row)
 {
-    const int p = row / c.page_size;
+    const int p = page_of(c, row);
     Slot s;
     s.slot = row - p * c.page_size;
     s.page = c.table[(size_t)n * c.max_pages + p];

@@ -55,12 +55,16 @@ ec::PagedView view(const ec_paged *c)
     v.page_step = (uint32_t)(c->page_stride / 8);
     v.head_step = (uint32_t)(c->head_stride / 8);
     v.row_step = (uint32_t)(c->row_stride / 8);
+    ec::set_page_division(v);
     return v;
 }
 
 int check_heads(const ec_paged *c, int Hq)
 {
     if (Hq < 1 || Hq % c->H != 0 || Hq / c->H > 128 || (long long)c->N * Hq >= (1LL << 24)) return EC_ERR_SHAPE;
+    // work is counted in blocks of 64 rows, in 31 bits
+    const long long units = (long long)c->N * c->H * ((Hq / c->H + 7) / 8);
+    if (units * ((long long)c->max_pages * c->page_size / 64 + 2) >= (1LL << 31)) return EC_ERR_SHAPE;
     return EC_OK;
 }
 

@@ -19,11 +19,7 @@ namespace ec {
 
 namespace {
 
-constexpr int kWarps = 4;
-constexpr int kThreads = kWarps * 32;
 constexpr int kTile = 16;                        // rows of a warp's tile
-constexpr int kBlockRows = kWarps * kTile;       // rows of a block, the unit of work distribution
-constexpr int kCtasPerSm = 2;
 constexpr float kLazy = 8.f;                     // the running maximum is raised when exceeded by more than this (log2)
 
 struct Bf16 {
@@ -63,6 +59,10 @@ __device__ __forceinline__ void copy_piece(uint32_t dst, const uint4 *src, uint3
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
+__device__ __forceinline__ void copy_piece(uint32_t dst, const uint4 *src)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
@@ -82,15 +82,15 @@ struct AttnArgs {
     const uint32_t *q;
     const uint4 *k_new, *v_new;                  // k_new == nullptr: the cached rows alone
     int G;                                       // query heads per key / value head
-    float scale_log2e, decay;
+    float scale_log2e, inv_scale, decay;         // inv_scale: 1 / scale_log2e
     uint32_t *out;
     float *lse, *w_new;
     // workspace
     float2 *stat;                                // [N, Hq] (maximum in the log2 domain, 1 / sum)
-    float *score_new;                            // [N, Hq] score of the step's own row
+    float *score_new;                            // [N, Hq] the same of the step's own row
     float *part_o;                               // [2 * CTAs][8 NT][D]
     float2 *part_ml;                             // [2 * CTAs][8 NT]
-    float *scores;                               // [n_pages, H, page_size, G], log2 domain
+    float *scores;                               // [n_pages, H, G, page_size]: <q, k>, not scaled
 };
 
 // Rows of problem n with its own new row, 0 when there is nothing to attend to.
@@ -100,104 +100,265 @@ __device__ __forceinline__ int rows_of(const AttnArgs &a, int n)
     return len < 0 ? 0 : len + (a.k_new ? 1 : 0);
 }
 
-__device__ __forceinline__ int blocks_of(int rows) { return (rows + kBlockRows - 1) / kBlockRows; }
+// Every CTA derives the same plan from the lengths. Work is counted in blocks of W tiles, and every unit counts for
+// kUnitCost blocks more: putting its results together takes about as long (measured with 8 warps: 2200 clocks for a
+// full block, 4200 for a unit of one tile), and without that a CTA whose share is many short units ends last (32 ragged
+// problems of 1 .. 8192 rows: 42 us without it).
+constexpr int kUnitCost = 1;
 
-// Every CTA derives the same plan from the lengths: `per` blocks for each CTA, and where its own begin.
 struct Plan {
-    int per, n;                                  // n < 0: nothing to do
-    long long before;                            // blocks in front of problem n
+    int per, n, rows, before;                    // n < 0: nothing to do; the count in front of problem n
 };
 
+template <int W>
+__device__ __forceinline__ int blocks_of(int rows) { return (rows + W * kTile - 1) / (W * kTile); }
+
+template <int W>
+__device__ __forceinline__ int cost_of(int rows) { return rows > 0 ? blocks_of<W>(rows) + kUnitCost : 0; }
+
+template <int W>
 __device__ __forceinline__ void make_plan(const AttnArgs &a, int units, int min_per, Plan *plan)
 {
-    __shared__ long long warp_sum[kWarps];
+    __shared__ int warp_sum[W];
     const int N = a.c.N;
-    const int span = (N + kThreads - 1) / kThreads;
+    const int span = (N + W * 32 - 1) / (W * 32);
     const int n0 = min((int)threadIdx.x * span, N), n1 = min(n0 + span, N);
-    long long mine = 0;
-    for (int n = n0; n < n1; ++n) mine += blocks_of(rows_of(a, n));
-    long long incl = mine;
+    int mine = 0;
+    for (int n = n0; n < n1; ++n) mine += cost_of<W>(rows_of(a, n));
+    int incl = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const long long up = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+        const int up = __shfl_up_sync(0xFFFFFFFFu, incl, o);
         if ((threadIdx.x & 31) >= o) incl += up;
     }
     if ((threadIdx.x & 31) == 31) warp_sum[threadIdx.x >> 5] = incl;
     if (threadIdx.x == 0) plan->n = -1;
     __syncthreads();
-    long long total = 0, base = incl - mine;
+    int total = 0, base = incl - mine;
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
+    for (int w = 0; w < W; ++w) {
         if (w < (int)(threadIdx.x >> 5)) base += warp_sum[w];
         total += warp_sum[w];
     }
-    long long per = (total * units + gridDim.x - 1) / gridDim.x;
-    if (per < min_per) per = min_per;
-    const long long first = per * blockIdx.x;
-    if (threadIdx.x == 0) plan->per = (int)per;
+    const int per = max((int)(((unsigned)(total * units) + gridDim.x - 1) / gridDim.x), min_per);
+    const int first = per * blockIdx.x;
+    if (threadIdx.x == 0) plan->per = per;
     // the thread whose span holds the CTA's first block names the problem
     if (first >= base * units && first < (base + mine) * units) {
-        long long at = base * units;
+        int at = base * units;
         for (int n = n0; n < n1; ++n) {
-            const long long nb = (long long)blocks_of(rows_of(a, n)) * units;
-            if (first < at + nb) {
+            const int rows = rows_of(a, n), cost = cost_of<W>(rows) * units;
+            if (first < at + cost) {
                 plan->n = n;
+                plan->rows = rows;
                 plan->before = at;
                 break;
             }
-            at += nb;
+            at += cost;
         }
     }
     __syncthreads();
 }
 
-// A place in the CTA's run of blocks. The loader and the consumer of a warp each walk it, the loader ahead.
+// A place in the CTA's run of blocks. Every warp walks it three times: for the page table, S tiles behind for the copies,
+// S tiles behind those for the arithmetic.
 struct Walk {
     int n, rows, nb;                             // problem, its rows and blocks
-    int unit, blk;                               // (head, head block) of the problem, block of the unit
-    int left;                                    // blocks still to do, this one included
+    int h, hb, blk;                              // head, block of the group's query heads, block of the unit
+    int left;                                    // what is left of the CTA's count, this block included
 };
 
-__device__ __forceinline__ void walk_on(const AttnArgs &a, int units, Walk &w)
+template <int W>
+__device__ __forceinline__ void next_unit(const AttnArgs &a, int head_blocks, Walk &w)
 {
-    --w.left;
-    if (++w.blk < w.nb) return;
     w.blk = 0;
-    if (++w.unit < units) return;
-    w.unit = 0;
+    if (++w.hb < head_blocks) return;
+    w.hb = 0;
+    if (++w.h < a.c.H) return;
+    w.h = 0;
     do {
         if (++w.n >= a.c.N) {
             w.left = 0;
             return;
         }
         w.rows = rows_of(a, w.n);
-        w.nb = blocks_of(w.rows);
+        w.nb = blocks_of<W>(w.rows);
     } while (w.nb == 0);
 }
 
-template <int D> struct Ring {
+template <int W>
+__device__ __forceinline__ void walk_on(const AttnArgs &a, int head_blocks, Walk &w)
+{
+    --w.left;
+    if (++w.blk < w.nb) return;
+    w.left -= kUnitCost;
+    if (w.left > 0) next_unit<W>(a, head_blocks, w);
+}
+
+// Shared memory of a CTA of W warps that handles 8 NT query heads.
+template <int D, int NT, int W> struct Smem {
     static constexpr int kTileBytes = kTile * D * 2;                      // of K, and of V behind it
     static constexpr int kStages = D == 128 ? 3 : 6;                      // 24 KB per warp
-    static constexpr int kBytes = kWarps * kStages * 2 * kTileBytes;
     static constexpr int kPitch = D + 4;                                  // floats of a head in the merge buffer: no bank conflicts
-    static constexpr int kMergeHeads = 4;
-    static constexpr int kMergeFloats = kWarps * kMergeHeads * kPitch;
-    static constexpr int kSmem = kBytes + kMergeFloats * 4 + kWarps * kStages * kTile * 4;
+    static constexpr int kMergeHeads = W == 8 && NT == 1 ? 4 : 2;
+    static constexpr int kMergeFloats = W * kMergeHeads * kPitch;
+    static constexpr int kQBytes = 8 * NT * D * 2;
+    static constexpr int kQSlots = kStages + 1;                           // the copies run at most kStages units ahead
+    static constexpr int kRing = 0;
+    static constexpr int kMerge = kRing + W * kStages * 2 * kTileBytes;
+    static constexpr int kQ = (kMerge + kMergeFloats * 4 + 255) / 256 * 256;   // fragments are addressed with XORs below 256
+    static constexpr int kInfo = kQ + kQSlots * kQBytes;
+    static constexpr int kPages = kInfo + W * kStages * kTile * 8;
+    static constexpr int kTotal = kPages + W * kStages * kTile * 4;
 };
 
-// NT: groups of 8 query heads that share a pass over the rows. GATHER: scores are stored for the weights.
-template <typename E, int D, int NT, bool GATHER>
-__global__ void __launch_bounds__(kThreads, kCtasPerSm) paged_attention_kernel(AttnArgs a, int head_blocks, int min_per)
+// Joins the parts of a unit that the CTAs c0 .. c1 hold. A thread owns four dimensions of a head and has several parts in
+// flight, the first of them before the parts' factors are known; `buf` (kMergeFloats floats) takes the factors.
+template <typename E, int D, int NT, int W>
+__device__ __forceinline__ void join_parts(const AttnArgs &a, int c0, int c1, int heads, size_t head_at, float *buf, float *sm_inv)
 {
-    using R = Ring<D>;
+    using M_ = Smem<D, NT, W>;
+    constexpr int kThreads = W * 32;
+    constexpr int kChunk = M_::kMergeFloats / (8 * NT);
+    constexpr int kItems = (8 * NT * (D / 4) + kThreads - 1) / kThreads;
+    constexpr int kFlight = NT == 1 ? 8 : 4;      // eight would spill beside the registers of 16 heads
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int parts = c1 - c0 + 1;
+    auto part_at = [&](int i) { return (size_t)(2 * (c0 + i) + (i == 0)) * 8 * NT; };
+    if (parts <= kFlight) {                      // one round of reads, every thread on its own
+#pragma unroll 1
+        for (int i = threadIdx.x; i < heads * (D / 4); i += kThreads) {
+            const int hd = i / (D / 4), d = 4 * (i - hd * (D / 4));
+            float4 v[kFlight];
+            float2 ml[kFlight];
+#pragma unroll
+            for (int c = 0; c < kFlight; ++c) {
+                if (c >= parts) continue;
+                v[c] = __ldcg(reinterpret_cast<const float4 *>(a.part_o + (part_at(c) + hd) * D + d));
+                ml[c] = __ldcg(&a.part_ml[part_at(c) + hd]);
+            }
+            float M = -INFINITY, L = 0.f;
+            float4 A = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int c = 0; c < kFlight; ++c)
+                if (c < parts) M = fmaxf(M, ml[c].x);
+            const float mu = M == -INFINITY ? 0.f : M;
+#pragma unroll
+            for (int c = 0; c < kFlight; ++c) {
+                if (c >= parts) continue;
+                const float f = fast_exp2(ml[c].x - mu);
+                L = fmaf(ml[c].y, f, L);
+                A.x = fmaf(v[c].x, f, A.x);
+                A.y = fmaf(v[c].y, f, A.y);
+                A.z = fmaf(v[c].z, f, A.z);
+                A.w = fmaf(v[c].w, f, A.w);
+            }
+            const float inv = L == 0.f ? 0.f : 1.f / L;
+            uint2 r;
+            r.x = E::pack(A.x * inv, A.y * inv);
+            r.y = E::pack(A.z * inv, A.w * inv);
+            *reinterpret_cast<uint2 *>(a.out + ((head_at + hd) * D + d) / 2) = r;
+            if (d == 0) {
+                a.stat[head_at + hd] = make_float2(mu, inv);
+                if (a.lse) a.lse[head_at + hd] = M == -INFINITY ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+            }
+        }
+        return;
+    }
+    float4 A[kItems], first[kItems][kFlight];
+#pragma unroll
+    for (int k = 0; k < kItems; ++k) {
+        const int i = threadIdx.x + k * kThreads, hd = i / (D / 4), d = 4 * (i - hd * (D / 4));
+        A[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int c = 0; c < kFlight; ++c)
+            first[k][c] = hd < heads && c < parts ? __ldcg(reinterpret_cast<const float4 *>(a.part_o + (part_at(c) + hd) * D + d))
+                                                  : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+    // maximum and sum of every head: a warp per head
+    float *sm_m = sm_inv + 8 * NT;
+    for (int hd = warp; hd < heads; hd += W) {
+        float M = -INFINITY, L = 0.f;
+        for (int c = lane; c < parts; c += 32) {
+            const float2 v = __ldcg(&a.part_ml[part_at(c) + hd]);
+            const float mn = fmaxf(M, v.x);
+            if (mn != -INFINITY) L = L * fast_exp2(M - mn) + v.y * fast_exp2(v.x - mn);
+            M = mn;
+            if (c < kChunk) buf[hd * kChunk + c] = v.x;
+        }
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const float m2 = __shfl_xor_sync(0xFFFFFFFFu, M, d), l2 = __shfl_xor_sync(0xFFFFFFFFu, L, d);
+            const float mn = fmaxf(M, m2);
+            if (mn != -INFINITY) L = L * fast_exp2(M - mn) + l2 * fast_exp2(m2 - mn);
+            M = mn;
+        }
+        const float mu = M == -INFINITY ? 0.f : M, inv = L == 0.f ? 0.f : 1.f / L;
+        if (lane == 0) {
+            sm_inv[hd] = inv;
+            sm_m[hd] = mu;
+            a.stat[head_at + hd] = make_float2(mu, inv);
+            if (a.lse) a.lse[head_at + hd] = M == -INFINITY ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+        }
+        for (int c = lane; c < min(parts, kChunk); c += 32) buf[hd * kChunk + c] = fast_exp2(buf[hd * kChunk + c] - mu);
+    }
+    __syncthreads();
+    for (int cb = 0; cb < parts; cb += kChunk) {
+        const int cn = min(kChunk, parts - cb);
+        if (cb > 0) {
+            __syncthreads();
+            for (int i = threadIdx.x; i < heads * cn; i += kThreads) {
+                const int hd = i / cn, c = i - hd * cn;
+                buf[hd * kChunk + c] = fast_exp2(__ldcg(&a.part_ml[part_at(cb + c) + hd].x) - sm_m[hd]);
+            }
+            __syncthreads();
+        }
+#pragma unroll
+        for (int k = 0; k < kItems; ++k) {
+            const int i = threadIdx.x + k * kThreads, hd = i / (D / 4), d = 4 * (i - hd * (D / 4));
+            if (hd >= heads) continue;
+            const float *f = buf + hd * kChunk;
+            auto add = [&](float w, const float4 &v) {
+                A[k].x = fmaf(v.x, w, A[k].x);
+                A[k].y = fmaf(v.y, w, A[k].y);
+                A[k].z = fmaf(v.z, w, A[k].z);
+                A[k].w = fmaf(v.w, w, A[k].w);
+            };
+            int c = 0;
+            if (cb == 0) {
+#pragma unroll
+                for (; c < kFlight; ++c)
+                    if (c < parts) add(f[c], first[k][c]);
+            }
+#pragma unroll 8
+            for (; c < cn; ++c) add(f[c], __ldcg(reinterpret_cast<const float4 *>(a.part_o + (part_at(cb + c) + hd) * D + d)));
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < kItems; ++k) {
+        const int i = threadIdx.x + k * kThreads, hd = i / (D / 4), d = 4 * (i - hd * (D / 4));
+        if (hd >= heads) continue;
+        const float inv = sm_inv[hd];
+        uint2 r;
+        r.x = E::pack(A[k].x * inv, A[k].y * inv);
+        r.y = E::pack(A[k].z * inv, A[k].w * inv);
+        *reinterpret_cast<uint2 *>(a.out + ((head_at + hd) * D + d) / 2) = r;
+    }
+}
+
+// NT: groups of 8 query heads that share a pass over the rows. W: warps of a CTA. GATHER: scores are stored for the weights.
+template <typename E, int D, int NT, int W, bool GATHER>
+__global__ void __launch_bounds__(W * 32, 8 / W) paged_attention_kernel(AttnArgs a, int head_blocks, int min_per)
+{
+    using M_ = Smem<D, NT, W>;
+    constexpr int kThreads = W * 32, kBlockRows = W * kTile;
     constexpr int C = D / 8;                     // 16-byte pieces of a row
     constexpr int KS = D / 16, MT = D / 16;
-    constexpr int S = R::kStages;
-    extern __shared__ __align__(128) unsigned char smem[];
-    float *sm_o = reinterpret_cast<float *>(smem + R::kBytes);
-    uint32_t *sm_row = reinterpret_cast<uint32_t *>(smem + R::kBytes + R::kMergeFloats * 4);
-    __shared__ float2 sm_ml[kWarps][8 * NT];
-    __shared__ float sm_m[8 * NT], sm_inv[8 * NT];
+    constexpr int S = M_::kStages;
+    extern __shared__ __align__(1024) unsigned char smem[];
+    float *sm_o = reinterpret_cast<float *>(smem + M_::kMerge);
+    __shared__ float2 sm_ml[W][8 * NT];
+    __shared__ float sm_inv[2 * 8 * NT];
     __shared__ Plan plan;
     __shared__ int sm_last;
 
@@ -206,7 +367,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) paged_attention_kernel(A
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int G = a.G, H = a.c.H, Hq = H * G;
     const int units = H * head_blocks;           // of a problem
-    make_plan(a, units, min_per, &plan);
+    make_plan<W>(a, units, min_per, &plan);
     // problems without a row to attend to have no block: their outputs are written here
     for (int n = blockIdx.x; n < a.c.N; n += gridDim.x) {
         if (rows_of(a, n) > 0) continue;
@@ -220,103 +381,149 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) paged_attention_kernel(A
 
     Walk use;
     use.n = plan.n;
-    use.rows = rows_of(a, use.n);
-    use.nb = blocks_of(use.rows);
+    use.rows = plan.rows;
+    use.nb = blocks_of<W>(use.rows);
     use.left = plan.per;
     {
-        const long long in = (long long)plan.per * blockIdx.x - plan.before;
-        use.unit = (int)(in / use.nb);
-        use.blk = (int)(in - (long long)use.unit * use.nb);
-    }
-    Walk ahead = use;
-
-    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + warp * (S * 2 * R::kTileBytes);
-    uint32_t *rows_info = sm_row + warp * (S * kTile);
-
-    // Loader: lane i (and i + 16) looks up row i of a tile, one tile before it is copied, so that the table's latency is
-    // not in the way.
-    int next_page = -1, next_slot = 0;
-    uint32_t next_kind = kRowNone;               // kRowNone, kRowNew, or 0: a cached row
-    auto look_up = [&]() {
-        next_kind = kRowNone;
-        if (ahead.left <= 0) return;
-        const int row = ahead.blk * kBlockRows + warp * kTile + (lane & 15);
-        const int len = ahead.rows - (a.k_new ? 1 : 0);
-        if (row < len) {
-            const int p = row / a.c.page_size;
-            next_kind = 0;
-            next_slot = row - p * a.c.page_size;
-            next_page = a.c.table[(size_t)ahead.n * a.c.max_pages + p];
-        } else if (row < ahead.rows) {
-            next_kind = kRowNew;
+        const unsigned in = (unsigned)(plan.per * (int)blockIdx.x - plan.before);
+        const unsigned cost = (unsigned)(use.nb + kUnitCost);
+        const int unit = (int)(in / cost);
+        use.blk = (int)(in - (unsigned)unit * cost);
+        use.h = unit / head_blocks;
+        use.hb = unit - use.h * head_blocks;
+        if (use.blk >= use.nb) {                 // the share begins behind the unit's blocks
+            use.left -= (int)cost - use.blk;
+            if (use.left > 0) next_unit<W>(a, head_blocks, use);
         }
+    }
+    Walk ahead = use, scout = use;
+
+    const uint32_t base = (uint32_t)__cvta_generic_to_shared(smem);
+    const uint32_t ring = base + M_::kRing + warp * (S * 2 * M_::kTileBytes);
+    uint2 *rows_info = reinterpret_cast<uint2 *>(smem + M_::kInfo) + warp * (S * kTile);   // (page and head, slot) of a row
+    const int *pages = reinterpret_cast<const int *>(smem + M_::kPages) + warp * (S * kTile);
+    const uint32_t pages_at = base + M_::kPages + warp * (S * kTile * 4);
+    const int tile_row = warp * kTile + (lane & 15);                      // of a block, described by this lane
+    const int own_row = a.k_new ? 1 : 0;
+
+    // The page of every row of the tile at `scout`, S tiles before the copies need it.
+    auto scout_tile = [&](int slot) {
+        if (scout.left <= 0) return;
+        const int row = scout.blk * kBlockRows + tile_row;
+        if (lane < kTile && row < scout.rows - own_row) {
+            const int *src = a.c.table + (size_t)scout.n * a.c.max_pages + page_of(a.c, row);
+            asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(pages_at + (slot * kTile + lane) * 4), "l"(src) : "memory");
+        }
+        walk_on<W>(a, head_blocks, scout);
     };
-    auto copy_tile = [&](int stage) {            // the tile at `ahead`, which then moves on
+    int q_slot_ahead = 0;
+    bool fresh_ahead = true;
+    auto copy_tile = [&](int stage) {            // the tile at `ahead`, which then moves on; its pages have arrived
         if (ahead.left > 0) {
-            if (ahead.blk * kBlockRows + warp * kTile < ahead.rows) {
-                const int h = ahead.unit / head_blocks;
-                uint32_t off = next_kind, info = next_kind;
-                if (next_kind == 0) {
+            const int h = ahead.h;
+            if (fresh_ahead) {                   // the unit's queries, every warp a share of them
+                const int head0 = ahead.hb * 8 * NT;
+                const size_t head_at = (size_t)ahead.n * Hq + (size_t)h * G + head0;
+                for (int i = threadIdx.x; i < 8 * NT * C; i += kThreads) {
+                    const int hd = i / C, piece = i - hd * C;
+                    const bool there = head0 + hd < G;
+                    copy_piece(base + M_::kQ + q_slot_ahead * M_::kQBytes + hd * (D * 2) + ((piece ^ (hd & 7)) << 4),
+                               reinterpret_cast<const uint4 *>(a.q) + (there ? (head_at + hd) * C + piece : 0), there ? 16u : 0u);
+                }
+                q_slot_ahead = q_slot_ahead + 1 == M_::kQSlots ? 0 : q_slot_ahead + 1;
+            }
+            const int row0 = ahead.blk * kBlockRows + warp * kTile;
+            if (row0 < ahead.rows) {
+                const int row = row0 + (lane & 15), len = ahead.rows - own_row;
+                uint32_t off = kRowNone;
+                uint2 info = make_uint2(kRowNone, 0);
+                if (row < len) {
                     Slot s;
-                    s.page = next_page;
-                    s.slot = next_slot;
-                    if ((unsigned)next_page >= (unsigned)a.c.n_pages) {
-                        atomicExch(a.c.state, kStatusPage);
-                        off = info = kRowNone;
-                    } else {
+                    s.page = pages[stage * kTile + (lane & 15)];
+                    s.slot = row - page_of(a.c, row) * a.c.page_size;
+                    if ((unsigned)s.page < (unsigned)a.c.n_pages) {
                         off = row_offset(a.c, s);
-                        info = meta_index(a.c, h, s);
+                        info = make_uint2((uint32_t)s.page * (uint32_t)H + (uint32_t)h, (uint32_t)s.slot);
+                    } else {
+                        atomicExch(a.c.state, kStatusPage);
                     }
+                } else if (row < ahead.rows) {
+                    off = info.x = kRowNew;
                 }
                 if (lane < kTile) rows_info[stage * kTile + lane] = info;
-                const uint4 *Kh = a.c.K + (size_t)h * a.c.head_step, *Vh = a.c.V + (size_t)h * a.c.head_step;
-                const size_t own = ((size_t)ahead.n * H + h) * C;
-                const int piece = lane % C;
-                const uint32_t dst0 = ring + stage * (2 * R::kTileBytes);
+                const uint4 *Kh = a.c.K + (size_t)h * a.c.head_step + lane % C, *Vh = a.c.V + (size_t)h * a.c.head_step + lane % C;
+                // rows of one copy instruction lie 32 / C apart from the next one's: their swizzles differ by a constant
+                const uint32_t dst0 = (ring + stage * (2 * M_::kTileBytes) + (lane / C) * (D * 2)) + ((lane % C ^ lane / C) << 4);
+                const bool plain = __all_sync(0xFFFFFFFFu, off < kRowNew);
+                if (plain) {                     // sixteen cached rows
 #pragma unroll
-                for (int i = 0; i < kTile * C / 32; ++i) {
-                    const int row = i * (32 / C) + lane / C;
-                    const uint32_t o = __shfl_sync(0xFFFFFFFFu, off, row);
-                    const uint32_t dst = dst0 + row * (D * 2) + ((piece ^ (row & 7)) << 4);
-                    const bool is_new = o == kRowNew;
-                    const uint32_t bytes = o == kRowNone ? 0u : 16u;      // absent rows are filled with zeros
-                    const size_t at = o == kRowNone ? 0 : o;
-                    copy_piece(dst, (is_new ? a.k_new + own : Kh + at) + piece, bytes);
-                    copy_piece(dst + R::kTileBytes, (is_new ? a.v_new + own : Vh + at) + piece, bytes);
+                    for (int i = 0; i < kTile * C / 32; ++i) {
+                        const uint32_t o = __shfl_sync(0xFFFFFFFFu, off, i * (32 / C) + lane / C);
+                        const uint32_t dst = (dst0 ^ (((i * (32 / C)) & 7) << 4)) + i * 512;
+                        copy_piece(dst, Kh + o);
+                        copy_piece(dst + M_::kTileBytes, Vh + o);
+                    }
+                } else {                         // the unit's last rows, or pages that do not exist
+                    const size_t own = ((size_t)ahead.n * H + h) * C + lane % C;
+#pragma unroll 1
+                    for (int i = 0; i < kTile * C / 32; ++i) {
+                        const uint32_t o = __shfl_sync(0xFFFFFFFFu, off, i * (32 / C) + lane / C);
+                        const uint32_t dst = (dst0 ^ (((i * (32 / C)) & 7) << 4)) + i * 512;
+                        const uint32_t bytes = o == kRowNone ? 0u : 16u;  // absent rows are filled with zeros
+                        const size_t at = o == kRowNone ? 0 : o;
+                        copy_piece(dst, o == kRowNew ? a.k_new + own : Kh + at, bytes);
+                        copy_piece(dst + M_::kTileBytes, o == kRowNew ? a.v_new + own : Vh + at, bytes);
+                    }
                 }
             }
-            walk_on(a, units, ahead);
-            look_up();
+            fresh_ahead = ahead.blk + 1 == ahead.nb;
+            walk_on<W>(a, head_blocks, ahead);
+            __syncwarp();                        // the pages have been read
+            scout_tile(stage);
         }
         copies_commit();
     };
 
-    look_up();
+#pragma unroll 1
+    for (int i = 0; i < S; ++i) scout_tile(i);
+    copies_commit();
+    copies_wait<0>();
+    __syncwarp();
 #pragma unroll 1
     for (int i = 0; i < S; ++i) copy_tile(i);
+    copies_wait<S - 1>();
+    __syncthreads();                             // the first unit's queries are here
 
-    uint32_t qf[NT][KS][2];
-    float o[NT][MT][4], m[NT][2], l[NT][2];
-    int stage = 0, first_block = 0;
+    // Q's fragments stay in registers for 8 heads; for 16 they would spill, and are read again for every tile
+    constexpr bool kHoldQ = NT == 1;
+    uint32_t qf[kHoldQ ? NT : 1][kHoldQ ? KS : 1][2], q_at = 0;
+    float o[NT][MT][4], m[NT][2], l[NT][2], limit[NT][2], neg_m[NT][2];
+    int stage = 0, q_slot = 0, first_block = 0;
     bool begin = true;
     while (use.left > 0) {
-        const int hb = use.unit % head_blocks, h = use.unit / head_blocks;
-        const int head0 = hb * 8 * NT;                                    // first query head of the block within the group
+        const int h = use.h, head0 = use.hb * 8 * NT;                     // first query head of the block within the group
         const int heads = min(G - head0, 8 * NT);
         const size_t head_at = (size_t)use.n * Hq + (size_t)h * G + head0;
         if (begin) {
             begin = false;
             first_block = use.blk;
+            q_at = base + M_::kQ + q_slot * M_::kQBytes + (lane & 7) * (D * 2) + (((lane >> 3) ^ (lane & 7)) << 4);
+            q_slot = q_slot + 1 == M_::kQSlots ? 0 : q_slot + 1;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-                const bool there = nt * 8 + g < heads;
-                const uint32_t *q = a.q + (head_at + nt * 8 + g) * (D / 2) + t;
+                if (kHoldQ) {
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks) {
-                    qf[nt][ks][0] = there ? q[ks * 8] : 0u;
-                    qf[nt][ks][1] = there ? q[ks * 8 + 4] : 0u;
+                    for (int ks = 0; ks < KS; ks += 2) {
+                        uint32_t r[4];
+                        load_matrices(r, (q_at ^ (ks << 5)) + nt * 8 * (D * 2));
+                        qf[nt][ks][0] = r[0];
+                        qf[nt][ks][1] = r[1];
+                        qf[nt][ks + 1][0] = r[2];
+                        qf[nt][ks + 1][1] = r[3];
+                    }
                 }
-                m[nt][0] = m[nt][1] = -INFINITY;
+                m[nt][0] = m[nt][1] = limit[nt][0] = limit[nt][1] = -INFINITY;
+                neg_m[nt][0] = neg_m[nt][1] = 0.f;
                 l[nt][0] = l[nt][1] = 0.f;
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt)
@@ -327,7 +534,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) paged_attention_kernel(A
         copies_wait<S - 1>();
         __syncwarp();
         if (use.blk * kBlockRows + warp * kTile < use.rows) {
-            const uint32_t base = ring + stage * (2 * R::kTileBytes);
+            const uint32_t tile = ring + stage * (2 * M_::kTileBytes);
             // S^T of this tile, even and odd steps in chains of their own
             float s[NT][4], s1[NT][4];
 #pragma unroll
@@ -335,34 +542,51 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) paged_attention_kernel(A
 #pragma unroll
                 for (int i = 0; i < 4; ++i) s[nt][i] = s1[nt][i] = 0.f;
             {
-                const int row = (lane & 7) + ((lane >> 3) & 1) * 8;
+                const int row = lane & 15;
+                const uint32_t at = (tile + row * (D * 2)) + (((lane >> 4) ^ (row & 7)) << 4);
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks) {
-                    uint32_t av[4];
-                    load_matrices(av, base + row * (D * 2) + (((2 * ks + (lane >> 4)) ^ (row & 7)) << 4));
+                for (int ks = 0; ks < KS; ks += 2) {
+                    uint32_t a0[4], a1[4];
+                    load_matrices(a0, at ^ (ks << 5));
+                    load_matrices(a1, at ^ ((ks + 1) << 5));
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) E::mma(ks & 1 ? s1[nt] : s[nt], av, qf[nt][ks][0], qf[nt][ks][1]);
+                    for (int nt = 0; nt < NT; ++nt) {
+                        uint32_t r[4];
+                        if (kHoldQ) {
+                            r[0] = qf[nt][ks][0];
+                            r[1] = qf[nt][ks][1];
+                            r[2] = qf[nt][ks + 1][0];
+                            r[3] = qf[nt][ks + 1][1];
+                        } else {
+                            load_matrices(r, (q_at ^ (ks << 5)) + nt * 8 * (D * 2));
+                        }
+                        E::mma(s[nt], a0, r[0], r[1]);
+                        E::mma(s1[nt], a1, r[2], r[3]);
+                    }
                 }
             }
-            const uint32_t info0 = rows_info[stage * kTile + g], info1 = rows_info[stage * kTile + g + 8];
-            bool raise = false;
+            const uint2 info0 = rows_info[stage * kTile + g], info1 = rows_info[stage * kTile + g + 8];
+            const bool there0 = info0.x != kRowNone, there1 = info1.x != kRowNone;
+            bool raise = false;                  // scale > 0: the scores are compared before they are scaled
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    s[nt][i] = info0 != kRowNone ? (s[nt][i] + s1[nt][i]) * a.scale_log2e : -INFINITY;
-                    s[nt][2 + i] = info1 != kRowNone ? (s[nt][2 + i] + s1[nt][2 + i]) * a.scale_log2e : -INFINITY;
-                    raise |= fmaxf(s[nt][i], s[nt][2 + i]) > m[nt][i] + kLazy;
+                    s[nt][i] = there0 ? s[nt][i] + s1[nt][i] : -INFINITY;
+                    s[nt][2 + i] = there1 ? s[nt][2 + i] + s1[nt][2 + i] : -INFINITY;
+                    raise |= fmaxf(s[nt][i], s[nt][2 + i]) > limit[nt][i];
                 }
                 if (GATHER) {
                     const int hd = nt * 8 + 2 * t;
 #pragma unroll
                     for (int r = 0; r < 2; ++r) {
-                        const uint32_t info = r ? info1 : info0;
-                        if (info == kRowNone) continue;
-                        float *dst = info == kRowNew ? a.score_new + head_at : a.scores + (size_t)info * G + head0;
-                        if (hd < heads) dst[hd] = s[nt][2 * r];
-                        if (hd + 1 < heads) dst[hd + 1] = s[nt][2 * r + 1];
+                        const uint2 info = r ? info1 : info0;
+                        if (info.x == kRowNone) continue;
+                        const bool own = info.x == kRowNew;
+                        float *dst = own ? a.score_new + head_at : a.scores + ((size_t)info.x * G + head0) * a.c.page_size + info.y;
+                        const int step = own ? 1 : a.c.page_size;
+                        if (hd < heads) dst[(size_t)hd * step] = s[nt][2 * r];
+                        if (hd + 1 < heads) dst[(size_t)(hd + 1) * step] = s[nt][2 * r + 1];
                     }
                 }
             }
@@ -374,9 +598,11 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) paged_attention_kernel(A
                         float x = fmaxf(s[nt][i], s[nt][2 + i]);
 #pragma unroll
                         for (int d = 4; d < 32; d <<= 1) x = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, d));
-                        const float mn = fmaxf(m[nt][i], x);
+                        const float mn = fmaxf(m[nt][i], x * a.scale_log2e);
                         const float corr = mn == -INFINITY ? 1.f : fast_exp2(m[nt][i] - mn);   // first tile: 2^-inf = 0
                         m[nt][i] = mn;
+                        limit[nt][i] = (mn + kLazy) * a.inv_scale;
+                        neg_m[nt][i] = mn == -INFINITY ? 0.f : -mn;
                         l[nt][i] *= corr;
 #pragma unroll
                         for (int mt = 0; mt < MT; ++mt) {
@@ -390,7 +616,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) paged_attention_kernel(A
             for (int nt = 0; nt < NT; ++nt) {
                 float p[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) p[i] = fast_exp2(s[nt][i] - (m[nt][i & 1] == -INFINITY ? 0.f : m[nt][i & 1]));
+                for (int i = 0; i < 4; ++i) p[i] = fast_exp2(fmaf(s[nt][i], a.scale_log2e, neg_m[nt][i & 1]));
                 l[nt][0] += p[0] + p[2];
                 l[nt][1] += p[1] + p[3];
 #pragma unroll
@@ -403,10 +629,11 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) paged_attention_kernel(A
             }
             {
                 const int row = (lane & 7) + (lane >> 4) * 8;
+                const uint32_t at = (tile + M_::kTileBytes + row * (D * 2)) + ((((lane >> 3) & 1) ^ (row & 7)) << 4);
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt) {
                     uint32_t av[4];
-                    load_matrices_trans(av, base + R::kTileBytes + row * (D * 2) + (((2 * mt + ((lane >> 3) & 1)) ^ (row & 7)) << 4));
+                    load_matrices_trans(av, at ^ (mt << 5));
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
                         E::mma(o[nt][mt], av, hi[nt][0], hi[nt][1]);
@@ -420,7 +647,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) paged_attention_kernel(A
         stage = stage + 1 == S ? 0 : stage + 1;
 
         if (use.blk + 1 == use.nb || use.left == 1) {
-            // the four warps' results meet in shared memory, four heads at a time
+            // the warps' results meet in shared memory, a few heads at a time
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -432,47 +659,50 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) paged_attention_kernel(A
                 }
             const bool whole = first_block == 0 && use.blk + 1 == use.nb;
             const int part = 2 * blockIdx.x + (first_block == 0 ? 1 : 0); // a CTA holds at most one part of each kind
-            for (int hc = 0; hc * R::kMergeHeads < heads; ++hc) {
+            constexpr int kShare = W / M_::kMergeHeads;                   // warps that put one head together
+            for (int h0 = 0; h0 < heads; h0 += M_::kMergeHeads) {
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    if (nt != (hc >> 1) || (t >> 1) != (hc & 1)) continue;
+                for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        float *dst = sm_o + (warp * R::kMergeHeads + 2 * (t & 1) + i) * R::kPitch + g;
+                        const int at = nt * 8 + 2 * t + i - h0;
+                        if (at < 0 || at >= M_::kMergeHeads) continue;
+                        float *dst = sm_o + (warp * M_::kMergeHeads + at) * M_::kPitch + g;
 #pragma unroll
                         for (int mt = 0; mt < MT; ++mt) {
                             dst[mt * 16] = o[nt][mt][i];
                             dst[mt * 16 + 8] = o[nt][mt][2 + i];
                         }
                     }
-                }
                 __syncthreads();
-                const int hd = hc * R::kMergeHeads + warp;                // a warp per head
+                const int hd = h0 + warp / kShare;
                 if (hd < heads) {
                     float M = -INFINITY;
 #pragma unroll
-                    for (int w = 0; w < kWarps; ++w) M = fmaxf(M, sm_ml[w][hd].x);
+                    for (int w = 0; w < W; ++w) M = fmaxf(M, sm_ml[w][hd].x);
                     const float mu = M == -INFINITY ? 0.f : M;
-                    float L = 0.f, f[kWarps];
+                    float L = 0.f, f[W];
 #pragma unroll
-                    for (int w = 0; w < kWarps; ++w) {
+                    for (int w = 0; w < W; ++w) {
                         f[w] = fast_exp2(sm_ml[w][hd].x - mu);
                         L = fmaf(sm_ml[w][hd].y, f[w], L);
                     }
                     const float inv = L == 0.f ? 0.f : 1.f / L;           // nothing left by the scores: the output is zero
 #pragma unroll
                     for (int d = 0; d < D; d += 64) {
+                        if ((d / 64) % kShare != warp % kShare) continue;
                         float2 A = make_float2(0.f, 0.f);
 #pragma unroll
-                        for (int w = 0; w < kWarps; ++w) {
-                            const float2 v = *reinterpret_cast<const float2 *>(sm_o + (w * R::kMergeHeads + warp) * R::kPitch + d + 2 * lane);
+                        for (int w = 0; w < W; ++w) {
+                            const float2 v = *reinterpret_cast<const float2 *>(
+                                sm_o + (w * M_::kMergeHeads + warp / kShare) * M_::kPitch + d + 2 * lane);
                             A.x = fmaf(v.x, f[w], A.x);
                             A.y = fmaf(v.y, f[w], A.y);
                         }
                         if (whole) a.out[(head_at + hd) * (D / 2) + d / 2 + lane] = E::pack(A.x * inv, A.y * inv);
                         else *reinterpret_cast<float2 *>(a.part_o + ((size_t)part * 8 * NT + hd) * D + d + 2 * lane) = A;
                     }
-                    if (lane == 0) {
+                    if (lane == 0 && warp % kShare == 0) {
                         if (whole) {
                             a.stat[head_at + hd] = make_float2(mu, inv);
                             if (a.lse) a.lse[head_at + hd] = M == -INFINITY ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
@@ -481,65 +711,34 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) paged_attention_kernel(A
                         }
                     }
                 }
+                copies_wait<S - 1>();            // with the barrier: the next unit's queries are here
                 __syncthreads();
             }
             if (!whole) {
                 // the unit's first and last CTA follow from its first block; the last of them to get here joins the parts
-                const long long b0 = (long long)plan.per * blockIdx.x + (plan.per - use.left) - use.blk;
-                const int c0 = (int)(b0 / plan.per), c1 = (int)((b0 + use.nb - 1) / plan.per);
+                const int b0 = plan.per * blockIdx.x + (plan.per - use.left) - use.blk;
+                const int c0 = b0 / plan.per, c1 = (b0 + use.nb - 1) / plan.per;
                 int *arrived = a.c.state + kStateAttention + c0;          // a CTA is the first of one shared unit at most
-                __threadfence();
-                __syncthreads();
-                if (threadIdx.x == 0) sm_last = atomicAdd(arrived, 1) == c1 - c0;
+                if (threadIdx.x == 0) sm_last = arrive(arrived) == c1 - c0;
                 __syncthreads();
                 if (sm_last) {
-                    __threadfence();
                     if (threadIdx.x == 0) *arrived = 0;
-                    for (int hd = warp; hd < heads; hd += kWarps) {
-                        float M = -INFINITY, L = 0.f;
-                        for (int c = c0 + lane; c <= c1; c += 32) M = fmaxf(M, __ldcg(&a.part_ml[(size_t)(2 * c + (c == c0)) * 8 * NT + hd].x));
-#pragma unroll
-                        for (int d = 1; d < 32; d <<= 1) M = fmaxf(M, __shfl_xor_sync(0xFFFFFFFFu, M, d));
-                        const float mu = M == -INFINITY ? 0.f : M;
-                        for (int c = c0 + lane; c <= c1; c += 32) {
-                            const float2 v = __ldcg(&a.part_ml[(size_t)(2 * c + (c == c0)) * 8 * NT + hd]);
-                            L = fmaf(v.y, fast_exp2(v.x - mu), L);
-                        }
-#pragma unroll
-                        for (int d = 1; d < 32; d <<= 1) L += __shfl_xor_sync(0xFFFFFFFFu, L, d);
-                        const float inv = L == 0.f ? 0.f : 1.f / L;
-                        if (lane == 0) {
-                            sm_m[hd] = mu;
-                            sm_inv[hd] = inv;
-                            a.stat[head_at + hd] = make_float2(mu, inv);
-                            if (a.lse) a.lse[head_at + hd] = M == -INFINITY ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
-                        }
-                    }
-                    __syncthreads();
-                    for (int i = threadIdx.x; i < heads * (D / 2); i += kThreads) {
-                        const int hd = i / (D / 2), d = i - hd * (D / 2);
-                        float2 A = make_float2(0.f, 0.f);
-#pragma unroll 8
-                        for (int c = c0; c <= c1; ++c) {
-                            const size_t p = (size_t)(2 * c + (c == c0)) * 8 * NT + hd;
-                            const float f = fast_exp2(__ldcg(&a.part_ml[p].x) - sm_m[hd]);
-                            const float2 v = __ldcg(reinterpret_cast<const float2 *>(a.part_o + p * D + 2 * d));
-                            A.x = fmaf(v.x, f, A.x);
-                            A.y = fmaf(v.y, f, A.y);
-                        }
-                        a.out[(head_at + hd) * (D / 2) + d] = E::pack(A.x * sm_inv[hd], A.y * sm_inv[hd]);
-                    }
+                    join_parts<E, D, NT, W>(a, c0, c1, heads, head_at, sm_o, sm_inv);
                     __syncthreads();
                 }
             }
             begin = true;
         }
-        walk_on(a, units, use);
+        walk_on<W>(a, head_blocks, use);
     }
 }
 
-// `splits` CTAs per (problem, head) add the probabilities to the weights.
-__global__ void __launch_bounds__(kThreads) paged_weights_kernel(AttnArgs a, int splits)
+constexpr int kWThreads = 128;
+constexpr int kWRows = 4;                        // rows a thread has in flight
+
+// `splits` CTAs per (problem, head) add the probabilities to the weights. A chain of dependent reads (length, page,
+// score), so every thread takes several rows through it side by side.
+__global__ void __launch_bounds__(kWThreads) paged_weights_kernel(AttnArgs a, int splits)
 {
     extern __shared__ float2 sm_stat[];          // [G]
     const int at = blockIdx.x / splits, z = blockIdx.x - at * splits;
@@ -549,23 +748,46 @@ __global__ void __launch_bounds__(kThreads) paged_weights_kernel(AttnArgs a, int
     grid_release();
     const int len = read_len(a.c, n);
     const size_t head_at = ((size_t)n * a.c.H + h) * G;
+    for (int i = threadIdx.x; i < G; i += kWThreads) sm_stat[i] = a.stat[head_at + i];
     if (len < 0) {
         if (z == 0 && threadIdx.x == 0 && a.w_new) a.w_new[at] = 0.f;
         return;
     }
-    for (int i = threadIdx.x; i < G; i += kThreads) sm_stat[i] = a.stat[head_at + i];
-    __syncthreads();
-    for (int row = z * kThreads + threadIdx.x; row < len; row += splits * kThreads) {
-        const Slot s = find_slot(a.c, n, row);
-        if (s.page < 0) continue;
-        const size_t m = meta_index(a.c, h, s);
-        float w = 0.f;
-        for (int hd = 0; hd < G; ++hd) w = fmaf(fast_exp2(a.scores[m * G + hd] - sm_stat[hd].x), sm_stat[hd].y, w);
-        a.c.weight[m] = fmaf(a.c.weight[m], a.decay, w);
+    bool first = true;
+    for (int row0 = z * kWThreads * kWRows; first || row0 < len; row0 += splits * kWThreads * kWRows) {
+        size_t m[kWRows], at_score[kWRows];
+        float w[kWRows], old[kWRows];
+        bool there[kWRows];
+#pragma unroll
+        for (int r = 0; r < kWRows; ++r) {
+            const int row = row0 + r * kWThreads + threadIdx.x;
+            there[r] = false;
+            if (row >= len) continue;
+            const Slot s = find_slot(a.c, n, row);
+            there[r] = s.page >= 0;
+            m[r] = meta_index(a.c, h, s);
+            at_score[r] = ((size_t)((uint32_t)s.page * (uint32_t)a.c.H + (uint32_t)h) * G) * a.c.page_size + s.slot;
+        }
+#pragma unroll
+        for (int r = 0; r < kWRows; ++r) {
+            w[r] = 0.f;
+            if (there[r]) old[r] = a.c.weight[m[r]];
+        }
+        if (first) __syncthreads();
+        first = false;
+        for (int hd = 0; hd < G; ++hd) {
+            const float2 st = sm_stat[hd];
+#pragma unroll
+            for (int r = 0; r < kWRows; ++r)
+                if (there[r]) w[r] = fmaf(fast_exp2(fmaf(a.scores[at_score[r] + (size_t)hd * a.c.page_size], a.scale_log2e, -st.x)), st.y, w[r]);
+        }
+#pragma unroll
+        for (int r = 0; r < kWRows; ++r)
+            if (there[r]) a.c.weight[m[r]] = fmaf(old[r], a.decay, w[r]);
     }
     if (z == 0 && threadIdx.x == 0 && a.w_new) {
         float w = 0.f;
-        for (int hd = 0; hd < G; ++hd) w = fmaf(fast_exp2(a.score_new[head_at + hd] - sm_stat[hd].x), sm_stat[hd].y, w);
+        for (int hd = 0; hd < G; ++hd) w = fmaf(fast_exp2(fmaf(a.score_new[head_at + hd], a.scale_log2e, -sm_stat[hd].x)), sm_stat[hd].y, w);
         a.w_new[at] = w;
     }
 }
@@ -603,29 +825,44 @@ WsLayout layout(int N, int H, int D, int n_pages, int page_size, int G, int accu
     return w;
 }
 
-template <typename E, int D, int NT, bool GATHER>
+#ifndef EC_PAGED_MINPER
+#define EC_PAGED_MINPER 1
+#endif
+template <typename E, int D, int NT, int W, bool GATHER>
 cudaError_t launch(const AttnArgs &a, cudaStream_t stream)
 {
+    auto kernel = paged_attention_kernel<E, D, NT, W, GATHER>;
+    constexpr int smem = Smem<D, NT, W>::kTotal;
     const int head_blocks = (a.G + 8 * NT - 1) / (8 * NT);
-    int ctas = sm_count_here() * kCtasPerSm;
+    int ctas = sm_count_here() * (8 / W);
     if (ctas > kPagedMaxCtas) ctas = kPagedMaxCtas;
-    cudaError_t e = cudaFuncSetAttribute(paged_attention_kernel<E, D, NT, GATHER>, cudaFuncAttributeMaxDynamicSharedMemorySize, Ring<D>::kSmem);
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
-    e = launch_chained(paged_attention_kernel<E, D, NT, GATHER>, dim3((unsigned)ctas), kThreads, Ring<D>::kSmem, stream, a, head_blocks, 2);
+    e = launch_chained(kernel, dim3((unsigned)ctas), W * 32, smem, stream, a, head_blocks, EC_PAGED_MINPER);
     if (e != cudaSuccess || !GATHER) return e;
     // enough CTAs for the GPU, no more than there are rows
     const long long units = (long long)a.c.N * a.c.H;
     long long z = (148LL * 8 + units - 1) / units;
-    const long long most = ((long long)a.c.max_pages * a.c.page_size + kThreads - 1) / kThreads;
+    const long long most = ((long long)a.c.max_pages * a.c.page_size + kWThreads * kWRows - 1) / (kWThreads * kWRows);
     if (z > most) z = most;
-    return launch_chained(paged_weights_kernel, dim3((unsigned)(z * units)), kThreads, a.G * sizeof(float2), stream, a, (int)z);
+    return launch_chained(paged_weights_kernel, dim3((unsigned)(z * units)), kWThreads, a.G * sizeof(float2), stream, a, (int)z);
+}
+
+#ifndef EC_PAGED_NARROW
+#define EC_PAGED_NARROW 512
+#endif
+template <typename E, int D, bool GATHER>
+cudaError_t launch_g(const AttnArgs &a, cudaStream_t stream)
+{
+    if (a.G > 8) return launch<E, D, 2, 8, GATHER>(a, stream);
+    if ((long long)a.c.N * a.c.H >= EC_PAGED_NARROW) return launch<E, D, 1, 4, GATHER>(a, stream);
+    return launch<E, D, 1, 8, GATHER>(a, stream);
 }
 
 template <typename E, int D>
 cudaError_t launch_d(const AttnArgs &a, int accumulate, cudaStream_t stream)
 {
-    if (a.G <= 8) return accumulate ? launch<E, D, 1, true>(a, stream) : launch<E, D, 1, false>(a, stream);
-    return accumulate ? launch<E, D, 2, true>(a, stream) : launch<E, D, 2, false>(a, stream);
+    return accumulate ? launch_g<E, D, true>(a, stream) : launch_g<E, D, false>(a, stream);
 }
 
 }  // namespace
@@ -646,6 +883,7 @@ cudaError_t launch_paged_attention(const PagedView &c, int D, int dtype, const v
     a.v_new = static_cast<const uint4 *>(v_new);
     a.G = Hq / c.H;
     a.scale_log2e = scale * 1.4426950408889634f;
+    a.inv_scale = 1.f / a.scale_log2e;
     a.decay = decay;
     a.out = static_cast<uint32_t *>(out);
     a.lse = lse;
