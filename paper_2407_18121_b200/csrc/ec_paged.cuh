@@ -126,13 +126,34 @@ __device__ __forceinline__ int read_len(const PagedView &c, int n)
 
 }  // namespace
 
+// What turns an attention call's stored scores into weights: p = 2^(score * scale_log2e - maximum) / sum.
+struct GatherArgs {
+    const float2 *stat;                          // [N, Hq] (maximum in the log2 domain, 1 / sum); (0, 0) where no row is left
+    const float *scores;                         // [n_pages, H, G, page_size]: <q, k>, not scaled
+    const float *score_new;                      // [N, Hq] the same of the step's own row
+    float *w_new;                                // [N, H]; nullptr: the step has no row of its own
+    float scale_log2e, decay;
+    int G;
+};
+
+struct AppendArgs {
+    const uint4 *K_new, *V_new;
+    const float *w_new;
+    const int *pos_new, *counts;
+    int T, fresh, budget, recent, sinks;
+    int *moves;                                  // workspace: [N * H] rows to move
+    int2 *list;                                  // workspace: [N * H][budget]: .x = slot to fill, .y = candidate to take
+    unsigned long long *lowest;                  // workspace: [N * H][kMaxSplits] lowest candidate of every part
+};
+
 size_t paged_attention_workspace_bytes(const ec_paged *c, int Hq, int accumulate);
+// accumulate: *gather is filled for the launch that adds the probabilities to the weights.
 cudaError_t launch_paged_attention(const PagedView &c, int D, int dtype, const void *q, const void *k_new, const void *v_new,
                                    int Hq, float scale, int accumulate, float decay, void *out, float *lse, float *w_new,
-                                   void *ws, cudaStream_t stream);
+                                   void *ws, GatherArgs *gather, cudaStream_t stream);
 size_t paged_append_workspace_bytes(const ec_paged *c, int T, int budget);
-cudaError_t launch_paged_append(const PagedView &c, int D, const void *K_new, const void *V_new, const float *w_new,
-                                const int *pos_new, const int *counts, int T, int fresh, int budget, int recent, int sinks,
-                                void *ws, cudaStream_t stream);
+// Either may be nullptr, not both. With both, append->w_new is gather->w_new.
+cudaError_t launch_paged_rows(const PagedView &c, int D, const GatherArgs *gather, AppendArgs *append, void *ws_append,
+                              cudaStream_t stream);
 
 }  // namespace ec

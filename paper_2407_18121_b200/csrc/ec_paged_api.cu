@@ -91,6 +91,23 @@ int check_budget(const ec_paged *c, int T, int budget, int recent, int sinks)
     return EC_OK;
 }
 
+ec::AppendArgs append_args(const void *K_new, const void *V_new, const float *w_new, const int32_t *pos_new, const int32_t *counts,
+                           int T, int fresh, int budget, int recent, int sinks)
+{
+    ec::AppendArgs a = {};
+    a.K_new = static_cast<const uint4 *>(K_new);
+    a.V_new = static_cast<const uint4 *>(V_new);
+    a.w_new = w_new;
+    a.pos_new = pos_new;
+    a.counts = counts;
+    a.T = T;
+    a.fresh = fresh;
+    a.budget = budget;
+    a.recent = recent;
+    a.sinks = sinks;
+    return a;
+}
+
 int check_ws(const void *ws, size_t have, size_t need)
 {
     if (!ws || have < need) return EC_ERR_WORKSPACE;
@@ -176,8 +193,11 @@ int ec_paged_attention(const void *q, const void *k_new, const void *v_new, cons
     if (!aligned(w_new, 4)) return EC_ERR_ALIGN;
     st = check_ws(ws, ws_bytes, ec::paged_attention_workspace_bytes(c, Hq, accumulate));
     if (st != EC_OK) return st;
-    return ec::launch_paged_attention(view(c), c->D, c->dtype, q, k_new, v_new, Hq, scale, accumulate, decay, out, lse, w_new, ws,
-                                      (cudaStream_t)stream) == cudaSuccess ? EC_OK : EC_ERR_CUDA;
+    ec::GatherArgs gather;
+    cudaError_t e = ec::launch_paged_attention(view(c), c->D, c->dtype, q, k_new, v_new, Hq, scale, accumulate, decay, out, lse, w_new,
+                                               ws, &gather, (cudaStream_t)stream);
+    if (e == cudaSuccess && accumulate) e = ec::launch_paged_rows(view(c), c->D, &gather, nullptr, nullptr, (cudaStream_t)stream);
+    return e == cudaSuccess ? EC_OK : EC_ERR_CUDA;
 }
 
 size_t ec_paged_append_workspace(const ec_paged *c, int T, int budget)
@@ -199,8 +219,8 @@ int ec_paged_append(const void *K_new, const void *V_new, const float *w_new, co
         return EC_ERR_ALIGN;
     st = check_ws(ws, ws_bytes, ec::paged_append_workspace_bytes(c, T, budget));
     if (st != EC_OK) return st;
-    return ec::launch_paged_append(view(c), c->D, K_new, V_new, w_new, pos_new, counts, T, fresh, budget, recent, sinks, ws,
-                                   (cudaStream_t)stream) == cudaSuccess ? EC_OK : EC_ERR_CUDA;
+    ec::AppendArgs a = append_args(K_new, V_new, w_new, pos_new, counts, T, fresh, budget, recent, sinks);
+    return ec::launch_paged_rows(view(c), c->D, nullptr, &a, ws, (cudaStream_t)stream) == cudaSuccess ? EC_OK : EC_ERR_CUDA;
 }
 
 size_t ec_paged_step_workspace(const ec_paged *c, int Hq, int budget)
@@ -224,11 +244,13 @@ int ec_paged_decode_step(const void *q, const void *k_new, const void *v_new, co
     char *p = static_cast<char *>(ws);
     float *w_new = reinterpret_cast<float *>(p + ec::paged_attention_workspace_bytes(c, Hq, 1));
     void *ws_append = reinterpret_cast<char *>(w_new) + round256((size_t)c->N * c->H * sizeof(float));
+    ec::GatherArgs gather;
     cudaError_t e = ec::launch_paged_attention(view(c), c->D, c->dtype, q, k_new, v_new, Hq, scale, 1, decay, out, lse, w_new, ws,
-                                               (cudaStream_t)stream);
-    if (e == cudaSuccess)
-        e = ec::launch_paged_append(view(c), c->D, k_new, v_new, w_new, nullptr, nullptr, 1, 0, budget, recent, sinks, ws_append,
-                                    (cudaStream_t)stream);
+                                               &gather, (cudaStream_t)stream);
+    if (e == cudaSuccess) {
+        ec::AppendArgs a = append_args(k_new, v_new, w_new, nullptr, nullptr, 1, 0, budget, recent, sinks);
+        e = ec::launch_paged_rows(view(c), c->D, &gather, &a, ws_append, (cudaStream_t)stream);
+    }
     return e == cudaSuccess ? EC_OK : EC_ERR_CUDA;
 }
 

@@ -82,9 +82,9 @@ struct AttnArgs {
     const uint32_t *q;
     const uint4 *k_new, *v_new;                  // k_new == nullptr: the cached rows alone
     int G;                                       // query heads per key / value head
-    float scale_log2e, inv_scale, decay;         // inv_scale: 1 / scale_log2e
+    float scale_log2e, inv_scale;                // inv_scale: 1 / scale_log2e
     uint32_t *out;
-    float *lse, *w_new;
+    float *lse;
     // workspace
     float2 *stat;                                // [N, Hq] (maximum in the log2 domain, 1 / sum)
     float *score_new;                            // [N, Hq] the same of the step's own row
@@ -733,65 +733,6 @@ __global__ void __launch_bounds__(W * 32, 8 / W) paged_attention_kernel(AttnArgs
     }
 }
 
-constexpr int kWThreads = 128;
-constexpr int kWRows = 4;                        // rows a thread has in flight
-
-// `splits` CTAs per (problem, head) add the probabilities to the weights. A chain of dependent reads (length, page,
-// score), so every thread takes several rows through it side by side.
-__global__ void __launch_bounds__(kWThreads) paged_weights_kernel(AttnArgs a, int splits)
-{
-    extern __shared__ float2 sm_stat[];          // [G]
-    const int at = blockIdx.x / splits, z = blockIdx.x - at * splits;
-    const int n = at / a.c.H, h = at - n * a.c.H;
-    const int G = a.G;
-    grid_wait();
-    grid_release();
-    const int len = read_len(a.c, n);
-    const size_t head_at = ((size_t)n * a.c.H + h) * G;
-    for (int i = threadIdx.x; i < G; i += kWThreads) sm_stat[i] = a.stat[head_at + i];
-    if (len < 0) {
-        if (z == 0 && threadIdx.x == 0 && a.w_new) a.w_new[at] = 0.f;
-        return;
-    }
-    bool first = true;
-    for (int row0 = z * kWThreads * kWRows; first || row0 < len; row0 += splits * kWThreads * kWRows) {
-        size_t m[kWRows], at_score[kWRows];
-        float w[kWRows], old[kWRows];
-        bool there[kWRows];
-#pragma unroll
-        for (int r = 0; r < kWRows; ++r) {
-            const int row = row0 + r * kWThreads + threadIdx.x;
-            there[r] = false;
-            if (row >= len) continue;
-            const Slot s = find_slot(a.c, n, row);
-            there[r] = s.page >= 0;
-            m[r] = meta_index(a.c, h, s);
-            at_score[r] = ((size_t)((uint32_t)s.page * (uint32_t)a.c.H + (uint32_t)h) * G) * a.c.page_size + s.slot;
-        }
-#pragma unroll
-        for (int r = 0; r < kWRows; ++r) {
-            w[r] = 0.f;
-            if (there[r]) old[r] = a.c.weight[m[r]];
-        }
-        if (first) __syncthreads();
-        first = false;
-        for (int hd = 0; hd < G; ++hd) {
-            const float2 st = sm_stat[hd];
-#pragma unroll
-            for (int r = 0; r < kWRows; ++r)
-                if (there[r]) w[r] = fmaf(fast_exp2(fmaf(a.scores[at_score[r] + (size_t)hd * a.c.page_size], a.scale_log2e, -st.x)), st.y, w[r]);
-        }
-#pragma unroll
-        for (int r = 0; r < kWRows; ++r)
-            if (there[r]) a.c.weight[m[r]] = fmaf(old[r], a.decay, w[r]);
-    }
-    if (z == 0 && threadIdx.x == 0 && a.w_new) {
-        float w = 0.f;
-        for (int hd = 0; hd < G; ++hd) w = fmaf(fast_exp2(fmaf(a.score_new[head_at + hd], a.scale_log2e, -sm_stat[hd].x)), sm_stat[hd].y, w);
-        a.w_new[at] = w;
-    }
-}
-
 inline size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
 inline int sm_count_here()
@@ -838,14 +779,7 @@ cudaError_t launch(const AttnArgs &a, cudaStream_t stream)
     if (ctas > kPagedMaxCtas) ctas = kPagedMaxCtas;
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
-    e = launch_chained(kernel, dim3((unsigned)ctas), W * 32, smem, stream, a, head_blocks, EC_PAGED_MINPER);
-    if (e != cudaSuccess || !GATHER) return e;
-    // enough CTAs for the GPU, no more than there are rows
-    const long long units = (long long)a.c.N * a.c.H;
-    long long z = (148LL * 8 + units - 1) / units;
-    const long long most = ((long long)a.c.max_pages * a.c.page_size + kWThreads * kWRows - 1) / (kWThreads * kWRows);
-    if (z > most) z = most;
-    return launch_chained(paged_weights_kernel, dim3((unsigned)(z * units)), kWThreads, a.G * sizeof(float2), stream, a, (int)z);
+    return launch_chained(kernel, dim3((unsigned)ctas), W * 32, smem, stream, a, head_blocks, EC_PAGED_MINPER);
 }
 
 #ifndef EC_PAGED_NARROW
@@ -874,7 +808,7 @@ size_t paged_attention_workspace_bytes(const ec_paged *c, int Hq, int accumulate
 
 cudaError_t launch_paged_attention(const PagedView &c, int D, int dtype, const void *q, const void *k_new, const void *v_new,
                                    int Hq, float scale, int accumulate, float decay, void *out, float *lse, float *w_new,
-                                   void *ws, cudaStream_t stream)
+                                   void *ws, GatherArgs *gather, cudaStream_t stream)
 {
     AttnArgs a;
     a.c = c;
@@ -884,10 +818,8 @@ cudaError_t launch_paged_attention(const PagedView &c, int D, int dtype, const v
     a.G = Hq / c.H;
     a.scale_log2e = scale * 1.4426950408889634f;
     a.inv_scale = 1.f / a.scale_log2e;
-    a.decay = decay;
     a.out = static_cast<uint32_t *>(out);
     a.lse = lse;
-    a.w_new = k_new ? w_new : nullptr;
     const WsLayout w = layout(c.N, c.H, D, c.n_pages, c.page_size, a.G, accumulate);
     char *p = static_cast<char *>(ws);
     a.stat = reinterpret_cast<float2 *>(p + w.stat);
@@ -895,6 +827,7 @@ cudaError_t launch_paged_attention(const PagedView &c, int D, int dtype, const v
     a.part_o = reinterpret_cast<float *>(p + w.part_o);
     a.part_ml = reinterpret_cast<float2 *>(p + w.part_ml);
     a.scores = reinterpret_cast<float *>(p + w.scores);
+    if (accumulate) *gather = {a.stat, a.scores, a.score_new, k_new ? w_new : nullptr, a.scale_log2e, decay, a.G};
     if (dtype == EC_BF16) return D == 128 ? launch_d<Bf16, 128>(a, accumulate, stream) : launch_d<Bf16, 64>(a, accumulate, stream);
     return D == 128 ? launch_d<Fp16, 128>(a, accumulate, stream) : launch_d<Fp16, 64>(a, accumulate, stream);
 }
