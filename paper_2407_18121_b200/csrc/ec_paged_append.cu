@@ -17,7 +17,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kFewRows = 16;                     // up to this many new rows the deciding CTA moves them itself
-constexpr int kMaxSplits = 160;                  // CTAs that share a unit's rows in a step
+constexpr int kMaxSplits = 512;                  // CTAs that share a unit's rows in a step
 
 constexpr uint32_t kKeyProtected = 0xFFFFFFFFu, kKeyNan = 0xFFFFFFFEu;
 
@@ -277,7 +277,12 @@ __global__ void paged_commit_kernel(PagedView c, AppendArgs a)
 }
 
 constexpr int kRowThreads = 128;
-constexpr int kRowsHeld = 4;                     // rows a thread has in flight
+#ifndef EC_RC
+#define EC_RC 8
+#endif
+constexpr int kRowCtas = EC_RC;                      // per SM
+constexpr int kScoresHeld = 4;                   // query heads whose scores a thread reads side by side
+constexpr int kRowsHeld = 4;                      // rows a thread has in flight
 
 // The row that leaves first has the smallest of these: key, then the higher candidate.
 __device__ __forceinline__ unsigned long long leave_order(uint32_t key, int j)
@@ -289,14 +294,15 @@ __device__ __forceinline__ unsigned long long leave_order(uint32_t key, int j)
 // new row per problem joins; of the problem's CTAs the one that arrives last changes its length, and where a unit's rows
 // are shared, decides and moves for all of its heads.
 template <bool GATHER, bool APPEND>
-__global__ void __launch_bounds__(kRowThreads) paged_rows_kernel(PagedView c, GatherArgs ga, AppendArgs ap, int lpr, int splits)
+__global__ void __launch_bounds__(kRowThreads, kRowCtas) paged_rows_kernel(PagedView c, GatherArgs ga, AppendArgs ap, int lpr, int splits)
 {
     extern __shared__ float2 sm_stat[];          // [G]
     __shared__ unsigned long long sm_low[kRowThreads / 32];
     __shared__ int sm_last;
     __shared__ SelectSmem<kRowThreads> sm_select;
-    grid_wait();
-    grid_release();
+    // With GATHER the launch in front is the attention of the same call, which lets this one in only when everything
+    // before it is complete and writes no length, page, weight or position: those are read ahead of the wait.
+    if (!GATHER) grid_wait();
     const int unit = blockIdx.x / splits, z = blockIdx.x - unit * splits;
     const int n = unit / c.H, h = unit - n * c.H;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -311,9 +317,9 @@ __global__ void __launch_bounds__(kRowThreads) paged_rows_kernel(PagedView c, Ga
         u.u = unit;
         u.had = read_len(c, n);
     }
-    if (GATHER)
-        for (int i = threadIdx.x; i < G; i += kRowThreads) sm_stat[i] = ga.stat[head_at + i];
     if (u.had < 0) {                             // an empty place of the batch
+        if (GATHER) grid_wait();
+        grid_release();
         if (GATHER && z == 0 && threadIdx.x == 0 && ga.w_new) ga.w_new[unit] = 0.f;
         return;
     }
@@ -323,7 +329,7 @@ __global__ void __launch_bounds__(kRowThreads) paged_rows_kernel(PagedView c, Ga
     bool first = true;
     for (int row0 = z * kRowThreads * kRowsHeld; first || row0 < u.had; row0 += splits * kRowThreads * kRowsHeld) {
         uint32_t m[kRowsHeld];
-        size_t at_score[kRowsHeld];
+        const float *score[kRowsHeld];
         float w[kRowsHeld];
         int pos[kRowsHeld];
         bool there[kRowsHeld];
@@ -335,7 +341,7 @@ __global__ void __launch_bounds__(kRowThreads) paged_rows_kernel(PagedView c, Ga
             const Slot s = find_slot(c, n, row);
             there[r] = s.page >= 0;
             m[r] = meta_index(c, h, s);
-            at_score[r] = ((size_t)((uint32_t)s.page * (uint32_t)c.H + (uint32_t)h) * G) * c.page_size + s.slot;
+            if (GATHER) score[r] = ga.scores + (size_t)((uint32_t)s.page * (uint32_t)c.H + (uint32_t)h) * G * c.page_size + s.slot;
             if (APPEND && !there[r]) low = min(low, leave_order(0, row)); // a row that cannot be read leaves first
         }
 #pragma unroll
@@ -345,18 +351,31 @@ __global__ void __launch_bounds__(kRowThreads) paged_rows_kernel(PagedView c, Ga
             w[r] = c.weight[m[r]];
             if (APPEND) pos[r] = c.pos[m[r]];
         }
-        if (GATHER && first) __syncthreads();
-        first = false;
         if (GATHER) {
-            float p[kRowsHeld];
+            if (first) {
+                grid_wait();
+                for (int i = threadIdx.x; i < G; i += kRowThreads) sm_stat[i] = __ldcg(&ga.stat[head_at + i]);
+            }
+            float p[kRowsHeld], x[kScoresHeld][kRowsHeld];
 #pragma unroll
             for (int r = 0; r < kRowsHeld; ++r) p[r] = 0.f;
-#pragma unroll 4
-            for (int hd = 0; hd < G; ++hd) {
-                const float2 st = sm_stat[hd];
+            for (int h0 = 0; h0 < G; h0 += kScoresHeld) {
 #pragma unroll
-                for (int r = 0; r < kRowsHeld; ++r)
-                    if (there[r]) p[r] = fmaf(fast_exp2(fmaf(ga.scores[at_score[r] + (size_t)hd * c.page_size], ga.scale_log2e, -st.x)), st.y, p[r]);
+                for (int i = 0; i < kScoresHeld; ++i) {
+                    if (h0 + i >= G) continue;
+#pragma unroll
+                    for (int r = 0; r < kRowsHeld; ++r)
+                        if (there[r]) x[i][r] = __ldcg(score[r] + (size_t)(h0 + i) * c.page_size);
+                }
+                if (first && h0 == 0) __syncthreads();
+#pragma unroll
+                for (int i = 0; i < kScoresHeld; ++i) {
+                    if (h0 + i >= G) continue;
+                    const float2 st = sm_stat[h0 + i];
+#pragma unroll
+                    for (int r = 0; r < kRowsHeld; ++r)
+                        if (there[r]) p[r] = fmaf(fast_exp2(fmaf(x[i][r], ga.scale_log2e, -st.x)), st.y, p[r]);
+                }
             }
 #pragma unroll
             for (int r = 0; r < kRowsHeld; ++r) {
@@ -365,6 +384,7 @@ __global__ void __launch_bounds__(kRowThreads) paged_rows_kernel(PagedView c, Ga
                 c.weight[m[r]] = w[r];
             }
         }
+        first = false;
         if (APPEND) {
 #pragma unroll
             for (int r = 0; r < kRowsHeld; ++r) {
@@ -374,6 +394,7 @@ __global__ void __launch_bounds__(kRowThreads) paged_rows_kernel(PagedView c, Ga
             }
         }
     }
+    grid_release();
     // the new row's own share
     float w_own = 0.f;
     if (GATHER && ga.w_new && z == 0 && warp == 0) {
@@ -460,7 +481,7 @@ __global__ void __launch_bounds__(kRowThreads) paged_rows_kernel(PagedView c, Ga
 // CTAs per unit of a rows launch: one round of rows each, up to about 16 CTAs per SM in all.
 inline int row_splits(long long units, long long rows)
 {
-    long long z = (148LL * 16 + units - 1) / units;
+    long long z = (148LL * kRowCtas + units - 1) / units;
     const long long most = (rows + kRowThreads * kRowsHeld - 1) / (kRowThreads * kRowsHeld);
     if (z > most) z = most;
     if (z > kMaxSplits) z = kMaxSplits;

@@ -362,6 +362,8 @@ __global__ void __launch_bounds__(W * 32, 8 / W) paged_attention_kernel(AttnArgs
     __shared__ Plan plan;
     __shared__ int sm_last;
 
+    // The release stands behind the wait on purpose: a launch that this one lets in early may then read whatever earlier
+    // launches wrote before it waits for this one (paged_rows_kernel does).
     grid_wait();
     grid_release();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
@@ -576,19 +578,6 @@ __global__ void __launch_bounds__(W * 32, 8 / W) paged_attention_kernel(AttnArgs
                     s[nt][2 + i] = there1 ? s[nt][2 + i] + s1[nt][2 + i] : -INFINITY;
                     raise |= fmaxf(s[nt][i], s[nt][2 + i]) > limit[nt][i];
                 }
-                if (GATHER) {
-                    const int hd = nt * 8 + 2 * t;
-#pragma unroll
-                    for (int r = 0; r < 2; ++r) {
-                        const uint2 info = r ? info1 : info0;
-                        if (info.x == kRowNone) continue;
-                        const bool own = info.x == kRowNew;
-                        float *dst = own ? a.score_new + head_at : a.scores + ((size_t)info.x * G + head0) * a.c.page_size + info.y;
-                        const int step = own ? 1 : a.c.page_size;
-                        if (hd < heads) dst[(size_t)hd * step] = s[nt][2 * r];
-                        if (hd + 1 < heads) dst[(size_t)(hd + 1) * step] = s[nt][2 * r + 1];
-                    }
-                }
             }
             if (__any_sync(0xFFFFFFFFu, raise)) {
 #pragma unroll
@@ -638,6 +627,23 @@ __global__ void __launch_bounds__(W * 32, 8 / W) paged_attention_kernel(AttnArgs
                     for (int nt = 0; nt < NT; ++nt) {
                         E::mma(o[nt][mt], av, hi[nt][0], hi[nt][1]);
                         E::mma(o[nt][mt], av, lo[nt][0], lo[nt][1]);
+                    }
+                }
+            }
+            if (GATHER) {                        // behind the products: the stores' addresses are in nobody's way here
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    const uint2 info = r ? info1 : info0;
+                    if (info.x == kRowNone) continue;
+                    const bool own = info.x == kRowNew;
+                    const int step = own ? 1 : a.c.page_size;
+                    float *dst = (own ? a.score_new + head_at : a.scores + ((size_t)info.x * G + head0) * a.c.page_size + info.y) +
+                                 (size_t)(2 * t) * step;
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        const int hd = nt * 8 + 2 * t;
+                        if (hd < heads) dst[(size_t)(nt * 8) * step] = s[nt][2 * r];
+                        if (hd + 1 < heads) dst[(size_t)(nt * 8 + 1) * step] = s[nt][2 * r + 1];
                     }
                 }
             }
