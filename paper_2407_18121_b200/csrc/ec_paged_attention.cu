@@ -93,11 +93,11 @@ struct AttnArgs {
     float *scores;                               // [n_pages, H, G, page_size]: <q, k>, not scaled
 };
 
-// Rows of problem n with its own new row, 0 when there is nothing to attend to.
+// Rows of problem n with its own new row, 0 when there is nothing to attend to. A length past the table's reach is cut.
 __device__ __forceinline__ int rows_of(const AttnArgs &a, int n)
 {
-    const int len = read_len(a.c, n);
-    return len < 0 ? 0 : len + (a.k_new ? 1 : 0);
+    const int len = a.c.lens[n];
+    return len < 0 ? 0 : min(len, a.c.max_pages * a.c.page_size) + (a.k_new ? 1 : 0);
 }
 
 // Every CTA derives the same plan from the lengths. Work is counted in blocks of W tiles, and every unit counts for
@@ -116,48 +116,53 @@ __device__ __forceinline__ int blocks_of(int rows) { return (rows + W * kTile - 
 template <int W>
 __device__ __forceinline__ int cost_of(int rows) { return rows > 0 ? blocks_of<W>(rows) + kUnitCost : 0; }
 
+// Each warp works it out for itself: a lane sums a span of problems, no barrier.
 template <int W>
-__device__ __forceinline__ void make_plan(const AttnArgs &a, int units, int min_per, Plan *plan)
+__device__ __forceinline__ Plan make_plan(const AttnArgs &a, int units)
 {
-    __shared__ int warp_sum[W];
-    const int N = a.c.N;
-    const int span = (N + W * 32 - 1) / (W * 32);
-    const int n0 = min((int)threadIdx.x * span, N), n1 = min(n0 + span, N);
-    int mine = 0;
-    for (int n = n0; n < n1; ++n) mine += cost_of<W>(rows_of(a, n));
+    const int N = a.c.N, lane = threadIdx.x & 31;
+    const int span = (N + 31) >> 5;
+    const int n0 = min(lane * span, N), n1 = min(n0 + span, N);
+    int mine = 0, rows = 0;
+#pragma unroll 8
+    for (int n = n0; n < n1; ++n) {
+        rows = rows_of(a, n);                    // with one problem a lane this is the one needed below
+        mine += cost_of<W>(rows);
+    }
     int incl = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
         const int up = __shfl_up_sync(0xFFFFFFFFu, incl, o);
-        if ((threadIdx.x & 31) >= o) incl += up;
+        if (lane >= o) incl += up;
     }
-    if ((threadIdx.x & 31) == 31) warp_sum[threadIdx.x >> 5] = incl;
-    if (threadIdx.x == 0) plan->n = -1;
-    __syncthreads();
-    int total = 0, base = incl - mine;
-#pragma unroll
-    for (int w = 0; w < W; ++w) {
-        if (w < (int)(threadIdx.x >> 5)) base += warp_sum[w];
-        total += warp_sum[w];
-    }
-    const int per = max((int)(((unsigned)(total * units) + gridDim.x - 1) / gridDim.x), min_per);
-    const int first = per * blockIdx.x;
-    if (threadIdx.x == 0) plan->per = per;
-    // the thread whose span holds the CTA's first block names the problem
-    if (first >= base * units && first < (base + mine) * units) {
-        int at = base * units;
-        for (int n = n0; n < n1; ++n) {
-            const int rows = rows_of(a, n), cost = cost_of<W>(rows) * units;
-            if (first < at + cost) {
-                plan->n = n;
-                plan->rows = rows;
-                plan->before = at;
-                break;
+    const int total = __shfl_sync(0xFFFFFFFFu, incl, 31) * units;
+    Plan plan;
+    plan.per = (int)(((unsigned)total + gridDim.x - 1) / gridDim.x);
+    plan.n = -1;
+    plan.rows = plan.before = 0;
+    const int first = plan.per * (int)blockIdx.x;
+    if (first >= total) return plan;
+    // the lane whose span holds the CTA's first block names the problem
+    int at = (incl - mine) * units, n = n0;
+    const bool here = first >= at && first < incl * units;
+    if (here && span > 1) {
+        int begin = at;
+#pragma unroll 8
+        for (int i = n0; i < n1; ++i) {
+            const int r = rows_of(a, i), cost = cost_of<W>(r) * units;
+            if (first >= begin && first < begin + cost) {
+                n = i;
+                rows = r;
+                at = begin;
             }
-            at += cost;
+            begin += cost;
         }
     }
-    __syncthreads();
+    const int src = __ffs(__ballot_sync(0xFFFFFFFFu, here)) - 1;
+    plan.n = __shfl_sync(0xFFFFFFFFu, n, src);
+    plan.rows = __shfl_sync(0xFFFFFFFFu, rows, src);
+    plan.before = __shfl_sync(0xFFFFFFFFu, at, src);
+    return plan;
 }
 
 // A place in the CTA's run of blocks. Every warp walks it three times: for the page table, S tiles behind for the copies,
@@ -348,7 +353,7 @@ __device__ __forceinline__ void join_parts(const AttnArgs &a, int c0, int c1, in
 
 // NT: groups of 8 query heads that share a pass over the rows. W: warps of a CTA. GATHER: scores are stored for the weights.
 template <typename E, int D, int NT, int W, bool GATHER>
-__global__ void __launch_bounds__(W * 32, 8 / W) paged_attention_kernel(AttnArgs a, int head_blocks, int min_per)
+__global__ void __launch_bounds__(W * 32, 8 / W) paged_attention_kernel(AttnArgs a, int head_blocks)
 {
     using M_ = Smem<D, NT, W>;
     constexpr int kThreads = W * 32, kBlockRows = W * kTile;
@@ -359,7 +364,6 @@ __global__ void __launch_bounds__(W * 32, 8 / W) paged_attention_kernel(AttnArgs
     float *sm_o = reinterpret_cast<float *>(smem + M_::kMerge);
     __shared__ float2 sm_ml[W][8 * NT];
     __shared__ float sm_inv[2 * 8 * NT];
-    __shared__ Plan plan;
     __shared__ int sm_last;
 
     // The release stands behind the wait on purpose: a launch that this one lets in early may then read whatever earlier
@@ -369,9 +373,10 @@ __global__ void __launch_bounds__(W * 32, 8 / W) paged_attention_kernel(AttnArgs
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int G = a.G, H = a.c.H, Hq = H * G;
     const int units = H * head_blocks;           // of a problem
-    make_plan<W>(a, units, min_per, &plan);
+    const Plan plan = make_plan<W>(a, units);
     // problems without a row to attend to have no block: their outputs are written here
     for (int n = blockIdx.x; n < a.c.N; n += gridDim.x) {
+        read_len(a.c, n);                        // reports a length past the table's reach
         if (rows_of(a, n) > 0) continue;
         for (int i = threadIdx.x; i < Hq * (D / 2); i += kThreads) a.out[(size_t)n * Hq * (D / 2) + i] = 0;
         for (int i = threadIdx.x; i < Hq; i += kThreads) {
@@ -772,9 +777,6 @@ WsLayout layout(int N, int H, int D, int n_pages, int page_size, int G, int accu
     return w;
 }
 
-#ifndef EC_PAGED_MINPER
-#define EC_PAGED_MINPER 1
-#endif
 template <typename E, int D, int NT, int W, bool GATHER>
 cudaError_t launch(const AttnArgs &a, cudaStream_t stream)
 {
@@ -785,7 +787,7 @@ cudaError_t launch(const AttnArgs &a, cudaStream_t stream)
     if (ctas > kPagedMaxCtas) ctas = kPagedMaxCtas;
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
-    return launch_chained(kernel, dim3((unsigned)ctas), W * 32, smem, stream, a, head_blocks, EC_PAGED_MINPER);
+    return launch_chained(kernel, dim3((unsigned)ctas), W * 32, smem, stream, a, head_blocks);
 }
 
 #ifndef EC_PAGED_NARROW
