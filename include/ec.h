@@ -21,8 +21,9 @@
  *  - Pointers named "dev" are CUDA device pointers of the current device; "host" pointers
  *    are ordinary host memory. The caller owns every buffer. No call allocates device
  *    memory, and no call depends on an earlier one except through the buffers and the
- *    ec_cache struct the caller passes (the library only caches a driver entry point and,
- *    for ec_decode_step_noalloc, the address of its built-in scratch).
+ *    ec_cache struct the caller passes (the library only caches a driver entry point, which
+ *    kernels have had their shared memory raised, and, for ec_decode_step_noalloc, the address
+ *    of its built-in scratch).
  *  - bf16 tensors are passed as `const void*` to 2-byte elements, row-major, innermost
  *    dimension contiguous, base address 16-byte aligned. D (head_dim) is 64 or 128.
  *  - N counts independent problems (batch x layers folded), H heads per problem. A "unit"

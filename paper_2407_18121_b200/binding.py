@@ -429,20 +429,26 @@ def _want(t: Optional[torch.Tensor], name: str, dtype: torch.dtype, shape: tuple
     """Device pointer of an argument after checking type, shape, layout and device (None stays None)."""
     if t is None:
         return None
-    if t.dtype != dtype or t.shape != shape:
-        raise ValueError(f"{name} must be {dtype} {list(shape)}, got {t.dtype} {list(t.shape)}")
-    if t.get_device() != device:
-        raise ValueError(f"{name} must be on the cache's device")
-    if not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != device or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor {list(shape)} on the cache's device {device}, "
+                         f"got {t.dtype} {list(t.shape)} on {t.device}")
     return t.data_ptr()
 
 
-def _paged_stream(cache: ec_paged) -> int:
+def _scratch(ws: torch.Tensor, device: int) -> int:
+    if ws.get_device() != device or not ws.is_contiguous():
+        raise ValueError("ws must be a contiguous tensor on the cache's device")
+    return ws.data_ptr()
+
+
+_current_device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+
+
+def _paged_stream(device: int) -> int:
     """The current stream; the cache's device has to be the current one, as the kernels launch there."""
-    if torch.cuda.current_device() != cache._device:
+    if _current_device() != device:
         raise ValueError("the cache's device is not the current CUDA device")
-    return torch._C._cuda_getCurrentRawStream(cache._device)
+    return _raw_stream(device)
 
 
 def ec_paged_state_bytes(N: int) -> int:
@@ -462,9 +468,8 @@ def ec_paged_init(Kp: torch.Tensor, Vp: torch.Tensor, weight: torch.Tensor, pos:
     N, max_pages = table.shape
     dev = Kp.device.index
     c = ec_paged()
-    c._device = dev
+    c._dims = (N, H, D, Kp.dtype, dev)
     c._tensors = (Kp, Vp, weight, pos, table, lens, seen, state)
-    c._dtype = Kp.dtype
     rows = (n_pages, H, page_size)
     if state.numel() * state.element_size() < ec_paged_state_bytes(N) or not state.is_contiguous() or state.device != Kp.device:
         raise ValueError("state must hold ec_paged_state_bytes(N) bytes on the cache's device")
@@ -477,7 +482,7 @@ def ec_paged_init(Kp: torch.Tensor, Vp: torch.Tensor, weight: torch.Tensor, pos:
                              _want(pos, "pos", torch.int32, rows, dev), _want(table, "table", torch.int32, (N, max_pages), dev),
                              _want(lens, "lens", torch.int32, (N,), dev), _want(seen, "seen", torch.int32, (N,), dev),
                              state.data_ptr(), N, H, D, page_size, n_pages, max_pages, _ELEM[Kp.dtype], ps, hs, rs,
-                             _paged_stream(c))
+                             _paged_stream(dev))
     _check(st, "ec_paged_init")
     return c
 
@@ -501,13 +506,13 @@ def ec_paged_attention(q: torch.Tensor, k_new: Optional[torch.Tensor], v_new: Op
     """Attention of one new token per problem over its paged rows and its own row. q, out (out): [N,Hq,D]; k_new,
     v_new: [N,H,D], both None for the cached rows alone; lse (out, optional): fp32 [N,Hq]. accumulate: every cached
     row's weight becomes decay * weight + the group's probability, and w_new (out) fp32 [N,H] is the new row's."""
-    N, H, D, dt, dev = cache.N, cache.H, cache.D, cache._dtype, cache._device
+    N, H, D, dt, dev = cache._dims
     Hq = q.shape[1]
     st = lib().ec_paged_attention(_want(q, "q", dt, (N, Hq, D), dev), _want(k_new, "k_new", dt, (N, H, D), dev),
                                   _want(v_new, "v_new", dt, (N, H, D), dev), C.byref(cache), Hq, scale, int(bool(accumulate)),
                                   decay, _want(out, "out", dt, (N, Hq, D), dev), _want(lse, "lse", torch.float32, (N, Hq), dev),
-                                  _want(w_new, "w_new", torch.float32, (N, H), dev), _ptr(ws),
-                                  ws.numel() * ws.element_size(), _paged_stream(cache))
+                                  _want(w_new, "w_new", torch.float32, (N, H), dev), _scratch(ws, dev),
+                                  ws.nbytes, _paged_stream(dev))
     _check(st, "ec_paged_attention")
 
 
@@ -520,13 +525,13 @@ def ec_paged_append(K_new: Optional[torch.Tensor], V_new: Optional[torch.Tensor]
                     budget: int, recent: int, sinks: int, ws: torch.Tensor) -> None:
     """T new rows per problem join the cache, each head then keeps its `budget` rows of largest weight. K_new, V_new:
     [N,H,T,D] (None: eviction alone); w_new fp32, pos_new int32 [N,H,T] and counts int32 [N] are optional."""
-    N, H, D, dt, dev = cache.N, cache.H, cache.D, cache._dtype, cache._device
+    N, H, D, dt, dev = cache._dims
     T = 0 if K_new is None else K_new.shape[2]
     st = lib().ec_paged_append(_want(K_new, "K_new", dt, (N, H, T, D), dev), _want(V_new, "V_new", dt, (N, H, T, D), dev),
                                _want(w_new, "w_new", torch.float32, (N, H, T), dev),
                                _want(pos_new, "pos_new", torch.int32, (N, H, T), dev),
                                _want(counts, "counts", torch.int32, (N,), dev), C.byref(cache), T, int(bool(fresh)), int(budget),
-                               int(recent), int(sinks), _ptr(ws), ws.numel() * ws.element_size(), _paged_stream(cache))
+                               int(recent), int(sinks), _scratch(ws, dev), ws.nbytes, _paged_stream(dev))
     _check(st, "ec_paged_append")
 
 
@@ -539,11 +544,11 @@ def ec_paged_decode_step(q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tens
                          ws: torch.Tensor) -> None:
     """One generation step on a paged cache: attention with the weights gathered, then the step's row joins and the
     heads above `budget` rows evict by weight. Nothing comes back to the host: the call can be captured and replayed."""
-    N, H, D, dt, dev = cache.N, cache.H, cache.D, cache._dtype, cache._device
+    N, H, D, dt, dev = cache._dims
     Hq = q.shape[1]
     st = lib().ec_paged_decode_step(_want(q, "q", dt, (N, Hq, D), dev), _want(k_new, "k_new", dt, (N, H, D), dev),
                                     _want(v_new, "v_new", dt, (N, H, D), dev), C.byref(cache), Hq, scale, decay, int(budget),
                                     int(recent), int(sinks), _want(out, "out", dt, (N, Hq, D), dev),
-                                    _want(lse, "lse", torch.float32, (N, Hq), dev), _ptr(ws),
-                                    ws.numel() * ws.element_size(), _paged_stream(cache))
+                                    _want(lse, "lse", torch.float32, (N, Hq), dev), _scratch(ws, dev),
+                                    ws.nbytes, _paged_stream(dev))
     _check(st, "ec_paged_decode_step")

@@ -141,7 +141,7 @@ struct AppendArgs {
     const float *w_new;
     const int *pos_new, *counts;
     int T, fresh, budget, recent, sinks;
-    int *moves;                                  // workspace: [N * H] rows to move
+    int4 *moves;                                 // workspace: [N * H] rows to move, and what the unit was
     int2 *list;                                  // workspace: [N * H][budget]: .x = slot to fill, .y = candidate to take
     unsigned long long *lowest;                  // workspace: [N * H][kMaxSplits] lowest candidate of every part
 };

@@ -3,10 +3,12 @@
 //  - One new row (a generation step): one launch does all of it. A row's new weight is on hand when the row that leaves is
 //    looked for, so the weights are read once; the search is a minimum over (key, row). Bound by latency: a chain of
 //    length, page, score and weight reads, which every thread walks for several rows side by side.
-//  - More new rows (a prompt): a CTA per (problem, head) finds the key of the last row that leaves by radix descent over
-//    8-bit digits and lists, in an ordered pass, the holes below the new length and the kept rows that have to move there
-//    (kept rows never shift, so only as many rows move as join or sit behind the new length); a second launch moves them
-//    with all CTAs of the GPU, bound by the copied bytes.
+//  - More new rows (a prompt): a CTA per (problem, head) finds the key of the last row that leaves and lists, in an ordered
+//    pass, the holes below the new length and the kept rows that have to move there (kept rows never shift, so only as
+//    many rows move as join or sit behind the new length); a second launch moves them with all CTAs of the GPU, bound by
+//    the copied bytes. The key is found with histograms of 1024 bins laid over the range the keys really have, so that
+//    their counts spread (8-bit digits of float images put most keys into a few bins, whose shared-memory additions then
+//    queue up), narrowed to one bin after the other: two or three passes over keys held in shared memory.
 // Keys are order-preserving unsigned images of the weights; rows at protected positions get the largest key. Equal keys:
 // the higher candidate leaves first (cached rows in slot order, then the new rows).
 #include "ec_paged.cuh"
@@ -15,7 +17,7 @@ namespace ec {
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256;                    // of a move
 constexpr int kFewRows = 16;                     // up to this many new rows the deciding CTA moves them itself
 constexpr int kMaxSplits = 512;                  // CTAs that share a unit's rows in a step
 
@@ -33,6 +35,9 @@ struct Unit {
     int n, h, had, cnt, final, seen;
     size_t u;
 };
+
+// What a selection leaves for the launch that moves the rows: by then the lengths have changed.
+__device__ __forceinline__ int4 unit_record(const Unit &u, int movers) { return make_int4(movers, u.had, u.cnt, u.seen); }
 
 __device__ __forceinline__ bool is_protected(const AppendArgs &a, const Unit &u, int pos)
 {
@@ -92,23 +97,48 @@ __device__ __forceinline__ void move_row(const PagedView &c, const AppendArgs &a
     }
 }
 
-// Exclusive prefix of a flag over the block; returns it and adds the block's count to `total` (uniform).
+constexpr int kBins = 1024;
+
+template <int THREADS> struct SelectSmem {
+    int hist[kBins];
+    int a[THREADS / 32], b[THREADS / 32];
+    uint32_t lo[THREADS / 32], hi[THREADS / 32];
+    uint32_t bin;
+    int left, here;
+};
+
+// Exclusive prefix over the block of x and y; the totals come back in `sum`.
 template <int THREADS>
-__device__ __forceinline__ int block_prefix(bool flag, int *warp_counts, int &total)
+__device__ __forceinline__ int2 block_prefix(int x, int y, SelectSmem<THREADS> &sm, int2 &sum)
 {
-    const unsigned mask = __ballot_sync(0xFFFFFFFFu, flag);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    __syncthreads();                             // the previous use of warp_counts is over
-    if (lane == 0) warp_counts[warp] = __popc(mask);
+    int ix = x, iy = y;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int ux = __shfl_up_sync(0xFFFFFFFFu, ix, o), uy = __shfl_up_sync(0xFFFFFFFFu, iy, o);
+        if (lane >= o) {
+            ix += ux;
+            iy += uy;
+        }
+    }
+    __syncthreads();                             // the previous use of a and b is over
+    if (lane == 31) {
+        sm.a[warp] = ix;
+        sm.b[warp] = iy;
+    }
     __syncthreads();
-    int before = total, sum = 0;
+    int2 before = make_int2(ix - x, iy - y);
+    sum = make_int2(0, 0);
 #pragma unroll
     for (int w = 0; w < THREADS / 32; ++w) {
-        if (w < warp) before += warp_counts[w];
-        sum += warp_counts[w];
+        if (w < warp) {
+            before.x += sm.a[w];
+            before.y += sm.b[w];
+        }
+        sum.x += sm.a[w];
+        sum.y += sm.b[w];
     }
-    total += sum;
-    return before + __popc(mask & ((1u << lane) - 1u));
+    return before;
 }
 
 __device__ __forceinline__ Unit load_unit(const PagedView &c, const AppendArgs &a, int n, int h)
@@ -131,90 +161,145 @@ __device__ __forceinline__ Unit load_unit(const PagedView &c, const AppendArgs &
     return u;
 }
 
-template <int THREADS> struct SelectSmem {
-    int hist[256];
-    int warp_counts[THREADS / 32];
-    uint32_t digit;
-    int left;
-};
-
-// The whole CTA: lists the moves of unit u (slot to fill, candidate to take) and returns their number.
+// The whole CTA: lists the moves of unit u (slot to fill, candidate to take) and returns their number. `keys` takes the
+// candidates' keys when there is room for `room` of them; otherwise they are worked out again for every pass.
 template <int THREADS>
-__device__ __forceinline__ int select_unit(const PagedView &c, const AppendArgs &a, const Unit &u, SelectSmem<THREADS> &sm)
+__device__ __forceinline__ int select_unit(const PagedView &c, const AppendArgs &a, const Unit &u, SelectSmem<THREADS> &sm,
+                                           uint32_t *keys, int room)
 {
-    int *hist = sm.hist, *warp_counts = sm.warp_counts;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int all = u.had + u.cnt, leave = all - u.final;
-    uint32_t edge = 0;                           // rows with a smaller key leave, `left` of those with this key
-    int left = 0, equal_kept = 0;
-    if (leave > 0) {
-        left = leave;
-#pragma unroll 1
-        for (int shift = 24; shift >= 0; shift -= 8) {
-            for (int i = threadIdx.x; i < 256; i += THREADS) hist[i] = 0;
+    int2 *list = a.list + u.u * a.budget;
+    if (leave <= 0) {                            // nothing leaves: the new rows go behind the others
+        for (int k = threadIdx.x; k < u.cnt; k += THREADS) list[k] = make_int2(u.had + k, u.had + k);
+        __syncthreads();
+        return u.cnt;
+    }
+    const bool held = all <= room;
+    auto key_of = [&](int j) { return held ? keys[j] : candidate_key(c, a, u, j); };
+
+    // the range of the keys that are not protected, and their number
+    uint32_t lo = 0xFFFFFFFFu, hi = 0;
+    int open = 0;
+    for (int j = threadIdx.x; j < all; j += THREADS) {
+        const uint32_t key = candidate_key(c, a, u, j);
+        if (held) keys[j] = key;
+        if (key != kKeyProtected) {
+            lo = min(lo, key);
+            hi = max(hi, key);
+            ++open;
+        }
+    }
+    lo = __reduce_min_sync(0xFFFFFFFFu, lo);
+    hi = __reduce_max_sync(0xFFFFFFFFu, hi);
+    open = __reduce_add_sync(0xFFFFFFFFu, open);
+    __syncthreads();
+    if (lane == 0) {
+        sm.lo[warp] = lo;
+        sm.hi[warp] = hi;
+        sm.a[warp] = open;
+    }
+    __syncthreads();
+    open = 0;
+#pragma unroll
+    for (int w = 0; w < THREADS / 32; ++w) {
+        lo = min(lo, sm.lo[w]);
+        hi = max(hi, sm.hi[w]);
+        open += sm.a[w];
+    }
+    // Of the keys in [lo, hi] `left` leave, and every smaller one. Narrowed until all of the range leaves or it is one key.
+    int left = leave, equal = 0;                 // equal > 0: rows at key lo, of which the last `left` leave
+    uint32_t edge;                               // rows with a smaller key leave
+    if (left >= open) {                          // protected rows leave too, where they are all that is left
+        left -= open;
+        equal = all - open;
+        edge = kKeyProtected;
+    } else {
+        for (;;) {
+            const int bits = 32 - __clz(hi - lo), shift = max(0, bits - 10);
             __syncthreads();
-            const uint32_t high = shift == 24 ? 0u : 0xFFFFFFFFu << (shift + 8);
+            for (int i = threadIdx.x; i < kBins; i += THREADS) sm.hist[i] = 0;
+            __syncthreads();
             for (int j = threadIdx.x; j < all; j += THREADS) {
-                const uint32_t key = candidate_key(c, a, u, j);
-                if ((key & high) == edge) atomicAdd(&hist[(key >> shift) & 255u], 1);
+                const uint32_t key = key_of(j);
+                if (key >= lo && key <= hi) atomicAdd(&sm.hist[(key - lo) >> shift], 1);
             }
             __syncthreads();
-            if (threadIdx.x < 32) {              // the digit in which the running count passes `left`
-                int sum = 0;
+            if (warp == 0) {                     // the bin in which the running count reaches `left`
+                int mine = 0;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) sum += hist[threadIdx.x * 8 + i];
-                int incl = sum;
+                for (int i = 0; i < kBins / 32; ++i) mine += sm.hist[lane * (kBins / 32) + ((i + lane) & 31)];
+                int incl = mine;
 #pragma unroll
                 for (int o = 1; o < 32; o <<= 1) {
                     const int up = __shfl_up_sync(0xFFFFFFFFu, incl, o);
-                    if (threadIdx.x >= o) incl += up;
+                    if (lane >= o) incl += up;
                 }
-                int at = incl - sum;
-                if (at < left && left <= incl) {
-                    for (int i = 0; i < 8; ++i) {
-                        const int here = hist[threadIdx.x * 8 + i];
-                        if (at + here >= left) {
-                            sm.digit = threadIdx.x * 8 + i;
-                            sm.left = left - at;
-                            equal_kept = here;
-                            break;
-                        }
-                        at += here;
-                    }
-                    hist[0] = equal_kept;        // rows with the edge key, for the last digit
+                const unsigned reached = __ballot_sync(0xFFFFFFFFu, incl >= left);
+                const int src = __ffs(reached) - 1;
+                int at = __shfl_sync(0xFFFFFFFFu, incl - mine, src);
+                int bin = sm.hist[src * 32 + lane];
+                int run = bin;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const int up = __shfl_up_sync(0xFFFFFFFFu, run, o);
+                    if (lane >= o) run += up;
+                }
+                const int sub = __ffs(__ballot_sync(0xFFFFFFFFu, at + run >= left)) - 1;
+                if (lane == sub) {
+                    sm.bin = src * 32 + sub;
+                    sm.left = left - (at + run - bin);
+                    sm.here = bin;
                 }
             }
             __syncthreads();
-            edge |= sm.digit << shift;
             left = sm.left;
-            equal_kept = hist[0] - left;         // after the last digit: of the rows at the edge the first ones stay
-            __syncthreads();
+            const int here = sm.here;
+            lo += sm.bin << shift;
+            hi = lo + min(hi - lo, (1u << shift) - 1u);                   // the bin's last key
+            if (left == here) {                  // the whole bin leaves (its end is below the protected key)
+                edge = hi + 1u;
+                left = 0;
+                break;
+            }
+            if (shift == 0) {
+                edge = lo;
+                equal = here;
+                break;
+            }
         }
     }
-    // ordered pass: k-th hole <- k-th kept row from behind
-    int equals = 0, holes = 0, movers = 0;
-    int2 *list = a.list + u.u * a.budget;
-    for (int base = 0; base < all; base += THREADS) {
-        const int j = base + threadIdx.x;
-        bool stay = j < all, equal = false;
-        if (leave > 0 && j < all) {
-            const uint32_t key = candidate_key(c, a, u, j);
-            equal = key == edge;
-            stay = key > edge;
-        }
-        if (leave > 0) {
-            const int rank = block_prefix<THREADS>(equal, warp_counts, equals);
-            if (equal) stay = rank < equal_kept;
-        }
-        const bool low = j < u.had && j < u.final;
-        const bool hole = low && !stay, mover = j < all && stay && !low;
-        const int hk = block_prefix<THREADS>(hole, warp_counts, holes);
-        const int mk = block_prefix<THREADS>(mover, warp_counts, movers);
-        if (hole) list[hk].x = j;
-        if (mover) list[mk].y = j;
+    // Ordered pass, a run of candidates per thread (odd, against bank conflicts): k-th hole <- k-th kept row from behind.
+    const int span = ((all + THREADS - 1) / THREADS) | 1;
+    const int j0 = min((int)threadIdx.x * span, all), j1 = min(j0 + span, all);
+    int2 sum;
+    int rank = 0;
+    const int equal_kept = equal - left;
+    if (left > 0) {                              // of the rows at the edge the first ones stay
+        int mine = 0;
+        for (int j = j0; j < j1; ++j) mine += key_of(j) == edge;
+        rank = block_prefix<THREADS>(mine, 0, sm, sum).x;
     }
-    for (int s = u.had + threadIdx.x; s < u.final; s += THREADS) list[holes + (s - u.had)].x = s;   // slots behind the old length
+    int holes = 0, movers = 0;
+    auto each = [&](auto hole, auto mover) {
+        int r = rank;
+        for (int j = j0; j < j1; ++j) {
+            const uint32_t key = key_of(j);
+            bool stay = key >= edge;
+            if (left > 0 && key == edge) stay = r++ < equal_kept;
+            if (j < u.had && j < u.final) {
+                if (!stay) hole(j);
+            } else if (stay) {
+                mover(j);
+            }
+        }
+    };
+    each([&](int) { ++holes; }, [&](int) { ++movers; });
+    int2 at = block_prefix<THREADS>(holes, movers, sm, sum);
+    each([&](int j) { list[at.x++].x = j; }, [&](int j) { list[at.y++].y = j; });
+    for (int s = u.had + threadIdx.x; s < u.final; s += THREADS) list[sum.x + (s - u.had)].x = s;   // slots behind the old length
     __syncthreads();                             // the list is complete, every key has been read
-    return movers;
+    return sum.y;
 }
 
 // The listed rows of a unit, by the whole CTA.
@@ -229,20 +314,30 @@ __device__ __forceinline__ void move_listed(const PagedView &c, const AppendArgs
     }
 }
 
-__global__ void __launch_bounds__(kThreads) paged_select_kernel(PagedView c, AppendArgs a, int lpr, int move_here)
+// A CTA per (problem, head). move_here: few rows, moved by the CTA that listed them.
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS) paged_select_kernel(PagedView c, AppendArgs a, int lpr, int move_here, int room)
 {
-    __shared__ SelectSmem<kThreads> sm;
+    extern __shared__ uint32_t sm_keys[];        // [room]
+    __shared__ SelectSmem<THREADS> sm;
     grid_wait();
     grid_release();
     const int n = blockIdx.x / c.H, h = blockIdx.x - n * c.H;
     const Unit u = load_unit(c, a, n, h);
     if (u.had < 0) {                             // an empty place of the batch
-        if (threadIdx.x == 0) a.moves[u.u] = 0;
+        if (threadIdx.x == 0) a.moves[u.u] = make_int4(0, 0, 0, 0);
         return;
     }
-    const int movers = select_unit<kThreads>(c, a, u, sm);
-    if (threadIdx.x == 0) a.moves[u.u] = movers;
-    if (move_here) move_listed<kThreads>(c, a, u, movers, lpr);
+    const int movers = select_unit<THREADS>(c, a, u, sm, sm_keys, room);
+    if (threadIdx.x == 0) a.moves[u.u] = unit_record(u, movers);
+    if (move_here) move_listed<THREADS>(c, a, u, movers, lpr);
+    // of the problem's CTAs, all of which have read its length, the last one changes it
+    int *arrived = c.state + kStateAppend + n;
+    if (threadIdx.x == 0 && arrive(arrived) == c.H - 1) {
+        *arrived = 0;
+        c.lens[n] = u.final;
+        c.seen[n] = u.seen + u.cnt;
+    }
 }
 
 // `parts` CTAs per unit: the listed rows of every unit.
@@ -251,10 +346,16 @@ __global__ void __launch_bounds__(kThreads) paged_move_kernel(PagedView c, Appen
     grid_wait();
     grid_release();
     const int unit = blockIdx.x / parts, part = blockIdx.x - unit * parts;
-    const int n = unit / c.H, h = unit - n * c.H;
-    const Unit u = load_unit(c, a, n, h);
-    if (u.had < 0) return;
-    const int movers = a.moves[u.u];
+    const int4 record = a.moves[unit];
+    const int movers = record.x;
+    Unit u;
+    u.n = unit / c.H;
+    u.h = unit - u.n * c.H;
+    u.u = unit;
+    u.had = record.y;
+    u.cnt = record.z;
+    u.seen = record.w;
+    u.final = 0;                                 // not looked at when rows are moved
     const int groups = kThreads / lpr, group = threadIdx.x / lpr, l = threadIdx.x - group * lpr;
     const int2 *list = a.list + u.u * a.budget;
     for (int k = part * groups + group; k < movers; k += parts * groups) {
@@ -263,26 +364,10 @@ __global__ void __launch_bounds__(kThreads) paged_move_kernel(PagedView c, Appen
     }
 }
 
-// The lengths change when every unit of their problem has been dealt with: a launch of its own.
-__global__ void paged_commit_kernel(PagedView c, AppendArgs a)
-{
-    grid_wait();
-    grid_release();
-    const int n = blockIdx.x * blockDim.x + threadIdx.x;
-    if (n >= c.N) return;
-    const Unit u = load_unit(c, a, n, 0);
-    if (u.had < 0) return;
-    c.lens[n] = u.final;
-    c.seen[n] = u.seen + u.cnt;
-}
-
 constexpr int kRowThreads = 128;
-#ifndef EC_RC
-#define EC_RC 8
-#endif
-constexpr int kRowCtas = EC_RC;                      // per SM
+constexpr int kRowCtas = 8;                      // per SM
+constexpr int kRowsHeld = 4;                     // rows a thread has in flight
 constexpr int kScoresHeld = 4;                   // query heads whose scores a thread reads side by side
-constexpr int kRowsHeld = 4;                      // rows a thread has in flight
 
 // The row that leaves first has the smallest of these: key, then the higher candidate.
 __device__ __forceinline__ unsigned long long leave_order(uint32_t key, int j)
@@ -437,7 +522,7 @@ __global__ void __launch_bounds__(kRowThreads, kRowCtas) paged_rows_kernel(Paged
         if (simple) {
             if (warp == 0) place(u, sm_low[0], lane);
         } else {
-            const int movers = select_unit<kRowThreads>(c, ap, u, sm_select);
+            const int movers = select_unit<kRowThreads>(c, ap, u, sm_select, nullptr, 0);
             move_listed<kRowThreads>(c, ap, u, movers, lpr);
         }
         if (threadIdx.x == 0 && arrive(arrived) == c.H - 1) {
@@ -466,7 +551,7 @@ __global__ void __launch_bounds__(kRowThreads, kRowCtas) paged_rows_kernel(Paged
             Unit v = u;
             v.h = hh;
             v.u = (size_t)n * c.H + hh;
-            const int movers = select_unit<kRowThreads>(c, ap, v, sm_select);
+            const int movers = select_unit<kRowThreads>(c, ap, v, sm_select, nullptr, 0);
             move_listed<kRowThreads>(c, ap, v, movers, lpr);
             __syncthreads();
         }
@@ -495,7 +580,7 @@ inline size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 size_t paged_append_workspace_bytes(const ec_paged *c, int T, int budget)
 {
     const size_t units = (size_t)c->N * c->H;
-    return up256(units * sizeof(int)) + up256(units * budget * sizeof(int2)) +
+    return up256(units * sizeof(int4)) + up256(units * budget * sizeof(int2)) +
            (T <= 1 ? up256(units * row_splits(units, budget) * sizeof(unsigned long long)) : 0);
 }
 
@@ -507,8 +592,8 @@ cudaError_t launch_paged_rows(const PagedView &c, int D, const GatherArgs *gathe
     if (append) {
         a = *append;
         char *p = static_cast<char *>(ws);
-        a.moves = reinterpret_cast<int *>(p);
-        p += up256(units * sizeof(int));
+        a.moves = reinterpret_cast<int4 *>(p);
+        p += up256(units * sizeof(int4));
         a.list = reinterpret_cast<int2 *>(p);
         p += up256(units * a.budget * sizeof(int2));
         a.lowest = reinterpret_cast<unsigned long long *>(p);
@@ -520,7 +605,16 @@ cudaError_t launch_paged_rows(const PagedView &c, int D, const GatherArgs *gathe
         return launch_chained(kernel, dim3((unsigned)(splits * units)), kRowThreads, g.G * sizeof(float2), stream, c, g, a, lpr, splits);
     }
     const bool few = a.T <= kFewRows;
-    cudaError_t e = launch_chained(paged_select_kernel, dim3((unsigned)units), kThreads, 0, stream, c, a, lpr, few ? 1 : 0);
+    // Keys of budget + T candidates are held in shared memory up to 48K of them. Wide CTAs for long lists: one that a CTA of
+    // 256 threads walks in 64 steps or more.
+    const long long most_keys = (long long)a.budget + a.T;
+    const int room = most_keys <= 48 * 1024 ? (int)most_keys : 0;
+    const bool wide = most_keys >= 16 * 1024;
+    auto kernel = wide ? paged_select_kernel<1024> : paged_select_kernel<256>;
+    cudaError_t e = cudaSuccess;
+    if (room > 10 * 1024) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, room * (int)sizeof(uint32_t));
+    if (e == cudaSuccess)
+        e = launch_chained(kernel, dim3((unsigned)units), wide ? 1024u : 256u, room * sizeof(uint32_t), stream, c, a, lpr, few ? 1 : 0, room);
     if (e == cudaSuccess && !few) {
         const int groups = kThreads / lpr;
         long long parts = (148LL * 8 + units - 1) / units;
@@ -528,7 +622,6 @@ cudaError_t launch_paged_rows(const PagedView &c, int D, const GatherArgs *gathe
         if (parts > most) parts = most;
         e = launch_chained(paged_move_kernel, dim3((unsigned)(parts * units)), kThreads, 0, stream, c, a, lpr, (int)parts);
     }
-    if (e == cudaSuccess) e = launch_chained(paged_commit_kernel, dim3((unsigned)((c.N + 127) / 128)), 128, 0, stream, c, a);
     return e;
 }
 

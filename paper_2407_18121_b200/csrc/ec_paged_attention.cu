@@ -15,6 +15,8 @@
 //    whole units between; of the CTAs that share a unit the one that arrives last joins the parts (nobody waits).
 #include "ec_paged.cuh"
 
+#include <atomic>
+
 namespace ec {
 
 namespace {
@@ -746,14 +748,6 @@ __global__ void __launch_bounds__(W * 32, 8 / W) paged_attention_kernel(AttnArgs
 
 inline size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
-inline int sm_count_here()
-{
-    int dev = 0, n = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess) return 148;
-    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) return 148;
-    return n;
-}
-
 struct WsLayout {
     size_t stat, score_new, part_o, part_ml, scores, total;
 };
@@ -783,10 +777,19 @@ cudaError_t launch(const AttnArgs &a, cudaStream_t stream)
     auto kernel = paged_attention_kernel<E, D, NT, W, GATHER>;
     constexpr int smem = Smem<D, NT, W>::kTotal;
     const int head_blocks = (a.G + 8 * NT - 1) / (8 * NT);
-    int ctas = sm_count_here() * (8 / W);
-    if (ctas > kPagedMaxCtas) ctas = kPagedMaxCtas;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    int dev = 0, ctas = 148;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&ctas, cudaDevAttrMultiProcessorCount, dev);
     if (e != cudaSuccess) return e;
+    ctas *= 8 / W;
+    if (ctas > kPagedMaxCtas) ctas = kPagedMaxCtas;
+    static std::atomic<unsigned long long> allowed{0};                    // devices on which the kernel may use this much
+    const unsigned long long bit = dev < 64 ? 1ull << dev : 0ull;
+    if (!(allowed.load(std::memory_order_relaxed) & bit) || !bit) {
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        if (e != cudaSuccess) return e;
+        allowed.fetch_or(bit, std::memory_order_relaxed);
+    }
     return launch_chained(kernel, dim3((unsigned)ctas), W * 32, smem, stream, a, head_blocks);
 }
 
