@@ -87,15 +87,26 @@ struct Slot {
     int page, slot;        // page < 0: the table has no valid page here
 };
 
-__device__ __forceinline__ Slot find_slot(const PagedView &c, int n, int row)
+// The table's entry as it is: to be looked at with valid_page before anything is read through it.
+__device__ __forceinline__ Slot look_up_slot(const PagedView &c, int n, int row)
 {
     const int p = page_of(c, row);
     Slot s;
     s.slot = row - p * c.page_size;
     s.page = c.table[(size_t)n * c.max_pages + p];
-    if ((unsigned)s.page >= (unsigned)c.n_pages) {
+    return s;
+}
+
+__device__ __forceinline__ bool valid_page(const PagedView &c, const Slot &s) { return (unsigned)s.page < (unsigned)c.n_pages; }
+
+__device__ __forceinline__ void report_page(const PagedView &c) { atomicExch(c.state, kStatusPage); }
+
+__device__ __forceinline__ Slot find_slot(const PagedView &c, int n, int row)
+{
+    Slot s = look_up_slot(c, n, row);
+    if (!valid_page(c, s)) {
         s.page = -1;
-        atomicExch(c.state, kStatusPage);
+        report_page(c);
     }
     return s;
 }

@@ -3,22 +3,26 @@
 //  - One new row (a generation step): one launch does all of it. A row's new weight is on hand when the row that leaves is
 //    looked for, so the weights are read once; the search is a minimum over (key, row). Bound by latency: a chain of
 //    length, page, score and weight reads, which every thread walks for several rows side by side.
-//  - More new rows (a prompt): a CTA per (problem, head) finds the key of the last row that leaves and lists, in an ordered
-//    pass, the holes below the new length and the kept rows that have to move there (kept rows never shift, so only as
-//    many rows move as join or sit behind the new length); a second launch moves them with all CTAs of the GPU, bound by
-//    the copied bytes. The key is found with histograms of 1024 bins laid over the range the keys really have, so that
-//    their counts spread (8-bit digits of float images put most keys into a few bins, whose shared-memory additions then
-//    queue up), narrowed to one bin after the other: two or three passes over keys held in shared memory.
+//  - More new rows (a prompt): a CTA, or a cluster of them when units are few and long, finds the key of the last row that
+//    leaves and lists, in an ordered pass, the holes below the new length and the kept rows that have to move there (kept
+//    rows never shift, so only as many rows move as join or sit behind the new length); a second launch moves them with
+//    all CTAs of the GPU, bound by the copied bytes. The key is found with histograms of 1024 bins laid over the range the
+//    keys really have, so that their counts spread (8-bit digits of float images put most keys into a few bins, whose
+//    shared-memory additions then queue up), narrowed to one bin after the other: two or three passes over keys held in
+//    shared memory. A list of 16384 costs one SM about 20 us of instructions; over a cluster the histograms are summed and
+//    the ordered counts carried on through distributed shared memory.
 // Keys are order-preserving unsigned images of the weights; rows at protected positions get the largest key. Equal keys:
 // the higher candidate leaves first (cached rows in slot order, then the new rows).
 #include "ec_paged.cuh"
+
+#include <cooperative_groups.h>
 
 namespace ec {
 
 namespace {
 
-constexpr int kThreads = 256;                    // of a move
-constexpr int kFewRows = 16;                     // up to this many new rows the deciding CTA moves them itself
+constexpr int kThreads = 256;                    // of a move, and of a selection but for long lists
+constexpr int kFewRows = 64;                     // up to this many new rows the deciding CTAs move them themselves
 constexpr int kMaxSplits = 512;                  // CTAs that share a unit's rows in a step
 
 constexpr uint32_t kKeyProtected = 0xFFFFFFFFu, kKeyNan = 0xFFFFFFFEu;
@@ -62,19 +66,19 @@ __device__ __forceinline__ uint32_t candidate_key(const PagedView &c, const Appe
     return is_protected(a, u, pos) ? kKeyProtected : weight_key(w);
 }
 
-// Row j of the candidates -> slot `dst`, by LPR = D / 8 lanes of which this is lane l.
+// Candidate j -> slot `dst`, as lane l of the LPR = D / 8 lanes that copy a row.
 __device__ __forceinline__ void move_row(const PagedView &c, const AppendArgs &a, const Unit &u, int dst, int j, int lpr, int l)
 {
-    const Slot d = find_slot(c, u.n, dst);
-    if (d.page < 0) return;
-    const size_t to = (size_t)u.h * c.head_step + row_offset(c, d) + l;
-    const uint32_t meta_to = meta_index(c, u.h, d);
+    const Slot d = look_up_slot(c, u.n, dst);
     const uint4 *k, *v;
     float w;
     int pos;
     if (j < u.had) {
-        const Slot s = find_slot(c, u.n, j);
-        if (s.page < 0) return;
+        const Slot s = look_up_slot(c, u.n, j);
+        if (!valid_page(c, s)) {
+            report_page(c);
+            return;
+        }
         const size_t from = (size_t)u.h * c.head_step + row_offset(c, s) + l;
         k = c.K + from;
         v = c.V + from;
@@ -88,15 +92,22 @@ __device__ __forceinline__ void move_row(const PagedView &c, const AppendArgs &a
         w = a.w_new ? a.w_new[at] : 0.f;
         pos = a.pos_new ? a.pos_new[at] : u.seen + (j - u.had);
     }
-    const uint4 kv = *k, vv = *v;
+    const uint4 kv = *k, vv = *v;                // a new row's reads do not wait for the page it goes to
+    if (!valid_page(c, d)) {
+        report_page(c);
+        return;
+    }
+    const size_t to = (size_t)u.h * c.head_step + row_offset(c, d) + l;
     c.K[to] = kv;
     c.V[to] = vv;
     if (l == 0) {
-        c.weight[meta_to] = w;
-        c.pos[meta_to] = pos;
+        const uint32_t m = meta_index(c, u.h, d);
+        c.weight[m] = w;
+        c.pos[m] = pos;
     }
 }
 
+constexpr int kUnroll = 2;                       // candidates of a thread side by side in the passes over held keys
 constexpr int kBins = 1024;
 
 template <int THREADS> struct SelectSmem {
@@ -105,40 +116,27 @@ template <int THREADS> struct SelectSmem {
     uint32_t lo[THREADS / 32], hi[THREADS / 32];
     uint32_t bin;
     int left, here;
+    int coarse[32];                              // sums of 32 bins each
+    uint32_t all_lo, all_hi;                     // of the CTA, for the others of its cluster
+    int all_open, all_equal;
+    int2 all_moves;
 };
 
-// Exclusive prefix over the block of x and y; the totals come back in `sum`.
+// Exclusive prefix over the warps of x and y, uniform within each warp; the totals come back in `sum`.
 template <int THREADS>
-__device__ __forceinline__ int2 block_prefix(int x, int y, SelectSmem<THREADS> &sm, int2 &sum)
+__device__ __forceinline__ int2 warps_prefix(int x, int y, SelectSmem<THREADS> &sm, int2 &sum)
 {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    int ix = x, iy = y;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const int ux = __shfl_up_sync(0xFFFFFFFFu, ix, o), uy = __shfl_up_sync(0xFFFFFFFFu, iy, o);
-        if (lane >= o) {
-            ix += ux;
-            iy += uy;
-        }
-    }
     __syncthreads();                             // the previous use of a and b is over
-    if (lane == 31) {
-        sm.a[warp] = ix;
-        sm.b[warp] = iy;
+    if (lane == 0) {
+        sm.a[warp] = x;
+        sm.b[warp] = y;
     }
     __syncthreads();
-    int2 before = make_int2(ix - x, iy - y);
-    sum = make_int2(0, 0);
-#pragma unroll
-    for (int w = 0; w < THREADS / 32; ++w) {
-        if (w < warp) {
-            before.x += sm.a[w];
-            before.y += sm.b[w];
-        }
-        sum.x += sm.a[w];
-        sum.y += sm.b[w];
-    }
-    return before;
+    constexpr int kWarps = THREADS / 32;
+    const int vx = lane < kWarps ? sm.a[lane] : 0, vy = lane < kWarps ? sm.b[lane] : 0;
+    sum = make_int2(__reduce_add_sync(0xFFFFFFFFu, vx), __reduce_add_sync(0xFFFFFFFFu, vy));
+    return make_int2(__reduce_add_sync(0xFFFFFFFFu, lane < warp ? vx : 0), __reduce_add_sync(0xFFFFFFFFu, lane < warp ? vy : 0));
 }
 
 __device__ __forceinline__ Unit load_unit(const PagedView &c, const AppendArgs &a, int n, int h)
@@ -161,33 +159,88 @@ __device__ __forceinline__ Unit load_unit(const PagedView &c, const AppendArgs &
     return u;
 }
 
-// The whole CTA: lists the moves of unit u (slot to fill, candidate to take) and returns their number. `keys` takes the
-// candidates' keys when there is room for `room` of them; otherwise they are worked out again for every pass.
-template <int THREADS>
-__device__ __forceinline__ int select_unit(const PagedView &c, const AppendArgs &a, const Unit &u, SelectSmem<THREADS> &sm,
-                                           uint32_t *keys, int room)
+// The whole CTA, or with SPREAD the whole cluster: lists the moves of unit u (slot to fill, candidate to take) and returns
+// their number. `keys` takes the keys of the CTA's candidates when there is room for `room` of them; otherwise they are
+// worked out again for every pass.
+template <int THREADS, bool SPREAD, bool HELD>
+__device__ __forceinline__ int select_body(const PagedView &c, const AppendArgs &a, const Unit &u, SelectSmem<THREADS> &sm,
+                                           uint32_t *keys)
 {
+    namespace cg = cooperative_groups;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    constexpr int kWarps = THREADS / 32;
+    const int rank = SPREAD ? (int)cg::this_cluster().block_rank() : 0, ranks = SPREAD ? (int)cg::this_cluster().num_blocks() : 1;
+    auto meet = [] {
+        if (SPREAD) cg::this_cluster().sync();
+        else __syncthreads();
+    };
+    auto of = [&](int r) { return SPREAD ? cg::this_cluster().map_shared_rank(&sm, r) : &sm; };   // rank r's shared memory
     const int all = u.had + u.cnt, leave = all - u.final;
     int2 *list = a.list + u.u * a.budget;
     if (leave <= 0) {                            // nothing leaves: the new rows go behind the others
-        for (int k = threadIdx.x; k < u.cnt; k += THREADS) list[k] = make_int2(u.had + k, u.had + k);
-        __syncthreads();
+        for (int k = rank * THREADS + threadIdx.x; k < u.cnt; k += ranks * THREADS) list[k] = make_int2(u.had + k, u.had + k);
+        meet();
         return u.cnt;
     }
-    const bool held = all <= room;
-    auto key_of = [&](int j) { return held ? keys[j] : candidate_key(c, a, u, j); };
+    const int share = (all + 32 * ranks - 1) / (32 * ranks) * 32;         // of the candidates, in order
+    const int c0 = min(rank * share, all), c1 = min(c0 + share, all);
+    const bool held = HELD;
+    auto key_of = [&](int j) { return held ? keys[j - c0] : candidate_key(c, a, u, j); };
 
     // the range of the keys that are not protected, and their number
     uint32_t lo = 0xFFFFFFFFu, hi = 0;
     int open = 0;
-    for (int j = threadIdx.x; j < all; j += THREADS) {
-        const uint32_t key = candidate_key(c, a, u, j);
-        if (held) keys[j] = key;
+    auto take = [&](int j, uint32_t key) {
+        if (held) keys[j - c0] = key;
         if (key != kKeyProtected) {
             lo = min(lo, key);
             hi = max(hi, key);
             ++open;
+        }
+    };
+    constexpr int kBatch = 4;                    // candidates of a thread that walk their chain of reads side by side
+    const int cached = min(c1, u.had);
+    for (int base = c0 + threadIdx.x; base < cached; base += kBatch * THREADS) {
+        Slot s[kBatch];
+        float w[kBatch];
+        int pos[kBatch];
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+            const int j = base + i * THREADS;
+            s[i].page = -1;
+            if (j < cached) s[i] = look_up_slot(c, u.n, j);
+        }
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+            if (!valid_page(c, s[i])) continue;
+            const uint32_t m = meta_index(c, u.h, s[i]);
+            w[i] = c.weight[m];
+            pos[i] = c.pos[m];
+        }
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+            const int j = base + i * THREADS;
+            if (j >= cached) continue;
+            uint32_t key = 0;                    // a row that cannot be read leaves first
+            if (!valid_page(c, s[i])) report_page(c);
+            else key = is_protected(a, u, pos[i]) ? kKeyProtected : weight_key(w[i]);
+            take(j, key);
+        }
+    }
+    for (int base = max(c0, u.had) + threadIdx.x; base < c1; base += kBatch * THREADS) {
+        float w[kBatch];
+        int pos[kBatch];
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+            const int j = base + i * THREADS, t = j - u.had;
+            if (j >= c1) continue;
+            w[i] = a.w_new ? a.w_new[u.u * a.T + t] : 0.f;
+            pos[i] = a.pos_new ? a.pos_new[u.u * a.T + t] : u.seen + t;
+        }
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+            const int j = base + i * THREADS;
+            if (j < c1) take(j, is_protected(a, u, pos[i]) ? kKeyProtected : weight_key(w[i]));
         }
     }
     lo = __reduce_min_sync(0xFFFFFFFFu, lo);
@@ -200,15 +253,23 @@ __device__ __forceinline__ int select_unit(const PagedView &c, const AppendArgs 
         sm.a[warp] = open;
     }
     __syncthreads();
-    open = 0;
-#pragma unroll
-    for (int w = 0; w < THREADS / 32; ++w) {
-        lo = min(lo, sm.lo[w]);
-        hi = max(hi, sm.hi[w]);
-        open += sm.a[w];
+    lo = __reduce_min_sync(0xFFFFFFFFu, lane < kWarps ? sm.lo[lane] : 0xFFFFFFFFu);
+    hi = __reduce_max_sync(0xFFFFFFFFu, lane < kWarps ? sm.hi[lane] : 0u);
+    open = __reduce_add_sync(0xFFFFFFFFu, lane < kWarps ? sm.a[lane] : 0);
+    if (SPREAD) {
+        if (threadIdx.x == 0) {
+            sm.all_lo = lo;
+            sm.all_hi = hi;
+            sm.all_open = open;
+        }
+        meet();
+        const SelectSmem<THREADS> *other = of(lane < ranks ? lane : 0);
+        lo = __reduce_min_sync(0xFFFFFFFFu, other->all_lo);
+        hi = __reduce_max_sync(0xFFFFFFFFu, other->all_hi);
+        open = __reduce_add_sync(0xFFFFFFFFu, lane < ranks ? other->all_open : 0);
     }
     // Of the keys in [lo, hi] `left` leave, and every smaller one. Narrowed until all of the range leaves or it is one key.
-    int left = leave, equal = 0;                 // equal > 0: rows at key lo, of which the last `left` leave
+    int left = leave, equal = 0;                 // equal > 0: rows at the edge, of which the last `left` leave
     uint32_t edge;                               // rows with a smaller key leave
     if (left >= open) {                          // protected rows leave too, where they are all that is left
         left -= open;
@@ -217,39 +278,73 @@ __device__ __forceinline__ int select_unit(const PagedView &c, const AppendArgs 
     } else {
         for (;;) {
             const int bits = 32 - __clz(hi - lo), shift = max(0, bits - 10);
-            __syncthreads();
+            meet();                              // nobody reads the last histogram any more
             for (int i = threadIdx.x; i < kBins; i += THREADS) sm.hist[i] = 0;
             __syncthreads();
-            for (int j = threadIdx.x; j < all; j += THREADS) {
+#pragma unroll kUnroll
+            for (int j = c0 + threadIdx.x; j < c1; j += THREADS) {
                 const uint32_t key = key_of(j);
                 if (key >= lo && key <= hi) atomicAdd(&sm.hist[(key - lo) >> shift], 1);
             }
             __syncthreads();
-            if (warp == 0) {                     // the bin in which the running count reaches `left`
-                int mine = 0;
+            // the bin in which the running count reaches `left`
+            if (SPREAD) {                        // first among sums of 32 bins, then within one: little crosses the cluster
+                for (int i = warp; i < 32; i += kWarps) {
+                    const int group = __reduce_add_sync(0xFFFFFFFFu, sm.hist[i * 32 + lane]);
+                    if (lane == 0) sm.coarse[i] = group;
+                }
+                meet();
+                if (warp == 0) {
+                    auto find = [&](int mine, int &at) {                  // the lane that passes `left`; at: the count in front of it
+                        int incl = mine;
 #pragma unroll
-                for (int i = 0; i < kBins / 32; ++i) mine += sm.hist[lane * (kBins / 32) + ((i + lane) & 31)];
-                int incl = mine;
+                        for (int o = 1; o < 32; o <<= 1) {
+                            const int up = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+                            if (lane >= o) incl += up;
+                        }
+                        const int src = __ffs(__ballot_sync(0xFFFFFFFFu, at + incl >= left)) - 1;
+                        at += __shfl_sync(0xFFFFFFFFu, incl - mine, src);
+                        return src;
+                    };
+                    int mine = 0, fine = 0, at = 0;
+#pragma unroll 8
+                    for (int r = 0; r < ranks; ++r) mine += of(r)->coarse[lane];
+                    const int group = find(mine, at);
+#pragma unroll 8
+                    for (int r = 0; r < ranks; ++r) fine += of(r)->hist[group * 32 + lane];
+                    const int src = find(fine, at);
+                    if (lane == src) {
+                        sm.bin = group * 32 + src;
+                        sm.left = left - at;
+                        sm.here = fine;
+                    }
+                }
+            } else {
+                constexpr int kOwn = kBins / THREADS;                     // bins of a thread, in order
+                int mine[kOwn], total = 0;
+#pragma unroll
+                for (int i = 0; i < kOwn; ++i) {
+                    mine[i] = sm.hist[threadIdx.x * kOwn + i];
+                    total += mine[i];
+                }
+                int incl = total;
 #pragma unroll
                 for (int o = 1; o < 32; o <<= 1) {
                     const int up = __shfl_up_sync(0xFFFFFFFFu, incl, o);
                     if (lane >= o) incl += up;
                 }
-                const unsigned reached = __ballot_sync(0xFFFFFFFFu, incl >= left);
-                const int src = __ffs(reached) - 1;
-                int at = __shfl_sync(0xFFFFFFFFu, incl - mine, src);
-                int bin = sm.hist[src * 32 + lane];
-                int run = bin;
+                int2 sum;
+                int at = warps_prefix<THREADS>(__shfl_sync(0xFFFFFFFFu, incl, 31), 0, sm, sum).x + incl - total;
+                if (at < left && left <= at + total) {
 #pragma unroll
-                for (int o = 1; o < 32; o <<= 1) {
-                    const int up = __shfl_up_sync(0xFFFFFFFFu, run, o);
-                    if (lane >= o) run += up;
-                }
-                const int sub = __ffs(__ballot_sync(0xFFFFFFFFu, at + run >= left)) - 1;
-                if (lane == sub) {
-                    sm.bin = src * 32 + sub;
-                    sm.left = left - (at + run - bin);
-                    sm.here = bin;
+                    for (int i = 0; i < kOwn; ++i) {
+                        if (at < left && left <= at + mine[i]) {
+                            sm.bin = threadIdx.x * kOwn + i;
+                            sm.left = left - at;
+                            sm.here = mine[i];
+                        }
+                        at += mine[i];
+                    }
                 }
             }
             __syncthreads();
@@ -269,71 +364,108 @@ __device__ __forceinline__ int select_unit(const PagedView &c, const AppendArgs 
             }
         }
     }
-    // Ordered pass, a run of candidates per thread (odd, against bank conflicts): k-th hole <- k-th kept row from behind.
-    const int span = ((all + THREADS - 1) / THREADS) | 1;
-    const int j0 = min((int)threadIdx.x * span, all), j1 = min(j0 + span, all);
+    // Ordered pass, a run of candidates per warp, 32 at a time: k-th hole <- k-th kept row from behind.
+    const int span = (share + 32 * kWarps - 1) / (32 * kWarps) * 32;
+    const int j0 = min(c0 + warp * span, c1), j1 = min(j0 + span, c1);
+    const unsigned below = (1u << lane) - 1u;
     int2 sum;
-    int rank = 0;
+    int rank_equal = 0;
     const int equal_kept = equal - left;
     if (left > 0) {                              // of the rows at the edge the first ones stay
-        int mine = 0;
-        for (int j = j0; j < j1; ++j) mine += key_of(j) == edge;
-        rank = block_prefix<THREADS>(mine, 0, sm, sum).x;
+        int count = 0;
+        for (int j = j0 + lane; j - lane < j1; j += 32) count += __popc(__ballot_sync(0xFFFFFFFFu, j < j1 && key_of(j) == edge));
+        rank_equal = warps_prefix<THREADS>(count, 0, sm, sum).x;
+        if (SPREAD) {
+            if (threadIdx.x == 0) sm.all_equal = sum.x;
+            meet();
+            rank_equal += __reduce_add_sync(0xFFFFFFFFu, lane < rank ? of(lane)->all_equal : 0);
+        }
     }
-    int holes = 0, movers = 0;
-    auto each = [&](auto hole, auto mover) {
-        int r = rank;
-        for (int j = j0; j < j1; ++j) {
-            const uint32_t key = key_of(j);
+    auto each = [&](auto use) {                  // use(candidate, mask of holes, mask of movers)
+        int r = rank_equal;
+#pragma unroll kUnroll
+        for (int j = j0 + lane; j - lane < j1; j += 32) {
+            const uint32_t key = j < j1 ? key_of(j) : 0u;
             bool stay = key >= edge;
-            if (left > 0 && key == edge) stay = r++ < equal_kept;
-            if (j < u.had && j < u.final) {
-                if (!stay) hole(j);
-            } else if (stay) {
-                mover(j);
+            if (left > 0) {
+                const unsigned equals = __ballot_sync(0xFFFFFFFFu, j < j1 && key == edge);
+                if (key == edge) stay = r + __popc(equals & below) < equal_kept;
+                r += __popc(equals);
             }
+            const bool low = j < u.had && j < u.final;
+            const unsigned holes = __ballot_sync(0xFFFFFFFFu, j < j1 && low && !stay);
+            const unsigned movers = __ballot_sync(0xFFFFFFFFu, j < j1 && !low && stay);
+            use(j, holes, movers);
         }
     };
-    each([&](int) { ++holes; }, [&](int) { ++movers; });
-    int2 at = block_prefix<THREADS>(holes, movers, sm, sum);
-    each([&](int j) { list[at.x++].x = j; }, [&](int j) { list[at.y++].y = j; });
-    for (int s = u.had + threadIdx.x; s < u.final; s += THREADS) list[sum.x + (s - u.had)].x = s;   // slots behind the old length
-    __syncthreads();                             // the list is complete, every key has been read
+    int holes = 0, movers = 0;
+    each([&](int, unsigned hm, unsigned mm) {
+        holes += __popc(hm);
+        movers += __popc(mm);
+    });
+    int2 at = warps_prefix<THREADS>(holes, movers, sm, sum);
+    if (SPREAD) {
+        if (threadIdx.x == 0) sm.all_moves = sum;
+        meet();
+        const int2 other = lane < ranks ? of(lane)->all_moves : make_int2(0, 0);
+        at.x += __reduce_add_sync(0xFFFFFFFFu, lane < rank ? other.x : 0);
+        at.y += __reduce_add_sync(0xFFFFFFFFu, lane < rank ? other.y : 0);
+        sum = make_int2(__reduce_add_sync(0xFFFFFFFFu, other.x), __reduce_add_sync(0xFFFFFFFFu, other.y));
+    }
+    each([&](int j, unsigned hm, unsigned mm) {
+        if (hm >> lane & 1u) list[at.x + __popc(hm & below)].x = j;
+        if (mm >> lane & 1u) list[at.y + __popc(mm & below)].y = j;
+        at.x += __popc(hm);
+        at.y += __popc(mm);
+    });
+    for (int s = u.had + rank * THREADS + threadIdx.x; s < u.final; s += ranks * THREADS)
+        list[sum.x + (s - u.had)].x = s;         // slots behind the old length
+    meet();                                      // the list is complete, every key has been read
     return sum.y;
 }
 
-// The listed rows of a unit, by the whole CTA.
-template <int THREADS>
-__device__ __forceinline__ void move_listed(const PagedView &c, const AppendArgs &a, const Unit &u, int movers, int lpr)
+template <int THREADS, bool SPREAD>
+__device__ __forceinline__ int select_unit(const PagedView &c, const AppendArgs &a, const Unit &u, SelectSmem<THREADS> &sm,
+                                           uint32_t *keys, int room)
 {
-    const int group = threadIdx.x / lpr, l = threadIdx.x - group * lpr;
+    const int ranks = SPREAD ? (int)cooperative_groups::this_cluster().num_blocks() : 1;
+    const int share = (u.had + u.cnt + 32 * ranks - 1) / (32 * ranks) * 32;
+    return share <= room ? select_body<THREADS, SPREAD, true>(c, a, u, sm, keys) : select_body<THREADS, SPREAD, false>(c, a, u, sm, keys);
+}
+
+// The listed rows of a unit, by `ranks` CTAs of which this is number `rank`.
+template <int THREADS>
+__device__ __forceinline__ void move_listed(const PagedView &c, const AppendArgs &a, const Unit &u, int movers, int lpr, int rank, int ranks)
+{
+    const int groups = THREADS / lpr, group = threadIdx.x / lpr, l = threadIdx.x - group * lpr;
     const int2 *list = a.list + u.u * a.budget;
-    for (int k = group; k < movers; k += THREADS / lpr) {
+    for (int k = rank * groups + group; k < movers; k += ranks * groups) {
         const int2 e = list[k];
         move_row(c, a, u, e.x, e.y, lpr, l);
     }
 }
 
-// A CTA per (problem, head). move_here: few rows, moved by the CTA that listed them.
-template <int THREADS>
-__global__ void __launch_bounds__(THREADS) paged_select_kernel(PagedView c, AppendArgs a, int lpr, int move_here, int room)
+// A CTA or a cluster of `ranks` CTAs per (problem, head). move_here: few rows, moved by those that listed them.
+template <int THREADS, bool SPREAD>
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) paged_select_kernel(PagedView c, AppendArgs a, int lpr, int move_here, int room, int ranks)
 {
     extern __shared__ uint32_t sm_keys[];        // [room]
     __shared__ SelectSmem<THREADS> sm;
     grid_wait();
     grid_release();
-    const int n = blockIdx.x / c.H, h = blockIdx.x - n * c.H;
+    const int unit = SPREAD ? blockIdx.x / ranks : blockIdx.x, rank = SPREAD ? blockIdx.x - unit * ranks : 0;
+    const int n = unit / c.H, h = unit - n * c.H;
     const Unit u = load_unit(c, a, n, h);
     if (u.had < 0) {                             // an empty place of the batch
-        if (threadIdx.x == 0) a.moves[u.u] = make_int4(0, 0, 0, 0);
+        if (threadIdx.x == 0 && rank == 0) a.moves[u.u] = make_int4(0, 0, 0, 0);
         return;
     }
-    const int movers = select_unit<THREADS>(c, a, u, sm, sm_keys, room);
-    if (threadIdx.x == 0) a.moves[u.u] = unit_record(u, movers);
-    if (move_here) move_listed<THREADS>(c, a, u, movers, lpr);
+    const int movers = select_unit<THREADS, SPREAD>(c, a, u, sm, sm_keys, room);
+    if (threadIdx.x == 0 && rank == 0) a.moves[u.u] = unit_record(u, movers);
+    if (move_here) move_listed<THREADS>(c, a, u, movers, lpr, rank, ranks);
     // of the problem's CTAs, all of which have read its length, the last one changes it
     int *arrived = c.state + kStateAppend + n;
-    if (threadIdx.x == 0 && arrive(arrived) == c.H - 1) {
+    if (threadIdx.x == 0 && arrive(arrived) == c.H * ranks - 1) {
         *arrived = 0;
         c.lens[n] = u.final;
         c.seen[n] = u.seen + u.cnt;
@@ -356,12 +488,9 @@ __global__ void __launch_bounds__(kThreads) paged_move_kernel(PagedView c, Appen
     u.cnt = record.z;
     u.seen = record.w;
     u.final = 0;                                 // not looked at when rows are moved
-    const int groups = kThreads / lpr, group = threadIdx.x / lpr, l = threadIdx.x - group * lpr;
-    const int2 *list = a.list + u.u * a.budget;
-    for (int k = part * groups + group; k < movers; k += parts * groups) {
-        const int2 e = list[k];
-        move_row(c, a, u, e.x, e.y, lpr, l);
-    }
+    // one row per group of lanes at a time: two measured 30% slower, the registers cost more warps than the second
+    // row's reads bring
+    move_listed<kThreads>(c, a, u, movers, lpr, part, parts);
 }
 
 constexpr int kRowThreads = 128;
@@ -522,8 +651,8 @@ __global__ void __launch_bounds__(kRowThreads, kRowCtas) paged_rows_kernel(Paged
         if (simple) {
             if (warp == 0) place(u, sm_low[0], lane);
         } else {
-            const int movers = select_unit<kRowThreads>(c, ap, u, sm_select, nullptr, 0);
-            move_listed<kRowThreads>(c, ap, u, movers, lpr);
+            const int movers = select_unit<kRowThreads, false>(c, ap, u, sm_select, nullptr, 0);
+            move_listed<kRowThreads>(c, ap, u, movers, lpr, 0, 1);
         }
         if (threadIdx.x == 0 && arrive(arrived) == c.H - 1) {
             *arrived = 0;
@@ -551,8 +680,8 @@ __global__ void __launch_bounds__(kRowThreads, kRowCtas) paged_rows_kernel(Paged
             Unit v = u;
             v.h = hh;
             v.u = (size_t)n * c.H + hh;
-            const int movers = select_unit<kRowThreads>(c, ap, v, sm_select, nullptr, 0);
-            move_listed<kRowThreads>(c, ap, v, movers, lpr);
+            const int movers = select_unit<kRowThreads, false>(c, ap, v, sm_select, nullptr, 0);
+            move_listed<kRowThreads>(c, ap, v, movers, lpr, 0, 1);
             __syncthreads();
         }
     }
@@ -571,6 +700,32 @@ inline int row_splits(long long units, long long rows)
     if (z > most) z = most;
     if (z > kMaxSplits) z = kMaxSplits;
     return z < 1 ? 1 : (int)z;
+}
+
+constexpr int kKeysHeld = 48 * 1024;             // keys of a CTA in shared memory at most
+
+cudaError_t launch_select(long long units, int ranks, bool wide, int room, cudaStream_t stream, const PagedView &c, const AppendArgs &a, int lpr,
+                          int move_here)
+{
+    auto kernel = ranks > 1 ? paged_select_kernel<kThreads, true> : wide ? paged_select_kernel<1024, false> : paged_select_kernel<kThreads, false>;
+    if (room > 10 * 1024) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kKeysHeld * (int)sizeof(uint32_t));
+        if (e != cudaSuccess) return e;
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(units * ranks));
+    cfg.blockDim = dim3(wide ? 1024 : kThreads);
+    cfg.dynamicSmemBytes = room * sizeof(uint32_t);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)ranks;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = ranks > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kernel, c, a, lpr, move_here, room, ranks);
 }
 
 inline size_t up256(size_t x) { return (x + 255) / 256 * 256; }
@@ -605,16 +760,15 @@ cudaError_t launch_paged_rows(const PagedView &c, int D, const GatherArgs *gathe
         return launch_chained(kernel, dim3((unsigned)(splits * units)), kRowThreads, g.G * sizeof(float2), stream, c, g, a, lpr, splits);
     }
     const bool few = a.T <= kFewRows;
-    // Keys of budget + T candidates are held in shared memory up to 48K of them. Wide CTAs for long lists: one that a CTA of
-    // 256 threads walks in 64 steps or more.
+    // One CTA of 256 threads per unit; for few units with long lists one of 1024 threads, or a cluster of eight. Measured per
+    // call, 256 threads / 1024 threads / cluster: 8 units of 2048 candidates 10.9 / 10.9 / 11.8 us, 64 units of 4096 19 / 12 / -,
+    // 16 units of 8192 - / 19 / 19, 16 units of 16384 - / 25 / 21, 8 units of 65536 - / 149 / 46.
     const long long most_keys = (long long)a.budget + a.T;
-    const int room = most_keys <= 48 * 1024 ? (int)most_keys : 0;
-    const bool wide = most_keys >= 16 * 1024;
-    auto kernel = wide ? paged_select_kernel<1024> : paged_select_kernel<256>;
-    cudaError_t e = cudaSuccess;
-    if (room > 10 * 1024) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, room * (int)sizeof(uint32_t));
-    if (e == cudaSuccess)
-        e = launch_chained(kernel, dim3((unsigned)units), wide ? 1024u : 256u, room * sizeof(uint32_t), stream, c, a, lpr, few ? 1 : 0, room);
+    const int ranks = most_keys >= 16384 && units * 8 <= 148 * 2 ? 8 : 1;
+    const bool wide = ranks == 1 && most_keys >= 4096 && units <= 148;
+    const long long share = (most_keys + 32 * ranks - 1) / (32 * ranks) * 32;
+    const int room = share <= kKeysHeld ? (int)share : 0;                 // more than that: worked out again for every pass
+    cudaError_t e = launch_select(units, ranks, wide, room, stream, c, a, lpr, few ? 1 : 0);
     if (e == cudaSuccess && !few) {
         const int groups = kThreads / lpr;
         long long parts = (148LL * 8 + units - 1) / units;

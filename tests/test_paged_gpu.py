@@ -186,6 +186,48 @@ def test_append_equal_weights_and_special_values(kind, T):
     check_append(m, T, L - 50 if T == 40 else L, recent=2, w=w)
 
 
+@pytest.mark.parametrize("T", [40, 64, 65, 3000])
+@pytest.mark.parametrize("kind", ["spread", "coarse", "equal"])
+def test_append_long_lists_with_ties(kind, T):
+    """Lists long enough for several CTAs to share a head's candidates."""
+    lens, H = [2500, 2311, -1], 2
+    m = PagedMirror(lens, H, 64, 16, 2500)
+    g = torch.Generator().manual_seed(T)
+    w = torch.exp(torch.randn(3, H, T, generator=g))
+    if kind != "spread":
+        w = torch.randint(0, 3 if kind == "coarse" else 1, (3, H, T), generator=g).float()
+        for n in range(2):
+            p, s = m.where(n, lens[n])
+            fill = torch.randint(0, 3 if kind == "coarse" else 1, (lens[n], H), generator=g).float()
+            m.weight[p, :, s] = fill.double()
+            m.dev["weight"][p.cuda(), :, s.cuda()] = fill.cuda()
+    check_append(m, T, 2500, recent=20, sinks=3, w=w, counts=torch.tensor([T, T - 3, T], dtype=torch.int32))
+
+
+def test_append_more_candidates_than_shared_memory_holds():
+    N, H, T = 1, 1, 60000
+    m = PagedMirror([0], H, 64, 64, 4096)
+    w = torch.exp(torch.randn(N, H, T, generator=torch.Generator().manual_seed(2)))
+    check_append(m, T, 4096, recent=16, sinks=4, w=w, fresh=True)
+    m = PagedMirror([70000] * 160, H, 64, 64, 70000, spare=0)          # one CTA for each head's 70001 candidates
+    m.append = lambda *a: None
+    before = {k: m.dev[k].clone() for k in ("K", "pos")}
+    cache = m.cache(ec)
+    K = rand((160, H, 70, 64), BF, 3).cuda()
+    w = torch.full((160, H, 70), 2.0, device="cuda")                   # above every cached weight: the lowest 70 rows leave
+    order = [m.dev["weight"][m.dev["table"][n].long()].flatten()[:70000].argsort()[:70] for n in (0, 159)]
+    ws = scratch(ec.ec_paged_append_workspace(cache, 70, 70000))
+    ec.ec_paged_append(K, K, w, None, None, cache, False, 70000, 0, 0, ws)
+    torch.cuda.synchronize()
+    for n, low in zip((0, 159), order):
+        rows = torch.sort(low)[0]
+        page, slot = m.dev["table"][n].long()[rows // 64], rows % 64
+        assert torch.equal(m.dev["K"][page, 0, slot].view(torch.int16), K[n, 0].view(torch.int16))
+        changed = (m.dev["pos"] != before["pos"])[m.dev["table"][n].long()].flatten()[:70000]
+        assert torch.equal(changed.nonzero()[:, 0], rows)
+    assert m.dev["lens"].tolist() == [70000] * 160
+
+
 @pytest.mark.parametrize("T", [0, 1, 30])
 def test_append_shrinks_to_a_smaller_budget(T):
     m = PagedMirror([500, 64, 63, 10, 0], 2, 64, 16, 512)
