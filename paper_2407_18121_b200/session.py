@@ -145,3 +145,75 @@ class ElasticCacheSession:
                                 self._up, self._down, chunk)
         nb = q_host.numel() * q_host.element_size()
         return 3 * nb, nb
+
+
+class PagedCacheSession:
+    """Buffers of a paged cache that stays within `budget` rows per problem and evicts by gathered attention weight.
+
+        s = PagedCacheSession(N, H, D, budget=320, recent=16, sinks=4, scale=1/sqrt(D))
+        s.prompt(Q, K, V)                    # importance of the prompt's rows, the best `budget` of them into the pages
+        s.append(K, V, scores, fresh=True)   # the same with scores from elsewhere (grouped heads, ragged prompts)
+        s.decode(q, k_new, v_new, out)       # one token per problem: [N, Hq, D], [N, H, D], [N, H, D] -> [N, Hq, D]
+
+    Every problem owns the pages of its `budget` rows. A problem whose entry of `lens` is negative is an empty place of
+    the batch: set it to 0 to begin a sequence there, to -1 to end one.
+    """
+
+    def __init__(self, N: int, H: int, D: int, budget: int, recent: int, sinks: int, scale: float, Hq: Optional[int] = None,
+                 page_size: int = 64, dtype: torch.dtype = torch.bfloat16, decay: float = 1.0,
+                 device: Optional[torch.device] = None):
+        self.N, self.H, self.D, self.Hq = N, H, D, Hq or H
+        self.budget, self.recent, self.sinks = int(budget), int(recent), int(sinks)
+        self.scale, self.decay = float(scale), float(decay)
+        dev = device or torch.device("cuda", torch.cuda.current_device())
+        self.device = dev
+        pages = -(-self.budget // page_size)
+        self.Kp = torch.empty((N * pages, H, page_size, D), dtype=dtype, device=dev)
+        self.Vp = torch.empty_like(self.Kp)
+        self.weight = torch.zeros((N * pages, H, page_size), dtype=torch.float32, device=dev)
+        self.pos = torch.full((N * pages, H, page_size), -1, dtype=torch.int32, device=dev)
+        self.table = torch.arange(N * pages, dtype=torch.int32, device=dev).view(N, pages)
+        self.lens = torch.zeros(N, dtype=torch.int32, device=dev)
+        self.seen = torch.zeros(N, dtype=torch.int32, device=dev)
+        self.state = torch.empty(ec.ec_paged_state_bytes(N), dtype=torch.uint8, device=dev)
+        self.cache = ec.ec_paged_init(self.Kp, self.Vp, self.weight, self.pos, self.table, self.lens, self.seen, self.state)
+        self.ws_step = torch.empty(ec.ec_paged_step_workspace(self.cache, self.Hq, self.budget), dtype=torch.uint8, device=dev)
+        self._ws = {}           # workspaces of the prompt calls, by prompt length
+
+    def _prompt_ws(self, T: int):
+        if T not in self._ws:
+            u8 = dict(dtype=torch.uint8, device=self.device)
+            self._ws = {T: (torch.empty(ec.ec_importance_workspace(self.N, self.H, T, self.D), **u8),
+                            torch.empty(ec.ec_paged_append_workspace(self.cache, T, self.budget), **u8),
+                            torch.empty((self.N, self.H, T), dtype=torch.float32, device=self.device))}
+        return self._ws[T]
+
+    def append(self, K: torch.Tensor, V: torch.Tensor, scores: Optional[torch.Tensor], counts: Optional[torch.Tensor] = None,
+               fresh: bool = False) -> None:
+        """Rows [N,H,T,D] with their weights [N,H,T] join the cache; counts [N] when they are not T for every problem."""
+        T = K.shape[2]
+        ws = torch.empty(ec.ec_paged_append_workspace(self.cache, T, self.budget), dtype=torch.uint8, device=self.device)
+        ec.ec_paged_append(K, V, scores, None, counts, self.cache, fresh, self.budget, self.recent, self.sinks, ws)
+
+    def prompt(self, Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, out: Optional[torch.Tensor] = None,
+               lse: Optional[torch.Tensor] = None) -> None:
+        """Prompts of T tokens, [N,H,T,D] each (one query head per key head): their rows enter with the importance of
+        Eq. 1 as weight. With `out` the prompt's attention output comes from the same call (ec_prefill_attention)."""
+        if self.Hq != self.H:
+            raise ValueError("grouped query heads: pass the rows' weights to append()")
+        ws_imp, ws_app, scores = self._prompt_ws(K.shape[2])
+        if out is None:
+            ec.ec_importance(Q, K, scores, lse, self.scale, ws_imp)
+        else:
+            ec.ec_prefill_attention(Q, K, V, out, lse, scores, self.scale, ws_imp)
+        ec.ec_paged_append(K, V, scores, None, None, self.cache, True, self.budget, self.recent, self.sinks, ws_app)
+
+    def decode(self, q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor, out: torch.Tensor,
+               lse: Optional[torch.Tensor] = None) -> None:
+        """One generation step. May be captured into a CUDA graph and replayed with new values in the same tensors."""
+        ec.ec_paged_decode_step(q, k_new, v_new, self.cache, self.scale, self.decay, self.budget, self.recent, self.sinks, out,
+                                lse, self.ws_step)
+
+    def status(self) -> int:
+        """Synchronises; EC_OK, or EC_ERR_PAGE once a length or a table entry was out of range."""
+        return ec.ec_device_status(self.state)

@@ -8,6 +8,7 @@ import torch
 
 from paged_reference import PagedMirror, attention_bounds
 from paper_2407_18121_b200 import binding as ec
+from paper_2407_18121_b200.session import PagedCacheSession
 
 pytestmark = pytest.mark.gpu
 BF, HF = torch.bfloat16, torch.float16
@@ -378,3 +379,68 @@ def test_offsets_past_32_bits():
     torch.cuda.synchronize()
     assert torch.equal(K[n_pages - 2, :, 300 - 256], one[0, :, 0]) and int(m.dev["lens"][0]) == 301
     assert ec.ec_device_status(state) == ec.EC_OK
+
+
+# ---------------------------------------------------------------------------------------- as they are used
+
+def adopt(session):
+    """A host mirror of a session's cache as it is now."""
+    s = session
+    m = PagedMirror([0] * s.N, s.H, s.D, s.Kp.shape[2], s.budget, s.Kp.dtype, device=None, spare=0)
+    m.table, m.lens, m.seen = s.table.cpu(), s.lens.cpu().clone(), s.seen.cpu().clone()
+    m.K, m.V, m.weight, m.pos = s.Kp.cpu().clone(), s.Vp.cpu().clone(), s.weight.cpu().double(), s.pos.cpu().clone()
+    m.dev = dict(K=s.Kp, V=s.Vp, weight=s.weight, pos=s.pos, lens=s.lens, seen=s.seen)
+    return m
+
+
+@pytest.mark.parametrize("with_output", [False, True])
+def test_prompt_then_steps_then_a_new_prompt(with_output):
+    N, H, D, T, budget = 3, 2, 64, 150, 80
+    s = PagedCacheSession(N, H, D, budget, recent=12, sinks=2, scale=0.125, page_size=32)
+    s.lens[1] = -1                                                     # an empty place
+    for round_ in range(2):
+        Q, K, V = (rand((N, H, T, D), BF, 10 * round_ + i) for i in range(3))
+        m = adopt(s)
+        out = torch.empty(N, H, T, D, dtype=BF, device="cuda") if with_output else None
+        s.prompt(Q.cuda(), K.cuda(), V.cuda(), out)
+        torch.cuda.synchronize()
+        scores = s._ws[T][2].cpu()
+        x = torch.einsum("nhmd,nhkd->nhmk", Q.double(), K.double()) * 0.125
+        p = torch.softmax(x.masked_fill(torch.ones(T, T).triu(1).bool(), -math.inf), -1)
+        assert (scores.double() - p.sum(2)).abs().max() <= 1e-3 * p.sum(2).max()
+        if with_output:
+            assert ((out.cpu().double() - p @ V.double()).abs() <= 2e-2 + 2.0 ** -8 * (p @ V.double()).abs()).all()
+        m.append(K, V, scores, None, None, T, True, budget, 12, 2)
+        m.assert_same_rows(0.0, "prompt")
+        for i in range(10):
+            q, k, v = (rand((N, H, D), BF, 100 + 3 * i + j) for j in range(3))
+            got = torch.empty(N, H, D, dtype=BF, device="cuda")
+            s.decode(q.cuda(), k.cuda(), v.cuda(), got)
+            ref, mass, dx = m.attention(q, k, v, 0.125, True)
+            out_tol, _, w_tol = attention_bounds(ref, mass, dx, BF, 1)
+            m.append(k[:, :, None], v[:, :, None], ref[2][:, :, None], None, None, 1, False, budget, 12, 2)
+            assert ((got.cpu().double() - ref[0]).abs() <= out_tol).all()
+            m.assert_same_rows((i + 1) * (w_tol + float(m.weight.max()) * 2.0 ** -22), f"step {i}")
+        assert s.status() == ec.EC_OK and s.lens.tolist() == [budget, -1, budget] and s.seen.tolist()[0] == T + 10
+
+
+def test_binding_refuses_wrong_tensors():
+    s = PagedCacheSession(2, 2, 64, 64, 4, 0, 0.125)
+    q = torch.zeros(2, 2, 64, dtype=BF, device="cuda")
+    out = torch.empty_like(q)
+    for bad in (q.half(), q[:1], q.cpu(), torch.zeros(2, 64, 2, dtype=BF, device="cuda").transpose(1, 2)):
+        with pytest.raises(ValueError):
+            s.decode(q, bad, q, out)
+    with pytest.raises(ValueError):
+        ec.ec_paged_init(s.Kp, s.Vp.transpose(1, 2), s.weight, s.pos, s.table, s.lens, s.seen, s.state)
+    with pytest.raises(ValueError):
+        ec.ec_paged_init(s.Kp, s.Vp, s.weight[:1], s.pos, s.table, s.lens, s.seen, s.state)
+    with pytest.raises(ValueError):
+        ec.ec_paged_init(s.Kp, s.Vp, s.weight, s.pos, s.table, s.lens, s.seen, s.state[:256])
+    with pytest.raises(ec.EcError) as e:
+        ec.ec_paged_append(q[:, :, None], q[:, :, None], None, None, None, s.cache, False, 65, 4, 0, s.ws_step)
+    assert e.value.status == ec.EC_ERR_ARG
+    with pytest.raises(ec.EcError) as e:
+        ec.ec_paged_decode_step(q, q, q, s.cache, 0.125, 1.0, 64, 4, 0, out, None, s.ws_step[:256])
+    assert e.value.status == ec.EC_ERR_WORKSPACE
+    assert s.lens.tolist() == [0, 0]
