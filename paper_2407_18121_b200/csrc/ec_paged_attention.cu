@@ -21,7 +21,7 @@ namespace ec {
 
 namespace {
 
-constexpr int kTile = 16;                        // rows of a warp's tile
+template <int D> constexpr int kTileRows = 2048 / D;                      // rows of a warp's tile: 4 KB of K, 4 KB of V
 constexpr float kLazy = 8.f;                     // the running maximum is raised when exceeded by more than this (log2)
 
 struct Bf16 {
@@ -79,6 +79,8 @@ __device__ __forceinline__ void load_matrices_trans(uint32_t (&r)[4], uint32_t a
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
 
+template <int V> struct Int { static constexpr int value = V; };
+
 struct AttnArgs {
     PagedView c;
     const uint32_t *q;
@@ -112,14 +114,14 @@ struct Plan {
     int per, n, rows, before;                    // n < 0: nothing to do; the count in front of problem n
 };
 
-template <int W>
-__device__ __forceinline__ int blocks_of(int rows) { return (rows + W * kTile - 1) / (W * kTile); }
+template <int BR>                                // rows of a block
+__device__ __forceinline__ int blocks_of(int rows) { return (rows + BR - 1) / BR; }
 
-template <int W>
-__device__ __forceinline__ int cost_of(int rows) { return rows > 0 ? blocks_of<W>(rows) + kUnitCost : 0; }
+template <int BR>
+__device__ __forceinline__ int cost_of(int rows) { return rows > 0 ? blocks_of<BR>(rows) + kUnitCost : 0; }
 
 // Each warp works it out for itself: a lane sums a span of problems, no barrier.
-template <int W>
+template <int BR>
 __device__ __forceinline__ Plan make_plan(const AttnArgs &a, int units)
 {
     const int N = a.c.N, lane = threadIdx.x & 31;
@@ -129,7 +131,7 @@ __device__ __forceinline__ Plan make_plan(const AttnArgs &a, int units)
 #pragma unroll 8
     for (int n = n0; n < n1; ++n) {
         rows = rows_of(a, n);                    // with one problem a lane this is the one needed below
-        mine += cost_of<W>(rows);
+        mine += cost_of<BR>(rows);
     }
     int incl = mine;
 #pragma unroll
@@ -151,7 +153,7 @@ __device__ __forceinline__ Plan make_plan(const AttnArgs &a, int units)
         int begin = at;
 #pragma unroll 8
         for (int i = n0; i < n1; ++i) {
-            const int r = rows_of(a, i), cost = cost_of<W>(r) * units;
+            const int r = rows_of(a, i), cost = cost_of<BR>(r) * units;
             if (first >= begin && first < begin + cost) {
                 n = i;
                 rows = r;
@@ -175,7 +177,7 @@ struct Walk {
     int left;                                    // what is left of the CTA's count, this block included
 };
 
-template <int W>
+template <int BR>
 __device__ __forceinline__ void next_unit(const AttnArgs &a, int head_blocks, Walk &w)
 {
     w.blk = 0;
@@ -189,26 +191,28 @@ __device__ __forceinline__ void next_unit(const AttnArgs &a, int head_blocks, Wa
             return;
         }
         w.rows = rows_of(a, w.n);
-        w.nb = blocks_of<W>(w.rows);
+        w.nb = blocks_of<BR>(w.rows);
     } while (w.nb == 0);
 }
 
-template <int W>
+template <int BR>
 __device__ __forceinline__ void walk_on(const AttnArgs &a, int head_blocks, Walk &w)
 {
     --w.left;
     if (++w.blk < w.nb) return;
     w.left -= kUnitCost;
-    if (w.left > 0) next_unit<W>(a, head_blocks, w);
+    if (w.left > 0) next_unit<BR>(a, head_blocks, w);
 }
 
 // Shared memory of a CTA of W warps that handles 8 NT query heads.
 template <int D, int NT, int W> struct Smem {
+    static constexpr int kTile = kTileRows<D>;
     static constexpr int kTileBytes = kTile * D * 2;                      // of K, and of V behind it
-    static constexpr int kStages = D == 128 ? 3 : 6;                      // 24 KB per warp
+    static constexpr int kStages = 3;                                     // 24 KB per warp
     static constexpr int kPitch = D + 4;                                  // floats of a head in the merge buffer: no bank conflicts
-    static constexpr int kMergeHeads = W == 8 && NT == 1 ? 4 : 2;
-    static constexpr int kMergeFloats = W * kMergeHeads * kPitch;
+    static constexpr int kMergeHeads = (W == 8 && NT == 1) || D == 64 ? 4 : 2;
+    static constexpr int kMergeSlots = W * kMergeHeads;                   // (warp, head) pairs that fit the merge buffer
+    static constexpr int kMergeFloats = kMergeSlots * kPitch;
     static constexpr int kQBytes = 8 * NT * D * 2;
     static constexpr int kQSlots = kStages + 1;                           // the copies run at most kStages units ahead
     static constexpr int kRing = 0;
@@ -358,7 +362,8 @@ template <typename E, int D, int NT, int W, bool GATHER>
 __global__ void __launch_bounds__(W * 32, 8 / W) paged_attention_kernel(AttnArgs a, int head_blocks)
 {
     using M_ = Smem<D, NT, W>;
-    constexpr int kThreads = W * 32, kBlockRows = W * kTile;
+    constexpr int kThreads = W * 32, kTile = M_::kTile, kBlockRows = W * kTile;
+    constexpr int RT = kTile / 16;               // 16-row sides of the products in a tile
     constexpr int C = D / 8;                     // 16-byte pieces of a row
     constexpr int KS = D / 16, MT = D / 16;
     constexpr int S = M_::kStages;
@@ -375,7 +380,7 @@ __global__ void __launch_bounds__(W * 32, 8 / W) paged_attention_kernel(AttnArgs
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int G = a.G, H = a.c.H, Hq = H * G;
     const int units = H * head_blocks;           // of a problem
-    const Plan plan = make_plan<W>(a, units);
+    const Plan plan = make_plan<kBlockRows>(a, units);
     // problems without a row to attend to have no block: their outputs are written here
     for (int n = blockIdx.x; n < a.c.N; n += gridDim.x) {
         read_len(a.c, n);                        // reports a length past the table's reach
@@ -391,7 +396,7 @@ __global__ void __launch_bounds__(W * 32, 8 / W) paged_attention_kernel(AttnArgs
     Walk use;
     use.n = plan.n;
     use.rows = plan.rows;
-    use.nb = blocks_of<W>(use.rows);
+    use.nb = blocks_of<kBlockRows>(use.rows);
     use.left = plan.per;
     {
         const unsigned in = (unsigned)(plan.per * (int)blockIdx.x - plan.before);
@@ -402,7 +407,7 @@ __global__ void __launch_bounds__(W * 32, 8 / W) paged_attention_kernel(AttnArgs
         use.hb = unit - use.h * head_blocks;
         if (use.blk >= use.nb) {                 // the share begins behind the unit's blocks
             use.left -= (int)cost - use.blk;
-            if (use.left > 0) next_unit<W>(a, head_blocks, use);
+            if (use.left > 0) next_unit<kBlockRows>(a, head_blocks, use);
         }
     }
     Walk ahead = use, scout = use;
@@ -412,7 +417,7 @@ __global__ void __launch_bounds__(W * 32, 8 / W) paged_attention_kernel(AttnArgs
     uint2 *rows_info = reinterpret_cast<uint2 *>(smem + M_::kInfo) + warp * (S * kTile);   // (page and head, slot) of a row
     const int *pages = reinterpret_cast<const int *>(smem + M_::kPages) + warp * (S * kTile);
     const uint32_t pages_at = base + M_::kPages + warp * (S * kTile * 4);
-    const int tile_row = warp * kTile + (lane & 15);                      // of a block, described by this lane
+    const int tile_row = warp * kTile + lane % kTile;                     // of a block, described by this lane
     const int own_row = a.k_new ? 1 : 0;
 
     // The page of every row of the tile at `scout`, S tiles before the copies need it.
@@ -423,7 +428,7 @@ __global__ void __launch_bounds__(W * 32, 8 / W) paged_attention_kernel(AttnArgs
             const int *src = a.c.table + (size_t)scout.n * a.c.max_pages + page_of(a.c, row);
             asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(pages_at + (slot * kTile + lane) * 4), "l"(src) : "memory");
         }
-        walk_on<W>(a, head_blocks, scout);
+        walk_on<kBlockRows>(a, head_blocks, scout);
     };
     int q_slot_ahead = 0;
     bool fresh_ahead = true;
@@ -443,12 +448,12 @@ __global__ void __launch_bounds__(W * 32, 8 / W) paged_attention_kernel(AttnArgs
             }
             const int row0 = ahead.blk * kBlockRows + warp * kTile;
             if (row0 < ahead.rows) {
-                const int row = row0 + (lane & 15), len = ahead.rows - own_row;
+                const int row = row0 + lane % kTile, len = ahead.rows - own_row;
                 uint32_t off = kRowNone;
                 uint2 info = make_uint2(kRowNone, 0);
                 if (row < len) {
                     Slot s;
-                    s.page = pages[stage * kTile + (lane & 15)];
+                    s.page = pages[stage * kTile + lane % kTile];
                     s.slot = row - page_of(a.c, row) * a.c.page_size;
                     if ((unsigned)s.page < (unsigned)a.c.n_pages) {
                         off = row_offset(a.c, s);
@@ -486,7 +491,7 @@ __global__ void __launch_bounds__(W * 32, 8 / W) paged_attention_kernel(AttnArgs
                 }
             }
             fresh_ahead = ahead.blk + 1 == ahead.nb;
-            walk_on<W>(a, head_blocks, ahead);
+            walk_on<kBlockRows>(a, head_blocks, ahead);
             __syncwarp();                        // the pages have been read
             scout_tile(stage);
         }
@@ -545,53 +550,67 @@ __global__ void __launch_bounds__(W * 32, 8 / W) paged_attention_kernel(AttnArgs
         if (use.blk * kBlockRows + warp * kTile < use.rows) {
             const uint32_t tile = ring + stage * (2 * M_::kTileBytes);
             // S^T of this tile, even and odd steps in chains of their own
-            float s[NT][4], s1[NT][4];
+            float s[RT][NT][4], s1[RT][NT][4];
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
+            for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) s[nt][i] = s1[nt][i] = 0.f;
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s[rt][nt][i] = s1[rt][nt][i] = 0.f;
             {
                 const int row = lane & 15;
                 const uint32_t at = (tile + row * (D * 2)) + (((lane >> 4) ^ (row & 7)) << 4);
 #pragma unroll
                 for (int ks = 0; ks < KS; ks += 2) {
-                    uint32_t a0[4], a1[4];
-                    load_matrices(a0, at ^ (ks << 5));
-                    load_matrices(a1, at ^ ((ks + 1) << 5));
+                    uint32_t r[NT][4];
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
-                        uint32_t r[4];
                         if (kHoldQ) {
-                            r[0] = qf[nt][ks][0];
-                            r[1] = qf[nt][ks][1];
-                            r[2] = qf[nt][ks + 1][0];
-                            r[3] = qf[nt][ks + 1][1];
+                            r[nt][0] = qf[nt][ks][0];
+                            r[nt][1] = qf[nt][ks][1];
+                            r[nt][2] = qf[nt][ks + 1][0];
+                            r[nt][3] = qf[nt][ks + 1][1];
                         } else {
-                            load_matrices(r, (q_at ^ (ks << 5)) + nt * 8 * (D * 2));
+                            load_matrices(r[nt], (q_at ^ (ks << 5)) + nt * 8 * (D * 2));
                         }
-                        E::mma(s[nt], a0, r[0], r[1]);
-                        E::mma(s1[nt], a1, r[2], r[3]);
+                    }
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt) {
+                        uint32_t a0[4], a1[4];
+                        load_matrices(a0, (at ^ (ks << 5)) + rt * 16 * (D * 2));
+                        load_matrices(a1, (at ^ ((ks + 1) << 5)) + rt * 16 * (D * 2));
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) {
+                            E::mma(s[rt][nt], a0, r[nt][0], r[nt][1]);
+                            E::mma(s1[rt][nt], a1, r[nt][2], r[nt][3]);
+                        }
                     }
                 }
             }
-            const uint2 info0 = rows_info[stage * kTile + g], info1 = rows_info[stage * kTile + g + 8];
-            const bool there0 = info0.x != kRowNone, there1 = info1.x != kRowNone;
+            uint2 info[RT][2];                   // rows g and g + 8 of every 16
             bool raise = false;                  // scale > 0: the scores are compared before they are scaled
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
+            for (int rt = 0; rt < RT; ++rt) {
+                info[rt][0] = rows_info[stage * kTile + rt * 16 + g];
+                info[rt][1] = rows_info[stage * kTile + rt * 16 + g + 8];
+                const bool there0 = info[rt][0].x != kRowNone, there1 = info[rt][1].x != kRowNone;
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    s[nt][i] = there0 ? s[nt][i] + s1[nt][i] : -INFINITY;
-                    s[nt][2 + i] = there1 ? s[nt][2 + i] + s1[nt][2 + i] : -INFINITY;
-                    raise |= fmaxf(s[nt][i], s[nt][2 + i]) > limit[nt][i];
-                }
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        s[rt][nt][i] = there0 ? s[rt][nt][i] + s1[rt][nt][i] : -INFINITY;
+                        s[rt][nt][2 + i] = there1 ? s[rt][nt][2 + i] + s1[rt][nt][2 + i] : -INFINITY;
+                        raise |= fmaxf(s[rt][nt][i], s[rt][nt][2 + i]) > limit[nt][i];
+                    }
             }
             if (__any_sync(0xFFFFFFFFu, raise)) {
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        float x = fmaxf(s[nt][i], s[nt][2 + i]);
+                        float x = fmaxf(s[0][nt][i], s[0][nt][2 + i]);
+#pragma unroll
+                        for (int rt = 1; rt < RT; ++rt) x = fmaxf(x, fmaxf(s[rt][nt][i], s[rt][nt][2 + i]));
 #pragma unroll
                         for (int d = 4; d < 32; d <<= 1) x = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, d));
                         const float mn = fmaxf(m[nt][i], x * a.scale_log2e);
@@ -607,50 +626,54 @@ __global__ void __launch_bounds__(W * 32, 8 / W) paged_attention_kernel(AttnArgs
                         }
                     }
             }
-            uint32_t hi[NT][2], lo[NT][2];       // P as the sum of two rounded parts: 16 bits of it or more meet V
+            uint32_t hi[RT][NT][2], lo[RT][NT][2];   // P as the sum of two rounded parts: 16 bits of it or more meet V
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                float p[4];
+            for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) p[i] = fast_exp2(fmaf(s[nt][i], a.scale_log2e, neg_m[nt][i & 1]));
-                l[nt][0] += p[0] + p[2];
-                l[nt][1] += p[1] + p[3];
+                for (int nt = 0; nt < NT; ++nt) {
+                    float p[4];
 #pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    const uint32_t x = E::pack(p[2 * r], p[2 * r + 1]);
-                    const float2 f = E::unpack(x);
-                    hi[nt][r] = transpose8x8(x);
-                    lo[nt][r] = transpose8x8(E::pack(p[2 * r] - f.x, p[2 * r + 1] - f.y));
+                    for (int i = 0; i < 4; ++i) p[i] = fast_exp2(fmaf(s[rt][nt][i], a.scale_log2e, neg_m[nt][i & 1]));
+                    l[nt][0] += p[0] + p[2];
+                    l[nt][1] += p[1] + p[3];
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) {
+                        const uint32_t x = E::pack(p[2 * r], p[2 * r + 1]);
+                        const float2 f = E::unpack(x);
+                        hi[rt][nt][r] = transpose8x8(x);
+                        lo[rt][nt][r] = transpose8x8(E::pack(p[2 * r] - f.x, p[2 * r + 1] - f.y));
+                    }
                 }
-            }
             {
                 const int row = (lane & 7) + (lane >> 4) * 8;
                 const uint32_t at = (tile + M_::kTileBytes + row * (D * 2)) + ((((lane >> 3) & 1) ^ (row & 7)) << 4);
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt) {
-                    uint32_t av[4];
-                    load_matrices_trans(av, at ^ (mt << 5));
+                for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) {
-                        E::mma(o[nt][mt], av, hi[nt][0], hi[nt][1]);
-                        E::mma(o[nt][mt], av, lo[nt][0], lo[nt][1]);
+                    for (int mt = 0; mt < MT; ++mt) {
+                        uint32_t av[4];
+                        load_matrices_trans(av, (at ^ (mt << 5)) + rt * 16 * (D * 2));
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) {
+                            E::mma(o[nt][mt], av, hi[rt][nt][0], hi[rt][nt][1]);
+                            E::mma(o[nt][mt], av, lo[rt][nt][0], lo[rt][nt][1]);
+                        }
                     }
-                }
             }
             if (GATHER) {                        // behind the products: the stores' addresses are in nobody's way here
 #pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    const uint2 info = r ? info1 : info0;
-                    if (info.x == kRowNone) continue;
-                    const bool own = info.x == kRowNew;
+                for (int r = 0; r < 2 * RT; ++r) {
+                    const uint2 at = info[r >> 1][r & 1];
+                    if (at.x == kRowNone) continue;
+                    const bool own = at.x == kRowNew;
                     const int step = own ? 1 : a.c.page_size;
-                    float *dst = (own ? a.score_new + head_at : a.scores + ((size_t)info.x * G + head0) * a.c.page_size + info.y) +
+                    float *dst = (own ? a.score_new + head_at : a.scores + ((size_t)at.x * G + head0) * a.c.page_size + at.y) +
                                  (size_t)(2 * t) * step;
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
                         const int hd = nt * 8 + 2 * t;
-                        if (hd < heads) dst[(size_t)(nt * 8) * step] = s[nt][2 * r];
-                        if (hd + 1 < heads) dst[(size_t)(nt * 8 + 1) * step] = s[nt][2 * r + 1];
+                        if (hd < heads) dst[(size_t)(nt * 8) * step] = s[r >> 1][nt][2 * (r & 1)];
+                        if (hd + 1 < heads) dst[(size_t)(nt * 8 + 1) * step] = s[r >> 1][nt][2 * (r & 1) + 1];
                     }
                 }
             }
@@ -660,73 +683,91 @@ __global__ void __launch_bounds__(W * 32, 8 / W) paged_attention_kernel(AttnArgs
         stage = stage + 1 == S ? 0 : stage + 1;
 
         if (use.blk + 1 == use.nb || use.left == 1) {
-            // the warps' results meet in shared memory, a few heads at a time
+            const bool whole = first_block == 0 && use.blk + 1 == use.nb;
+            const int part = 2 * blockIdx.x + (first_block == 0 ? 1 : 0); // a CTA holds at most one part of each kind
+            const int seen_rows = min(use.rows, (use.blk + 1) * kBlockRows) - first_block * kBlockRows;
+            const int nw = min(W, (seen_rows + kTile - 1) / kTile);       // warps that had a tile of it
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    float x = l[nt][i];
+                for (int i = 0; i < 2; ++i)
 #pragma unroll
-                    for (int d = 4; d < 32; d <<= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, d);
-                    if (g == 0) sm_ml[warp][nt * 8 + 2 * t + i] = make_float2(m[nt][i], x);
+                    for (int d = 4; d < 32; d <<= 1) l[nt][i] += __shfl_xor_sync(0xFFFFFFFFu, l[nt][i], d);
+            auto finish = [&](int hd, float M, float L, float mu, float inv) {   // what is kept of a head beside its output
+                if (whole) {
+                    a.stat[head_at + hd] = make_float2(mu, inv);
+                    if (a.lse) a.lse[head_at + hd] = M == -INFINITY ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+                } else {
+                    a.part_ml[(size_t)part * 8 * NT + hd] = make_float2(M, L);
                 }
-            const bool whole = first_block == 0 && use.blk + 1 == use.nb;
-            const int part = 2 * blockIdx.x + (first_block == 0 ? 1 : 0); // a CTA holds at most one part of each kind
-            constexpr int kShare = W / M_::kMergeHeads;                   // warps that put one head together
-            for (int h0 = 0; h0 < heads; h0 += M_::kMergeHeads) {
+            };
+            if (warp < nw && g == 0) {
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const int at = nt * 8 + 2 * t + i - h0;
-                        if (at < 0 || at >= M_::kMergeHeads) continue;
-                        float *dst = sm_o + (warp * M_::kMergeHeads + at) * M_::kPitch + g;
+                    for (int i = 0; i < 2; ++i) sm_ml[warp][nt * 8 + 2 * t + i] = make_float2(m[nt][i], l[nt][i]);
+            }
+            // the warps' results meet in shared memory, `per_round` heads of up to `most` warps at a time
+            auto meet = [&](auto per_round_, auto most_) {
+                constexpr int per_round = decltype(per_round_)::value, most = decltype(most_)::value;
+                for (int h0 = 0; h0 < heads; h0 += per_round) {
+                    if (warp < nw) {
 #pragma unroll
-                        for (int mt = 0; mt < MT; ++mt) {
-                            dst[mt * 16] = o[nt][mt][i];
-                            dst[mt * 16 + 8] = o[nt][mt][2 + i];
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) {
+                                const int at = nt * 8 + 2 * t + i - h0;
+                                if (at < 0 || at >= per_round) continue;
+                                float *dst = sm_o + (warp * per_round + at) * M_::kPitch + g;
+#pragma unroll
+                                for (int mt = 0; mt < MT; ++mt) {
+                                    dst[mt * 16] = o[nt][mt][i];
+                                    dst[mt * 16 + 8] = o[nt][mt][2 + i];
+                                }
+                            }
+                    }
+                    __syncthreads();
+                    const int items = min(per_round, heads - h0) * (D / 64);   // 64 dimensions of a head, by a warp
+                    for (int it = warp; it < items; it += W) {
+                        const int at = it / (D / 64), hd = h0 + at, d = (it % (D / 64)) * 64 + 2 * lane;
+                        float2 ml[most];
+                        float M = -INFINITY, L = 0.f;
+#pragma unroll
+                        for (int w = 0; w < most; ++w) {
+                            ml[w] = w < nw ? sm_ml[w][hd] : make_float2(-INFINITY, 0.f);
+                            M = fmaxf(M, ml[w].x);
                         }
-                    }
-                __syncthreads();
-                const int hd = h0 + warp / kShare;
-                if (hd < heads) {
-                    float M = -INFINITY;
-#pragma unroll
-                    for (int w = 0; w < W; ++w) M = fmaxf(M, sm_ml[w][hd].x);
-                    const float mu = M == -INFINITY ? 0.f : M;
-                    float L = 0.f, f[W];
-#pragma unroll
-                    for (int w = 0; w < W; ++w) {
-                        f[w] = fast_exp2(sm_ml[w][hd].x - mu);
-                        L = fmaf(sm_ml[w][hd].y, f[w], L);
-                    }
-                    const float inv = L == 0.f ? 0.f : 1.f / L;           // nothing left by the scores: the output is zero
-#pragma unroll
-                    for (int d = 0; d < D; d += 64) {
-                        if ((d / 64) % kShare != warp % kShare) continue;
+                        const float mu = M == -INFINITY ? 0.f : M;
                         float2 A = make_float2(0.f, 0.f);
 #pragma unroll
-                        for (int w = 0; w < W; ++w) {
-                            const float2 v = *reinterpret_cast<const float2 *>(
-                                sm_o + (w * M_::kMergeHeads + warp / kShare) * M_::kPitch + d + 2 * lane);
-                            A.x = fmaf(v.x, f[w], A.x);
-                            A.y = fmaf(v.y, f[w], A.y);
+                        for (int w = 0; w < most; ++w) {
+                            if (w >= nw) continue;
+                            const float f = fast_exp2(ml[w].x - mu);
+                            const float2 v = *reinterpret_cast<const float2 *>(sm_o + (w * per_round + at) * M_::kPitch + d);
+                            L = fmaf(ml[w].y, f, L);
+                            A.x = fmaf(v.x, f, A.x);
+                            A.y = fmaf(v.y, f, A.y);
                         }
-                        if (whole) a.out[(head_at + hd) * (D / 2) + d / 2 + lane] = E::pack(A.x * inv, A.y * inv);
-                        else *reinterpret_cast<float2 *>(a.part_o + ((size_t)part * 8 * NT + hd) * D + d + 2 * lane) = A;
-                    }
-                    if (lane == 0 && warp % kShare == 0) {
-                        if (whole) {
-                            a.stat[head_at + hd] = make_float2(mu, inv);
-                            if (a.lse) a.lse[head_at + hd] = M == -INFINITY ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
-                        } else {
-                            a.part_ml[(size_t)part * 8 * NT + hd] = make_float2(M, L);
+                        const float inv = L == 0.f ? 0.f : 1.f / L;       // nothing left by the scores: the output is zero
+                        if (whole) a.out[((head_at + hd) * D + d) >> 1] = E::pack(A.x * inv, A.y * inv);
+                        else *reinterpret_cast<float2 *>(a.part_o + ((size_t)part * 8 * NT + hd) * D + d) = A;
+                        if (d == 0) {            // what is kept of a head beside its output
+                            if (whole) {
+                                a.stat[head_at + hd] = make_float2(mu, inv);
+                                if (a.lse) a.lse[head_at + hd] = M == -INFINITY ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+                            } else {
+                                a.part_ml[(size_t)part * 8 * NT + hd] = make_float2(M, L);
+                            }
                         }
                     }
+                    copies_wait<S - 1>();        // with the barrier: the next unit's queries are here
+                    __syncthreads();
                 }
-                copies_wait<S - 1>();            // with the barrier: the next unit's queries are here
-                __syncthreads();
-            }
+            };
+            // sixteen heads leave room for two at a time from eight warps: a unit of one or two tiles takes them in two
+            // rounds instead of eight (49 x 40 units of 22 rows: 118 -> 80 us)
+            if (NT == 2 && nw <= 2) meet(Int<M_::kMergeSlots / 2>(), Int<2>());
+            else meet(Int<M_::kMergeHeads>(), Int<W>());
             if (!whole) {
                 // the unit's first and last CTA follow from its first block; the last of them to get here joins the parts
                 const int b0 = plan.per * blockIdx.x + (plan.per - use.left) - use.blk;
@@ -742,7 +783,7 @@ __global__ void __launch_bounds__(W * 32, 8 / W) paged_attention_kernel(AttnArgs
             }
             begin = true;
         }
-        walk_on<W>(a, head_blocks, use);
+        walk_on<kBlockRows>(a, head_blocks, use);
     }
 }
 
