@@ -522,6 +522,8 @@ __global__ void __launch_bounds__(kRowThreads, kRowCtas) paged_rows_kernel(Paged
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int G = GATHER ? ga.G : 0;
     const size_t head_at = (size_t)unit * G;
+    const bool by_row = scores_by_row(c.page_size);
+    const int score_rows = by_row ? c.max_pages * c.page_size : c.page_size;
     Unit u;
     if (APPEND) {
         u = load_unit(c, ap, n, h);
@@ -555,7 +557,9 @@ __global__ void __launch_bounds__(kRowThreads, kRowCtas) paged_rows_kernel(Paged
             const Slot s = find_slot(c, n, row);
             there[r] = s.page >= 0;
             m[r] = meta_index(c, h, s);
-            if (GATHER) score[r] = ga.scores + (size_t)((uint32_t)s.page * (uint32_t)c.H + (uint32_t)h) * G * c.page_size + s.slot;
+            if (GATHER)
+                score[r] = by_row ? ga.scores + head_at * score_rows + row
+                                  : ga.scores + (size_t)((uint32_t)s.page * (uint32_t)c.H + (uint32_t)h) * G * score_rows + s.slot;
             if (APPEND && !there[r]) low = min(low, leave_order(0, row)); // a row that cannot be read leaves first
         }
 #pragma unroll
@@ -579,7 +583,7 @@ __global__ void __launch_bounds__(kRowThreads, kRowCtas) paged_rows_kernel(Paged
                     if (h0 + i >= G) continue;
 #pragma unroll
                     for (int r = 0; r < kRowsHeld; ++r)
-                        if (there[r]) x[i][r] = __ldcg(score[r] + (size_t)(h0 + i) * c.page_size);
+                        if (there[r]) x[i][r] = __ldcg(score[r] + (size_t)(h0 + i) * score_rows);
                 }
                 if (first && h0 == 0) __syncthreads();
 #pragma unroll

@@ -94,7 +94,8 @@ struct AttnArgs {
     float *score_new;                            // [N, Hq] the same of the step's own row
     float *part_o;                               // [2 * CTAs][8 NT][D]
     float2 *part_ml;                             // [2 * CTAs][8 NT]
-    float *scores;                               // [n_pages, H, G, page_size]: <q, k>, not scaled
+    float *scores;                               // <q, k>, not scaled, see scores_by_row
+    int score_rows;                              // of one query head in a run: page_size or max_pages * page_size
 };
 
 // Rows of problem n with its own new row, 0 when there is nothing to attend to. A length past the table's reach is cut.
@@ -414,7 +415,7 @@ __global__ void __launch_bounds__(W * 32, 8 / W) paged_attention_kernel(AttnArgs
 
     const uint32_t base = (uint32_t)__cvta_generic_to_shared(smem);
     const uint32_t ring = base + M_::kRing + warp * (S * 2 * M_::kTileBytes);
-    uint2 *rows_info = reinterpret_cast<uint2 *>(smem + M_::kInfo) + warp * (S * kTile);   // (page and head, slot) of a row
+    uint2 *rows_info = reinterpret_cast<uint2 *>(smem + M_::kInfo) + warp * (S * kTile);   // where a row's score lies: (run, row in the run)
     const int *pages = reinterpret_cast<const int *>(smem + M_::kPages) + warp * (S * kTile);
     const uint32_t pages_at = base + M_::kPages + warp * (S * kTile * 4);
     const int tile_row = warp * kTile + lane % kTile;                     // of a block, described by this lane
@@ -457,7 +458,8 @@ __global__ void __launch_bounds__(W * 32, 8 / W) paged_attention_kernel(AttnArgs
                     s.slot = row - page_of(a.c, row) * a.c.page_size;
                     if ((unsigned)s.page < (unsigned)a.c.n_pages) {
                         off = row_offset(a.c, s);
-                        info = make_uint2((uint32_t)s.page * (uint32_t)H + (uint32_t)h, (uint32_t)s.slot);
+                        info = scores_by_row(a.c.page_size) ? make_uint2((uint32_t)ahead.n * (uint32_t)H + (uint32_t)h, (uint32_t)row)
+                                                            : make_uint2((uint32_t)s.page * (uint32_t)H + (uint32_t)h, (uint32_t)s.slot);
                     } else {
                         atomicExch(a.c.state, kStatusPage);
                     }
@@ -666,8 +668,8 @@ __global__ void __launch_bounds__(W * 32, 8 / W) paged_attention_kernel(AttnArgs
                     const uint2 at = info[r >> 1][r & 1];
                     if (at.x == kRowNone) continue;
                     const bool own = at.x == kRowNew;
-                    const int step = own ? 1 : a.c.page_size;
-                    float *dst = (own ? a.score_new + head_at : a.scores + ((size_t)at.x * G + head0) * a.c.page_size + at.y) +
+                    const int step = own ? 1 : a.score_rows;
+                    float *dst = (own ? a.score_new + head_at : a.scores + ((size_t)at.x * G + head0) * a.score_rows + at.y) +
                                  (size_t)(2 * t) * step;
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
@@ -793,7 +795,7 @@ struct WsLayout {
     size_t stat, score_new, part_o, part_ml, scores, total;
 };
 
-WsLayout layout(int N, int H, int D, int n_pages, int page_size, int G, int accumulate)
+WsLayout layout(int N, int H, int D, int n_pages, int page_size, int max_pages, int G, int accumulate)
 {
     const int nt = G > 8 ? 2 : 1;
     WsLayout w;
@@ -807,7 +809,8 @@ WsLayout layout(int N, int H, int D, int n_pages, int page_size, int G, int accu
     w.score_new = take((size_t)N * H * G * sizeof(float));
     w.part_o = take((size_t)2 * kPagedMaxCtas * 8 * nt * D * sizeof(float));
     w.part_ml = take((size_t)2 * kPagedMaxCtas * 8 * nt * sizeof(float2));
-    w.scores = take(accumulate ? (size_t)n_pages * H * page_size * G * sizeof(float) : 0);
+    const size_t rows = scores_by_row(page_size) ? (size_t)N * max_pages * page_size : (size_t)n_pages * page_size;
+    w.scores = take(accumulate ? rows * H * G * sizeof(float) : 0);
     w.total = at;
     return w;
 }
@@ -855,7 +858,7 @@ cudaError_t launch_d(const AttnArgs &a, int accumulate, cudaStream_t stream)
 
 size_t paged_attention_workspace_bytes(const ec_paged *c, int Hq, int accumulate)
 {
-    return layout(c->N, c->H, c->D, c->n_pages, c->page_size, Hq / c->H, accumulate).total;
+    return layout(c->N, c->H, c->D, c->n_pages, c->page_size, c->max_pages, Hq / c->H, accumulate).total;
 }
 
 cudaError_t launch_paged_attention(const PagedView &c, int D, int dtype, const void *q, const void *k_new, const void *v_new,
@@ -872,13 +875,14 @@ cudaError_t launch_paged_attention(const PagedView &c, int D, int dtype, const v
     a.inv_scale = 1.f / a.scale_log2e;
     a.out = static_cast<uint32_t *>(out);
     a.lse = lse;
-    const WsLayout w = layout(c.N, c.H, D, c.n_pages, c.page_size, a.G, accumulate);
+    const WsLayout w = layout(c.N, c.H, D, c.n_pages, c.page_size, c.max_pages, a.G, accumulate);
     char *p = static_cast<char *>(ws);
     a.stat = reinterpret_cast<float2 *>(p + w.stat);
     a.score_new = reinterpret_cast<float *>(p + w.score_new);
     a.part_o = reinterpret_cast<float *>(p + w.part_o);
     a.part_ml = reinterpret_cast<float2 *>(p + w.part_ml);
     a.scores = reinterpret_cast<float *>(p + w.scores);
+    a.score_rows = scores_by_row(c.page_size) ? c.max_pages * c.page_size : c.page_size;
     if (accumulate) *gather = {a.stat, a.scores, a.score_new, k_new ? w_new : nullptr, a.scale_log2e, decay, a.G};
     if (dtype == EC_BF16) return D == 128 ? launch_d<Bf16, 128>(a, accumulate, stream) : launch_d<Bf16, 64>(a, accumulate, stream);
     return D == 128 ? launch_d<Fp16, 128>(a, accumulate, stream) : launch_d<Fp16, 64>(a, accumulate, stream);
