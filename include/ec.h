@@ -490,9 +490,11 @@ int ec_decode_step_noalloc(const void *q_dev, const void *k_new_dev, const void 
  * (ec_device_status(state, stream); ec_paged_init clears it). ec_paged_check looks a host copy over
  * before that happens.
  *
- * Calls that change a cache (append, attention that gathers weights, steps) are ordered by the
- * caller: one stream, or events. Pages may be shared between problems only while nothing appends to
- * or gathers weights in them.
+ * Calls on one description are ordered by the caller (one stream, or events), reading ones too: they
+ * count in `state`. Two calls that may run at once need two descriptions with a state of their own
+ * and two workspaces; over the same pool only calls that change nothing (attention without
+ * accumulate). Pages may be shared between problems only while nothing appends to or gathers weights
+ * in them.
  */
 typedef enum { EC_BF16 = 0, EC_FP16 = 1 } ec_dtype;
 
@@ -540,7 +542,8 @@ int ec_paged_check(const ec_paged *c, const int32_t *table_host, const int32_t *
  *   q_dev                 [N, Hq, D], elements of c->dtype                                  (in)
  *   k_new_dev, v_new_dev  [N, H, D]; both NULL: the cached rows alone                       (in)
  *   out_dev               [N, Hq, D]; fp32 accumulation, one rounding of the result. Zero where no row
- *                         is left (an empty place, length 0 without a new row, all scores -inf) (out)
+ *                         is left (an empty place, length 0 without a new row, all scores -inf);
+ *                         an infinity in a value row that takes part may come out as NaN      (out)
  *   lse_dev               fp32 [N, Hq], natural log-sum-exp (-inf where no row is left); nullable
  *   w_new_dev             fp32 [N, H], the new row's share of the group's probability; required
  *                         with accumulate and k_new, else NULL                               (out)

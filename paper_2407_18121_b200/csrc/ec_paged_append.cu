@@ -699,7 +699,7 @@ __global__ void __launch_bounds__(kRowThreads, kRowCtas) paged_rows_kernel(Paged
 // CTAs per unit of a rows launch: one round of rows each, up to about 16 CTAs per SM in all.
 inline int row_splits(long long units, long long rows)
 {
-    long long z = (148LL * kRowCtas + units - 1) / units;
+    long long z = 148LL * kRowCtas / units;
     const long long most = (rows + kRowThreads * kRowsHeld - 1) / (kRowThreads * kRowsHeld);
     if (z > most) z = most;
     if (z > kMaxSplits) z = kMaxSplits;

@@ -201,6 +201,8 @@ class PagedCacheSession:
         Eq. 1 as weight. With `out` the prompt's attention output comes from the same call (ec_prefill_attention)."""
         if self.Hq != self.H:
             raise ValueError("grouped query heads: pass the rows' weights to append()")
+        if any(t.dtype != torch.bfloat16 or t.shape != K.shape for t in (Q, K, V)) or self.Kp.dtype != torch.bfloat16:
+            raise ValueError("the importance of a prompt is computed in bf16, from Q, K and V of one shape")
         ws_imp, ws_app, scores = self._prompt_ws(K.shape[2])
         if out is None:
             ec.ec_importance(Q, K, scores, lse, self.scale, ws_imp)

@@ -350,6 +350,53 @@ def test_two_caches_share_a_workspace_in_one_stream():
         assert torch.equal(a.nan_to_num(7.0) if a.is_floating_point() else a, b.nan_to_num(7.0) if b.is_floating_point() else b)
 
 
+def test_two_caches_on_two_streams_at_once():
+    """Each with its own description and workspace, interleaved without waiting; the same as one after the other."""
+    def build():
+        ms = [PagedMirror([700, 400, 33, -1], 4, 128, 16, 704, seed=s, ranked=True, G=2) for s in (3, 4)]
+        ins = [[rand((4, h, 128), BF, 20 * s + h).cuda() for h in (8, 4, 4)] for s in (0, 1)]
+        cs = [m.cache(ec) for m in ms]
+        ws = [scratch(ec.ec_paged_step_workspace(c, 8, 704)) for c in cs]
+        outs = [torch.zeros(30, 4, 8, 128, dtype=BF, device="cuda") for _ in cs]
+        return ms, ins, cs, ws, outs
+    got = []
+    for at_once in (True, False):
+        ms, ins, cs, ws, outs = build()
+        streams = [torch.cuda.Stream(), torch.cuda.Stream()] if at_once else [torch.cuda.current_stream()] * 2
+        torch.cuda.synchronize()
+        for i in range(30):
+            for (q, k, v), c, w, o, st in zip(ins, cs, ws, outs, streams):
+                with torch.cuda.stream(st):
+                    ec.ec_paged_decode_step(q, k, v, c, 0.088, 1.0, 704, 16, 2, o[i], None, w)
+        torch.cuda.synchronize()
+        got.append(outs + [m.dev[x] for m in ms for x in ("pos", "lens", "seen")] + [m.dev["weight"].nan_to_num(7.0) for m in ms])
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
+
+
+def test_shared_pages_can_be_read():
+    """A common beginning in the same pages for two problems."""
+    m = PagedMirror([96, 80], 2, 64, 32, 96)
+    for t in (m.table, m.dev["table"]):
+        t[1, :2] = t[0, :2]
+    check_attention(m, 3)
+
+
+def test_values_that_are_infinite_stay_where_they_belong():
+    m = PagedMirror([100, 60], 1, 64, 16, 112)
+    p, s = m.where(0, 100)
+    for pool in (m.V, m.dev["V"]):
+        pool[p[7], 0, s[7], 5] = math.inf                              # one dimension of one row
+    cache = m.cache(ec)
+    q, k, v = (rand((2, 1, 64), BF, i).cuda() for i in range(3))
+    out = torch.empty_like(q)
+    ws = scratch(ec.ec_paged_attention_workspace(cache, 1, False))
+    ec.ec_paged_attention(q, k, v, cache, 0.125, False, 1.0, out, None, None, ws)
+    torch.cuda.synchronize()
+    fine = torch.isfinite(out)
+    assert not fine[0, 0, 5] and int((~fine).sum()) == 1
+
+
 def test_offsets_past_32_bits():
     """Rows more than 2^32 bytes and 2^31 elements into the pool."""
     H, D, page, n_pages = 4, 128, 128, 36000                           # 36000 * 4 * 128 * 128 elements = 4.7 GB a pool
@@ -444,3 +491,9 @@ def test_binding_refuses_wrong_tensors():
         ec.ec_paged_decode_step(q, q, q, s.cache, 0.125, 1.0, 64, 4, 0, out, None, s.ws_step[:256])
     assert e.value.status == ec.EC_ERR_WORKSPACE
     assert s.lens.tolist() == [0, 0]
+    half = PagedCacheSession(2, 2, 64, 64, 4, 0, 0.125, dtype=HF)
+    x = torch.zeros(2, 2, 70, 64, dtype=HF, device="cuda")
+    with pytest.raises(ValueError):
+        half.prompt(x, x, x)
+    with pytest.raises(ValueError):
+        PagedCacheSession(2, 2, 64, 64, 4, 0, 0.125, Hq=4).prompt(x.bfloat16(), x.bfloat16(), x.bfloat16())
