@@ -539,6 +539,13 @@ __global__ void __launch_bounds__(kRowThreads, kRowCtas) paged_rows_kernel(Paged
         if (GATHER && z == 0 && threadIdx.x == 0 && ga.w_new) ga.w_new[unit] = 0.f;
         return;
     }
+    // a unit of one CTA: its new row is on its way while the rows that may leave are looked over
+    uint4 own_k = make_uint4(0, 0, 0, 0), own_v = own_k;
+    const bool carry = APPEND && splits == 1 && warp == 0 && lane < lpr && u.cnt > 0;
+    if (carry) {
+        own_k = ap.K_new[u.u * lpr + lane];
+        own_v = ap.V_new[u.u * lpr + lane];
+    }
     const int leave = APPEND ? u.had + u.cnt - u.final : 0;
     const bool simple = leave <= 0 || (leave == 1 && u.cnt == 1);         // else: more rows leave than join
     unsigned long long low = ~0ull;
@@ -652,16 +659,31 @@ __global__ void __launch_bounds__(kRowThreads, kRowCtas) paged_rows_kernel(Paged
     };
     int *arrived = c.state + kStateAppend + n;
     if (splits == 1) {
-        if (simple) {
-            if (warp == 0) place(u, sm_low[0], lane);
-        } else {
-            const int movers = select_unit<kRowThreads, false>(c, ap, u, sm_select, nullptr, 0);
-            move_listed<kRowThreads>(c, ap, u, movers, lpr, 0, 1);
-        }
-        if (threadIdx.x == 0 && arrive(arrived) == c.H - 1) {
+        // the length has been read: a warp of its own counts the CTA in while the row is placed
+        if (threadIdx.x == 32 && arrive(arrived) == c.H - 1) {
             *arrived = 0;
             c.lens[n] = u.final;
             c.seen[n] = u.seen + u.cnt;
+        }
+        if (!simple) {
+            const int movers = select_unit<kRowThreads, false>(c, ap, u, sm_select, nullptr, 0);
+            move_listed<kRowThreads>(c, ap, u, movers, lpr, 0, 1);
+        } else if (carry) {
+            const int dst = leave <= 0 ? u.had : (int)(0xFFFFFFFFu - (uint32_t)sm_low[0]);
+            if (leave > 0 && dst == u.had) return;                        // the new row itself is the one that leaves
+            const Slot s = look_up_slot(c, n, dst);
+            if (!valid_page(c, s)) {
+                report_page(c);
+                return;
+            }
+            const size_t to = (size_t)h * c.head_step + row_offset(c, s) + lane;
+            c.K[to] = own_k;
+            c.V[to] = own_v;
+            if (lane == 0) {
+                const uint32_t m = meta_index(c, h, s);
+                c.weight[m] = w_own;
+                c.pos[m] = ap.pos_new ? ap.pos_new[unit] : u.seen;
+            }
         }
         return;
     }

@@ -514,39 +514,37 @@ __global__ void __launch_bounds__(W * 32, 8 / W) paged_attention_kernel(AttnArgs
     constexpr bool kHoldQ = NT == 1;
     uint32_t qf[kHoldQ ? NT : 1][kHoldQ ? KS : 1][2], q_at = 0;
     float o[NT][MT][4], m[NT][2], l[NT][2], limit[NT][2], neg_m[NT][2];
-    int stage = 0, q_slot = 0, first_block = 0;
-    bool begin = true;
+    int stage = 0, q_slot = 0, first_block = use.blk;
+    auto begin_unit = [&] {                      // the queries of the next unit are here; nothing has been seen of it
+        q_at = base + M_::kQ + q_slot * M_::kQBytes + (lane & 7) * (D * 2) + (((lane >> 3) ^ (lane & 7)) << 4);
+        q_slot = q_slot + 1 == M_::kQSlots ? 0 : q_slot + 1;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            if (kHoldQ) {
+#pragma unroll
+                for (int ks = 0; ks < KS; ks += 2) {
+                    uint32_t r[4];
+                    load_matrices(r, (q_at ^ (ks << 5)) + nt * 8 * (D * 2));
+                    qf[nt][ks][0] = r[0];
+                    qf[nt][ks][1] = r[1];
+                    qf[nt][ks + 1][0] = r[2];
+                    qf[nt][ks + 1][1] = r[3];
+                }
+            }
+            m[nt][0] = m[nt][1] = limit[nt][0] = limit[nt][1] = -INFINITY;
+            neg_m[nt][0] = neg_m[nt][1] = 0.f;
+            l[nt][0] = l[nt][1] = 0.f;
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[nt][mt][i] = 0.f;
+        }
+    };
+    begin_unit();
     while (use.left > 0) {
         const int h = use.h, head0 = use.hb * 8 * NT;                     // first query head of the block within the group
         const int heads = min(G - head0, 8 * NT);
         const size_t head_at = (size_t)use.n * Hq + (size_t)h * G + head0;
-        if (begin) {
-            begin = false;
-            first_block = use.blk;
-            q_at = base + M_::kQ + q_slot * M_::kQBytes + (lane & 7) * (D * 2) + (((lane >> 3) ^ (lane & 7)) << 4);
-            q_slot = q_slot + 1 == M_::kQSlots ? 0 : q_slot + 1;
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                if (kHoldQ) {
-#pragma unroll
-                    for (int ks = 0; ks < KS; ks += 2) {
-                        uint32_t r[4];
-                        load_matrices(r, (q_at ^ (ks << 5)) + nt * 8 * (D * 2));
-                        qf[nt][ks][0] = r[0];
-                        qf[nt][ks][1] = r[1];
-                        qf[nt][ks + 1][0] = r[2];
-                        qf[nt][ks + 1][1] = r[3];
-                    }
-                }
-                m[nt][0] = m[nt][1] = limit[nt][0] = limit[nt][1] = -INFINITY;
-                neg_m[nt][0] = neg_m[nt][1] = 0.f;
-                l[nt][0] = l[nt][1] = 0.f;
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) o[nt][mt][i] = 0.f;
-            }
-        }
         copies_wait<S - 1>();
         __syncwarp();
         if (use.blk * kBlockRows + warp * kTile < use.rows) {
@@ -783,9 +781,12 @@ __global__ void __launch_bounds__(W * 32, 8 / W) paged_attention_kernel(AttnArgs
                     __syncthreads();
                 }
             }
-            begin = true;
+            walk_on<kBlockRows>(a, head_blocks, use);
+            first_block = use.blk;
+            begin_unit();
+        } else {
+            walk_on<kBlockRows>(a, head_blocks, use);
         }
-        walk_on<kBlockRows>(a, head_blocks, use);
     }
 }
 

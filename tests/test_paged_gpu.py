@@ -314,6 +314,25 @@ def test_steps_follow_the_definition(G, dt, D):
     run_steps(PagedMirror([40, 37, 0, -1, 12], 2, D, 16, 40, dt, G=G, ranked=True), G, 12, 40, 14, 2)
 
 
+@pytest.mark.parametrize("G", [2, 12])
+@pytest.mark.parametrize("lens,budget", [([300, 150, 299, -1], 120), ([700], 650), ([2600, 2590], 2500)])
+def test_steps_after_the_budget_shrank(lens, budget, G):
+    """More rows leave than join: the first step brings every problem down to the new budget."""
+    cap = max(lens) + 8
+    run_steps(PagedMirror(lens, 2, 64, 16, cap, G=G, ranked=True, seed=budget), G, 2, budget, 14, 2)
+
+
+def test_steps_of_long_problems():
+    """Rows beyond what one CTA brings up to date by itself."""
+    run_steps(PagedMirror([5000, 4700], 2, 64, 64, 5000, G=1, ranked=True), 1, 3, 5000, 14, 2)
+
+
+def test_steps_of_many_units():
+    lens = [60 - (n % 9) for n in range(40)]
+    lens[3], lens[17] = -1, 0
+    run_steps(PagedMirror(lens, 16, 64, 16, 60, G=1, ranked=True), 1, 2, 60, 8, 2)
+
+
 def test_steps_captured_once_and_replayed():
     run_steps(PagedMirror([100, 97, -1], 2, 64, 16, 100, ranked=True, G=2), 2, 8, 100, 10, 1, use_graph=True)
 
