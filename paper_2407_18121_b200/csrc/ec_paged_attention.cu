@@ -2,17 +2,26 @@
 // cached row receives added to the row's gathered weight.
 //   x[g][j] = scale * <q_g, k_j>,  p = softmax_j(x),  out_g = sum_j p[g][j] v_j,  weight_j <- decay * weight_j + sum_g p[g][j]
 // Bound by the K and V rows read from HBM (4 D bytes per row and head); the products ride on mma.sync, whose rate
-// (24 instructions per 16 rows and 8 query heads) is far above what the loads can feed, so the tcgen05 pipe would
-// only add latency here: a tile has 8 to 16 query rows, not 128.
+// (24 instructions per 16 rows and 8 query heads at D = 128) is far above what the loads can feed, so the tcgen05 pipe
+// would only add latency here: a tile has 8 to 16 query rows, not 128.
 //  - Both products are taken transposed, S^T = K Q^T and O^T = V^T P^T, so that the 16-row side of the instruction
 //    is the cache and the 8-column side the group's query heads. P goes from accumulator to operand layout with
-//    movmatrix.
-//  - Every warp streams its own 16-row tiles through a ring of asynchronous copies in shared memory (96 KB per CTA, two
-//    CTAs per SM) and runs ahead over the borders of units, so that the reads never pause while a unit's results
-//    are put together.
-//  - Work is handed out in blocks of 64 rows, evenly over the CTAs of one resident wave, from the lengths on the device: a
-//    ragged batch and one long sequence spread alike. A CTA's share is at most one partial unit at either end and
+//    movmatrix, in two rounded parts, so that the result's own rounding is all that its type costs (one rounding of P
+//    measured 1.35 times the error; the second part's products are not seen in the time).
+//  - Every warp streams its own tiles of 4 KB of K and 4 KB of V through a ring of three asynchronous copies in shared memory
+//    (192 KB per SM) and runs ahead over the borders of units, so that the reads never pause while a unit's results are
+//    put together. Page numbers are fetched a ring's length before the copies that need them, queries with a unit's
+//    first tile. (Fragments straight from global memory to registers, without the ring: 528 us where this takes 338.)
+//  - Work is handed out in blocks of a tile per warp, evenly over the CTAs of one resident wave, from the lengths on the
+//    device: a ragged batch and one long sequence spread alike. A CTA's share is at most one partial unit at either end and
 //    whole units between; of the CTAs that share a unit the one that arrives last joins the parts (nobody waits).
+//  - The running maximum is raised only when a tile exceeds it by 2^8, so that most tiles need no reduction across lanes.
+// Measured per call, all launches, bf16, D = 128: 16 problems x 32 heads x 8192 rows 334 us (6.4 TB/s; 374 us with the weights),
+// one problem of 131071 rows, 8 heads for 64 query heads 91 us (5.9 TB/s), 32 problems of 1 .. 8192 rows 29 us (4.7 TB/s),
+// one problem of 37 rows 4.7 us. What is left at small sizes is a chain of dependent reads (length, page, row), the
+// merge of the warps and, for shared units, the arrival and the join: about 8 us beside the streaming.
+// Tried and dropped: bringing the weights up to date in this launch, by the CTA that completes a unit (a step of 1024 units
+// at budget 320: 61 us instead of 43; the chain of reads stalls the SM for longer than the ring lasts).
 #include "ec_paged.cuh"
 
 #include <atomic>
@@ -838,14 +847,17 @@ cudaError_t launch(const AttnArgs &a, cudaStream_t stream)
     return launch_chained(kernel, dim3((unsigned)ctas), W * 32, smem, stream, a, head_blocks);
 }
 
-#ifndef EC_PAGED_NARROW
-#define EC_PAGED_NARROW 512
-#endif
+// Units from which CTAs have four warps, two to an SM, instead of eight: with many units the barriers of one CTA hide behind
+// the other; with few, half as many CTAs leave half as many parts to join. Four / eight warps: 2048 units of 127 rows 33 / 43 us,
+// 1024 units of 640 rows with weights 66 / 70 us, 512 units of 8192 rows 340 / 337 us, 8 units of 131071 rows 103 / 92 us.
+// Groups of more than eight query heads need the shared memory of eight warps.
+constexpr long long kNarrowUnits = 512;
+
 template <typename E, int D, bool GATHER>
 cudaError_t launch_g(const AttnArgs &a, cudaStream_t stream)
 {
     if (a.G > 8) return launch<E, D, 2, 8, GATHER>(a, stream);
-    if ((long long)a.c.N * a.c.H >= EC_PAGED_NARROW) return launch<E, D, 1, 4, GATHER>(a, stream);
+    if ((long long)a.c.N * a.c.H >= kNarrowUnits) return launch<E, D, 1, 4, GATHER>(a, stream);
     return launch<E, D, 1, 8, GATHER>(a, stream);
 }
 
