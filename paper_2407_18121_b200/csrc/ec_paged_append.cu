@@ -720,11 +720,15 @@ __global__ void __launch_bounds__(kRowThreads, kRowCtas) paged_rows_kernel(Paged
     }
 }
 
-// CTAs per unit of a rows launch: one round of rows each, up to about 16 CTAs per SM in all.
+// CTAs per unit of a rows launch: as many as fit the GPU at once (a second, partial wave measured 2% of a call of 512 units of
+// 8192 rows), but no more than two rounds of rows each, so that the longest of a ragged batch are not left to one CTA
+// (34 x 32 units of up to 3836 rows: 68 -> 56 us).
 inline int row_splits(long long units, long long rows)
 {
+    constexpr long long kRound = kRowThreads * kRowsHeld;
     long long z = 148LL * kRowCtas / units;
-    const long long most = (rows + kRowThreads * kRowsHeld - 1) / (kRowThreads * kRowsHeld);
+    const long long least = (rows + 2 * kRound - 1) / (2 * kRound), most = (rows + kRound - 1) / kRound;
+    if (z < least) z = least;
     if (z > most) z = most;
     if (z > kMaxSplits) z = kMaxSplits;
     return z < 1 ? 1 : (int)z;
