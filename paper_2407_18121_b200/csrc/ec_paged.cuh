@@ -87,13 +87,18 @@ struct Slot {
     int page, slot;        // page < 0: the table has no valid page here
 };
 
+// AHEAD: a read in front of the launch's wait, from the L2: an L1 may still hold what it read for an earlier launch.
+template <bool AHEAD, typename T>
+__device__ __forceinline__ T read_at(const T *p) { return AHEAD ? __ldcg(p) : *p; }
+
 // The table's entry as it is: to be looked at with valid_page before anything is read through it.
+template <bool AHEAD = false>
 __device__ __forceinline__ Slot look_up_slot(const PagedView &c, int n, int row)
 {
     const int p = page_of(c, row);
     Slot s;
     s.slot = row - p * c.page_size;
-    s.page = c.table[(size_t)n * c.max_pages + p];
+    s.page = read_at<AHEAD>(c.table + (size_t)n * c.max_pages + p);
     return s;
 }
 
@@ -101,9 +106,10 @@ __device__ __forceinline__ bool valid_page(const PagedView &c, const Slot &s) { 
 
 __device__ __forceinline__ void report_page(const PagedView &c) { atomicExch(c.state, kStatusPage); }
 
+template <bool AHEAD = false>
 __device__ __forceinline__ Slot find_slot(const PagedView &c, int n, int row)
 {
-    Slot s = look_up_slot(c, n, row);
+    Slot s = look_up_slot<AHEAD>(c, n, row);
     if (!valid_page(c, s)) {
         s.page = -1;
         report_page(c);
@@ -124,9 +130,10 @@ __device__ __forceinline__ uint32_t row_offset(const PagedView &c, const Slot &s
 }
 
 // Valid rows of problem n: negative for an empty place; a length past the table's reach is cut and reported.
+template <bool AHEAD = false>
 __device__ __forceinline__ int read_len(const PagedView &c, int n)
 {
-    const int len = c.lens[n];
+    const int len = read_at<AHEAD>(c.lens + n);
     const long long cap = (long long)c.max_pages * c.page_size;
     if (len > cap) {
         atomicExch(c.state, kStatusPage);

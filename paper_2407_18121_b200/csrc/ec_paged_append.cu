@@ -141,20 +141,21 @@ __device__ __forceinline__ int2 warps_prefix(int x, int y, SelectSmem<THREADS> &
     return make_int2(__reduce_add_sync(0xFFFFFFFFu, lane < warp ? vx : 0), __reduce_add_sync(0xFFFFFFFFu, lane < warp ? vy : 0));
 }
 
+template <bool AHEAD = false>
 __device__ __forceinline__ Unit load_unit(const PagedView &c, const AppendArgs &a, int n, int h)
 {
     Unit u;
     u.n = n;
     u.h = h;
     u.u = (size_t)n * c.H + h;
-    const int len = read_len(c, n);
+    const int len = read_len<AHEAD>(c, n);
     if (len < 0) {
         u.had = u.cnt = u.final = -1;
         u.seen = 0;
         return u;
     }
     u.had = a.fresh ? 0 : len;
-    u.seen = a.fresh ? 0 : c.seen[n];
+    u.seen = a.fresh ? 0 : read_at<AHEAD>(c.seen + n);
     int cnt = a.counts ? a.counts[n] : a.T;
     u.cnt = min(max(cnt, 0), a.T);
     u.final = (int)min((long long)u.had + u.cnt, (long long)a.budget);
@@ -528,12 +529,12 @@ __global__ void __launch_bounds__(kRowThreads, kRowCtas) paged_rows_kernel(Paged
     const int score_rows = by_row ? c.max_pages * c.page_size : c.page_size;
     Unit u;
     if (APPEND) {
-        u = load_unit(c, ap, n, h);
+        u = load_unit<GATHER>(c, ap, n, h);
     } else {
         u.n = n;
         u.h = h;
         u.u = unit;
-        u.had = read_len(c, n);
+        u.had = read_len<GATHER>(c, n);
     }
     if (u.had < 0) {                             // an empty place of the batch
         if (GATHER) grid_wait();
@@ -545,8 +546,8 @@ __global__ void __launch_bounds__(kRowThreads, kRowCtas) paged_rows_kernel(Paged
     uint4 own_k = make_uint4(0, 0, 0, 0), own_v = own_k;
     const bool carry = APPEND && splits == 1 && warp == 0 && lane < lpr && u.cnt > 0;
     if (carry) {
-        own_k = ap.K_new[u.u * lpr + lane];
-        own_v = ap.V_new[u.u * lpr + lane];
+        own_k = __ldcg(ap.K_new + u.u * lpr + lane);
+        own_v = __ldcg(ap.V_new + u.u * lpr + lane);
     }
     const int leave = APPEND ? u.had + u.cnt - u.final : 0;
     const bool simple = leave <= 0 || (leave == 1 && u.cnt == 1);         // else: more rows leave than join
@@ -563,7 +564,7 @@ __global__ void __launch_bounds__(kRowThreads, kRowCtas) paged_rows_kernel(Paged
             const int row = row0 + r * kRowThreads + threadIdx.x;
             there[r] = false;
             if (row >= u.had) continue;
-            const Slot s = find_slot(c, n, row);
+            const Slot s = GATHER && first ? find_slot<true>(c, n, row) : find_slot(c, n, row);
             there[r] = s.page >= 0;
             m[r] = meta_index(c, h, s);
             if (GATHER)
@@ -575,8 +576,8 @@ __global__ void __launch_bounds__(kRowThreads, kRowCtas) paged_rows_kernel(Paged
         for (int r = 0; r < kRowsHeld; ++r) {
             w[r] = 0.f;
             if (!there[r]) continue;
-            w[r] = c.weight[m[r]];
-            if (APPEND) pos[r] = c.pos[m[r]];
+            w[r] = __ldcg(c.weight + m[r]);
+            if (APPEND) pos[r] = __ldcg(c.pos + m[r]);
         }
         if (GATHER) {
             if (first) {

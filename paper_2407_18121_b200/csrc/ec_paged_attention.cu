@@ -489,7 +489,7 @@ __global__ void __launch_bounds__(W * 32, 8 / W) paged_attention_kernel(AttnArgs
                 // rows of one copy instruction lie 32 / C apart from the next one's: their swizzles differ by a constant
                 const uint32_t dst0 = (ring + stage * (2 * M_::kTileBytes) + (lane / C) * (D * 2)) + ((lane % C ^ lane / C) << 4);
                 const bool plain = __all_sync(0xFFFFFFFFu, off < kRowNew);
-                if (plain) {                     // sixteen cached rows
+                if (plain) {                     // cached rows all through
 #pragma unroll
                     for (int i = 0; i < kTile * C / 32; ++i) {
                         const uint32_t o = __shfl_sync(0xFFFFFFFFu, off, i * (32 / C) + lane / C);

@@ -314,6 +314,12 @@ def test_steps_follow_the_definition(G, dt, D):
     run_steps(PagedMirror([40, 37, 0, -1, 12], 2, D, 16, 40, dt, G=G, ranked=True), G, 12, 40, 14, 2)
 
 
+@pytest.mark.parametrize("page,rows", [(1, "tokens"), (1, "heads"), (5, "tokens"), (3, "heads")])
+def test_steps_with_heads_side_by_side_in_memory(page, rows):
+    """Weights and scores of several heads within 32 bytes, changed by different CTAs step after step."""
+    run_steps(PagedMirror([70, 64, 70, 11], 8, 64, page, 70, rows=rows, G=2, ranked=True), 2, 8, 70, 12, 2)
+
+
 @pytest.mark.parametrize("G", [2, 12])
 @pytest.mark.parametrize("lens,budget", [([300, 150, 299, -1], 120), ([700], 650), ([2600, 2590], 2500)])
 def test_steps_after_the_budget_shrank(lens, budget, G):
