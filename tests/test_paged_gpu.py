@@ -83,6 +83,28 @@ def test_attention_edges_of_length_and_group(G, dt, D):
     check_attention(PagedMirror(EDGE, 2, D, 16, 208, dt, G=G), G, accumulate=True)
 
 
+@pytest.mark.parametrize("G,accumulate", [(33, True), (128, False), (128, True)])
+def test_attention_wide_groups(G, accumulate):
+    check_attention(PagedMirror([70, 0, 300], 2, 64, 16, 304, G=G), G, accumulate=accumulate)
+
+
+def test_attention_cuts_a_length_past_the_table():
+    m = PagedMirror([96, 40], 2, 64, 32, 96)
+    m.dev["lens"][0] = 5000
+    cache = m.cache(ec)
+    q = rand((2, 2, 64), BF, 1).cuda()
+    outs = []
+    for n in (5000, 96):
+        m.dev["lens"][0] = n
+        out = torch.empty_like(q)
+        ws = scratch(ec.ec_paged_attention_workspace(cache, 2, False))
+        ec.ec_paged_attention(q, None, None, cache, 0.125, False, 1.0, out, None, None, ws)
+        torch.cuda.synchronize()
+        outs.append(out)
+        assert ec.ec_device_status(state_of(cache)) == ec.EC_ERR_PAGE      # from the first call on
+    assert torch.equal(*outs)
+
+
 @pytest.mark.parametrize("page", [1, 5, 16, 24, 64, 300])
 @pytest.mark.parametrize("rows", ["heads", "tokens"])
 def test_attention_pages_and_strides(page, rows):
@@ -494,6 +516,34 @@ def test_prompt_then_steps_then_a_new_prompt(with_output):
             assert ((got.cpu().double() - ref[0]).abs() <= out_tol).all()
             m.assert_same_rows((i + 1) * (w_tol + float(m.weight.max()) * 2.0 ** -22), f"step {i}")
         assert s.status() == ec.EC_OK and s.lens.tolist() == [budget, -1, budget] and s.seen.tolist()[0] == T + 10
+
+
+def test_a_compacted_cache_in_pages_answers_as_the_dense_one():
+    """Merged rows of ec_select_merge, taken into pages with the anchors' scores and positions."""
+    N, H, D, T, keep = 2, 4, 128, 200, 100
+    Q, K, V = (rand((N, H, T, D), BF, i).cuda() for i in range(3))
+    scores = torch.empty(N, H, T, device="cuda")
+    ws = scratch(max(ec.ec_importance_workspace(N, H, T, D), ec.ec_select_merge_workspace(N, H, T, D, keep, ec.EC_PER_HEAD)))
+    ec.ec_importance(Q, K, scores, None, 0.088, ws)
+    Kc, Vc = (torch.empty(N, H, keep, D, dtype=BF, device="cuda") for _ in range(2))
+    anchors = torch.empty(N, H, keep, dtype=torch.int32, device="cuda")
+    ec.ec_select_merge(K, V, scores, keep, ec.EC_PER_HEAD, True, Kc, Vc, anchors, None, ws)
+    s = PagedCacheSession(N, H, D, keep, recent=8, sinks=1, scale=0.088, page_size=16)
+    app = scratch(ec.ec_paged_append_workspace(s.cache, keep, keep))
+    ec.ec_paged_append(Kc, Vc, scores.gather(2, anchors.long()), anchors, None, s.cache, True, keep, 8, 1, app)
+    s.seen.fill_(T)                                                    # the rows stand for T tokens
+    dense = ec.ec_cache_init(Kc, Vc, keep, keep, 16)
+    wd = scratch(ec.ec_decode_workspace(dense))
+    q, k, v = (rand((N, H, D), BF, 7 + i).cuda() for i in range(3))
+    a, b = torch.empty_like(q), torch.empty_like(q)
+    s.decode(q, k, v, a)
+    ec.ec_decode_step(q, k, v, dense, 0.088, b, wd)
+    torch.cuda.synchronize()
+    # both round the result once; the dense kernel and this one each carry fp32 sums besides
+    tol = torch.finfo(BF).eps * b.float().abs() + 2.0 ** -12
+    assert ((a.float() - b.float()).abs() <= tol).all()
+    new = (s.pos == T).nonzero()
+    assert new.shape[0] == N * H and s.lens.tolist() == [keep] * N and s.seen.tolist() == [T + 1] * N
 
 
 def test_binding_refuses_wrong_tensors():
