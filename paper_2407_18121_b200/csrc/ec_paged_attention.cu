@@ -11,15 +11,15 @@
 //  - Every warp streams its own tiles of 4 KB of K and 4 KB of V through a ring of three asynchronous copies in shared memory
 //    (192 KB per SM) and runs ahead over the borders of units, so that the reads never pause while a unit's results are
 //    put together. Page numbers are fetched a ring's length before the copies that need them, queries with a unit's
-//    first tile. (Fragments straight from global memory to registers, without the ring: 528 us where this takes 338.)
+//    first tile. (Fragments straight from global memory to registers, without the ring: 528 us, 338 with it.)
 //  - Work is handed out in blocks of a tile per warp, evenly over the CTAs of one resident wave, from the lengths on the
 //    device: a ragged batch and one long sequence spread alike. A CTA's share is at most one partial unit at either end and
 //    whole units between; of the CTAs that share a unit the one that arrives last joins the parts (nobody waits).
 //  - The running maximum is raised only when a tile exceeds it by 2^8, so that most tiles need no reduction across lanes.
-// Measured per call, all launches, bf16, D = 128: 16 problems x 32 heads x 8192 rows 334 us (6.4 TB/s; 374 us with the weights),
-// one problem of 131071 rows, 8 heads for 64 query heads 91 us (5.9 TB/s), 32 problems of 1 .. 8192 rows 29 us (4.7 TB/s),
+// Measured per call, all launches, bf16, D = 128: 16 problems x 32 heads x 8192 rows 329 us (6.5 TB/s; 377 us with the weights),
+// one problem of 131071 rows, 8 heads for 64 query heads 90 us (6.0 TB/s), 32 problems of 0 .. 8192 rows 27.5 us (5.0 TB/s),
 // one problem of 37 rows 4.7 us. What is left at small sizes is a chain of dependent reads (length, page, row), the
-// merge of the warps and, for shared units, the arrival and the join: about 8 us beside the streaming.
+// merge of the warps and, for shared units, the arrival and the join: about 6 us beside the streaming.
 // Tried and dropped: bringing the weights up to date in this launch, by the CTA that completes a unit (a step of 1024 units
 // at budget 320: 61 us instead of 43; the chain of reads stalls the SM for longer than the ring lasts).
 #include "ec_paged.cuh"
