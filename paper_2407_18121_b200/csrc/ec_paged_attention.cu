@@ -16,7 +16,7 @@
 //    device: a ragged batch and one long sequence spread alike. A CTA's share is at most one partial unit at either end and
 //    whole units between; of the CTAs that share a unit the one that arrives last joins the parts (nobody waits).
 //  - The running maximum is raised only when a tile exceeds it by 2^8, so that most tiles need no reduction across lanes.
-// Measured per call, all launches, bf16, D = 128: 16 problems x 32 heads x 8192 rows 329 us (6.5 TB/s; 377 us with the weights),
+// Measured per call, all launches, bf16, D = 128: 16 problems x 32 heads x 8192 rows 329 us (6.5 TB/s; 370 us with the weights),
 // one problem of 131071 rows, 8 heads for 64 query heads 90 us (6.0 TB/s), 32 problems of 0 .. 8192 rows 27.5 us (5.0 TB/s),
 // one problem of 37 rows 4.7 us. What is left at small sizes is a chain of dependent reads (length, page, row), the
 // merge of the warps and, for shared units, the arrival and the join: about 6 us beside the streaming.

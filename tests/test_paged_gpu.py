@@ -350,6 +350,31 @@ def test_steps_after_the_budget_shrank(lens, budget, G):
     run_steps(PagedMirror(lens, 2, 64, 16, cap, G=G, ranked=True, seed=budget), G, 2, budget, 14, 2)
 
 
+def shift_off_16_bytes(t, by=1):
+    held = torch.zeros(t.numel() + 4, dtype=t.dtype, device="cuda")
+    moved = held[by:by + t.numel()].view(t.shape)
+    moved.copy_(t)
+    assert moved.data_ptr() % 16 == 4 * by
+    return moved
+
+
+@pytest.mark.parametrize("which", ["weight", "pos"])
+@pytest.mark.parametrize("by", [1, 2])
+def test_weights_and_positions_off_16_bytes(which, by):
+    m = PagedMirror([100, 0, 1027], 3, 64, 16, 1100, G=2, ranked=True)
+    m.dev[which] = shift_off_16_bytes(m.dev[which], by)
+    check_attention(m, 2, accumulate=True)
+    m = PagedMirror([64, 62, 9], 3, 64, 16, 64, G=2, ranked=True)
+    m.dev[which] = shift_off_16_bytes(m.dev[which], by)
+    run_steps(m, 2, 6, 64, 8, 1)
+
+
+@pytest.mark.parametrize("page", [4, 12, 20])
+@pytest.mark.parametrize("length", [1, 2, 3, 4, 5, 511, 514])
+def test_steps_at_every_rest_of_four_rows(length, page):
+    run_steps(PagedMirror([length, max(0, length - 2)], 2, 64, page, 520, G=3, ranked=True), 3, 6, length + 3, 2, 1)
+
+
 def test_steps_of_long_problems():
     """Rows beyond what one CTA brings up to date by itself."""
     run_steps(PagedMirror([5000, 4700], 2, 64, 64, 5000, G=1, ranked=True), 1, 3, 5000, 14, 2)
