@@ -550,7 +550,8 @@ int ec_paged_check(const ec_paged *c, const int32_t *table_host, const int32_t *
  *   decay                 0 < decay <= 1, read with accumulate
  * Limits: Hq a multiple of H, Hq / H <= 128, N*Hq < 2^24, and N*H*ceil(Hq/H/8) times
  * (max_pages*page_size/64 + 2) below 2^31. Workspace: ec_paged_attention_workspace
- * bytes (0 on invalid arguments); its contents need not survive between calls. Deterministic.
+ * bytes (0 on invalid arguments); its contents need not survive between calls. The inputs must not
+ * overlap the outputs. Deterministic.
  */
 size_t ec_paged_attention_workspace(const ec_paged *c, int Hq, int accumulate);
 int ec_paged_attention(const void *q_dev, const void *k_new_dev, const void *v_new_dev, const ec_paged *c, int Hq,

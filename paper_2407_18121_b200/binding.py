@@ -451,6 +451,14 @@ def _paged_stream(device: int) -> int:
     return _raw_stream(device)
 
 
+def check_paged_args(cache: ec_paged, shape: tuple, dtype: Optional[torch.dtype] = None, **tensors: Optional[torch.Tensor]) -> None:
+    """ValueError unless every tensor (None passes) has this shape and type (the cache's own by default), is contiguous and
+    lies on the cache's device, which has to be the current one."""
+    _paged_stream(cache._dims[4])
+    for name, t in tensors.items():
+        _want(t, name, dtype or cache._dims[3], shape, cache._dims[4])
+
+
 def ec_paged_state_bytes(N: int) -> int:
     return int(lib().ec_paged_state_bytes(int(N)))
 

@@ -178,32 +178,33 @@ class PagedCacheSession:
         self.state = torch.empty(ec.ec_paged_state_bytes(N), dtype=torch.uint8, device=dev)
         self.cache = ec.ec_paged_init(self.Kp, self.Vp, self.weight, self.pos, self.table, self.lens, self.seen, self.state)
         self.ws_step = torch.empty(ec.ec_paged_step_workspace(self.cache, self.Hq, self.budget), dtype=torch.uint8, device=dev)
-        self._ws = {}           # workspaces of the prompt calls, by prompt length
 
-    def _prompt_ws(self, T: int):
-        if T not in self._ws:
-            u8 = dict(dtype=torch.uint8, device=self.device)
-            self._ws = {T: (torch.empty(ec.ec_importance_workspace(self.N, self.H, T, self.D), **u8),
-                            torch.empty(ec.ec_paged_append_workspace(self.cache, T, self.budget), **u8),
-                            torch.empty((self.N, self.H, T), dtype=torch.float32, device=self.device))}
-        return self._ws[T]
+    def _scratch(self, size: int) -> torch.Tensor:
+        # from the current stream's allocator with every call: a captured prompt keeps its own
+        return torch.empty(size, dtype=torch.uint8, device=self.device)
 
     def append(self, K: torch.Tensor, V: torch.Tensor, scores: Optional[torch.Tensor], counts: Optional[torch.Tensor] = None,
                fresh: bool = False) -> None:
         """Rows [N,H,T,D] with their weights [N,H,T] join the cache; counts [N] when they are not T for every problem."""
         T = K.shape[2]
-        ws = torch.empty(ec.ec_paged_append_workspace(self.cache, T, self.budget), dtype=torch.uint8, device=self.device)
+        ws = self._scratch(ec.ec_paged_append_workspace(self.cache, T, self.budget))
         ec.ec_paged_append(K, V, scores, None, counts, self.cache, fresh, self.budget, self.recent, self.sinks, ws)
 
     def prompt(self, Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, out: Optional[torch.Tensor] = None,
-               lse: Optional[torch.Tensor] = None) -> None:
+               lse: Optional[torch.Tensor] = None, scores: Optional[torch.Tensor] = None) -> None:
         """Prompts of T tokens, [N,H,T,D] each (one query head per key head): their rows enter with the importance of
-        Eq. 1 as weight. With `out` the prompt's attention output comes from the same call (ec_prefill_attention)."""
+        Eq. 1 as weight; it is left in `scores` (fp32 [N,H,T]) when given. With `out` the prompt's attention output comes from the same call (ec_prefill_attention)."""
         if self.Hq != self.H:
             raise ValueError("grouped query heads: pass the rows' weights to append()")
-        if any(t.dtype != torch.bfloat16 or t.shape != K.shape for t in (Q, K, V)) or self.Kp.dtype != torch.bfloat16:
-            raise ValueError("the importance of a prompt is computed in bf16, from Q, K and V of one shape")
-        ws_imp, ws_app, scores = self._prompt_ws(K.shape[2])
+        if self.Kp.dtype != torch.bfloat16 or K.dim() != 4:
+            raise ValueError("the importance of a prompt is computed in bf16, from Q, K and V [N, H, T, D]")
+        N, H, T, D = self.N, self.H, K.shape[2], self.D
+        ec.check_paged_args(self.cache, (N, H, T, D), Q=Q, K=K, V=V, out=out)
+        ec.check_paged_args(self.cache, (N, H, T), torch.float32, lse=lse, scores=scores)
+        ws_imp = self._scratch(ec.ec_importance_workspace(N, H, T, D))
+        ws_app = self._scratch(ec.ec_paged_append_workspace(self.cache, T, self.budget))
+        if scores is None:
+            scores = torch.empty((N, H, T), dtype=torch.float32, device=self.device)
         if out is None:
             ec.ec_importance(Q, K, scores, lse, self.scale, ws_imp)
         else:

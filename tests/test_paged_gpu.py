@@ -521,9 +521,10 @@ def test_prompt_then_steps_then_a_new_prompt(with_output):
         Q, K, V = (rand((N, H, T, D), BF, 10 * round_ + i) for i in range(3))
         m = adopt(s)
         out = torch.empty(N, H, T, D, dtype=BF, device="cuda") if with_output else None
-        s.prompt(Q.cuda(), K.cuda(), V.cuda(), out)
+        scores = torch.empty(N, H, T, device="cuda")
+        s.prompt(Q.cuda(), K.cuda(), V.cuda(), out, scores=scores)
         torch.cuda.synchronize()
-        scores = s._ws[T][2].cpu()
+        scores = scores.cpu()
         x = torch.einsum("nhmd,nhkd->nhmk", Q.double(), K.double()) * 0.125
         p = torch.softmax(x.masked_fill(torch.ones(T, T).triu(1).bool(), -math.inf), -1)
         assert (scores.double() - p.sum(2)).abs().max() <= 1e-3 * p.sum(2).max()
@@ -569,6 +570,47 @@ def test_a_compacted_cache_in_pages_answers_as_the_dense_one():
     assert ((a.float() - b.float()).abs() <= tol).all()
     new = (s.pos == T).nonzero()
     assert new.shape[0] == N * H and s.lens.tolist() == [keep] * N and s.seen.tolist() == [T + 1] * N
+
+
+def test_a_captured_prompt_keeps_its_workspaces():
+    """Prompts of other lengths between the replays of a captured one change nothing of it."""
+    N, H, D, T = 2, 2, 64, 200
+    s = PagedCacheSession(N, H, D, 96, recent=8, sinks=2, scale=0.125, page_size=32)
+    Q, K, V = (rand((N, H, T, D), BF, i).cuda() for i in range(3))
+    s.prompt(Q, K, V)
+    kept = lambda: [t.clone() for t in (s.weight, s.pos, s.lens, s.seen)]  # noqa: E731
+    want = kept()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        s.prompt(Q, K, V)
+    held = []
+    for other in (70, 333):
+        x = [rand((N, H, other, D), BF, other + i).cuda() for i in range(3)]
+        s.prompt(*x)
+        held.append([torch.full((1 << 16,), 0x5A, dtype=torch.uint8, device="cuda") for _ in range(20)])
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(kept(), want):
+            assert torch.equal(a, b)
+        assert all(bool((t == 0x5A).all()) for t in held[-1])
+
+
+def test_a_prompt_of_other_sizes_is_refused():
+    s = PagedCacheSession(2, 2, 64, 64, 4, 0, 0.125)
+    x = torch.zeros(2, 2, 70, 64, dtype=BF, device="cuda")
+    good = dict(Q=x, K=x, V=x, out=torch.empty_like(x), lse=torch.empty(2, 2, 70, device="cuda"))
+    wide = torch.zeros(4, 2, 70, 64, dtype=BF, device="cuda")
+    for name, bad in (("Q", wide), ("K", wide), ("V", wide), ("Q", x[:, :, :69]), ("K", x.half()), ("out", x[:1]), ("Q", x.cpu()),
+                      ("lse", torch.empty(2, 2, 69, device="cuda")), ("K", x[0])):
+        with pytest.raises(ValueError):
+            s.prompt(**{**good, name: bad})
+    with pytest.raises(ValueError):
+        s.prompt(wide, wide, wide)
+    with pytest.raises(ValueError):
+        s.prompt(**good, scores=torch.empty(2, 2, 71, device="cuda"))
+    assert s.lens.tolist() == [0, 0]
+    s.prompt(**good)
+    assert s.lens.tolist() == [64, 64]
 
 
 def test_binding_refuses_wrong_tensors():
