@@ -547,6 +547,7 @@ int ec_paged_check(const ec_paged *c, const int32_t *table_host, const int32_t *
  *   lse_dev               fp32 [N, Hq], natural log-sum-exp (-inf where no row is left); nullable
  *   w_new_dev             fp32 [N, H], the new row's share of the group's probability; required
  *                         with accumulate and k_new, else NULL                               (out)
+ *   scale                 > 0, scale * log2(e) finite in fp32
  *   decay                 0 < decay <= 1, read with accumulate
  * Limits: Hq a multiple of H, Hq / H <= 128, N*Hq < 2^24, and N*H*ceil(Hq/H/8) times
  * (max_pages*page_size/64 + 2) below 2^31. Workspace: ec_paged_attention_workspace

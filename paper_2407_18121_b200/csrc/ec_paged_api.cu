@@ -76,7 +76,7 @@ int check_attention(const void *q, const void *k_new, const void *v_new, const e
     if (!q || !out || (!k_new) != (!v_new)) return EC_ERR_NULL;
     st = check_heads(c, Hq);
     if (st != EC_OK) return st;
-    if (!(scale > 0.f) || !isfinite(scale)) return EC_ERR_ARG;
+    if (!(scale > 0.f) || !isfinite(scale * 1.4426950408889634f)) return EC_ERR_ARG;   // scores are scaled by scale * log2(e)
     if (accumulate && !(decay > 0.f && decay <= 1.f)) return EC_ERR_ARG;
     if (!aligned(q, 16) || !aligned(k_new, 16) || !aligned(v_new, 16) || !aligned(out, 16) || !aligned(lse, 4)) return EC_ERR_ALIGN;
     return EC_OK;

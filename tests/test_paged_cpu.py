@@ -76,6 +76,12 @@ def test_attention_refusals(L):
     assert L.ec_paged_attention_workspace(r, 6, 1) >= L.ec_paged_attention_workspace(r, 6, 0) + 10 * 16 * 6 * 4
 
 
+def test_a_scale_whose_log2_form_overflows_is_refused(L):
+    c = paged()
+    for accumulate, w_new in ((0, None), (1, P)):
+        assert L.ec_paged_attention(P, P, P, C.byref(c), 6, 3e38, accumulate, 1.0, P, None, w_new, P, 1 << 40, None) == 4
+
+
 def test_append_and_step_refusals(L):
     c, ws = paged(), 1 << 40
     r = C.byref(c)
