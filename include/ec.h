@@ -562,9 +562,12 @@ int ec_paged_attention(const void *q_dev, const void *k_new_dev, const void *v_n
 /*
  * New rows join the cache, and eviction by gathered weight keeps every problem within `budget` rows.
  * Candidates of a head are its cached rows, in row order, then the problem's new rows; F =
- * min(lens[n] + new, budget) of them stay: rows at positions below `sinks` or among the newest
- * `recent` ones first, then by weight (equal weights: the lower candidate stays; NaN counts as
- * largest). Cached rows that stay below row F do not move; the holes below F take, in ascending order, the
+ * min(lens[n] + new, budget) of them stay: protected rows first, which are those at positions below
+ * `sinks` or from seen[n] + new - `recent` on (of the tokens counted so far the newest), then by weight,
+ * among protected rows as among the others (equal weights: the lower candidate stays; NaN counts as
+ * largest). No more than budget rows are protected where positions count up with `seen`; positions of
+ * the caller's own that lie further out all count as newest, and where they do not fit, the lightest of
+ * them leave too. Rows that cannot be read (a bad page) leave first. Cached rows that stay below row F do not move; the holes below F take, in ascending order, the
  * staying rows from behind F and then the staying new rows. lens[n] becomes F, seen[n] grows by the new
  * rows. What the merging cache does by position (fixed truncation location), this does by weight.
  *   K_new_dev, V_new_dev  [N, H, T, D], elements of c->dtype; NULL when T = 0 (eviction alone)  (in)
@@ -584,7 +587,8 @@ int ec_paged_append(const void *K_new_dev, const void *V_new_dev, const float *w
 
 /*
  * One generation step on a paged cache: ec_paged_attention with the weights gathered, then
- * ec_paged_append of the step's own row with the weight it received. recent >= 1 keeps the new row.
+ * ec_paged_append of the step's own row with the weight it received. recent >= 1 keeps the new row (but
+ * where more rows are protected than fit, see ec_paged_append).
  * Nothing is read back to the host, so the call can be captured once and replayed for every token.
  * Arguments as in those two calls; lse_dev nullable. Workspace: ec_paged_step_workspace.
  */

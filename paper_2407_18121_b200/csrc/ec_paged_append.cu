@@ -13,8 +13,10 @@
 //    the ordered counts carried on through distributed shared memory.
 // Measured per call: one row to 1024 full units of 320 rows 4.3 us; 64 rows onto 256 full units of 2048 14 us; prompts of 640 rows
 // into 1024 units at budget 320 72 us (the move 57 us, 5.9 TB/s read and written); 16 units of up to 16384 rows 20 us.
-// Keys are order-preserving unsigned images of the weights; rows at protected positions get the largest key. Equal keys:
-// the higher candidate leaves first (cached rows in slot order, then the new rows).
+// Rows leave in this order: those that cannot be read, then by protection, then by weight (keys are order-preserving unsigned
+// images of the weights), and among equals the higher candidate first (cached rows in slot order, then the new rows). For a step that is
+// one number per row. A selection gives all protected rows the largest key, which is enough as long as they all stay; where they do not,
+// their weights are looked at in a second pass over the candidates, with the others marked as having left.
 #include "ec_paged.cuh"
 
 #include <cooperative_groups.h>
@@ -29,7 +31,7 @@ constexpr int kMaxSplits = 512;                  // CTAs that share a unit's row
 
 constexpr uint32_t kKeyProtected = 0xFFFFFFFFu, kKeyNan = 0xFFFFFFFEu;
 
-// Order-preserving image of a weight: -inf lowest, -0 = +0, NaN above +inf.
+// Order-preserving image of a weight: -inf lowest (0x007FFFFF, above the 0 of a row that cannot be read), -0 = +0, NaN above +inf.
 __device__ __forceinline__ uint32_t weight_key(float w)
 {
     if (w != w) return kKeyNan;
@@ -50,7 +52,14 @@ __device__ __forceinline__ bool is_protected(const AppendArgs &a, const Unit &u,
     return pos < a.sinks || (long long)pos >= (long long)u.seen + u.cnt - a.recent;
 }
 
-__device__ __forceinline__ uint32_t candidate_key(const PagedView &c, const AppendArgs &a, const Unit &u, int j)
+// What a selection goes by: the weight's image. `among_safe`: of the protected rows, when all others leave; else of the others.
+__device__ __forceinline__ uint32_t select_key(bool safe, float w, bool among_safe)
+{
+    if (safe != among_safe) return safe ? kKeyProtected : 0u;
+    return weight_key(w);
+}
+
+__device__ __forceinline__ uint32_t candidate_key(const PagedView &c, const AppendArgs &a, const Unit &u, int j, bool among_safe)
 {
     float w;
     int pos;
@@ -65,7 +74,7 @@ __device__ __forceinline__ uint32_t candidate_key(const PagedView &c, const Appe
         w = a.w_new ? a.w_new[at] : 0.f;
         pos = a.pos_new ? a.pos_new[at] : u.seen + (j - u.had);
     }
-    return is_protected(a, u, pos) ? kKeyProtected : weight_key(w);
+    return select_key(is_protected(a, u, pos), w, among_safe);
 }
 
 // Candidate j -> slot `dst`, as lane l of the LPR = D / 8 lanes that copy a row.
@@ -188,95 +197,115 @@ __device__ __forceinline__ int select_body(const PagedView &c, const AppendArgs 
     const int share = (all + 32 * ranks - 1) / (32 * ranks) * 32;         // of the candidates, in order
     const int c0 = min(rank * share, all), c1 = min(c0 + share, all);
     const bool held = HELD;
-    auto key_of = [&](int j) { return held ? keys[j - c0] : candidate_key(c, a, u, j); };
+    bool among_safe = false;
+    auto key_of = [&](int j) { return held ? keys[j - c0] : candidate_key(c, a, u, j, among_safe); };
 
-    // the range of the keys that are not protected, and their number
-    uint32_t lo = 0xFFFFFFFFu, hi = 0;
-    int open = 0;
-    auto take = [&](int j, uint32_t key) {
-        if (held) keys[j - c0] = key;
-        if (key != kKeyProtected) {
-            lo = min(lo, key);
-            hi = max(hi, key);
-            ++open;
-        }
-    };
+    // The range of the keys that the border can lie among, and the number of rows that leave before any other: the
+    // protected ones are counted out in the first pass, the others in a second one when protected rows have to leave too.
+    uint32_t lo, hi;
+    int left = leave, open;
     constexpr int kBatch = 4;                    // candidates of a thread that walk their chain of reads side by side
     const int cached = min(c1, u.had);
-    for (int base = c0 + threadIdx.x; base < cached; base += kBatch * THREADS) {
-        Slot s[kBatch];
-        float w[kBatch];
-        int pos[kBatch];
+    auto scan = [&](auto second_) {
+        constexpr bool second = decltype(second_)::value;
+        lo = 0xFFFFFFFFu;
+        hi = 0;
+        open = 0;
+        auto take = [&](int j, uint32_t key, bool counts) {
+            if (held) keys[j - c0] = key;
+            if (counts) {
+                lo = min(lo, key);
+                hi = max(hi, key);
+                ++open;
+            }
+        };
+        for (int base = c0 + threadIdx.x; base < cached; base += kBatch * THREADS) {
+            Slot s[kBatch];
+            float w[kBatch];
+            int pos[kBatch];
 #pragma unroll
-        for (int i = 0; i < kBatch; ++i) {
-            const int j = base + i * THREADS;
-            s[i].page = -1;
-            if (j < cached) s[i] = look_up_slot(c, u.n, j);
-        }
+            for (int i = 0; i < kBatch; ++i) {
+                const int j = base + i * THREADS;
+                s[i].page = -1;
+                if (j < cached) s[i] = look_up_slot(c, u.n, j);
+            }
 #pragma unroll
-        for (int i = 0; i < kBatch; ++i) {
-            if (!valid_page(c, s[i])) continue;
-            const uint32_t m = meta_index(c, u.h, s[i]);
-            w[i] = c.weight[m];
-            pos[i] = c.pos[m];
-        }
+            for (int i = 0; i < kBatch; ++i) {
+                if (!valid_page(c, s[i])) continue;
+                const uint32_t m = meta_index(c, u.h, s[i]);
+                w[i] = c.weight[m];
+                pos[i] = c.pos[m];
+            }
 #pragma unroll
-        for (int i = 0; i < kBatch; ++i) {
-            const int j = base + i * THREADS;
-            if (j >= cached) continue;
-            uint32_t key = 0;                    // a row that cannot be read leaves first
-            if (!valid_page(c, s[i])) report_page(c);
-            else key = is_protected(a, u, pos[i]) ? kKeyProtected : weight_key(w[i]);
-            take(j, key);
+            for (int i = 0; i < kBatch; ++i) {
+                const int j = base + i * THREADS;
+                if (j >= cached) continue;
+                if (!valid_page(c, s[i])) {      // a row that cannot be read leaves first, protected or not
+                    report_page(c);
+                    take(j, 0, !second);
+                } else {
+                    const bool safe = is_protected(a, u, pos[i]);
+                    take(j, select_key(safe, w[i], second), safe == second);
+                }
+            }
         }
-    }
-    for (int base = max(c0, u.had) + threadIdx.x; base < c1; base += kBatch * THREADS) {
-        float w[kBatch];
-        int pos[kBatch];
+        for (int base = max(c0, u.had) + threadIdx.x; base < c1; base += kBatch * THREADS) {
+            float w[kBatch];
+            int pos[kBatch];
 #pragma unroll
-        for (int i = 0; i < kBatch; ++i) {
-            const int j = base + i * THREADS, t = j - u.had;
-            if (j >= c1) continue;
-            w[i] = a.w_new ? a.w_new[u.u * a.T + t] : 0.f;
-            pos[i] = a.pos_new ? a.pos_new[u.u * a.T + t] : u.seen + t;
-        }
+            for (int i = 0; i < kBatch; ++i) {
+                const int j = base + i * THREADS, t = j - u.had;
+                if (j >= c1) continue;
+                w[i] = a.w_new ? a.w_new[u.u * a.T + t] : 0.f;
+                pos[i] = a.pos_new ? a.pos_new[u.u * a.T + t] : u.seen + t;
+            }
 #pragma unroll
-        for (int i = 0; i < kBatch; ++i) {
-            const int j = base + i * THREADS;
-            if (j < c1) take(j, is_protected(a, u, pos[i]) ? kKeyProtected : weight_key(w[i]));
+            for (int i = 0; i < kBatch; ++i) {
+                const int j = base + i * THREADS;
+                if (j >= c1) continue;
+                const bool safe = is_protected(a, u, pos[i]);
+                take(j, select_key(safe, w[i], second), safe == second);
+            }
         }
-    }
-    lo = __reduce_min_sync(0xFFFFFFFFu, lo);
-    hi = __reduce_max_sync(0xFFFFFFFFu, hi);
-    open = __reduce_add_sync(0xFFFFFFFFu, open);
-    __syncthreads();
-    if (lane == 0) {
-        sm.lo[warp] = lo;
-        sm.hi[warp] = hi;
-        sm.a[warp] = open;
-    }
-    __syncthreads();
-    lo = __reduce_min_sync(0xFFFFFFFFu, lane < kWarps ? sm.lo[lane] : 0xFFFFFFFFu);
-    hi = __reduce_max_sync(0xFFFFFFFFu, lane < kWarps ? sm.hi[lane] : 0u);
-    open = __reduce_add_sync(0xFFFFFFFFu, lane < kWarps ? sm.a[lane] : 0);
-    if (SPREAD) {
-        if (threadIdx.x == 0) {
-            sm.all_lo = lo;
-            sm.all_hi = hi;
-            sm.all_open = open;
+        lo = __reduce_min_sync(0xFFFFFFFFu, lo);
+        hi = __reduce_max_sync(0xFFFFFFFFu, hi);
+        open = __reduce_add_sync(0xFFFFFFFFu, open);
+        if (second) meet();                  // nobody reads what the first pass left here any more
+        else __syncthreads();
+        if (lane == 0) {
+            sm.lo[warp] = lo;
+            sm.hi[warp] = hi;
+            sm.a[warp] = open;
         }
-        meet();
-        const SelectSmem<THREADS> *other = of(lane < ranks ? lane : 0);
-        lo = __reduce_min_sync(0xFFFFFFFFu, other->all_lo);
-        hi = __reduce_max_sync(0xFFFFFFFFu, other->all_hi);
-        open = __reduce_add_sync(0xFFFFFFFFu, lane < ranks ? other->all_open : 0);
+        __syncthreads();
+        lo = __reduce_min_sync(0xFFFFFFFFu, lane < kWarps ? sm.lo[lane] : 0xFFFFFFFFu);
+        hi = __reduce_max_sync(0xFFFFFFFFu, lane < kWarps ? sm.hi[lane] : 0u);
+        open = __reduce_add_sync(0xFFFFFFFFu, lane < kWarps ? sm.a[lane] : 0);
+        if (SPREAD) {
+            if (threadIdx.x == 0) {
+                sm.all_lo = lo;
+                sm.all_hi = hi;
+                sm.all_open = open;
+            }
+            meet();
+            const SelectSmem<THREADS> *other = of(lane < ranks ? lane : 0);
+            lo = __reduce_min_sync(0xFFFFFFFFu, other->all_lo);
+            hi = __reduce_max_sync(0xFFFFFFFFu, other->all_hi);
+            open = __reduce_add_sync(0xFFFFFFFFu, lane < ranks ? other->all_open : 0);
+        }
+    };
+    scan(std::false_type{});
+    if (left > open) {                           // all of these leave, and some of the protected rows
+        left -= open;
+        among_safe = true;
+        scan(std::true_type{});
     }
     // Of the keys in [lo, hi] `left` leave, and every smaller one. Narrowed until all of the range leaves or it is one key.
-    int left = leave, equal = 0;                 // equal > 0: rows at the edge, of which the last `left` leave
+    // (At least one row stays, so that among protected rows fewer leave than there are.)
+    int equal = 0;                               // > 0: rows at the edge, of which the last `left` leave
     uint32_t edge;                               // rows with a smaller key leave
-    if (left >= open) {                          // protected rows leave too, where they are all that is left
-        left -= open;
-        equal = all - open;
+    if (left == open) {                          // all that are not protected, and nothing else
+        left = 0;
         edge = kKeyProtected;
     } else {
         for (;;) {
@@ -501,10 +530,21 @@ constexpr int kRowCtas = 8;                      // per SM
 constexpr int kRowsHeld = 4;                     // rows a thread has in flight
 constexpr int kScoresHeld = 4;                   // query heads whose scores a thread reads side by side
 
-// The row that leaves first has the smallest of these: key, then the higher candidate.
-__device__ __forceinline__ unsigned long long leave_order(uint32_t key, int j)
+// The row that leaves first has the smallest of these: protected or not (one bit), key (32), then the higher candidate (31 bits:
+// the host refuses more candidates).
+constexpr uint32_t kLastCandidate = 0x7FFFFFFFu;
+__device__ __forceinline__ unsigned long long leave_order(bool safe, uint32_t key, int j)
 {
-    return ((unsigned long long)key << 32) | (0xFFFFFFFFu - (uint32_t)j);
+    return ((unsigned long long)(safe ? 1u : 0u) << 63) | ((unsigned long long)key << 31) | (kLastCandidate - (uint32_t)j);
+}
+__device__ __forceinline__ int row_that_leaves(unsigned long long order) { return (int)(kLastCandidate - ((uint32_t)order & kLastCandidate)); }
+
+// More rows of a unit leave than join, which follows a smaller budget only: a call of its own keeps its registers out of the
+// kernel's ordinary way.
+__device__ __noinline__ void evict_many(const PagedView &c, const AppendArgs &a, const Unit &u, SelectSmem<kRowThreads> &sm, int lpr)
+{
+    const int movers = select_unit<kRowThreads, false>(c, a, u, sm, nullptr, 0);
+    move_listed<kRowThreads>(c, a, u, movers, lpr, 0, 1);
 }
 
 // `splits` CTAs per (problem, head). GATHER: weights <- decay * weights + probabilities of the step. APPEND: at most one
@@ -513,7 +553,8 @@ __device__ __forceinline__ unsigned long long leave_order(uint32_t key, int j)
 // QUAD: a thread's rows are neighbours in one page, so that one page number and reads of 16 bytes do for the four; else
 // they lie kRowThreads apart.
 template <bool GATHER, bool APPEND, bool QUAD>
-__global__ void __launch_bounds__(kRowThreads, kRowCtas) paged_rows_kernel(PagedView c, GatherArgs ga, AppendArgs ap, int lpr, int splits)
+__global__ void __launch_bounds__(kRowThreads, kRowCtas) paged_rows_kernel(const __grid_constant__ PagedView c, GatherArgs ga,
+                                                                            const __grid_constant__ AppendArgs ap, int lpr, int splits)
 {
     extern __shared__ float2 sm_stat[];          // [G]
     __shared__ unsigned long long sm_low[kRowThreads / 32];
@@ -577,7 +618,7 @@ __global__ void __launch_bounds__(kRowThreads, kRowCtas) paged_rows_kernel(Paged
             if (GATHER)
                 score[r] = by_row ? ga.scores + head_at * score_rows + row
                                   : ga.scores + (size_t)((uint32_t)s.page * (uint32_t)c.H + (uint32_t)h) * G * score_rows + s.slot;
-            if (APPEND && !there[r]) low = min(low, leave_order(0, row)); // a row that cannot be read leaves first
+            if (APPEND && !there[r]) low = min(low, leave_order(false, 0, row)); // a row that cannot be read leaves first
         }
         if (QUAD) {                              // what lies behind the last row is read with it and not used
             if (there[0]) {
@@ -642,8 +683,7 @@ __global__ void __launch_bounds__(kRowThreads, kRowCtas) paged_rows_kernel(Paged
 #pragma unroll
             for (int r = 0; r < kRowsHeld; ++r) {
                 if (!there[r]) continue;
-                const bool safe = is_protected(ap, u, pos[r]);
-                low = min(low, leave_order(safe ? kKeyProtected : weight_key(w[r]), thread_row + r * row_step));
+                low = min(low, leave_order(is_protected(ap, u, pos[r]), weight_key(w[r]), thread_row + r * row_step));
             }
         }
     }
@@ -662,7 +702,7 @@ __global__ void __launch_bounds__(kRowThreads, kRowCtas) paged_rows_kernel(Paged
     if (z == 0 && warp == 0 && u.cnt > 0) {
         if (!GATHER) w_own = ap.w_new ? ap.w_new[unit] : 0.f;
         const bool safe = is_protected(ap, u, ap.pos_new ? ap.pos_new[unit] : u.seen);
-        low = min(low, leave_order(safe ? kKeyProtected : weight_key(w_own), u.had));
+        low = min(low, leave_order(safe, weight_key(w_own), u.had));
     }
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) low = min(low, __shfl_xor_sync(0xFFFFFFFFu, low, d));
@@ -680,7 +720,7 @@ __global__ void __launch_bounds__(kRowThreads, kRowCtas) paged_rows_kernel(Paged
         if (v.cnt == 0) return;
         int dst = v.had;
         if (v.had + v.cnt > v.final) {
-            dst = (int)(0xFFFFFFFFu - (uint32_t)lowest);
+            dst = row_that_leaves(lowest);
             if (dst == v.had) return;            // the new row itself is the one that leaves
         }
         if (l < lpr) move_row(c, ap, v, dst, v.had, lpr, l);
@@ -694,10 +734,10 @@ __global__ void __launch_bounds__(kRowThreads, kRowCtas) paged_rows_kernel(Paged
             c.seen[n] = u.seen + u.cnt;
         }
         if (!simple) {
-            const int movers = select_unit<kRowThreads, false>(c, ap, u, sm_select, nullptr, 0);
-            move_listed<kRowThreads>(c, ap, u, movers, lpr, 0, 1);
+            const Unit v = u;
+            evict_many(c, ap, v, sm_select, lpr);
         } else if (carry) {
-            const int dst = leave <= 0 ? u.had : (int)(0xFFFFFFFFu - (uint32_t)sm_low[0]);
+            const int dst = leave <= 0 ? u.had : row_that_leaves(sm_low[0]);
             if (leave > 0 && dst == u.had) return;                        // the new row itself is the one that leaves
             const Slot s = look_up_slot(c, n, dst);
             if (!valid_page(c, s)) {
@@ -734,8 +774,7 @@ __global__ void __launch_bounds__(kRowThreads, kRowCtas) paged_rows_kernel(Paged
             Unit v = u;
             v.h = hh;
             v.u = (size_t)n * c.H + hh;
-            const int movers = select_unit<kRowThreads, false>(c, ap, v, sm_select, nullptr, 0);
-            move_listed<kRowThreads>(c, ap, v, movers, lpr, 0, 1);
+            evict_many(c, ap, v, sm_select, lpr);
             __syncthreads();
         }
     }
