@@ -6,8 +6,9 @@
 // would only add latency here: a tile has 8 to 16 query rows, not 128.
 //  - Both products are taken transposed, S^T = K Q^T and O^T = V^T P^T, so that the 16-row side of the instruction
 //    is the cache and the 8-column side the group's query heads. P goes from accumulator to operand layout with
-//    movmatrix, in two rounded parts, so that the result's own rounding is all that its type costs (one rounding of P
-//    measured 1.35 times the error; the second part's products are not seen in the time).
+//    movmatrix, in two parts, so that the result's own rounding is all that its type costs (one rounding of P
+//    measured 1.35 times the error; the second part's products are not seen in the time). fp16 has too few exponents for rows
+//    far below the leading one: see Fp16.
 //  - Every warp streams its own tiles of 4 KB of K and 4 KB of V through a ring of three asynchronous copies in shared memory
 //    (192 KB per SM) and runs ahead over the borders of units, so that the reads never pause while a unit's results are
 //    put together. Page numbers are fetched a ring's length before the copies that need them, queries with a unit's
@@ -15,7 +16,7 @@
 //  - Work is handed out in blocks of a tile per warp, evenly over the CTAs of one resident wave, from the lengths on the
 //    device: a ragged batch and one long sequence spread alike. A CTA's share is at most one partial unit at either end and
 //    whole units between; of the CTAs that share a unit the one that arrives last joins the parts (nobody waits).
-//  - The running maximum is raised only when a tile exceeds it by 2^8, so that most tiles need no reduction across lanes.
+//  - The running maximum is raised only when a tile exceeds it by 2^8 (fp16: 2^4), so that most tiles need no reduction across lanes.
 // Measured per call, all launches, bf16, D = 128: 16 problems x 32 heads x 8192 rows 329 us (6.5 TB/s; 370 us with the weights),
 // one problem of 131071 rows, 8 heads for 64 query heads 90 us (6.0 TB/s), 32 problems of 0 .. 8192 rows 27.5 us (5.0 TB/s),
 // one problem of 37 rows 4.7 us. What is left at small sizes is a chain of dependent reads (length, page, row), the
@@ -31,9 +32,11 @@ namespace ec {
 namespace {
 
 template <int D> constexpr int kTileRows = 2048 / D;                      // rows of a warp's tile: 4 KB of K, 4 KB of V
-constexpr float kLazy = 8.f;                     // the running maximum is raised when exceeded by more than this (log2)
 
 struct Bf16 {
+    static constexpr float kLazy = 8.f;          // the running maximum is raised when exceeded by more than this (log2)
+    static constexpr float kTop = 0.f;           // log2 of a probability at the running maximum
+    static constexpr float kLeast = -INFINITY;   // parts of this type hold every probability
     static __device__ __forceinline__ uint32_t pack(float a, float b) { return pack2(a, b); }
     static __device__ __forceinline__ float2 unpack(uint32_t w) { return make_float2(bf16lo(w), bf16hi(w)); }
     static __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
@@ -44,7 +47,16 @@ struct Bf16 {
     }
 };
 
+// Parts of P in fp16 are multiples of 2^-24, and rows of a peaked softmax lie further below its maximum than that (a row that
+// gathers the attention and has small values, and the output is made of the others). So P is counted from 2^11 at the running
+// maximum, which leaves the 2^4 that it may rise under the type's largest number, and is off by 2^-25: 2^-14 of a probability of
+// 2^-11, 2^-22 of the maximum's. Tiles with a smaller one take P and V as tf32, where two parts hold 22 bits over all of fp32's
+// exponents and V is exact, at twice the products and half the rate. All tiles as tf32 / only these, where there are none: 128 units x 16
+// query heads x 8192 rows, D = 64, 58 / 50 us; 1024 units of 640 rows with weights 64 / 60 us (58 without the question).
 struct Fp16 {
+    static constexpr float kLazy = 4.f;
+    static constexpr float kTop = 11.f;
+    static constexpr float kLeast = -11.f;       // log2 of the least probability that they hold
     static __device__ __forceinline__ uint32_t pack(float a, float b)
     {
         __half2 h = __floats2half2_rn(a, b);
@@ -58,6 +70,20 @@ struct Fp16 {
                      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
     }
 };
+
+// The 22 bits of a probability that two tf32 parts hold, from its fp32 value. The bits that the instruction does not use are cleared.
+__device__ __forceinline__ void split_tf32(uint32_t p, uint32_t &hi, uint32_t &lo)
+{
+    hi = p & 0xFFFFE000u;
+    lo = __float_as_uint(__uint_as_float(p) - __uint_as_float(hi)) & 0xFFFFE000u;
+}
+
+__device__ __forceinline__ void mma_tf32(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
 
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t x)
 {
@@ -107,8 +133,8 @@ struct AttnArgs {
     uint32_t *out;
     float *lse;
     // workspace
-    float2 *stat;                                // [N, Hq] (maximum in the log2 domain, 1 / sum)
-    float *score_new;                            // [N, Hq] the same of the step's own row
+    float2 *stat;                                // [N, Hq] (what the log2 scores are counted from, 1 / sum)
+    float *score_new;                            // [N, Hq] the score of the step's own row, not scaled
     float *part_o;                               // [2 * CTAs][8 NT][D]
     float2 *part_ml;                             // [2 * CTAs][8 NT]
     float *scores;                               // <q, k>, not scaled, see scores_by_row
@@ -241,6 +267,15 @@ template <int D, int NT, int W> struct Smem {
     static constexpr int kTotal = kPages + W * kStages * kTile * 4;
 };
 
+// What is kept of a head beside its output, from its maximum and its sum.
+template <typename E>
+__device__ __forceinline__ void keep_normaliser(const AttnArgs &a, size_t at, float M, float L)
+{
+    const float top = (M == -INFINITY ? 0.f : M) - E::kTop;               // exp2(x - top) / L is the probability of a score x
+    a.stat[at] = make_float2(top, L == 0.f ? 0.f : 1.f / L);
+    if (a.lse) a.lse[at] = M == -INFINITY ? -INFINITY : (top + log2f(L)) * 0.6931471805599453f;
+}
+
 // Joins the parts of a unit that the CTAs c0 .. c1 hold. A thread owns four dimensions of a head and has several parts in
 // flight, the first of them before the parts' factors are known; `buf` (kMergeFloats floats) takes the factors.
 template <typename E, int D, int NT, int W>
@@ -287,10 +322,7 @@ __device__ __forceinline__ void join_parts(const AttnArgs &a, int c0, int c1, in
             r.x = E::pack(A.x * inv, A.y * inv);
             r.y = E::pack(A.z * inv, A.w * inv);
             *reinterpret_cast<uint2 *>(a.out + ((head_at + hd) * D + d) / 2) = r;
-            if (d == 0) {
-                a.stat[head_at + hd] = make_float2(mu, inv);
-                if (a.lse) a.lse[head_at + hd] = M == -INFINITY ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
-            }
+            if (d == 0) keep_normaliser<E>(a, head_at + hd, M, L);
         }
         return;
     }
@@ -326,8 +358,7 @@ __device__ __forceinline__ void join_parts(const AttnArgs &a, int c0, int c1, in
         if (lane == 0) {
             sm_inv[hd] = inv;
             sm_m[hd] = mu;
-            a.stat[head_at + hd] = make_float2(mu, inv);
-            if (a.lse) a.lse[head_at + hd] = M == -INFINITY ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+            keep_normaliser<E>(a, head_at + hd, M, L);
         }
         for (int c = lane; c < min(parts, kChunk); c += 32) buf[hd * kChunk + c] = fast_exp2(buf[hd * kChunk + c] - mu);
     }
@@ -607,6 +638,7 @@ __global__ void __launch_bounds__(W * 32, 8 / W) paged_attention_kernel(AttnArgs
             }
             uint2 info[RT][2];                   // rows g and g + 8 of every 16
             bool raise = false;                  // scale > 0: the scores are compared before they are scaled
+            float low[NT][2];                    // the lowest of a head; an absent row counts with a score of zero
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
                 info[rt][0] = rows_info[stage * kTile + rt * 16 + g];
@@ -616,8 +648,10 @@ __global__ void __launch_bounds__(W * 32, 8 / W) paged_attention_kernel(AttnArgs
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        s[rt][nt][i] = there0 ? s[rt][nt][i] + s1[rt][nt][i] : -INFINITY;
-                        s[rt][nt][2 + i] = there1 ? s[rt][nt][2 + i] + s1[rt][nt][2 + i] : -INFINITY;
+                        const float x = s[rt][nt][i] + s1[rt][nt][i], y = s[rt][nt][2 + i] + s1[rt][nt][2 + i];
+                        if (E::kLeast > -INFINITY) low[nt][i] = rt == 0 ? fminf(x, y) : fminf(low[nt][i], fminf(x, y));
+                        s[rt][nt][i] = there0 ? x : -INFINITY;
+                        s[rt][nt][2 + i] = there1 ? y : -INFINITY;
                         raise |= fmaxf(s[rt][nt][i], s[rt][nt][2 + i]) > limit[nt][i];
                     }
             }
@@ -634,8 +668,8 @@ __global__ void __launch_bounds__(W * 32, 8 / W) paged_attention_kernel(AttnArgs
                         const float mn = fmaxf(m[nt][i], x * a.scale_log2e);
                         const float corr = mn == -INFINITY ? 1.f : fast_exp2(m[nt][i] - mn);   // first tile: 2^-inf = 0
                         m[nt][i] = mn;
-                        limit[nt][i] = (mn + kLazy) * a.inv_scale;
-                        neg_m[nt][i] = mn == -INFINITY ? 0.f : -mn;
+                        limit[nt][i] = (mn + E::kLazy) * a.inv_scale;
+                        neg_m[nt][i] = mn == -INFINITY ? 0.f : E::kTop - mn;
                         l[nt][i] *= corr;
 #pragma unroll
                         for (int mt = 0; mt < MT; ++mt) {
@@ -644,33 +678,80 @@ __global__ void __launch_bounds__(W * 32, 8 / W) paged_attention_kernel(AttnArgs
                         }
                     }
             }
-            uint32_t hi[RT][NT][2], lo[RT][NT][2];   // P as the sum of two rounded parts: 16 bits of it or more meet V
+            const int v_row = (lane & 7) + (lane >> 4) * 8;
+            const uint32_t v_at = (tile + M_::kTileBytes + v_row * (D * 2)) + ((((lane >> 3) & 1) ^ (v_row & 7)) << 4);
+            bool little = false;
+            if (E::kLeast > -INFINITY) {
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt)
+                for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    float p[4];
+                    for (int i = 0; i < 2; ++i) little |= fmaf(low[nt][i], a.scale_log2e, neg_m[nt][i]) < E::kLeast;
+            }
+            float p[RT][NT][4];                  // rows g, g, g + 8, g + 8 and heads 2t, 2t + 1, 2t, 2t + 1
+            auto probabilities = [&] {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) p[i] = fast_exp2(fmaf(s[rt][nt][i], a.scale_log2e, neg_m[nt][i & 1]));
-                    l[nt][0] += p[0] + p[2];
-                    l[nt][1] += p[1] + p[3];
+                for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-                    for (int r = 0; r < 2; ++r) {
-                        const uint32_t x = E::pack(p[2 * r], p[2 * r + 1]);
-                        const float2 f = E::unpack(x);
-                        hi[rt][nt][r] = transpose8x8(x);
-                        lo[rt][nt][r] = transpose8x8(E::pack(p[2 * r] - f.x, p[2 * r + 1] - f.y));
+                    for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) p[rt][nt][i] = fast_exp2(fmaf(s[rt][nt][i], a.scale_log2e, neg_m[nt][i & 1]));
+                        l[nt][0] += p[rt][nt][0] + p[rt][nt][2];
+                        l[nt][1] += p[rt][nt][1] + p[rt][nt][3];
+                    }
+            };
+            // decided ahead of the exponentials, which then run between the products (behind them: 3 to 9% of a call)
+            if (E::kLeast > -INFINITY && __any_sync(0xFFFFFFFFu, little)) {
+                probabilities();
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) {
+                    // Rows 2t, 2t + 1, 2t + 8, 2t + 9 of head g. V's fragment holds the same rows, two to a register, and the order of
+                    // the rows within a product is free: a register's low halves are one k of tf32, its high halves the next.
+                    uint32_t hi[NT][4], lo[NT][4];
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int r = 0; r < 2; ++r) {
+                            const uint32_t x = __float_as_uint(p[rt][nt][2 * r]), y = __float_as_uint(p[rt][nt][2 * r + 1]);
+                            const uint32_t low = transpose8x8(__byte_perm(x, y, 0x5410)), high = transpose8x8(__byte_perm(x, y, 0x7632));
+                            split_tf32(__byte_perm(low, high, 0x5410), hi[nt][2 * r], lo[nt][2 * r]);
+                            split_tf32(__byte_perm(low, high, 0x7632), hi[nt][2 * r + 1], lo[nt][2 * r + 1]);
+                        }
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt) {
+                        uint32_t av[4];
+                        load_matrices_trans(av, (v_at ^ (mt << 5)) + rt * 16 * (D * 2));
+#pragma unroll
+                        for (int r = 0; r < 2; ++r) {                     // eight rows each: 2t and 2t + 1, then 2t + 8 and 2t + 9
+                            const float2 v0 = E::unpack(av[2 * r]), v1 = E::unpack(av[2 * r + 1]);
+                            const uint32_t w[4] = {__float_as_uint(v0.x), __float_as_uint(v1.x), __float_as_uint(v0.y), __float_as_uint(v1.y)};
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt) {
+                                mma_tf32(o[nt][mt], w, hi[nt][2 * r], hi[nt][2 * r + 1]);
+                                mma_tf32(o[nt][mt], w, lo[nt][2 * r], lo[nt][2 * r + 1]);
+                            }
+                        }
                     }
                 }
-            {
-                const int row = (lane & 7) + (lane >> 4) * 8;
-                const uint32_t at = (tile + M_::kTileBytes + row * (D * 2)) + ((((lane >> 3) & 1) ^ (row & 7)) << 4);
+            } else {
+                probabilities();
+                uint32_t hi[RT][NT][2], lo[RT][NT][2];   // P as the sum of two rounded parts: 16 bits of it or more meet V (fp16: 14)
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int r = 0; r < 2; ++r) {
+                            const uint32_t x = E::pack(p[rt][nt][2 * r], p[rt][nt][2 * r + 1]);
+                            const float2 f = E::unpack(x);
+                            hi[rt][nt][r] = transpose8x8(x);
+                            lo[rt][nt][r] = transpose8x8(E::pack(p[rt][nt][2 * r] - f.x, p[rt][nt][2 * r + 1] - f.y));
+                        }
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
                     for (int mt = 0; mt < MT; ++mt) {
                         uint32_t av[4];
-                        load_matrices_trans(av, (at ^ (mt << 5)) + rt * 16 * (D * 2));
+                        load_matrices_trans(av, (v_at ^ (mt << 5)) + rt * 16 * (D * 2));
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt) {
                             E::mma(o[nt][mt], av, hi[rt][nt][0], hi[rt][nt][1]);
@@ -711,14 +792,6 @@ __global__ void __launch_bounds__(W * 32, 8 / W) paged_attention_kernel(AttnArgs
                 for (int i = 0; i < 2; ++i)
 #pragma unroll
                     for (int d = 4; d < 32; d <<= 1) l[nt][i] += __shfl_xor_sync(0xFFFFFFFFu, l[nt][i], d);
-            auto finish = [&](int hd, float M, float L, float mu, float inv) {   // what is kept of a head beside its output
-                if (whole) {
-                    a.stat[head_at + hd] = make_float2(mu, inv);
-                    if (a.lse) a.lse[head_at + hd] = M == -INFINITY ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
-                } else {
-                    a.part_ml[(size_t)part * 8 * NT + hd] = make_float2(M, L);
-                }
-            };
             if (warp < nw && g == 0) {
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
@@ -769,13 +842,9 @@ __global__ void __launch_bounds__(W * 32, 8 / W) paged_attention_kernel(AttnArgs
                         const float inv = L == 0.f ? 0.f : 1.f / L;       // nothing left by the scores: the output is zero
                         if (whole) a.out[((head_at + hd) * D + d) >> 1] = E::pack(A.x * inv, A.y * inv);
                         else *reinterpret_cast<float2 *>(a.part_o + ((size_t)part * 8 * NT + hd) * D + d) = A;
-                        if (d == 0) {            // what is kept of a head beside its output
-                            if (whole) {
-                                a.stat[head_at + hd] = make_float2(mu, inv);
-                                if (a.lse) a.lse[head_at + hd] = M == -INFINITY ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
-                            } else {
-                                a.part_ml[(size_t)part * 8 * NT + hd] = make_float2(M, L);
-                            }
+                        if (d == 0) {
+                            if (whole) keep_normaliser<E>(a, head_at + hd, M, L);
+                            else a.part_ml[(size_t)part * 8 * NT + hd] = make_float2(M, L);
                         }
                     }
                     copies_wait<S - 1>();        // with the barrier: the next unit's queries are here
