@@ -150,9 +150,9 @@ __device__ __forceinline__ int read_len(const PagedView &c, int n)
 // pages of one row: 81 us a call, 30 us row by row).
 inline __host__ __device__ bool scores_by_row(int page_size) { return page_size < 8; }
 
-// What turns an attention call's stored scores into weights: p = 2^(score * scale_log2e - top) / sum.
+// What turns an attention call's stored scores into weights: p = 2^((score - .x) * scale_log2e) * .y.
 struct GatherArgs {
-    const float2 *stat;                          // [N, Hq] (top, 1 / sum); 1 / sum is 0 where no row is left
+    const float2 *stat;                          // [N, Hq] (the largest score, factor); the factor is 0 where no row is left
     const float *scores;                         // <q, k>, not scaled, see scores_by_row
     const float *score_new;                      // [N, Hq] the same of the step's own row
     float *w_new;                                // [N, H]; nullptr: the step has no row of its own

@@ -666,7 +666,7 @@ __global__ void __launch_bounds__(kRowThreads, kRowCtas) paged_rows_kernel(const
                     const float2 st = sm_stat[h0 + i];
 #pragma unroll
                     for (int r = 0; r < kRowsHeld; ++r)
-                        if (there[r]) p[r] = fmaf(fast_exp2(fmaf(x[i][r], ga.scale_log2e, -st.x)), st.y, p[r]);
+                        if (there[r]) p[r] = fmaf(fast_exp2((x[i][r] - st.x) * ga.scale_log2e), st.y, p[r]);
                 }
             }
 #pragma unroll
@@ -692,7 +692,7 @@ __global__ void __launch_bounds__(kRowThreads, kRowCtas) paged_rows_kernel(const
     float w_own = 0.f;
     if (GATHER && ga.w_new && z == 0 && warp == 0) {
         for (int hd = lane; hd < G; hd += 32)
-            w_own = fmaf(fast_exp2(fmaf(ga.score_new[head_at + hd], ga.scale_log2e, -sm_stat[hd].x)), sm_stat[hd].y, w_own);
+            w_own = fmaf(fast_exp2((ga.score_new[head_at + hd] - sm_stat[hd].x) * ga.scale_log2e), sm_stat[hd].y, w_own);
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) w_own += __shfl_xor_sync(0xFFFFFFFFu, w_own, d);
         if (lane == 0) ga.w_new[unit] = w_own;

@@ -17,6 +17,8 @@
 //    device: a ragged batch and one long sequence spread alike. A CTA's share is at most one partial unit at either end and
 //    whole units between; of the CTAs that share a unit the one that arrives last joins the parts (nobody waits).
 //  - The running maximum is raised only when a tile exceeds it by 2^8 (fp16: 2^4), so that most tiles need no reduction across lanes.
+//    It is kept, as the scores are, before the scale: the difference of two scores that are near each other is exact, while the
+//    scaled maximum, rounded, may lie 2^128 from its own row (scores of 2^31). Costs one addition per score, not seen in the time.
 // Measured per call, all launches, bf16, D = 128: 16 problems x 32 heads x 8192 rows 329 us (6.5 TB/s; 370 us with the weights),
 // one problem of 131071 rows, 8 heads for 64 query heads 90 us (6.0 TB/s), 32 problems of 0 .. 8192 rows 27.5 us (5.0 TB/s),
 // one problem of 37 rows 4.7 us. What is left at small sizes is a chain of dependent reads (length, page, row), the
@@ -129,11 +131,11 @@ struct AttnArgs {
     const uint32_t *q;
     const uint4 *k_new, *v_new;                  // k_new == nullptr: the cached rows alone
     int G;                                       // query heads per key / value head
-    float scale_log2e, inv_scale;                // inv_scale: 1 / scale_log2e
+    float scale_log2e, inv_scale;                // inv_scale: 1 / scale_log2e, or a number as large as can be added to
     uint32_t *out;
     float *lse;
     // workspace
-    float2 *stat;                                // [N, Hq] (what the log2 scores are counted from, 1 / sum)
+    float2 *stat;                                // [N, Hq] (the largest score, what its sum leaves as factor)
     float *score_new;                            // [N, Hq] the score of the step's own row, not scaled
     float *part_o;                               // [2 * CTAs][8 NT][D]
     float2 *part_ml;                             // [2 * CTAs][8 NT]
@@ -267,13 +269,14 @@ template <int D, int NT, int W> struct Smem {
     static constexpr int kTotal = kPages + W * kStages * kTile * 4;
 };
 
-// What is kept of a head beside its output, from its maximum and its sum.
+// What is kept of a head beside its output, from its maximum and its sum: exp2((x - .x) * scale_log2e) * .y is the probability
+// of a score x.
 template <typename E>
 __device__ __forceinline__ void keep_normaliser(const AttnArgs &a, size_t at, float M, float L)
 {
-    const float top = (M == -INFINITY ? 0.f : M) - E::kTop;               // exp2(x - top) / L is the probability of a score x
-    a.stat[at] = make_float2(top, L == 0.f ? 0.f : 1.f / L);
-    if (a.lse) a.lse[at] = M == -INFINITY ? -INFINITY : (top + log2f(L)) * 0.6931471805599453f;
+    const float top = M == -INFINITY ? 0.f : M;
+    a.stat[at] = make_float2(top, L == 0.f ? 0.f : exp2f(E::kTop) / L);
+    if (a.lse) a.lse[at] = M == -INFINITY ? -INFINITY : fmaf(top, a.scale_log2e, log2f(L) - E::kTop) * 0.6931471805599453f;
 }
 
 // Joins the parts of a unit that the CTAs c0 .. c1 hold. A thread owns four dimensions of a head and has several parts in
@@ -310,7 +313,7 @@ __device__ __forceinline__ void join_parts(const AttnArgs &a, int c0, int c1, in
 #pragma unroll
             for (int c = 0; c < kFlight; ++c) {
                 if (c >= parts) continue;
-                const float f = fast_exp2(ml[c].x - mu);
+                const float f = fast_exp2((ml[c].x - mu) * a.scale_log2e);
                 L = fmaf(ml[c].y, f, L);
                 A.x = fmaf(v[c].x, f, A.x);
                 A.y = fmaf(v[c].y, f, A.y);
@@ -343,7 +346,7 @@ __device__ __forceinline__ void join_parts(const AttnArgs &a, int c0, int c1, in
         for (int c = lane; c < parts; c += 32) {
             const float2 v = __ldcg(&a.part_ml[part_at(c) + hd]);
             const float mn = fmaxf(M, v.x);
-            if (mn != -INFINITY) L = L * fast_exp2(M - mn) + v.y * fast_exp2(v.x - mn);
+            if (mn != -INFINITY) L = L * fast_exp2((M - mn) * a.scale_log2e) + v.y * fast_exp2((v.x - mn) * a.scale_log2e);
             M = mn;
             if (c < kChunk) buf[hd * kChunk + c] = v.x;
         }
@@ -351,7 +354,7 @@ __device__ __forceinline__ void join_parts(const AttnArgs &a, int c0, int c1, in
         for (int d = 1; d < 32; d <<= 1) {
             const float m2 = __shfl_xor_sync(0xFFFFFFFFu, M, d), l2 = __shfl_xor_sync(0xFFFFFFFFu, L, d);
             const float mn = fmaxf(M, m2);
-            if (mn != -INFINITY) L = L * fast_exp2(M - mn) + l2 * fast_exp2(m2 - mn);
+            if (mn != -INFINITY) L = L * fast_exp2((M - mn) * a.scale_log2e) + l2 * fast_exp2((m2 - mn) * a.scale_log2e);
             M = mn;
         }
         const float mu = M == -INFINITY ? 0.f : M, inv = L == 0.f ? 0.f : 1.f / L;
@@ -360,7 +363,7 @@ __device__ __forceinline__ void join_parts(const AttnArgs &a, int c0, int c1, in
             sm_m[hd] = mu;
             keep_normaliser<E>(a, head_at + hd, M, L);
         }
-        for (int c = lane; c < min(parts, kChunk); c += 32) buf[hd * kChunk + c] = fast_exp2(buf[hd * kChunk + c] - mu);
+        for (int c = lane; c < min(parts, kChunk); c += 32) buf[hd * kChunk + c] = fast_exp2((buf[hd * kChunk + c] - mu) * a.scale_log2e);
     }
     __syncthreads();
     for (int cb = 0; cb < parts; cb += kChunk) {
@@ -369,7 +372,7 @@ __device__ __forceinline__ void join_parts(const AttnArgs &a, int c0, int c1, in
             __syncthreads();
             for (int i = threadIdx.x; i < heads * cn; i += kThreads) {
                 const int hd = i / cn, c = i - hd * cn;
-                buf[hd * kChunk + c] = fast_exp2(__ldcg(&a.part_ml[part_at(cb + c) + hd].x) - sm_m[hd]);
+                buf[hd * kChunk + c] = fast_exp2((__ldcg(&a.part_ml[part_at(cb + c) + hd].x) - sm_m[hd]) * a.scale_log2e);
             }
             __syncthreads();
         }
@@ -562,7 +565,7 @@ __global__ void __launch_bounds__(W * 32, 8 / W) paged_attention_kernel(AttnArgs
     // Q's fragments stay in registers for 8 heads; for 16 they would spill, and are read again for every tile
     constexpr bool kHoldQ = NT == 1;
     uint32_t qf[kHoldQ ? NT : 1][kHoldQ ? KS : 1][2], q_at = 0;
-    float o[NT][MT][4], m[NT][2], l[NT][2], limit[NT][2], neg_m[NT][2];
+    float o[NT][MT][4], m[NT][2], l[NT][2], limit[NT][2], top[NT][2];
     int stage = 0, q_slot = 0, first_block = use.blk;
     auto begin_unit = [&] {                      // the queries of the next unit are here; nothing has been seen of it
         q_at = base + M_::kQ + q_slot * M_::kQBytes + (lane & 7) * (D * 2) + (((lane >> 3) ^ (lane & 7)) << 4);
@@ -581,7 +584,7 @@ __global__ void __launch_bounds__(W * 32, 8 / W) paged_attention_kernel(AttnArgs
                 }
             }
             m[nt][0] = m[nt][1] = limit[nt][0] = limit[nt][1] = -INFINITY;
-            neg_m[nt][0] = neg_m[nt][1] = 0.f;
+            top[nt][0] = top[nt][1] = 0.f;
             l[nt][0] = l[nt][1] = 0.f;
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt)
@@ -665,11 +668,11 @@ __global__ void __launch_bounds__(W * 32, 8 / W) paged_attention_kernel(AttnArgs
                         for (int rt = 1; rt < RT; ++rt) x = fmaxf(x, fmaxf(s[rt][nt][i], s[rt][nt][2 + i]));
 #pragma unroll
                         for (int d = 4; d < 32; d <<= 1) x = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, d));
-                        const float mn = fmaxf(m[nt][i], x * a.scale_log2e);
-                        const float corr = mn == -INFINITY ? 1.f : fast_exp2(m[nt][i] - mn);   // first tile: 2^-inf = 0
+                        const float mn = fmaxf(m[nt][i], x);
+                        const float corr = mn == -INFINITY ? 1.f : fast_exp2((m[nt][i] - mn) * a.scale_log2e);   // first tile: 2^-inf = 0
                         m[nt][i] = mn;
-                        limit[nt][i] = (mn + E::kLazy) * a.inv_scale;
-                        neg_m[nt][i] = mn == -INFINITY ? 0.f : E::kTop - mn;
+                        limit[nt][i] = __fadd_rd(mn, E::kLazy * a.inv_scale);   // rounded up it could let 2^(2 kLazy) pass
+                        top[nt][i] = mn == -INFINITY ? 0.f : mn;
                         l[nt][i] *= corr;
 #pragma unroll
                         for (int mt = 0; mt < MT; ++mt) {
@@ -685,7 +688,7 @@ __global__ void __launch_bounds__(W * 32, 8 / W) paged_attention_kernel(AttnArgs
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) little |= fmaf(low[nt][i], a.scale_log2e, neg_m[nt][i]) < E::kLeast;
+                    for (int i = 0; i < 2; ++i) little |= fmaf(low[nt][i] - top[nt][i], a.scale_log2e, E::kTop) < E::kLeast;
             }
             float p[RT][NT][4];                  // rows g, g, g + 8, g + 8 and heads 2t, 2t + 1, 2t, 2t + 1
             auto probabilities = [&] {
@@ -694,7 +697,7 @@ __global__ void __launch_bounds__(W * 32, 8 / W) paged_attention_kernel(AttnArgs
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) p[rt][nt][i] = fast_exp2(fmaf(s[rt][nt][i], a.scale_log2e, neg_m[nt][i & 1]));
+                        for (int i = 0; i < 4; ++i) p[rt][nt][i] = fast_exp2(fmaf(s[rt][nt][i] - top[nt][i & 1], a.scale_log2e, E::kTop));
                         l[nt][0] += p[rt][nt][0] + p[rt][nt][2];
                         l[nt][1] += p[rt][nt][1] + p[rt][nt][3];
                     }
@@ -833,7 +836,7 @@ __global__ void __launch_bounds__(W * 32, 8 / W) paged_attention_kernel(AttnArgs
 #pragma unroll
                         for (int w = 0; w < most; ++w) {
                             if (w >= nw) continue;
-                            const float f = fast_exp2(ml[w].x - mu);
+                            const float f = fast_exp2((ml[w].x - mu) * a.scale_log2e);
                             const float2 v = *reinterpret_cast<const float2 *>(sm_o + (w * per_round + at) * M_::kPitch + d);
                             L = fmaf(ml[w].y, f, L);
                             A.x = fmaf(v.x, f, A.x);
@@ -963,7 +966,7 @@ cudaError_t launch_paged_attention(const PagedView &c, int D, int dtype, const v
     a.v_new = static_cast<const uint4 *>(v_new);
     a.G = Hq / c.H;
     a.scale_log2e = scale * 1.4426950408889634f;
-    a.inv_scale = 1.f / a.scale_log2e;
+    a.inv_scale = fminf(1.f / a.scale_log2e, 0x1p120f);
     a.out = static_cast<uint32_t *>(out);
     a.lse = lse;
     const WsLayout w = layout(c.N, c.H, D, c.n_pages, c.page_size, c.max_pages, a.G, accumulate);
