@@ -482,8 +482,10 @@ int ec_decode_step_noalloc(const void *q_dev, const void *k_new_dev, const void 
  *
  * The struct is plain host data; the arrays are the caller's, on the device. Lengths live on the
  * device too, so that a captured step can be replayed. A negative length marks an empty place of a
- * padded batch: its outputs are zero and nothing of it is changed. Entries of the table that no row
- * reaches are not read.
+ * padded batch: its outputs are zero and nothing of it is changed. A sequence begins in a place with
+ * lens[n] = 0 and seen[n] = 0 (a count left in `seen` would give its rows later positions, and its first
+ * tokens no protection); its prompt joins by ec_paged_append with counts of 0 for the other places.
+ * Entries of the table that no row reaches are not read.
  *
  * A table entry outside [0, n_pages) or a length beyond max_pages * page_size is never followed:
  * the row counts as absent, and the status word at the head of `state` says EC_ERR_PAGE from then on

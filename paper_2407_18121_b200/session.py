@@ -156,7 +156,12 @@ class PagedCacheSession:
         s.decode(q, k_new, v_new, out)       # one token per problem: [N, Hq, D], [N, H, D], [N, H, D] -> [N, Hq, D]
 
     Every problem owns the pages of its `budget` rows. A problem whose entry of `lens` is negative is an empty place of
-    the batch: set it to 0 to begin a sequence there, to -1 to end one.
+    the batch. While the others run on:
+
+        s.end(n)                             # the sequence of place n is over: nothing of it is read or written any more
+        s.begin(n)                           # another one begins there, at position 0
+        s.append(K, V, scores, counts)       # its prompt: counts [N] is 0 for every other place (prompt() and fresh=True
+                                             # begin all of them anew)
     """
 
     def __init__(self, N: int, H: int, D: int, budget: int, recent: int, sinks: int, scale: float, Hq: Optional[int] = None,
@@ -178,6 +183,20 @@ class PagedCacheSession:
         self.state = torch.empty(ec.ec_paged_state_bytes(N), dtype=torch.uint8, device=dev)
         self.cache = ec.ec_paged_init(self.Kp, self.Vp, self.weight, self.pos, self.table, self.lens, self.seen, self.state)
         self.ws_step = torch.empty(ec.ec_paged_step_workspace(self.cache, self.Hq, self.budget), dtype=torch.uint8, device=dev)
+
+    def _place(self, t: torch.Tensor, n: int) -> torch.Tensor:
+        if not isinstance(n, int) or isinstance(n, bool) or not 0 <= n < self.N:
+            raise ValueError(f"a place is a whole number from 0 to {self.N - 1}, got {n!r}")
+        return t[n:n + 1]                        # filled by a kernel: an assignment would copy from the host
+
+    def begin(self, n: int) -> None:
+        """A sequence begins in place n, without rows and at position 0, whatever was there. In stream order; can be captured."""
+        self._place(self.lens, n).zero_()
+        self._place(self.seen, n).zero_()
+
+    def end(self, n: int) -> None:
+        """Place n is empty from here on. In stream order; can be captured."""
+        self._place(self.lens, n).fill_(-1)
 
     def _scratch(self, size: int) -> torch.Tensor:
         # from the current stream's allocator with every call: a captured prompt keeps its own
