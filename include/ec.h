@@ -553,7 +553,10 @@ int ec_paged_check(const ec_paged *c, const int32_t *table_host, const int32_t *
  *   decay                 0 < decay <= 1, read with accumulate
  * Limits: Hq a multiple of H, Hq / H <= 128, N*Hq < 2^24, and N*H*ceil(Hq/H/8) times
  * (max_pages*page_size/64 + 2) below 2^31. Workspace: ec_paged_attention_workspace
- * bytes (0 on invalid arguments); its contents need not survive between calls. The inputs must not
+ * bytes (0 on invalid arguments), with accumulate mostly an fp32 score per row and query head:
+ * n_pages*page_size*Hq*4 bytes (pages of fewer than 8 rows: N*max_pages*page_size*Hq*4), whatever the
+ * lengths are; its contents need not survive between calls. Groups of more than 16 query heads read
+ * the cached rows once per 16. The inputs must not
  * overlap the outputs. Deterministic.
  */
 size_t ec_paged_attention_workspace(const ec_paged *c, int Hq, int accumulate);

@@ -167,7 +167,7 @@ struct AppendArgs {
     int T, fresh, budget, recent, sinks;
     int4 *moves;                                 // workspace: [N * H] rows to move, and what the unit was
     int2 *list;                                  // workspace: [N * H][budget]: .x = slot to fill, .y = candidate to take
-    unsigned long long *lowest;                  // workspace: [N * H][kMaxSplits] lowest candidate of every part
+    unsigned long long *lowest;                  // workspace: [N * H][splits] first row to leave of every part
 };
 
 size_t paged_attention_workspace_bytes(const ec_paged *c, int Hq, int accumulate);

@@ -11,7 +11,7 @@
 //    shared-memory additions then queue up), narrowed to one bin after the other: two or three passes over keys held in
 //    shared memory. A list of 16384 costs one SM about 20 us of instructions; over a cluster the histograms are summed and
 //    the ordered counts carried on through distributed shared memory.
-// Measured per call: one row to 1024 full units of 320 rows 4.3 us; 64 rows onto 256 full units of 2048 14 us; prompts of 640 rows
+// Measured per call: one row to 1024 full units of 320 rows 4.6 us; 64 rows onto 256 full units of 2048 14.5 us; prompts of 640 rows
 // into 1024 units at budget 320 72 us (the move 57 us, 5.9 TB/s read and written); 16 units of up to 16384 rows 20 us.
 // Rows leave in this order: those that cannot be read, then by protection, then by weight (keys are order-preserving unsigned
 // images of the weights), and among equals the higher candidate first (cached rows in slot order, then the new rows). For a step that is
@@ -716,7 +716,7 @@ __global__ void __launch_bounds__(kRowThreads, kRowCtas) paged_rows_kernel(const
     }
     __syncthreads();
     // One row joins and at most one leaves: the new row goes behind the others or takes the place of the lowest.
-    auto place = [&](const Unit &v, unsigned long long lowest, int l) {   // by a warp: K on one half, V on the other
+    auto place = [&](const Unit &v, unsigned long long lowest, int l) {   // by a warp, of which the first lpr lanes copy
         if (v.cnt == 0) return;
         int dst = v.had;
         if (v.had + v.cnt > v.final) {
@@ -785,9 +785,11 @@ __global__ void __launch_bounds__(kRowThreads, kRowCtas) paged_rows_kernel(const
     }
 }
 
-// CTAs per unit of a rows launch: as many as fit the GPU at once (a second, partial wave measured 2% of a call of 512 units of
-// 8192 rows), but no more than two rounds of rows each, so that the longest of a ragged batch are not left to one CTA
-// (34 x 32 units of up to 3836 rows: 68 -> 56 us).
+// CTAs per unit of a rows launch, from the most rows that a unit can hold (the budget, or without an append what the table
+// reaches), as the lengths are on the device: as many as fit the GPU at once (a second, partial wave measured 2% of a call of 512
+// units of 8192 rows), but no more than two rounds of rows each, so that the longest of a ragged batch are not left to one CTA
+// (34 x 32 units of up to 3836 rows: 68 -> 56 us). Sequences far shorter than that pay for CTAs that find nothing to do (64 x 8
+// heads x 1000 rows with weights: 58 us under a table of 1024 or 8192 rows, 145 us under one of 131072).
 inline int row_splits(long long units, long long rows)
 {
     constexpr long long kRound = kRowThreads * kRowsHeld;

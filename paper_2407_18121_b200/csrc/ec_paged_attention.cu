@@ -19,8 +19,8 @@
 //  - The running maximum is raised only when a tile exceeds it by 2^8 (fp16: 2^4), so that most tiles need no reduction across lanes.
 //    It is kept, as the scores are, before the scale: the difference of two scores that are near each other is exact, while the
 //    scaled maximum, rounded, may lie 2^128 from its own row (scores of 2^31). Costs one addition per score, not seen in the time.
-// Measured per call, all launches, bf16, D = 128: 16 problems x 32 heads x 8192 rows 329 us (6.5 TB/s; 370 us with the weights),
-// one problem of 131071 rows, 8 heads for 64 query heads 90 us (6.0 TB/s), 32 problems of 0 .. 8192 rows 27.5 us (5.0 TB/s),
+// Measured per call, all launches, bf16, D = 128: 16 problems x 32 heads x 8192 rows 335 us (6.4 TB/s; 372 us with the weights),
+// one problem of 131071 rows, 8 heads for 64 query heads 91 us (5.9 TB/s), 32 problems of 0 .. 8192 rows 27.9 us (4.9 TB/s),
 // one problem of 37 rows 4.7 us. What is left at small sizes is a chain of dependent reads (length, page, row), the
 // merge of the warps and, for shared units, the arrival and the join: about 6 us beside the streaming.
 // Tried and dropped: bringing the weights up to date in this launch, by the CTA that completes a unit (a step of 1024 units
@@ -98,8 +98,8 @@ __device__ __forceinline__ void copy_piece(uint32_t dst, const uint4 *src, uint3
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
-// K and V pass through once: marked to leave the L2 first, so that scores and weights stay there between their launches
-// (a step of 8 problems x 8 heads of 4096 rows 38 -> 34 us; 32 x 32 x 640 with weights 64 -> 61 us).
+// K and V pass through once (once per 16 query heads of a group): marked to leave the L2 first, so that scores and weights stay
+// there between their launches (a step of 8 problems x 8 heads of 4096 rows 38 -> 34 us; 32 x 32 x 640 with weights 64 -> 61 us).
 __device__ __forceinline__ void stream_piece(uint32_t dst, const uint4 *src, uint64_t policy)
 {
     asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "l"(policy) : "memory");
