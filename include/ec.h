@@ -15,7 +15,7 @@
  * shared populations and eviction-only compaction, a native multi-step decode loop, the
  * retention-ratio policy, host-resident tensors, a decode step with built-in scratch), and a
  * paged cache with grouped query heads whose eviction goes by the attention weight that every
- * row has gathered (ec_paged_*).
+ * row has gathered (ec_paged_*), with chunks of several new tokens per problem on it and rotary positions (ec_rotary).
  *
  * Conventions shared by every call
  *  - Pointers named "dev" are CUDA device pointers of the current device; "host" pointers
@@ -601,6 +601,143 @@ size_t ec_paged_step_workspace(const ec_paged *c, int Hq, int budget);
 int ec_paged_decode_step(const void *q_dev, const void *k_new_dev, const void *v_new_dev, const ec_paged *c, int Hq,
                          float scale, float decay, int budget, int recent, int sinks, void *out_dev, float *lse_dev,
                          void *ws_dev, size_t ws_bytes, void *stream);
+
+/* ---------------------------------------------------------------- chunks of new tokens on a paged cache */
+
+/*
+ * Several new tokens of every problem at once: a piece of a prompt, a whole prompt, drafted tokens to be verified. The tokens
+ * of all problems are packed one after the other: problem n has counts[n] of them from starts[n] on (device arrays, so that a
+ * captured run can be replayed on other lengths). A step:
+ *
+ *   ec_paged_release          pages that no row needs any more go back to the pool
+ *   ec_paged_reserve          the chunk's rows get pages; every token learns its slot and its position; lens and seen grow
+ *   ec_paged_join             rotary positions on queries and keys, keys and values into the slots
+ *   ec_paged_chunk_attention  every token over the rows of its problem up to its own
+ *   ec_paged_chunk_weights    what the chunk's queries attended to is added to the rows' weights
+ *   ec_paged_append           with T = 0: every head keeps its `budget` rows of largest weight
+ *
+ * The newest counts[n] rows of problem n are the chunk's own, in order; all rows before them are seen by every token, in any
+ * order (eviction may have mixed them). Calls on one description are ordered by the caller as above, and so are calls on one pool
+ * of pages. Where the status word says EC_ERR_TIMEOUT, ec_paged_init has to clear the state before the next call.
+ */
+
+/* The pages that no problem holds, and how many every problem holds (its table's first held[n] entries). Plain host data; the
+ * arrays are the caller's, on the device. At the start: free_pages = the pool's page numbers in any order, *n_free = their
+ * number, held = 0. */
+typedef struct {
+    int32_t *free_pages; /* [n_pages], a stack: entries 0 .. *n_free - 1                              */
+    int32_t *n_free;     /* one                                                                      */
+    int32_t *held;       /* [N]                                                                      */
+} ec_pages;
+
+/*
+ * Pages go back: problem n keeps its first min(held[n], ceil(lens[n] / page_size)) pages, none at an empty place (lens[n] < 0). The
+ * others go on top of the stack, problem by problem in ascending order of their place in the table. Their table entries stay as they are
+ * and are not read any more. Deterministic. Pages must belong to one problem only.
+ */
+int ec_paged_release(const ec_paged *c, const ec_pages *p, void *stream);
+
+/*
+ * Pages are handed out for counts[n] new rows per problem, in order of the problems: the pages that problem n needs beyond held[n] come
+ * off the top of the stack. A problem is granted its rows whole or not at all: not when it is an empty place, its rows would not fit the
+ * table, its tokens end behind `tokens`, or the stack does not hold what this problem and those before it ask for (a problem that needs no page is
+ * not held up by that). Negative counts count as 0.
+ *   counts_dev      int32 [N]                                                                                 (in)
+ *   tokens          rows of the packed tensors: length of slots and positions
+ *   advance         != 0: the new rows join: lens[n] and seen[n] grow by what is granted, and slots and positions are
+ *                   written. 0: only pages are handed out (for rows that ec_paged_append or ec_paged_decode_step will add), and
+ *                   slots and positions have to be NULL
+ *   limit           read with advance = 0: pages for no more than max(limit, lens[n]) rows (a budget); 0: no limit
+ *   starts_dev      int32 [N + 1] first token of every problem = sum of the counts before it, granted or not, at most `tokens`;
+ *                   nullable                                                                                  (out)
+ *   granted_dev     int32 [N] counts[n] or 0                                                                  (out)
+ *   slots_dev       int32 [tokens] page * page_size + place in the page of every token's row; -1: not granted, or behind the
+ *                   last problem; nullable                                                                    (out)
+ *   positions_dev   int32 [tokens] seen[n] + t, -1 likewise; nullable                                         (out)
+ * Limits: N <= 65536. Deterministic. A count of the stack or of held pages out of range is cut, or the problem not granted, and the status word
+ * says EC_ERR_PAGE; so for a page number out of range, whose rows have no slot.
+ */
+int ec_paged_reserve(const ec_paged *c, const ec_pages *p, const int32_t *counts_dev, int tokens, int advance, int limit,
+                     int32_t *starts_dev, int32_t *granted_dev, int32_t *slots_dev, int32_t *positions_dev, void *stream);
+
+/* How frequencies are changed for contexts longer than those that a model was trained on. With f_i = base^(-2 i / rot):
+ *   EC_ROTARY_PLAIN     f_i
+ *   EC_ROTARY_LINEAR    f_i / stretch (positions brought closer together)
+ *   EC_ROTARY_BASE      with base * stretch^(rot / (rot - 2)) for base
+ *   EC_ROTARY_BY_PARTS  pairs that turn more than `fast` times over `trained` positions keep f_i, those that turn less than `slow`
+ *                       times get f_i / stretch, those between a mixture, linear in i; factor = 0.1 ln(stretch) + 1 */
+typedef enum { EC_ROTARY_PLAIN = 0, EC_ROTARY_LINEAR = 1, EC_ROTARY_BASE = 2, EC_ROTARY_BY_PARTS = 3 } ec_rotary_scaling;
+
+/* Fills freqs_host[0 .. rot / 2 - 1] (radians per position) and *factor_host for the calls below. Host arithmetic in double.
+ * base > 1, stretch >= 1, trained > 0, fast >= slow > 0 (the last three are read for EC_ROTARY_BY_PARTS). */
+int ec_rotary_frequencies(double *freqs_host, float *factor_host, int rot, double base, int scaling, double stretch, double trained,
+                          double fast, double slow);
+
+/*
+ * Rotary positions: pair i of every head turns by the angle positions * freqs[i], scaled by `factor`:
+ *   (a, b) -> factor * (a cos - b sin, a sin + b cos);   inverse != 0: the transposed map (a cos + b sin, b cos - a sin), which is
+ * its gradient. Pairs are elements (2 i, 2 i + 1) (interleaved != 0) or (i, i + rot / 2) of the first `rot`; the others are
+ * copied. fp32 arithmetic, one rounding of the result; angles are exact to 2^-24 of a half turn at any position (negative ones too).
+ *   x_dev, out_dev  elements of `dtype` [N, T, heads, D] by strides in elements, multiples of 8; rows are contiguous and do not overlap
+ *                   (head stride >= D); out may be x with the same strides, else they must not overlap
+ *   positions_dev   int32 [N, T], rows pos_n apart (0: one row of positions for all)
+ *   freqs_dev       fp64 [rot / 2] (NULL when rot = 0)
+ *   rot             0 .. D, a multiple of 16 (interleaved: of 8)
+ * Limits: N * T < 2^31.
+ */
+int ec_rotary(const void *x_dev, int64_t x_n, int64_t x_t, int64_t x_h, void *out_dev, int64_t out_n, int64_t out_t, int64_t out_h,
+              const int32_t *positions_dev, int64_t pos_n, const double *freqs_dev, int N, int T, int heads, int D, int dtype, int rot,
+              int interleaved, float factor, int inverse, void *stream);
+
+/*
+ * The chunk's rows join the pages: queries and keys are turned as ec_rotary does (rot = 0: as they are), keys and values are written
+ * to the slots that ec_paged_reserve gave out, with their weight and position. Tokens whose slot is negative are left out: their row
+ * of q_out stays as it is.
+ *   q_dev, q_out_dev  [tokens, Hq, D] by strides in elements, multiples of 8 (for views of a projection's output); both NULL with
+ *                     Hq = 0: keys and values alone. q_out may be q with the same strides                  (in, out)
+ *   k_dev, v_dev      [tokens, H, D] by strides                                                            (in)
+ *   w_new_dev         fp32 [tokens, H] weights of the rows; NULL: zero                                     (in)
+ *   slots_dev, positions_dev  int32 [tokens]; slots that are not negative differ from each other           (in)
+ * A slot behind the pool is left out and the status word says EC_ERR_PAGE. Inputs must not overlap the pool.
+ */
+int ec_paged_join(const void *q_dev, int64_t q_t, int64_t q_h, void *q_out_dev, int64_t qo_t, int64_t qo_h, const void *k_dev,
+                  int64_t k_t, int64_t k_h, const void *v_dev, int64_t v_t, int64_t v_h, const float *w_new_dev, const int32_t *slots_dev,
+                  const int32_t *positions_dev, const ec_paged *c, int Hq, int tokens, const double *freqs_dev, int rot,
+                  int interleaved, float factor, void *stream);
+
+/*
+ * Attention of the chunk: token t of problem n sees rows 0 .. lens[n] - counts[n] + t of its problem,
+ *   x[j] = scale * <q, k_j>,   out = sum_j softmax(x)_j v_j,   lse = log sum_j exp(x_j)
+ * for Hq query heads; query head i reads key / value head i / (Hq / H). Nothing of the cache changes.
+ *   q_dev, out_dev    [tokens, Hq, D] by strides in elements, multiples of 8                               (in, out)
+ *   starts_dev        int32 [N] (or more) first token of every problem                                     (in)
+ *   counts_dev        int32 [N] its tokens; 0: none. Rows of tokens that no problem has are left as they are (in)
+ *   out               fp32 accumulation; probabilities are rounded once to the element type before they meet V (fp16: rows that lie
+ *                     more than 2^-35 below the leading one count as nothing), the result once. Zero where a token sees nothing (an
+ *                     empty place, absent pages, all scores -inf)
+ *   lse_dev           fp32 [tokens, Hq]; -inf where a token sees nothing; nullable                         (out)
+ * What a token does not see has no effect on it, values that are not finite included; an infinity in a value row that it does see comes
+ * out as NaN or as an infinity. A problem whose tokens lie outside 0 .. tokens is left out, and the status word says EC_ERR_PAGE.
+ * Limits: Hq / H <= 128, tokens * Hq < 2^31. Workspace: ec_paged_chunk_workspace bytes, which need not survive
+ * between calls; calls that may run at once need one each. q must not overlap out. Deterministic.
+ */
+size_t ec_paged_chunk_workspace(const ec_paged *c, int Hq);
+int ec_paged_chunk_attention(const void *q_dev, int64_t q_t, int64_t q_h, const int32_t *starts_dev, const int32_t *counts_dev,
+                             const ec_paged *c, int Hq, int tokens, float scale, void *out_dev, int64_t out_t, int64_t out_h,
+                             float *lse_dev, void *ws_dev, size_t ws_bytes, void *stream);
+
+/*
+ * The weights that the chunk leaves behind, from its normaliser: with p[t, g, j] = exp(scale * <q, k_j> - lse[t, g]) for the rows that
+ * token t sees, every row of a problem with counts[n] > 0 gets
+ *   weight_j <- decay^count * weight_j + sum_t decay^(count - 1 - t) * sum_g p[t, g, j]
+ * over the group's query heads: what counts[n] calls of ec_paged_attention for one token each would have left.
+ *   lse_dev           fp32 [tokens, Hq] as ec_paged_chunk_attention gives it, same q, scale and cache; -inf: the row takes no part (in)
+ * Other arguments, limits and workspace as there; 0 < decay <= 1, in double: its powers over a long chunk would show a rounding. NaN in q, lse or a key that is seen leaves the weights of the rows that
+ * meet it undefined. Deterministic.
+ */
+int ec_paged_chunk_weights(const void *q_dev, int64_t q_t, int64_t q_h, const float *lse_dev, const int32_t *starts_dev,
+                           const int32_t *counts_dev, const ec_paged *c, int Hq, int tokens, float scale, double decay, void *ws_dev,
+                           size_t ws_bytes, void *stream);
 
 #ifdef __cplusplus
 }

@@ -22,6 +22,7 @@ EC_BF16, EC_FP16 = 0, 1
 EC_PER_HEAD = 0
 EC_STAT_SUM, EC_STAT_MEAN, EC_STAT_MAX, EC_STAT_MOVING_AVERAGE = 0, 1, 2, 3
 EC_LAYER_SHARED = 1
+EC_ROTARY_PLAIN, EC_ROTARY_LINEAR, EC_ROTARY_BASE, EC_ROTARY_BY_PARTS = 0, 1, 2, 3
 
 EXPORTS = (
     "ec_status_string", "ec_keep_count",
@@ -32,6 +33,8 @@ EXPORTS = (
     "ec_probe_read_stream", "ec_probe_mixed_stream", "ec_decode_splits",
     "ec_paged_state_bytes", "ec_paged_init", "ec_paged_check", "ec_paged_attention_workspace", "ec_paged_attention",
     "ec_paged_append_workspace", "ec_paged_append", "ec_paged_step_workspace", "ec_paged_decode_step",
+    "ec_paged_release", "ec_paged_reserve", "ec_rotary_frequencies", "ec_rotary", "ec_paged_join",
+    "ec_paged_chunk_workspace", "ec_paged_chunk_attention", "ec_paged_chunk_weights",
 )
 
 
@@ -59,6 +62,11 @@ class ec_paged(C.Structure):
                 ("N", C.c_int), ("H", C.c_int), ("D", C.c_int),
                 ("page_size", C.c_int), ("n_pages", C.c_int), ("max_pages", C.c_int), ("dtype", C.c_int),
                 ("page_stride", C.c_int64), ("head_stride", C.c_int64), ("row_stride", C.c_int64)]
+
+
+class _ec_pages(C.Structure):
+    """Mirror of the C struct ec_pages (host-side plain data; the arrays are device tensors)."""
+    _fields_ = [("free_pages", C.c_void_p), ("n_free", C.c_void_p), ("held", C.c_void_p)]
 
 
 _lib = None
@@ -150,6 +158,23 @@ def lib() -> C.CDLL:
     L.ec_paged_step_workspace.argtypes = [pc, i, i]
     L.ec_paged_decode_step.restype = i
     L.ec_paged_decode_step.argtypes = [vp, vp, vp, pc, i, f, f, i, i, i, vp, vp, vp, sz, vp]
+    pp, d = C.POINTER(_ec_pages), C.c_double
+    L.ec_paged_release.restype = i
+    L.ec_paged_release.argtypes = [pc, pp, vp]
+    L.ec_paged_reserve.restype = i
+    L.ec_paged_reserve.argtypes = [pc, pp, vp, i, i, i, vp, vp, vp, vp, vp]
+    L.ec_rotary_frequencies.restype = i
+    L.ec_rotary_frequencies.argtypes = [vp, C.POINTER(f), i, d, i, d, d, d, d]
+    L.ec_rotary.restype = i
+    L.ec_rotary.argtypes = [vp, i64, i64, i64, vp, i64, i64, i64, vp, i64, vp, i, i, i, i, i, i, i, f, i, vp]
+    L.ec_paged_join.restype = i
+    L.ec_paged_join.argtypes = [vp, i64, i64, vp, i64, i64, vp, i64, i64, vp, i64, i64, vp, vp, vp, pc, i, i, vp, i, i, f, vp]
+    L.ec_paged_chunk_workspace.restype = sz
+    L.ec_paged_chunk_workspace.argtypes = [pc, i]
+    L.ec_paged_chunk_attention.restype = i
+    L.ec_paged_chunk_attention.argtypes = [vp, i64, i64, vp, vp, pc, i, i, f, vp, i64, i64, vp, vp, sz, vp]
+    L.ec_paged_chunk_weights.restype = i
+    L.ec_paged_chunk_weights.argtypes = [vp, i64, i64, vp, vp, vp, pc, i, i, f, d, vp, sz, vp]
     _lib = L
     return L
 
@@ -560,3 +585,143 @@ def ec_paged_decode_step(q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tens
                                     _want(lse, "lse", torch.float32, (N, Hq), dev), _scratch(ws, dev),
                                     ws.nbytes, _paged_stream(dev))
     _check(st, "ec_paged_decode_step")
+
+
+# ---- chunks of new tokens on a paged cache -------------------------------------------------
+
+class ec_pages:
+    """The pages of a pool that no problem holds: free_pages int32 [n_pages] (a stack of n_free[0] entries), n_free int32 [1],
+    held int32 [N], how many every problem holds. At the start free_pages holds all page numbers and held is zero."""
+
+    def __init__(self, free_pages: torch.Tensor, n_free: torch.Tensor, held: torch.Tensor):
+        self.free_pages, self.n_free, self.held = free_pages, n_free, held
+        self._for = None
+
+    def _c(self, cache: ec_paged) -> _ec_pages:
+        if self._for is None or self._for[0] is not cache:
+            dev = cache._dims[4]
+            i32 = torch.int32
+            self._for = (cache, _ec_pages(_want(self.free_pages, "free_pages", i32, (cache.n_pages,), dev),
+                                          _want(self.n_free, "n_free", i32, (1,), dev), _want(self.held, "held", i32, (cache.N,), dev)))
+        return self._for[1]
+
+
+def ec_paged_release(cache: ec_paged, pages: ec_pages) -> None:
+    """Pages behind the last row of every problem, and all pages of empty places, go back to the pool."""
+    _check(lib().ec_paged_release(C.byref(cache), C.byref(pages._c(cache)), _paged_stream(cache._dims[4])), "ec_paged_release")
+
+
+def ec_paged_reserve(cache: ec_paged, pages: ec_pages, counts: torch.Tensor, starts: Optional[torch.Tensor], granted: torch.Tensor,
+                     slots: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None, advance: bool = True,
+                     limit: int = 0) -> None:
+    """Pages for counts int32 [N] new rows per problem. starts (out) int32 [N + 1], granted (out) int32 [N], slots and positions (out)
+    int32 [tokens], one each for the packed tokens. advance: the rows join (lens and seen grow); else only pages are handed out, for
+    `limit` rows per problem at most (0: no limit), and slots and positions are None."""
+    N, dev, i32 = cache._dims[0], cache._dims[4], torch.int32
+    given = slots if slots is not None else positions
+    tokens = 0 if given is None else given.shape[0]
+    st = lib().ec_paged_reserve(C.byref(cache), C.byref(pages._c(cache)), _want(counts, "counts", i32, (N,), dev), tokens, int(bool(advance)),
+                                int(limit), _want(starts, "starts", i32, (N + 1,), dev), _want(granted, "granted", i32, (N,), dev),
+                                _want(slots, "slots", i32, (tokens,), dev), _want(positions, "positions", i32, (tokens,), dev),
+                                _paged_stream(dev))
+    _check(st, "ec_paged_reserve")
+
+
+def ec_rotary_frequencies(rot: int, base: float = 10000.0, scaling: int = EC_ROTARY_PLAIN, stretch: float = 1.0, trained: float = 0.0,
+                          fast: float = 32.0, slow: float = 1.0):
+    """(freqs, factor): host fp64 tensor [rot / 2] of radians per position, and what the turned elements are multiplied with."""
+    freqs, factor = torch.empty(max(int(rot) // 2, 1), dtype=torch.float64), C.c_float()
+    _check(lib().ec_rotary_frequencies(freqs.data_ptr(), C.byref(factor), int(rot), base, int(scaling), stretch, trained, fast, slow),
+           "ec_rotary_frequencies")
+    return freqs, factor.value
+
+
+def _rows(t: torch.Tensor, name: str, dtype: torch.dtype, shape: tuple, device: int):
+    """Pointer and strides (all but the last) of rows that are contiguous along D; a stride along an axis of extent 1 is never used,
+    a dense one stands in for it."""
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != device or t.stride(-1) != 1:
+        raise ValueError(f"{name} must be a {dtype} tensor {list(shape)} with contiguous rows on device {device}, "
+                         f"got {t.dtype} {list(t.shape)}, strides {list(t.stride())}, on {t.device}")
+    strides, dense = [], shape[-1]
+    for extent, stride in zip(reversed(shape[:-1]), reversed(t.stride()[:-1])):
+        strides.append(stride if extent > 1 else dense)
+        dense = max(dense, strides[-1]) * max(extent, 1)
+    return (t.data_ptr(), *reversed(strides))
+
+
+def ec_rotary(x: torch.Tensor, out: torch.Tensor, positions: torch.Tensor, freqs: Optional[torch.Tensor], rot: int, interleaved: bool,
+              factor: float = 1.0, inverse: bool = False) -> None:
+    """Rotary positions on x, out (out, may be x): bf16 or fp16 [N, T, heads, D], any strides with D contiguous. positions int32
+    [N, T] or [T] (the same for all N); freqs fp64 [rot / 2]. inverse: the transposed map, which is the gradient."""
+    if x.dim() != 4 or x.dtype not in _ELEM:
+        raise ValueError("x must be bf16 or fp16 [N, T, heads, D]")
+    N, T, heads, D = x.shape
+    dev = x.get_device()
+    if dev < 0:
+        raise ValueError("x must lie on a CUDA device")
+    stream = _paged_stream(dev)
+    px = _rows(x, "x", x.dtype, tuple(x.shape), dev)
+    po = _rows(out, "out", x.dtype, tuple(x.shape), dev)
+    if positions.dtype is not torch.int32 or positions.get_device() != dev or positions.shape not in ((N, T), (T,)) or \
+            (T > 1 and positions.stride(-1) != 1):
+        raise ValueError("positions must be int32 [N, T] or [T] on x's device")
+    pos_n = positions.stride(0) if positions.dim() == 2 and N > 1 else 0
+    st = lib().ec_rotary(*px, *po, positions.data_ptr(), pos_n, _want(freqs, "freqs", torch.float64, (int(rot) // 2,), dev), N, T, heads, D,
+                         _ELEM[x.dtype], int(rot), int(bool(interleaved)), factor, int(bool(inverse)), stream)
+    _check(st, "ec_rotary")
+
+
+def ec_paged_join(q: Optional[torch.Tensor], q_out: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor,
+                  w_new: Optional[torch.Tensor], slots: torch.Tensor, positions: torch.Tensor, cache: ec_paged,
+                  freqs: Optional[torch.Tensor], rot: int, interleaved: bool, factor: float = 1.0) -> None:
+    """The chunk's rows join the pages: q [tokens, Hq, D] is turned into q_out (both None: keys and values alone), k and v
+    [tokens, H, D], any strides with D contiguous, go to slots int32 [tokens] (negative: left out) with positions int32 [tokens] and
+    weights w_new fp32 [tokens, H] (None: zero). rot = 0 turns nothing."""
+    N, H, D, dt, dev = cache._dims
+    tokens = k.shape[0]
+    Hq = 0 if q is None else q.shape[1]
+    none = (None, 0, 0)
+    pq = none if q is None else _rows(q, "q", dt, (tokens, Hq, D), dev)
+    po = none if q_out is None else _rows(q_out, "q_out", dt, (tokens, Hq, D), dev)
+    st = lib().ec_paged_join(*pq, *po, *_rows(k, "k", dt, (tokens, H, D), dev), *_rows(v, "v", dt, (tokens, H, D), dev),
+                             _want(w_new, "w_new", torch.float32, (tokens, H), dev), _want(slots, "slots", torch.int32, (tokens,), dev),
+                             _want(positions, "positions", torch.int32, (tokens,), dev), C.byref(cache), Hq, tokens,
+                             _want(freqs, "freqs", torch.float64, (int(rot) // 2,), dev), int(rot), int(bool(interleaved)), factor,
+                             _paged_stream(dev))
+    _check(st, "ec_paged_join")
+
+
+def ec_paged_chunk_workspace(cache: ec_paged, Hq: int) -> int:
+    return int(lib().ec_paged_chunk_workspace(C.byref(cache), int(Hq)))
+
+
+def _first(starts: torch.Tensor, N: int, device: int) -> int:
+    if starts.shape not in ((N,), (N + 1,)):
+        raise ValueError(f"starts must be int32 [{N}] or [{N + 1}], got {list(starts.shape)}")
+    return _want(starts, "starts", torch.int32, tuple(starts.shape), device)
+
+
+def ec_paged_chunk_attention(q: torch.Tensor, starts: torch.Tensor, counts: torch.Tensor, cache: ec_paged, scale: float,
+                             out: torch.Tensor, lse: Optional[torch.Tensor], ws: torch.Tensor) -> None:
+    """Attention of packed tokens: token t of problem n, the packed token starts[n] + t, sees the rows 0 .. lens[n] - counts[n] + t of its
+    problem. q, out (out): [tokens, Hq, D], any strides with D contiguous; starts int32 [N] or [N + 1], counts int32 [N]; lse (out,
+    optional) fp32 [tokens, Hq]."""
+    N, H, D, dt, dev = cache._dims
+    tokens, Hq = q.shape[0], q.shape[1]
+    st = lib().ec_paged_chunk_attention(*_rows(q, "q", dt, (tokens, Hq, D), dev), _first(starts, N, dev),
+                                        _want(counts, "counts", torch.int32, (N,), dev), C.byref(cache), Hq, tokens, scale,
+                                        *_rows(out, "out", dt, (tokens, Hq, D), dev), _want(lse, "lse", torch.float32, (tokens, Hq), dev),
+                                        _scratch(ws, dev), ws.nbytes, _paged_stream(dev))
+    _check(st, "ec_paged_chunk_attention")
+
+
+def ec_paged_chunk_weights(q: torch.Tensor, lse: torch.Tensor, starts: torch.Tensor, counts: torch.Tensor, cache: ec_paged, scale: float,
+                           decay: float, ws: torch.Tensor) -> None:
+    """What the chunk's queries attended to joins the rows' weights: weight <- decay^count weight + sum_t decay^(count-1-t) sum_g p. lse fp32
+    [tokens, Hq] is ec_paged_chunk_attention's; the other arguments as there."""
+    N, H, D, dt, dev = cache._dims
+    tokens, Hq = q.shape[0], q.shape[1]
+    st = lib().ec_paged_chunk_weights(*_rows(q, "q", dt, (tokens, Hq, D), dev), _want(lse, "lse", torch.float32, (tokens, Hq), dev),
+                                      _first(starts, N, dev), _want(counts, "counts", torch.int32, (N,), dev), C.byref(cache), Hq, tokens,
+                                      scale, decay, _scratch(ws, dev), ws.nbytes, _paged_stream(dev))
+    _check(st, "ec_paged_chunk_weights")

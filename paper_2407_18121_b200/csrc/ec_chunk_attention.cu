@@ -1,0 +1,801 @@
+// Attention of a chunk of new tokens over a paged cache (grouped query heads, ragged batch), with each row's normaliser.
+//   token t of problem n sees rows j <= lens[n] - counts[n] + t:
+//   x[j] = scale * <q, k_j>,   out = sum_j softmax(x)_j v_j,   lse = log sum_j exp(x_j)
+#include "ec_chunk.cuh"
+
+namespace ec {
+
+namespace {
+
+constexpr int kThreads = 384;                    // warps: copies, products, value check, (none), 4 + 4 softmax
+constexpr int kItems = 4;                        // descriptions of work ahead
+constexpr int kInfos = 8;                        // absent rows of the tiles in flight (the rings hold 4 at most)
+constexpr int kTmemCols = 512;                   // S of both teams (2 x 128 columns), O of both teams (2 x up to 128)
+constexpr int kUnitRows = 256;                   // cost of a unit beside its rows
+constexpr int kLeastRows = 768;                  // smallest share of a CTA
+
+template <int DTYPE> struct Elem;
+template <> struct Elem<EC_BF16> {
+    static constexpr uint32_t kFormat = 1;       // of an operand in the instruction descriptor
+    static constexpr float kRaise = 8.f, kTop = 0.f;
+    static constexpr uint32_t kExponent = 0x7F807F80u;
+    static __device__ __forceinline__ uint32_t pack(float a, float b) { return pack2(a, b); }
+};
+// fp16 has few exponents: P is counted from 2^11 at the running maximum, which leaves the 2^4 that it may rise under the type's
+// largest number and takes in rows down to 2^-35 of the maximum's, with all bits down to 2^-25.
+template <> struct Elem<EC_FP16> {
+    static constexpr uint32_t kFormat = 0;
+    static constexpr float kRaise = 4.f, kTop = 11.f;
+    static constexpr uint32_t kExponent = 0x7C007C00u;
+    static __device__ __forceinline__ uint32_t pack(float a, float b)
+    {
+        __half2 h = __floats2half2_rn(a, b);
+        return *reinterpret_cast<uint32_t *>(&h);
+    }
+};
+
+struct PairUnits {                               // a unit: two adjacent query tiles of a head
+    static __device__ __forceinline__ int units(const ChunkArgs &a, const Problem &p) { return (p.count + 2 * a.tile_tokens - 1) / (2 * a.tile_tokens); }
+    static __device__ __forceinline__ long long before(const ChunkArgs &a, const Problem &p, int i)
+    {
+        const long long base = max(p.len - p.count, 0), step = 2 * a.tile_tokens;
+        const int full = units(a, p) - 1;
+        const long long k = i <= full ? i : full;
+        long long cost = k * (base + kUnitRows) + step * (k * (k + 1) / 2);
+        if (i > full) cost += base + p.count + kUnitRows;
+        return cost;
+    }
+};
+
+struct Item {
+    int n, h;                                    // n < 0: no work left
+    int token, ntok;                             // first token of the pair (packed), tokens
+    int limit;                                   // last row that the first token sees (may be negative)
+    int rows;                                    // rows that the pair sees at all
+    int kt0, kt1;                                // its tiles in this CTA
+    int parts, first, slot;                      // parts > 0: the unit is shared by CTAs first .. first + parts - 1
+    int pad;
+};
+
+struct Parts {                                   // workspace
+    float4 *o;                                   // [2 CTAs][2 teams][D / 4][128]
+    float2 *ml;                                  // [2 CTAs][2 teams][128] running maximum (not scaled), sum
+};
+
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+                 "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+                 "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+                 ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+                   "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
+                   "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
+                   "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+                 : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+                 "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+                 ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+                   "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+                 : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// MN-major operand with the 128-byte swizzle: 64 elements of the MN dimension per 128-byte row, 8 steps of the contraction
+// index per 1024 bytes; `lbo` bytes to the next 64 elements of the MN dimension, `sbo` to the next 8 steps.
+__device__ __forceinline__ uint64_t umma_desc_mn(uint32_t smem_addr, uint32_t lbo, uint32_t sbo)
+{
+    return (uint64_t)((smem_addr & 0x3FFFFu) >> 4) | ((uint64_t)(lbo >> 4) << 16) | ((uint64_t)(sbo >> 4) << 32) |
+           (1ull << 46) | (2ull << 61);
+}
+
+// D = A * B, A (two elements of the contraction index per 32-bit column) from TMEM, B from shared memory; M = 128, K = 16.
+__device__ __forceinline__ void umma_ts(uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile("{\n\t.reg .pred p;\n\t"
+                 "setp.ne.b32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+                 ::"r"(tmem_d), "r"(tmem_a), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
+}
+
+// NaN wins: a score that is not a number makes its row not a number, wherever it stands.
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float d;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+
+template <int D>
+struct Smem {
+    static constexpr int kTile = kTileRows * D * 2;
+    static constexpr int kKs = D == 128 ? 2 : 4, kVs = D == 128 ? 3 : 4;   // rings of tiles; V stays until its product is done
+    static constexpr int kQ = 0;                                          // both query tiles
+    static constexpr int kK = 2 * kTile;
+    static constexpr int kV = kK + kKs * kTile;
+    static constexpr int kOther = kV + kVs * kTile;                       // [128] maximum and sum of the second team
+    static constexpr int kBad = kOther + kTileRows * 8;                   // [items][D] 16 bits, see the value check
+    static constexpr int kBadAny = kBad + kItems * D * 2;                 // [items]
+    static constexpr int kItem = kBadAny + kItems * 4;
+    static constexpr int kInfo = kItem + kItems * (int)sizeof(Item);
+    static constexpr int kBars = kInfo + kInfos * 16;
+    // q_full, q_empty, k_full[], k_empty[], v_full[], v_empty[], v_ready[], per team: s_full, p_half[2], pv_done, o_free, rdv; other_done; item_full, item_empty
+    static constexpr int kNumBars = 2 + 2 * kKs + 3 * kVs + 2 * 6 + 1 + 2 * kItems;
+    static constexpr int kTmemSlot = kBars + kNumBars * 8;
+    static constexpr int kAbort = kTmemSlot + 4;
+    static constexpr int kLast = kAbort + 4;                              // [2] whether this CTA joins the unit's parts
+    static constexpr int kTotal = kLast + 8;
+    static_assert(kTotal <= 232448, "shared memory of a block");
+};
+
+template <int D, int DTYPE>
+__global__ void __launch_bounds__(kThreads, 1)
+chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                       const __grid_constant__ CUtensorMap map_v, const ChunkArgs a, uint16_t *__restrict__ out, int64_t out_token,
+                       int64_t out_head, float *__restrict__ lse, const Parts parts)
+{
+    using L = Smem<D>;
+    using E = Elem<DTYPE>;
+    constexpr int kTile = L::kTile, kKs = L::kKs, kVs = L::kVs;
+    constexpr int kBoxBytes = kTileRows * 128;
+    constexpr uint32_t kIdescS = (1u << 4) | (E::kFormat << 7) | (E::kFormat << 10) | ((kTileRows >> 3) << 17) | ((kTileRows >> 4) << 24);
+    constexpr uint32_t kIdescO = (1u << 4) | (E::kFormat << 7) | (E::kFormat << 10) | (1u << 16) | ((D >> 3) << 17) | ((kTileRows >> 4) << 24);
+
+    extern __shared__ __align__(1024) uint8_t smem[];
+    const uint32_t base = smem_u32(smem);
+    auto bar = [&](int i) { return base + (uint32_t)L::kBars + 8u * (uint32_t)i; };
+    const uint32_t q_full = bar(0), q_empty = bar(1);
+    auto k_full = [&](uint32_t s) { return bar(2 + s); };
+    auto k_empty = [&](uint32_t s) { return bar(2 + kKs + s); };
+    auto v_full = [&](uint32_t s) { return bar(2 + 2 * kKs + s); };
+    auto v_empty = [&](uint32_t s) { return bar(2 + 2 * kKs + kVs + s); };
+    auto v_ready = [&](uint32_t s) { return bar(2 + 2 * kKs + 2 * kVs + s); };
+    constexpr int kT0 = 2 + 2 * kKs + 3 * kVs;
+    auto s_full = [&](uint32_t x) { return bar(kT0 + 6 * x); };
+    auto p_half = [&](uint32_t x, uint32_t k) { return bar(kT0 + 6 * x + 1 + k); };
+    auto pv_done = [&](uint32_t x) { return bar(kT0 + 6 * x + 3); };
+    auto o_free = [&](uint32_t x) { return bar(kT0 + 6 * x + 4); };
+    auto rdv = [&](uint32_t x) { return bar(kT0 + 6 * x + 5); };
+    const uint32_t other_done = bar(kT0 + 12);
+    auto item_full = [&](uint32_t k) { return bar(kT0 + 13 + k); };
+    auto item_empty = [&](uint32_t k) { return bar(kT0 + 13 + kItems + k); };
+    Item *items = reinterpret_cast<Item *>(smem + L::kItem);
+    uint4 *infos = reinterpret_cast<uint4 *>(smem + L::kInfo);
+    float2 *other_s = reinterpret_cast<float2 *>(smem + L::kOther);
+    uint32_t *bad = reinterpret_cast<uint32_t *>(smem + L::kBad);
+    volatile int *bad_any = reinterpret_cast<volatile int *>(smem + L::kBadAny);
+    volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(smem + L::kTmemSlot);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + L::kAbort);
+    volatile int *last_s = reinterpret_cast<volatile int *>(smem + L::kLast);
+    int *status = a.c.state;
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        *abort_flag = 0;
+        mbar_init(q_full, 1);
+        mbar_init(q_empty, 1);
+        for (uint32_t s = 0; s < (uint32_t)kKs; ++s) { mbar_init(k_full(s), 1); mbar_init(k_empty(s), 1); }
+        for (uint32_t s = 0; s < (uint32_t)kVs; ++s) { mbar_init(v_full(s), 1); mbar_init(v_empty(s), 1); mbar_init(v_ready(s), 1); }
+        for (uint32_t x = 0; x < 2; ++x) {
+            mbar_init(s_full(x), 1);
+            mbar_init(p_half(x, 0), 4);
+            mbar_init(p_half(x, 1), 4);
+            mbar_init(pv_done(x), 1);
+            mbar_init(o_free(x), 4);
+            mbar_init(rdv(x), 4);
+        }
+        mbar_init(other_done, 4);
+        for (uint32_t k = 0; k < (uint32_t)kItems; ++k) {
+            mbar_init(item_full(k), 1);
+            mbar_init(item_empty(k), 1 + 1 + 8);                         // the products' thread, the value check, the softmax warps
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        fence_to_async();
+    }
+    if (threadIdx.x == 32) {
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_q) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_k) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_v) : "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
+                     ::"r"(base + (uint32_t)L::kTmemSlot), "r"((uint32_t)kTmemCols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    auto tmem_s = [&](uint32_t x) { return tmem + x * (uint32_t)kTileRows; };                 // S, and P over its first half
+    auto tmem_o = [&](uint32_t x) { return tmem + 2u * kTileRows + x * (uint32_t)kTileRows; };
+    grid_wait();
+    grid_release();
+
+    // A unit of two query tiles: a team per tile, every tile of rows serves both. A unit of one: both teams work on it and
+    // take its tiles of rows in turn; the first team puts the two results together.
+    auto is_pair = [&](const Item &it) { return it.ntok > a.tile_tokens; };
+    // Tiles of rows that the first team's tokens of a pair see (the second team's see all of the item's).
+    auto tiles_of_first = [&](const Item &it) {
+        const int sees = min(it.rows, it.limit + a.tile_tokens);
+        return max(min(it.kt1, (max(sees, 0) + kTileRows - 1) / kTileRows) - it.kt0, 0);
+    };
+    bool alive = true;
+
+    if (warp == 0) {
+        // ------------------------------------------------------------ plan and copies
+        Walk<PairUnits> w;
+        bool more = w.begin(a, kLeastRows);
+        uint32_t tg = 0, nk = 0, nv = 0, nq = 0;           // tiles; copies of K, V and queries started
+        for (uint32_t k = 0; alive; ++k) {
+            const uint32_t sl = k % kItems;
+            if (!mbar_wait(item_empty(sl), ((k / kItems) & 1u) ^ 1u, abort_flag, status, kWaitLimitNs, kPollBackoffNs)) { alive = false; break; }
+            Item it = {};
+            it.n = -1;
+            long long cost = 0;
+            if (more) {
+                const int step = 2 * a.tile_tokens;
+                it.n = w.n;
+                it.h = w.h;
+                it.token = w.p.start + w.i * step;
+                it.ntok = min(step, w.p.count - w.i * step);
+                it.limit = w.p.len - w.p.count + w.i * step;
+                it.rows = max(0, min(w.p.len, it.limit + it.ntok));
+                const int tiles = (it.rows + kTileRows - 1) / kTileRows;
+                cost = PairUnits::before(a, w.p, w.i + 1) - PairUnits::before(a, w.p, w.i);
+                const long long from = max(w.s.first - w.at, 0ll), to = min(w.s.last - w.at, cost);
+                auto tile_at = [&](long long x) { return (int)min(max((x - kUnitRows) / kTileRows, 0ll), (long long)tiles); };
+                it.kt0 = from == 0 ? 0 : tile_at(from);
+                it.kt1 = to >= cost ? tiles : tile_at(to);
+                if (from > 0 || to < cost) {
+                    it.first = (int)(w.at / w.s.per);
+                    it.parts = (int)((w.at + cost - 1) / w.s.per) - it.first + 1;
+                    it.slot = 2 * (int)blockIdx.x + (from == 0);
+                }
+            }
+            if (lane == 0) items[sl] = it;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(item_full(sl));
+            if (!more) break;
+            TilePages next = tile_pages(a, it.n, it.kt0 * kTileRows, it.kt0 < it.kt1 ? it.rows : 0);
+            for (int t = it.kt0; t < it.kt1 && alive; ++t, ++tg) {
+                TilePages now = next;
+                const int row0 = t * kTileRows;
+                const uint32_t bytes = (uint32_t)check_pages(a, now) * (uint32_t)a.box_rows * D * 2u;
+                const uint4 absent = absent_rows(a, now);
+                const uint32_t ks = tg % kKs, vs = tg % kVs;
+                if (!mbar_wait(k_empty(ks), ((tg / kKs) & 1u) ^ 1u, abort_flag, status, kWaitLimitNs, kPollBackoffNs)) { alive = false; break; }
+                if (lane == 0) {
+                    infos[tg % kInfos] = absent;
+                    mbar_expect_tx(k_full(ks), bytes);
+                }
+                __syncwarp();
+                copy_boxes<D>(a, &map_k, now, it.h, row0, base + L::kK + ks * kTile, k_full(ks));
+                ++nk;
+                if (t == it.kt0) {
+                    if (!mbar_wait(q_empty, (nq & 1u) ^ 1u, abort_flag, status, kWaitLimitNs, kPollBackoffNs)) { alive = false; break; }
+                    if (lane == 0) {
+                        const int tiles = it.ntok > a.tile_tokens ? 2 : 1;
+                        mbar_expect_tx(q_full, (uint32_t)(tiles * a.tile_tokens * a.G * D * 2));
+                        for (int x = 0; x < tiles; ++x)
+#pragma unroll
+                            for (int half = 0; half < D / 64; ++half)
+                                tma_load_3d(base + L::kQ + x * kTile + half * kBoxBytes, &map_q, half * 64, it.h * a.G,
+                                            it.token + x * a.tile_tokens, q_full);
+                    }
+                    ++nq;
+                }
+                next = tile_pages(a, it.n, row0 + kTileRows, t + 1 < it.kt1 ? it.rows : 0);
+                if (!mbar_wait(v_empty(vs), ((tg / kVs) & 1u) ^ 1u, abort_flag, status, kWaitLimitNs, kPollBackoffNs)) { alive = false; break; }
+                if (lane == 0) mbar_expect_tx(v_full(vs), bytes);
+                __syncwarp();
+                copy_boxes<D>(a, &map_v, now, it.h, row0, base + L::kV + vs * kTile, v_full(vs));
+                ++nv;
+            }
+            if (!alive) break;
+            more = w.next(a, cost);
+        }
+        if (*abort_flag) {
+            // let copies that are still in flight land before the CTA gives its memory back
+            if (nq > 0) mbar_wait(q_full, (nq - 1u) & 1u, abort_flag, status, 200000ull);
+            for (uint32_t t = nk > (uint32_t)kKs ? nk - kKs : 0; t < nk; ++t)
+                mbar_wait(k_full(t % kKs), (t / kKs) & 1u, abort_flag, status, 200000ull);
+            for (uint32_t t = nv > (uint32_t)kVs ? nv - kVs : 0; t < nv; ++t)
+                mbar_wait(v_full(t % kVs), (t / kVs) & 1u, abort_flag, status, 200000ull);
+        }
+    } else if (warp == 1) {
+        // ------------------------------------------------------------ products
+        if (lane == 0) {
+            uint32_t tg = 0, nq = 0, np0 = 0, np1 = 0, ni0 = 0, ni1 = 0;          // per team: tiles and items with tiles so far
+            auto wait = [&](uint32_t b, uint32_t phase) {
+                if (!mbar_wait(b, phase & 1u, abort_flag, status, kWaitLimitNs, kPollBackoffNs)) alive = false;
+                return alive;
+            };
+            // S of team x: query tile `qt` and the rows in stage ks
+            auto issue_s = [&](uint32_t x, uint32_t qt, uint32_t ks) {
+                const uint64_t da = umma_desc(base + L::kQ + qt * kTile), db = umma_desc(base + L::kK + ks * kTile);
+#pragma unroll
+                for (int kk = 0; kk < D / 16; ++kk) {
+                    const uint32_t off = ((uint32_t)(kk / 4) * kBoxBytes + (uint32_t)(kk % 4) * 32u) >> 4;
+                    umma_bf16(tmem_s(x), da + off, db + off, kIdescS, kk > 0 ? 1u : 0u);
+                }
+                umma_commit(s_full(x));
+            };
+            // O += P V of team x: 16 rows an instruction, 8 columns of P; its halves follow the softmax's
+            auto issue_pv = [&](uint32_t x, uint32_t &np, uint32_t vs, int steps, bool first) {
+                const uint64_t dv = umma_desc_mn(base + L::kV + vs * kTile, kBoxBytes, 1024u);
+#pragma unroll
+                for (uint32_t half = 0; half < 2; ++half) {
+                    if (!wait(p_half(x, half), np)) return;
+                    tc_fence_after();
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int kk = 4 * (int)half + i;
+                        if (kk < steps) umma_ts(tmem_o(x), tmem_s(x) + 8u * kk, dv + kk * (2048u >> 4), kIdescO, first && kk == 0 ? 0u : 1u);
+                    }
+                }
+                ++np;
+            };
+            for (uint32_t k = 0; alive; ++k) {
+                const uint32_t sl = k % kItems;
+                if (!wait(item_full(sl), k / kItems)) break;
+                const Item it = items[sl];
+                mbar_arrive(item_empty(sl));
+                if (it.n < 0) break;
+                const int tiles = it.kt1 - it.kt0;
+                if (tiles <= 0) continue;
+                const bool pair = is_pair(it);
+                const int most0 = pair ? tiles_of_first(it) : tiles;
+                if (!wait(q_full, nq++)) break;
+                // the first tile of rows; with one query tile the second as well
+#pragma unroll 1
+                for (uint32_t t = 0; t < (pair || tiles == 1 ? 1u : 2u); ++t) {
+                    if (!wait(k_full((tg + t) % kKs), (tg + t) / kKs)) break;
+                    tc_fence_after();
+                    if (pair ? most0 > 0 : t == 0) issue_s(0, 0, (tg + t) % kKs);
+                    if (pair || t == 1) issue_s(1, pair ? 1 : 0, (tg + t) % kKs);
+                    umma_commit(k_empty((tg + t) % kKs));
+                }
+                if (tiles <= (pair ? 1 : 2)) umma_commit(q_empty);
+#pragma unroll 1
+                for (int t = 0; t < tiles && alive; ++t, ++tg) {
+                    // a team's S of its next tile follows its P V at once: both run under the other team's softmax
+                    const uint32_t vs = tg % kVs, ahead = pair ? 1u : 2u, ks = (tg + ahead) % kKs;
+                    const int steps = min(kTileRows / 16, (it.rows - (it.kt0 + t) * kTileRows + 15) / 16);
+                    const bool more = t + (int)ahead < tiles, mine = pair || (t & 1) == 0, other = pair || (t & 1) == 1;
+                    if (!wait(v_ready(vs), tg / kVs)) break;
+                    if (mine && t < most0) {
+                        if (t == 0 && !wait(o_free(0), ni0 + 1u)) break;
+                        issue_pv(0, np0, vs, steps, t == 0);
+                        if (!alive) break;
+                        if (pair ? t + 1 == most0 : t + 2 >= tiles) { umma_commit(pv_done(0)); ++ni0; }
+                    }
+                    if (more) {
+                        if (!wait(k_full(ks), (tg + ahead) / kKs)) break;
+                        tc_fence_after();
+                        if (mine && t + (int)ahead < most0) issue_s(0, 0, ks);
+                    }
+                    if (other) {
+                        if (t == (pair ? 0 : 1) && !wait(o_free(1), ni1 + 1u)) break;
+                        issue_pv(1, np1, vs, steps, t == (pair ? 0 : 1));
+                        if (!alive) break;
+                        if (pair ? t + 1 == tiles : t + 2 >= tiles) { umma_commit(pv_done(1)); ++ni1; }
+                        if (more) issue_s(1, pair ? 1 : 0, ks);
+                    }
+                    umma_commit(v_empty(vs));
+                    if (more) {
+                        umma_commit(k_empty(ks));
+                        if (t + (int)ahead + 1 == tiles) umma_commit(q_empty);
+                    }
+                }
+            }
+        }
+    } else if (warp == 2) {
+        // ------------------------------------------------------------ value check
+        // A product with P = 0 does not hide a value that is not finite, so tiles whose rows some token must not see are
+        // looked over: such values become zeros, and the first row that has one is noted for every column (16 bits, counted from
+        // the last row that the first token sees), for the tokens that do see it. Rows behind the last one (memory that holds anything) and absent rows become zeros too.
+        uint32_t tg = 0;
+        for (uint32_t k = 0; alive; ++k) {
+            const uint32_t sl = k % kItems;
+            if (!mbar_wait(item_full(sl), (k / kItems) & 1u, abort_flag, status, kWaitLimitNs, kPollBackoffNs)) { alive = false; break; }
+            const Item it = items[sl];
+            uint32_t *mine = bad + sl * (D / 2);
+            for (int d = lane; d < D / 2; d += 32) mine[d] = 0xFFFFFFFFu;
+            if (lane == 0) bad_any[sl] = 0;
+            __syncwarp();
+            if (it.n < 0) break;
+            for (int t = it.kt0; t < it.kt1; ++t, ++tg) {
+                const uint32_t s = tg % kVs;
+                if (!mbar_wait(v_full(s), (tg / kVs) & 1u, abort_flag, status, kWaitLimitNs, kPollBackoffNs)) { alive = false; break; }
+                const int row0 = t * kTileRows, rows = min(kTileRows, it.rows - row0);
+                const uint4 absent = infos[tg % kInfos];
+                const bool any_absent = (absent.x | absent.y | absent.z | absent.w) != 0u;
+                const int check = any_absent ? 0 : max(0, it.limit + 1 - row0);           // rows before are seen by every token
+                const int end = (rows + 15) & ~15;
+                if (check < end) {
+                    uint8_t *tile = smem + L::kV + s * kTile;
+                    constexpr int kChunks = D / 8;                                         // 16-byte pieces of a row
+                    for (int i = check * kChunks + lane; i < end * kChunks; i += 32) {
+                        const int r = i / kChunks, c = i % kChunks;
+                        uint4 *at = reinterpret_cast<uint4 *>(tile + (c >> 3) * kBoxBytes + r * 128 + (((c & 7) ^ (r & 7)) << 4));
+                        const uint32_t word = r < 64 ? (r < 32 ? absent.x : absent.y) : (r < 96 ? absent.z : absent.w);
+                        if (r >= rows || (word >> (r & 31)) & 1u) {
+                            *at = make_uint4(0u, 0u, 0u, 0u);
+                            continue;
+                        }
+                        uint4 v = *at;
+                        uint32_t w[4] = {v.x, v.y, v.z, v.w};
+                        bool found = false;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const uint32_t e = w[j] & E::kExponent;
+                            const bool lo = (e & 0xFFFFu) == (E::kExponent & 0xFFFFu), hi = (e >> 16) == (E::kExponent >> 16);
+                            if (lo || hi) {
+                                const uint32_t row = (uint32_t)max(row0 + r - it.limit, 0), note = (lo ? row : 0xFFFFu) | (hi ? row : 0xFFFFu) << 16;
+                                uint32_t was = mine[c * 4 + j], got;
+                                while ((got = atomicCAS(mine + c * 4 + j, was, __vminu2(was, note))) != was) was = got;
+                                w[j] &= (lo ? 0u : 0xFFFFu) | (hi ? 0u : 0xFFFF0000u);
+                            }
+                            found |= lo || hi;
+                        }
+                        if (found) {
+                            *at = make_uint4(w[0], w[1], w[2], w[3]);
+                            bad_any[sl] = 1;
+                        }
+                    }
+                    fence_to_async();
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(v_ready(s));
+            }
+            if (lane == 0) mbar_arrive(item_empty(sl));
+        }
+    } else if (warp >= 4) {
+        // ------------------------------------------------------------ softmax: a thread owns a query row
+        const uint32_t x = (uint32_t)(warp - 4) >> 2;
+        const int q4 = warp & 3, r = q4 * 32 + lane;
+        const uint32_t lane_sel = (uint32_t)(q4 * 32) << 16;
+        const uint32_t s_addr = tmem_s(x) + lane_sel, o_addr = tmem_o(x) + lane_sel;
+        const float c = a.scale_log2e;
+        const float2 c2 = make_float2(c, c), top2 = make_float2(E::kTop, E::kTop);
+        const int my_token = r / a.G, my_head = r - my_token * a.G;
+        uint32_t n = 0, ni = 0, tg0 = 0, nr = 0, no = 0;  // the team's tiles and items; the CTA's tiles; rendezvous; results taken over
+        auto meet = [&]() {
+            __syncwarp();
+            if (lane == 0) mbar_arrive(rdv(x));
+            const bool ok = mbar_wait(rdv(x), nr & 1u, abort_flag, status);
+            ++nr;
+            return ok;
+        };
+        for (uint32_t k = 0; alive; ++k) {
+            const uint32_t sl = k % kItems;
+            if (!mbar_wait(item_full(sl), (k / kItems) & 1u, abort_flag, status)) { alive = false; break; }
+            const Item it = items[sl];
+            if (it.n < 0) break;
+            const bool pair = is_pair(it);
+            const int tiles = it.kt1 - it.kt0;
+            const int skip = pair ? (int)x * a.tile_tokens : 0;                             // tokens in front of the team's
+            const int ntok = min(a.tile_tokens, it.ntok - skip);
+            const int limit = it.limit + skip + my_token;                                   // last row that this row sees
+            const bool valid = my_token < ntok, live = q4 * 32 < ntok * a.G;                // live: some row of the warp counts
+            const int t0 = pair ? 0 : (int)x, step = pair ? 1 : 2, most = pair && x == 0 ? tiles_of_first(it) : tiles;
+            float m = -INFINITY, l = 0.f;                 // running maximum (not scaled), sum
+#pragma unroll 1
+            for (int t = t0; t < most; t += step, ++n) {
+                if (!mbar_wait(s_full(x), n & 1u, abort_flag, status)) { alive = false; break; }
+                if (!live) {
+                    if (lane == 0) {
+                        mbar_arrive(p_half(x, 0));
+                        mbar_arrive(p_half(x, 1));
+                    }
+                    continue;
+                }
+                tc_fence_after();
+                const int row0 = (it.kt0 + t) * kTileRows;
+                const uint4 absent = infos[(tg0 + (uint32_t)t) % kInfos];
+                const int lim = min(limit, it.rows - 1) - row0;
+                const bool masked = __any_sync(0xFFFFFFFFu, lim < kTileRows - 1) || (absent.x | absent.y | absent.z | absent.w) != 0u;
+                auto seen = [&](int ch) {                 // columns of 32 that the row sees, as bits
+                    const int last = lim - 32 * ch;
+                    const uint32_t gone = ch == 0 ? absent.x : ch == 1 ? absent.y : ch == 2 ? absent.z : absent.w;
+                    return (last >= 31 ? 0xFFFFFFFFu : last < 0 ? 0u : (2u << last) - 1u) & ~gone;
+                };
+                float mx;
+                if (masked) {
+                    mx = -INFINITY;
+#pragma unroll 1
+                    for (int ch = 0; ch < 4; ++ch) {
+                        uint32_t ra[32];
+                        tmem_ld32_async(s_addr + 32 * ch, ra);
+                        const uint32_t bits = seen(ch);
+                        tmem_ld_wait(ra);
+#pragma unroll
+                        for (int i = 0; i < 32; i += 2)
+                            mx = max3(mx, bits >> i & 1u ? __uint_as_float(ra[i]) : -INFINITY, bits >> (i + 1) & 1u ? __uint_as_float(ra[i + 1]) : -INFINITY);
+                    }
+                } else {
+                    uint32_t ra[32], rb[32], rc[32], rd[32];
+                    tmem_ld32_async(s_addr, ra);
+                    tmem_ld32_async(s_addr + 32, rb);
+                    tmem_ld32_async(s_addr + 64, rc);
+                    tmem_ld32_async(s_addr + 96, rd);
+                    tmem_ld_wait(ra);
+                    tmem_ld_wait(rb);
+                    tmem_ld_wait(rc);
+                    tmem_ld_wait(rd);
+                    float ma = __uint_as_float(ra[0]), mb = __uint_as_float(rb[0]), mc = __uint_as_float(rc[0]), md = __uint_as_float(rd[0]);
+#pragma unroll
+                    for (int i = 0; i < 32; i += 2) {
+                        ma = max3(ma, __uint_as_float(ra[i]), __uint_as_float(ra[i + 1]));
+                        mb = max3(mb, __uint_as_float(rb[i]), __uint_as_float(rb[i + 1]));
+                        mc = max3(mc, __uint_as_float(rc[i]), __uint_as_float(rc[i + 1]));
+                        md = max3(md, __uint_as_float(rd[i]), __uint_as_float(rd[i + 1]));
+                    }
+                    mx = max3(max3(ma, mb, mc), md, md);
+                }
+                float factor = 1.f;
+                bool raise = false;
+                if (m == -INFINITY) {
+                    m = mx;                               // what was added before (rows of -inf alone) is nothing
+                    if (m != -INFINITY) l = 0.f;
+                } else if ((mx - m) * c > E::kRaise) {
+                    raise = true;
+                    factor = fast_exp2((m - mx) * c);
+                    m = mx;
+                    l *= factor;
+                } else if (mx != mx) {
+                    l = mx;
+                }
+                const float m_use = m == -INFINITY ? 0.f : m;
+                // S was issued behind the previous tile's P V, and the tensor cores complete in issue order: O is at
+                // rest. TMEM accesses are warp-wide: the other rows multiply by one.
+                if (__any_sync(0xFFFFFFFFu, raise)) {
+#pragma unroll 1
+                    for (int j = 0; j < D / 32; ++j) {
+                        uint32_t ro[32];
+                        tmem_ld32_async(o_addr + 32 * j, ro);
+                        tmem_ld_wait(ro);
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) ro[i] = __float_as_uint(__uint_as_float(ro[i]) * factor);
+                        tmem_st32(o_addr + 32 * j, ro);
+                    }
+                }
+                const float2 nm = make_float2(-m_use, -m_use);
+                float2 sum = make_float2(0.f, 0.f);
+                // 32 columns: P lands on columns of S that were read before
+                auto chunk = [&](const uint32_t (&raw)[32], int ch) {
+                    float2 e[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        // the difference of two scores that are near each other is exact, at any scale
+                        const float2 d = __fadd2_rn(make_float2(__uint_as_float(raw[2 * i]), __uint_as_float(raw[2 * i + 1])), nm);
+                        e[i] = exp2_pair(__ffma2_rn(d, c2, top2), i);
+                    }
+                    if (masked) {
+                        const uint32_t bits = seen(ch);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            if (!(bits >> (2 * i) & 1u)) e[i].x = 0.f;
+                            if (!(bits >> (2 * i + 1) & 1u)) e[i].y = 0.f;
+                        }
+                    }
+                    uint32_t pk[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        sum = __fadd2_rn(sum, e[i]);
+                        pk[i] = E::pack(e[i].x, e[i].y);
+                    }
+                    tmem_st16(s_addr + 16 * ch, pk);
+                };
+                uint32_t ra[32], rb[32];
+                tmem_ld32_async(s_addr, ra);
+#pragma unroll 1
+                for (uint32_t half = 0; half < 2; ++half) {
+                    tmem_ld_wait(ra);
+                    tmem_ld32_async(s_addr + 64 * half + 32, rb);
+                    chunk(ra, 2 * half);
+                    tmem_ld_wait(rb);
+                    if (half == 0) tmem_ld32_async(s_addr + 64, ra);
+                    chunk(rb, 2 * half + 1);
+                    tmem_st_wait();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(p_half(x, half));
+                }
+                l += sum.x + sum.y;
+            }
+            if (!alive) break;
+            tg0 += (uint32_t)tiles;
+            bool some = most > t0;                        // the team's O holds something
+            if (some) {
+                if (!mbar_wait(pv_done(x), ni & 1u, abort_flag, status)) { alive = false; break; }
+                tc_fence_after();
+                ++ni;
+            }
+            bool some1 = false;                           // the second team's O of a single query tile does
+            float m1 = -INFINITY, f0 = 1.f, f1 = 0.f;
+            if (!pair && tiles > 1) {
+                if (x == 1) {
+                    other_s[r] = make_float2(m, l);
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(other_done);
+                } else {
+                    if (!mbar_wait(other_done, no & 1u, abort_flag, status)) { alive = false; break; }
+                    tc_fence_after();
+                    const float2 ml = other_s[r];
+                    ++no;
+                    some1 = true;
+                    m1 = ml.x;
+                    const float top = max3(m, m1, m1), use = top == -INFINITY ? 0.f : top;
+                    f0 = fast_exp2((m - use) * c);
+                    f1 = fast_exp2((m1 - use) * c);
+                    l = l * f0 + ml.y * f1;
+                    m = top;
+                }
+            }
+            if (pair || x == 0) {
+                const bool dirty = bad_any[sl] != 0;
+                const uint16_t *mine = reinterpret_cast<const uint16_t *>(bad + sl * (D / 2));
+                const size_t token = (size_t)it.token + skip + my_token, head = (size_t)it.h * a.G + my_head;
+                auto store = [&](uint16_t *row, const float (&f)[32], int j, float inv) {
+                    uint4 *to = reinterpret_cast<uint4 *>(row + 32 * j);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const float *g = f + 8 * q;
+                        to[q] = make_uint4(E::pack(g[0] * inv, g[1] * inv), E::pack(g[2] * inv, g[3] * inv),
+                                           E::pack(g[4] * inv, g[5] * inv), E::pack(g[6] * inv, g[7] * inv));
+                    }
+                };
+                auto log_sum = [&](float mt, float lt) { return mt == -INFINITY && lt == lt ? -INFINITY : fmaf(mt, c, log2f(lt) - E::kTop) * kLn2; };
+                const size_t at = (size_t)it.slot * 2 + x;
+                const bool none = m == -INFINITY && l == l;               // the row sees nothing, or scores of -inf alone
+                const float inv = none ? 0.f : 1.f / l;
+                if (live) {
+#pragma unroll 1
+                    for (int j = 0; j < D / 32; ++j) {
+                        float f[32];
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) f[i] = 0.f;
+                        if (some) {
+                            uint32_t ro[32];
+                            tmem_ld32_async(o_addr + 32 * j, ro);
+                            tmem_ld_wait(ro);
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) f[i] = none ? 0.f : __uint_as_float(ro[i]) * f0;
+                        }
+                        if (some1) {
+                            uint32_t ro[32];
+                            tmem_ld32_async(tmem_o(1) + lane_sel + 32 * j, ro);
+                            tmem_ld_wait(ro);
+#pragma unroll
+                            for (int i = 0; i < 32; ++i)
+                                if (m1 != -INFINITY) f[i] = fmaf(__uint_as_float(ro[i]), f1, f[i]);
+                        }
+                        if (dirty) {
+#pragma unroll
+                            for (int i = 0; i < 32; ++i)
+                                if (mine[32 * j + i] <= skip + my_token) f[i] = __int_as_float(0x7FFFFFFF);
+                        }
+                        if (!valid) continue;
+                        if (it.parts == 0) {
+                            store(out + (int64_t)token * out_token + (int64_t)head * out_head, f, j, inv);
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 8; ++i)
+                                __stcg(parts.o + (at * (D / 4) + 8 * j + i) * kTileRows + r, make_float4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]));
+                        }
+                    }
+                    if (valid && it.parts == 0 && lse) lse[token * a.Hq + head] = log_sum(m, l);
+                    if (valid && it.parts > 0) __stcg(parts.ml + at * kTileRows + r, make_float2(m, some ? l : 0.f));
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    if (some) mbar_arrive(o_free(x));
+                    if (some1) mbar_arrive(o_free(1));
+                }
+                if (it.parts > 0) {
+                    // the CTA that arrives last puts the parts together, in the order of the rows
+                    if (!meet()) { alive = false; break; }
+                    int *counter = a.c.state + kStateChunk + it.first * kChunkCounters + (int)x;
+                    if (q4 == 0 && lane == 0) {
+                        const bool last = arrive(counter) == it.parts - 1;
+                        if (last) *counter = 0;
+                        last_s[x] = last;
+                    }
+                    if (!meet()) { alive = false; break; }
+                    if (last_s[x]) {
+                        // a warp takes 32 rows at a time and a quarter of their columns
+                        auto part_at = [&](int p) { return (size_t)(2 * (it.first + p) + (p == 0)) * 2 + x; };
+#pragma unroll 1
+                        for (int row = lane; row < (ntok * a.G + 31) / 32 * 32; row += 32) {
+                            const int in = row / a.G;
+                            if (in >= ntok) continue;
+                            float M = -INFINITY;
+#pragma unroll 4
+                            for (int p = 0; p < it.parts; ++p) M = fmaxf(M, __ldcg(parts.ml + part_at(p) * kTileRows + row).x);
+                            const float mu = M == -INFINITY ? 0.f : M;
+                            float sum = 0.f, f[32] = {};
+#pragma unroll 2
+                            for (int p = 0; p < it.parts; ++p) {
+                                const float2 ml = __ldcg(parts.ml + part_at(p) * kTileRows + row);
+                                float4 o[D / 16];
+#pragma unroll
+                                for (int i = 0; i < D / 16; ++i) o[i] = __ldcg(parts.o + (part_at(p) * (D / 4) + q4 * (D / 16) + i) * kTileRows + row);
+                                const float g = fast_exp2((ml.x - mu) * c);
+                                sum = fmaf(ml.y, g, sum);
+                                if (ml.x == -INFINITY) continue;          // nothing was seen: its sums are none
+#pragma unroll
+                                for (int i = 0; i < D / 16; ++i) {
+                                    f[4 * i] = fmaf(o[i].x, g, f[4 * i]);
+                                    f[4 * i + 1] = fmaf(o[i].y, g, f[4 * i + 1]);
+                                    f[4 * i + 2] = fmaf(o[i].z, g, f[4 * i + 2]);
+                                    f[4 * i + 3] = fmaf(o[i].w, g, f[4 * i + 3]);
+                                }
+                            }
+                            const float scale = M == -INFINITY && sum == sum ? 0.f : 1.f / sum;
+                            const size_t tk = (size_t)it.token + skip + in, hd = (size_t)it.h * a.G + (row - in * a.G);
+                            uint4 *to = reinterpret_cast<uint4 *>(out + (int64_t)tk * out_token + (int64_t)hd * out_head + q4 * (D / 4));
+#pragma unroll
+                            for (int q = 0; q < D / 32; ++q) {
+                                const float *g = f + 8 * q;
+                                to[q] = make_uint4(E::pack(g[0] * scale, g[1] * scale), E::pack(g[2] * scale, g[3] * scale),
+                                                   E::pack(g[4] * scale, g[5] * scale), E::pack(g[6] * scale, g[7] * scale));
+                            }
+                            if (q4 == 0 && lse) lse[tk * a.Hq + hd] = log_sum(M, sum);
+                        }
+                    }
+                }
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(item_empty(sl));
+        }
+    }
+
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)kTmemCols) : "memory");
+    }
+}
+
+template <int D, int DTYPE>
+cudaError_t launch_t(const ChunkArgs &a, const CUtensorMap &mq, const CUtensorMap &mk, const CUtensorMap &mv, void *out, int64_t out_token,
+                     int64_t out_head, float *lse, const Parts &parts, cudaStream_t stream)
+{
+    auto kernel = chunk_attention_kernel<D, DTYPE>;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<D>::kTotal);
+    if (e != cudaSuccess) return e;
+    return launch_chained(kernel, dim3(chunk_grid()), kThreads, Smem<D>::kTotal, stream, mq, mk, mv, a, static_cast<uint16_t *>(out),
+                          out_token, out_head, lse, parts);
+}
+
+}  // namespace
+
+size_t chunk_attention_workspace_bytes(int D)
+{
+    return (size_t)2 * kChunkMaxCtas * 2 * kTileRows * ((size_t)D * sizeof(float) + sizeof(float2));
+}
+
+cudaError_t launch_chunk_attention(const ChunkArgs &a, int D, int dtype, const void *q, int64_t q_token, int64_t q_head, void *out,
+                                   int64_t out_token, int64_t out_head, float *lse, void *ws, cudaStream_t stream)
+{
+    CUtensorMap mq, mk, mv;
+    if (!make_query_map(&mq, a, D, dtype, q, q_token, q_head) || !make_pool_map(&mk, a, D, dtype, a.c.K) ||
+        !make_pool_map(&mv, a, D, dtype, a.c.V))
+        return cudaErrorInvalidValue;
+    Parts parts;
+    parts.o = static_cast<float4 *>(ws);
+    parts.ml = reinterpret_cast<float2 *>(static_cast<char *>(ws) + (size_t)2 * kChunkMaxCtas * 2 * kTileRows * D * sizeof(float));
+    if (D == 128)
+        return dtype == EC_BF16 ? launch_t<128, EC_BF16>(a, mq, mk, mv, out, out_token, out_head, lse, parts, stream)
+                                : launch_t<128, EC_FP16>(a, mq, mk, mv, out, out_token, out_head, lse, parts, stream);
+    return dtype == EC_BF16 ? launch_t<64, EC_BF16>(a, mq, mk, mv, out, out_token, out_head, lse, parts, stream)
+                            : launch_t<64, EC_FP16>(a, mq, mk, mv, out, out_token, out_head, lse, parts, stream);
+}
+
+}  // namespace ec

@@ -40,7 +40,8 @@ cudaError_t launch_chained(void (*kernel)(KArgs...), dim3 grid, unsigned block, 
 // status word). Every counter is zero between launches: whoever arrives last puts it back.
 constexpr int kPagedMaxCtas = 148 * 2;
 constexpr int kStateAttention = 64;
-constexpr int kStateAppend = kStateAttention + kPagedMaxCtas;      // one per problem
+constexpr int kStateChunk = kStateAttention + kPagedMaxCtas;       // four per CTA of a chunk's launches, see ec_chunk.cuh
+constexpr int kStateAppend = kStateChunk + 2 * kPagedMaxCtas;      // one per problem
 
 // The cache as the kernels take it. Offsets of rows are counted in 16-byte units, in 32 bits: the host refuses
 // pools that reach past 2^32 - 2 of them (64 GiB for K and as much for V).

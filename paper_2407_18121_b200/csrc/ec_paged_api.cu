@@ -1,17 +1,13 @@
 // C ABI of the paged cache: argument validation, workspace layout and kernel sequencing.
-#include "ec_paged.cuh"
+#include "ec_paged_api.cuh"
 
 #include <math.h>
 
 #include <new>
 #include <vector>
 
-namespace {
+namespace ec {
 
-inline bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
-inline size_t round256(size_t x) { return (x + 255) / 256 * 256; }
-
-// The caller owns the struct: every call repeats these checks.
 int check_paged(const ec_paged *c)
 {
     if (!c) return EC_ERR_NULL;
@@ -36,9 +32,9 @@ int check_paged(const ec_paged *c)
     return EC_OK;
 }
 
-ec::PagedView view(const ec_paged *c)
+PagedView view(const ec_paged *c)
 {
-    ec::PagedView v;
+    PagedView v;
     v.K = static_cast<uint4 *>(c->Kp);
     v.V = static_cast<uint4 *>(c->Vp);
     v.weight = c->weight;
@@ -55,9 +51,25 @@ ec::PagedView view(const ec_paged *c)
     v.page_step = (uint32_t)(c->page_stride / 8);
     v.head_step = (uint32_t)(c->head_stride / 8);
     v.row_step = (uint32_t)(c->row_stride / 8);
-    ec::set_page_division(v);
+    set_page_division(v);
     return v;
 }
+
+int check_ws(const void *ws, size_t have, size_t need)
+{
+    if (!ws || have < need) return EC_ERR_WORKSPACE;
+    return aligned(ws, 256) ? EC_OK : EC_ERR_ALIGN;
+}
+
+}  // namespace ec
+
+namespace {
+
+using ec::aligned;
+using ec::check_paged;
+using ec::check_ws;
+using ec::round256;
+using ec::view;
 
 int check_heads(const ec_paged *c, int Hq)
 {
@@ -106,12 +118,6 @@ ec::AppendArgs append_args(const void *K_new, const void *V_new, const float *w_
     a.recent = recent;
     a.sinks = sinks;
     return a;
-}
-
-int check_ws(const void *ws, size_t have, size_t need)
-{
-    if (!ws || have < need) return EC_ERR_WORKSPACE;
-    return aligned(ws, 256) ? EC_OK : EC_ERR_ALIGN;
 }
 
 }  // namespace

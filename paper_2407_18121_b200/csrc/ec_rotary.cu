@@ -1,0 +1,234 @@
+// Rotary positions, alone or on their way into a paged cache.
+//   pair i of a head turns by position * freq_i, scaled by `factor`: (a, b) -> (a cos - b sin, a sin + b cos); the inverse turns back
+//   (the transposed map, which is the gradient). Pairs are elements (2 i, 2 i + 1) or (i, i + rot / 2) of the first `rot`.
+// Bound by HBM: every element is read once and written once. What the angles cost is shared by the heads of a token: a CTA
+// works out the sines and cosines of its tokens once, in shared memory.
+//  - An angle is kept as a fraction of a turn in 64 bits of fixed point: freq / 2 pi from the frequency's 64-bit value, times the
+//    position as a whole-number product that drops whole turns by itself. Positions of 2^31 lose nothing: the frequency's own
+//    rounding, 2^-53, is all (in fp32 an angle of 10^6 is off by 0.06).
+#include "ec_paged.cuh"
+#include "ec_rotary.cuh"
+
+namespace ec {
+
+namespace {
+
+constexpr int kRotThreads = 256;
+constexpr int kFlight = 4;                       // items of a thread in flight
+
+template <int DTYPE> __device__ __forceinline__ void widen(const uint4 &v, float (&f)[8])
+{
+    if constexpr (DTYPE == EC_BF16) {
+        unpack8(v, f);
+    } else {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 p = __half22float2(*reinterpret_cast<const __half2 *>(&w[i]));
+            f[2 * i] = p.x;
+            f[2 * i + 1] = p.y;
+        }
+    }
+}
+
+template <int DTYPE> __device__ __forceinline__ uint4 narrow(const float (&f)[8])
+{
+    if constexpr (DTYPE == EC_BF16) {
+        return pack8(f);
+    } else {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const __half2 h = __floats2half2_rn(f[2 * i], f[2 * i + 1]);
+            w[i] = *reinterpret_cast<const uint32_t *>(&h);
+        }
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+
+// cos and sin of position * freq, both times factor.
+__device__ __forceinline__ float2 turn_of(double freq, int position, float factor, bool inverse)
+{
+    double turns = freq * 0.15915494309189533577;                         // 1 / 2 pi
+    turns -= floor(turns);
+    const unsigned long long step = __double2ull_rn(turns * 18446744073709551616.0);
+    const unsigned long long phase = step * (unsigned long long)(long long)position;
+    float s, c;
+    sincospif((float)(int)(phase >> 32) * 4.656612873077393e-10f, &s, &c);   // 2^-31: half turns
+    return make_float2(c * factor, (inverse ? -s : s) * factor);
+}
+
+// What one head row of a token becomes: its place in the input and in the output, nullptr: nothing.
+struct RowPlace {
+    const uint4 *from;
+    uint4 *to;
+};
+
+// A thread keeps its place in the head (piece `v`) and walks over the rows (token, head) of the CTA, kFlight at a time.
+// Places(row, token) gives the row's pointers.
+template <int DTYPE, bool HALF, typename Places>
+__device__ __forceinline__ void turn_rows(const RotaryTurn &r, int D, const float2 *table, int tokens, int heads, Places places)
+{
+    const int turning = r.rot / (HALF ? 16 : 8), pieces = turning + (D - r.rot) / 8;
+    const int step = kRotThreads / pieces, v = threadIdx.x % pieces, first = threadIdx.x / pieces;
+    if (first >= step) return;
+    const int rows = tokens * heads, half = r.rot / 2;
+    // offsets in pieces of 16 bytes
+    const bool turns = v < turning;
+    const int lo = turns ? v : v - turning + r.rot / 8, hi = HALF && turns ? v + half / 8 : -1;
+    for (int row0 = first; row0 < rows; row0 += kFlight * step) {
+        RowPlace at[kFlight];
+        uint4 a[kFlight], b[kFlight];
+        int token[kFlight];
+#pragma unroll
+        for (int u = 0; u < kFlight; ++u) {
+            const int row = row0 + u * step;
+            at[u].to = nullptr;
+            if (row >= rows) continue;
+            token[u] = row / heads;
+            at[u] = places(token[u], row - token[u] * heads);
+            if (at[u].to == nullptr) continue;
+            a[u] = at[u].from[lo];
+            if (hi >= 0) b[u] = at[u].from[hi];
+        }
+#pragma unroll
+        for (int u = 0; u < kFlight; ++u) {
+            if (at[u].to == nullptr) continue;
+            if (turns) {
+                const float2 *cs = table + token[u] * half;
+                float x[8];
+                widen<DTYPE>(a[u], x);
+                if (HALF) {
+                    float y[8];
+                    widen<DTYPE>(b[u], y);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float2 t = cs[8 * v + i];
+                        const float p = x[i] * t.x - y[i] * t.y, q = x[i] * t.y + y[i] * t.x;
+                        x[i] = p;
+                        y[i] = q;
+                    }
+                    at[u].to[hi] = narrow<DTYPE>(y);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float2 t = cs[4 * v + i];
+                        const float p = x[2 * i] * t.x - x[2 * i + 1] * t.y, q = x[2 * i] * t.y + x[2 * i + 1] * t.x;
+                        x[2 * i] = p;
+                        x[2 * i + 1] = q;
+                    }
+                }
+                a[u] = narrow<DTYPE>(x);
+            }
+            at[u].to[lo] = a[u];
+        }
+    }
+}
+
+template <int DTYPE, bool HALF>
+__global__ void __launch_bounds__(kRotThreads)
+rotary_kernel(const RotaryTurn r, const RotaryRows x, int D, int per)
+{
+    extern __shared__ float2 table[];
+    const int first = blockIdx.x * per, tokens = min(per, x.N * x.T - first);
+    grid_wait();
+    grid_release();
+    const int half = r.rot / 2;
+    for (int i = threadIdx.x; i < tokens * half; i += kRotThreads) {
+        const int t = i / half, token = first + t, n = token / x.T;
+        table[i] = turn_of(r.freqs[i - t * half], x.positions[n * x.pos_n + (token - n * x.T)], r.factor, r.inverse);
+    }
+    __syncthreads();
+    turn_rows<DTYPE, HALF>(r, D, table, tokens, x.heads, [&](int t, int h) {
+        const int token = first + t, n = token / x.T, at = token - n * x.T;
+        return RowPlace{x.x + n * x.x_n + at * x.x_t + h * x.x_h, x.out + n * x.out_n + at * x.out_t + h * x.out_h};
+    });
+}
+
+template <int DTYPE, bool HALF>
+__global__ void __launch_bounds__(kRotThreads)
+join_kernel(const RotaryTurn r, const PagedView c, const JoinArgs j, int D, int per)
+{
+    extern __shared__ float2 table[];
+    __shared__ int slot_s[kRotaryMostTokens], pos_s[kRotaryMostTokens];
+    const int first = blockIdx.x * per, tokens = min(per, j.tokens - first);
+    grid_wait();
+    grid_release();
+    if ((int)threadIdx.x < tokens) {
+        int slot = j.slots[first + threadIdx.x];
+        if (slot >= c.n_pages * c.page_size) {
+            report_page(c);
+            slot = -1;
+        }
+        slot_s[threadIdx.x] = slot;
+        pos_s[threadIdx.x] = j.positions[first + threadIdx.x];
+    }
+    const int half = r.rot / 2;
+    for (int i = threadIdx.x; i < tokens * half; i += kRotThreads) {
+        const int t = i / half;
+        table[i] = turn_of(r.freqs[i - t * half], j.positions[first + t], r.factor, false);
+    }
+    __syncthreads();
+    auto place = [&](int t) {
+        Slot s;
+        s.page = page_of(c, slot_s[t]);
+        s.slot = slot_s[t] - s.page * c.page_size;
+        return s;
+    };
+    turn_rows<DTYPE, HALF>(r, D, table, tokens, j.Hq + c.H, [&](int t, int h) {
+        if (slot_s[t] < 0) return RowPlace{nullptr, nullptr};
+        if (h < j.Hq) return RowPlace{j.q + (first + t) * j.q_t + h * j.q_h, j.q_out + (first + t) * j.qo_t + h * j.qo_h};
+        h -= j.Hq;
+        return RowPlace{j.k + (first + t) * j.k_t + h * j.k_h, c.K + row_offset(c, place(t)) + (size_t)h * c.head_step};
+    });
+    const int pieces = D / 8, v = threadIdx.x % pieces, step = kRotThreads / pieces, rows = tokens * c.H;
+    for (int row0 = threadIdx.x / pieces; row0 < rows; row0 += kFlight * step) {
+        uint4 x[kFlight];
+        uint4 *to[kFlight];
+#pragma unroll
+        for (int u = 0; u < kFlight; ++u) {
+            const int row = row0 + u * step;
+            to[u] = nullptr;
+            if (row >= rows) continue;
+            const int t = row / c.H, h = row - t * c.H;
+            if (slot_s[t] < 0) continue;
+            to[u] = c.V + row_offset(c, place(t)) + (size_t)h * c.head_step + v;
+            x[u] = j.v[(first + t) * j.v_t + h * j.v_h + v];
+        }
+#pragma unroll
+        for (int u = 0; u < kFlight; ++u)
+            if (to[u]) *to[u] = x[u];
+    }
+    for (int row = threadIdx.x; row < rows; row += kRotThreads) {
+        const int t = row / c.H, h = row - t * c.H;
+        if (slot_s[t] < 0) continue;
+        const uint32_t at = meta_index(c, h, place(t));
+        c.weight[at] = j.w_new ? j.w_new[(size_t)(first + t) * c.H + h] : 0.f;
+        c.pos[at] = pos_s[t];
+    }
+}
+
+// Tokens of a CTA: their angles are worked out together. Few tokens spread over as many CTAs.
+int tokens_per_cta(int tokens) { return tokens >= 2048 ? kRotaryMostTokens : 1; }
+
+}  // namespace
+
+cudaError_t launch_rotary(const RotaryTurn &r, const RotaryRows &x, int D, int dtype, bool half, cudaStream_t stream)
+{
+    const int per = tokens_per_cta(x.N * x.T);
+    const dim3 grid((x.N * x.T + per - 1) / per);
+    auto go = [&](auto kernel) { return launch_chained(kernel, grid, kRotThreads, (size_t)per * (r.rot / 2) * sizeof(float2), stream, r, x, D, per); };
+    if (dtype == EC_BF16) return half ? go(rotary_kernel<EC_BF16, true>) : go(rotary_kernel<EC_BF16, false>);
+    return half ? go(rotary_kernel<EC_FP16, true>) : go(rotary_kernel<EC_FP16, false>);
+}
+
+cudaError_t launch_join(const RotaryTurn &r, const PagedView &c, const JoinArgs &j, int D, int dtype, bool half, cudaStream_t stream)
+{
+    const int per = tokens_per_cta(j.tokens);
+    const dim3 grid((j.tokens + per - 1) / per);
+    auto go = [&](auto kernel) { return launch_chained(kernel, grid, kRotThreads, (size_t)per * (r.rot / 2) * sizeof(float2), stream, r, c, j, D, per); };
+    if (dtype == EC_BF16) return half ? go(join_kernel<EC_BF16, true>) : go(join_kernel<EC_BF16, false>);
+    return half ? go(join_kernel<EC_FP16, true>) : go(join_kernel<EC_FP16, false>);
+}
+
+}  // namespace ec
