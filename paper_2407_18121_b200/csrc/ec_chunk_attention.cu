@@ -3,11 +3,14 @@
 //   x[j] = scale * <q, k_j>,   out = sum_j softmax(x)_j v_j,   lse = log sum_j exp(x_j)
 #include "ec_chunk.cuh"
 
+#include <type_traits>
+
 namespace ec {
 
 namespace {
 
-constexpr int kThreads = 384;                    // warps: copies, products, value check, (none), 4 + 4 softmax
+constexpr int kThreads = 384;                    // warps: copies, products of a team, value check, products of the other, 4 + 4 softmax
+constexpr int kHalf = 64;                        // rows whose S a team works on at a time; the next 64 are under way
 constexpr int kItems = 4;                        // descriptions of work ahead
 constexpr int kInfos = 8;                        // absent rows of the tiles in flight (the rings hold 4 at most)
 constexpr int kTmemCols = 512;                   // S of both teams (2 x 128 columns), O of both teams (2 x up to 128)
@@ -73,13 +76,37 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32
                    "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
                  : "memory");
 }
-__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16])
+// 64 (32) columns of this thread's TMEM lane, complete when the statement ends: what the load fills is not to be touched before the
+// wait, and between two statements the compiler may copy registers.
+__device__ __forceinline__ void tmem_load(uint32_t taddr, uint32_t (&r)[64])
 {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
-                 "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
-                 ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
-                   "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
-                 : "memory");
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x64.b32 {"
+                 "%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+                 "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, "
+                 "%32, %33, %34, %35, %36, %37, %38, %39, %40, %41, %42, %43, %44, %45, %46, %47, "
+                 "%48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, %62, %63}, [%64];\n\t"
+                 "tcgen05.wait::ld.sync.aligned;"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+                   "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+                   "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+                   "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]),
+                   "=r"(r[32]), "=r"(r[33]), "=r"(r[34]), "=r"(r[35]), "=r"(r[36]), "=r"(r[37]), "=r"(r[38]), "=r"(r[39]),
+                   "=r"(r[40]), "=r"(r[41]), "=r"(r[42]), "=r"(r[43]), "=r"(r[44]), "=r"(r[45]), "=r"(r[46]), "=r"(r[47]),
+                   "=r"(r[48]), "=r"(r[49]), "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]), "=r"(r[54]), "=r"(r[55]),
+                   "=r"(r[56]), "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]), "=r"(r[62]), "=r"(r[63])
+                 : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_load(uint32_t taddr, uint32_t (&r)[32])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {"
+                 "%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+                 "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n\t"
+                 "tcgen05.wait::ld.sync.aligned;"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+                   "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+                   "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+                   "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+                 : "r"(taddr) : "memory");
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
@@ -121,14 +148,40 @@ struct Smem {
     static constexpr int kItem = kBadAny + kItems * 4;
     static constexpr int kInfo = kItem + kItems * (int)sizeof(Item);
     static constexpr int kBars = kInfo + kInfos * 16;
-    // q_full, q_empty, k_full[], k_empty[], v_full[], v_empty[], v_ready[], per team: s_full, p_half[2], pv_done, o_free, rdv; other_done; item_full, item_empty
-    static constexpr int kNumBars = 2 + 2 * kKs + 3 * kVs + 2 * 6 + 1 + 2 * kItems;
+    // q_full, q_empty, k_full[], k_empty[], v_full[], v_empty[], per team: s_full[2], p_full[2], pv, o_free, rdv; other_done; item_full, item_empty
+    static constexpr int kNumBars = 2 + 2 * kKs + 2 * kVs + 2 * 7 + 1 + 2 * kItems;
     static constexpr int kTmemSlot = kBars + kNumBars * 8;
     static constexpr int kAbort = kTmemSlot + 4;
     static constexpr int kLast = kAbort + 4;                              // [2] whether this CTA joins the unit's parts
-    static constexpr int kTotal = kLast + 8;
+    static constexpr int kCount = kLast + 8;                              // [3] see Counts
+    static constexpr int kTotal = kCount + 12;
     static_assert(kTotal <= 232448, "shared memory of a block");
 };
+
+// A count in shared memory that one thread raises and others wait for, as the barriers are waited for.
+__device__ __forceinline__ void publish(int *count, int value)
+{
+    asm volatile("st.release.cta.shared::cta.s32 [%0], %1;" ::"r"(smem_u32(count)), "r"(value) : "memory");
+}
+__device__ __forceinline__ bool reached(const int *count, int least, volatile int *abort_flag, int *status)
+{
+    unsigned long long t0 = 0;
+    for (uint32_t spin = 0;; ++spin) {
+        int now;
+        asm volatile("ld.acquire.cta.shared::cta.s32 %0, [%1];" : "=r"(now) : "r"(smem_u32(count)) : "memory");
+        if (now - least >= 0) return true;
+        if (spin == 0) t0 = global_ns();
+        __nanosleep(kPollBackoffNs);
+        if ((spin & 63u) == 63u) {
+            if (*abort_flag) return false;
+            if (global_ns() - t0 > kWaitLimitNs) {
+                *abort_flag = 1;
+                atomicExch(status, 1);
+                return false;
+            }
+        }
+    }
+}
 
 template <int D, int DTYPE>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -140,7 +193,6 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
     using E = Elem<DTYPE>;
     constexpr int kTile = L::kTile, kKs = L::kKs, kVs = L::kVs;
     constexpr int kBoxBytes = kTileRows * 128;
-    constexpr uint32_t kIdescS = (1u << 4) | (E::kFormat << 7) | (E::kFormat << 10) | ((kTileRows >> 3) << 17) | ((kTileRows >> 4) << 24);
     constexpr uint32_t kIdescO = (1u << 4) | (E::kFormat << 7) | (E::kFormat << 10) | (1u << 16) | ((D >> 3) << 17) | ((kTileRows >> 4) << 24);
 
     extern __shared__ __align__(1024) uint8_t smem[];
@@ -151,45 +203,50 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
     auto k_empty = [&](uint32_t s) { return bar(2 + kKs + s); };
     auto v_full = [&](uint32_t s) { return bar(2 + 2 * kKs + s); };
     auto v_empty = [&](uint32_t s) { return bar(2 + 2 * kKs + kVs + s); };
-    auto v_ready = [&](uint32_t s) { return bar(2 + 2 * kKs + 2 * kVs + s); };
-    constexpr int kT0 = 2 + 2 * kKs + 3 * kVs;
-    auto s_full = [&](uint32_t x) { return bar(kT0 + 6 * x); };
-    auto p_half = [&](uint32_t x, uint32_t k) { return bar(kT0 + 6 * x + 1 + k); };
-    auto pv_done = [&](uint32_t x) { return bar(kT0 + 6 * x + 3); };
-    auto o_free = [&](uint32_t x) { return bar(kT0 + 6 * x + 4); };
-    auto rdv = [&](uint32_t x) { return bar(kT0 + 6 * x + 5); };
-    const uint32_t other_done = bar(kT0 + 12);
-    auto item_full = [&](uint32_t k) { return bar(kT0 + 13 + k); };
-    auto item_empty = [&](uint32_t k) { return bar(kT0 + 13 + kItems + k); };
+    constexpr int kT0 = 2 + 2 * kKs + 2 * kVs;
+    auto s_full = [&](uint32_t x, uint32_t h) { return bar(kT0 + 7 * x + h); };
+    auto p_full = [&](uint32_t x, uint32_t h) { return bar(kT0 + 7 * x + 2 + h); };
+    auto pv = [&](uint32_t x) { return bar(kT0 + 7 * x + 4); };
+    auto o_free = [&](uint32_t x) { return bar(kT0 + 7 * x + 5); };
+    auto rdv = [&](uint32_t x) { return bar(kT0 + 7 * x + 6); };
+    const uint32_t other_done = bar(kT0 + 14);
+    auto item_full = [&](uint32_t k) { return bar(kT0 + 15 + k); };
+    auto item_empty = [&](uint32_t k) { return bar(kT0 + 15 + kItems + k); };
     Item *items = reinterpret_cast<Item *>(smem + L::kItem);
-    uint4 *infos = reinterpret_cast<uint4 *>(smem + L::kInfo);
+    uint2 *infos = reinterpret_cast<uint2 *>(smem + L::kInfo);           // [kInfos][2 halves]
     float2 *other_s = reinterpret_cast<float2 *>(smem + L::kOther);
     uint32_t *bad = reinterpret_cast<uint32_t *>(smem + L::kBad);
     volatile int *bad_any = reinterpret_cast<volatile int *>(smem + L::kBadAny);
     volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(smem + L::kTmemSlot);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + L::kAbort);
     volatile int *last_s = reinterpret_cast<volatile int *>(smem + L::kLast);
+    // A team does not wait for every copy, and a barrier's parity tells its phase only to who saw the phase before: so a team
+    // first waits until the copy that it needs has been asked for (or its values been checked).
+    int *counts = reinterpret_cast<int *>(smem + L::kCount);
+    int *const k_asked = counts, *const q_asked = counts + 1, *const v_checked = counts + 2;
     int *status = a.c.state;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         *abort_flag = 0;
+        counts[0] = counts[1] = counts[2] = 0;
         mbar_init(q_full, 1);
-        mbar_init(q_empty, 1);
-        for (uint32_t s = 0; s < (uint32_t)kKs; ++s) { mbar_init(k_full(s), 1); mbar_init(k_empty(s), 1); }
-        for (uint32_t s = 0; s < (uint32_t)kVs; ++s) { mbar_init(v_full(s), 1); mbar_init(v_empty(s), 1); mbar_init(v_ready(s), 1); }
+        mbar_init(q_empty, 2);                                           // k, v and queries are released by both teams
+        for (uint32_t s = 0; s < (uint32_t)kKs; ++s) { mbar_init(k_full(s), 1); mbar_init(k_empty(s), 2); }
+        for (uint32_t s = 0; s < (uint32_t)kVs; ++s) { mbar_init(v_full(s), 1); mbar_init(v_empty(s), 2); }
         for (uint32_t x = 0; x < 2; ++x) {
-            mbar_init(s_full(x), 1);
-            mbar_init(p_half(x, 0), 4);
-            mbar_init(p_half(x, 1), 4);
-            mbar_init(pv_done(x), 1);
+            for (uint32_t h = 0; h < 2; ++h) {
+                mbar_init(s_full(x, h), 1);
+                mbar_init(p_full(x, h), 4);
+            }
+            mbar_init(pv(x), 1);
             mbar_init(o_free(x), 4);
             mbar_init(rdv(x), 4);
         }
         mbar_init(other_done, 4);
         for (uint32_t k = 0; k < (uint32_t)kItems; ++k) {
             mbar_init(item_full(k), 1);
-            mbar_init(item_empty(k), 1 + 1 + 8);                         // the products' thread, the value check, the softmax warps
+            mbar_init(item_empty(k), 2 + 1 + 8);                         // the products' threads, the value check, the softmax warps
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_to_async();
@@ -216,10 +273,14 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
     // A unit of two query tiles: a team per tile, every tile of rows serves both. A unit of one: both teams work on it and
     // take its tiles of rows in turn; the first team puts the two results together.
     auto is_pair = [&](const Item &it) { return it.ntok > a.tile_tokens; };
-    // Tiles of rows that the first team's tokens of a pair see (the second team's see all of the item's).
-    auto tiles_of_first = [&](const Item &it) {
-        const int sees = min(it.rows, it.limit + a.tile_tokens);
-        return max(min(it.kt1, (max(sees, 0) + kTileRows - 1) / kTileRows) - it.kt0, 0);
+    // What team x does of an item: tiles first, first + step, .. below end of the item's, with the rows that its tokens see.
+    struct Part { int first, step, end, rows; };
+    auto part_of = [&](const Item &it, uint32_t x) {
+        const int tiles = it.kt1 - it.kt0;
+        if (!is_pair(it)) return Part{(int)x, 2, tiles, it.rows};
+        if (x == 1) return Part{0, 1, tiles, it.rows};
+        const int sees = max(min(it.rows, it.limit + a.tile_tokens), 0);
+        return Part{0, 1, max(min(tiles, (sees + kTileRows - 1) / kTileRows - it.kt0), 0), sees};
     };
     bool alive = true;
 
@@ -267,8 +328,10 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                 const uint32_t ks = tg % kKs, vs = tg % kVs;
                 if (!mbar_wait(k_empty(ks), ((tg / kKs) & 1u) ^ 1u, abort_flag, status, kWaitLimitNs, kPollBackoffNs)) { alive = false; break; }
                 if (lane == 0) {
-                    infos[tg % kInfos] = absent;
+                    infos[2 * (tg % kInfos)] = make_uint2(absent.x, absent.y);
+                    infos[2 * (tg % kInfos) + 1] = make_uint2(absent.z, absent.w);
                     mbar_expect_tx(k_full(ks), bytes);
+                    publish(k_asked, (int)tg + 1);
                 }
                 __syncwarp();
                 copy_boxes<D>(a, &map_k, now, it.h, row0, base + L::kK + ks * kTile, k_full(ks));
@@ -278,6 +341,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                     if (lane == 0) {
                         const int tiles = it.ntok > a.tile_tokens ? 2 : 1;
                         mbar_expect_tx(q_full, (uint32_t)(tiles * a.tile_tokens * a.G * D * 2));
+                        publish(q_asked, (int)nq + 1);
                         for (int x = 0; x < tiles; ++x)
 #pragma unroll
                             for (int half = 0; half < D / 64; ++half)
@@ -304,38 +368,35 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
             for (uint32_t t = nv > (uint32_t)kVs ? nv - kVs : 0; t < nv; ++t)
                 mbar_wait(v_full(t % kVs), (t / kVs) & 1u, abort_flag, status, 200000ull);
         }
-    } else if (warp == 1) {
-        // ------------------------------------------------------------ products
+    } else if (warp == 1 || warp == 3) {
+        // ------------------------------------------------------------ products of a team
         if (lane == 0) {
-            uint32_t tg = 0, nq = 0, np0 = 0, np1 = 0, ni0 = 0, ni1 = 0;          // per team: tiles and items with tiles so far
+            const uint32_t x = (uint32_t)warp >> 1;
+            uint32_t tg0 = 0, nq = 0, np = 0, ni = 0;     // the CTA's tiles and query loads; the team's halves and items so far
+            uint32_t nh[2] = {0, 0};
             auto wait = [&](uint32_t b, uint32_t phase) {
                 if (!mbar_wait(b, phase & 1u, abort_flag, status, kWaitLimitNs, kPollBackoffNs)) alive = false;
                 return alive;
             };
-            // S of team x: query tile `qt` and the rows in stage ks
-            auto issue_s = [&](uint32_t x, uint32_t qt, uint32_t ks) {
-                const uint64_t da = umma_desc(base + L::kQ + qt * kTile), db = umma_desc(base + L::kK + ks * kTile);
+            auto wait_count = [&](const int *count, uint32_t least) {
+                if (!reached(count, (int)least, abort_flag, status)) alive = false;
+                return alive;
+            };
+            // released by both teams: who works alone on it does so twice
+            auto release = [&](uint32_t b, bool alone) {
+                umma_commit(b);
+                if (alone) umma_commit(b);
+            };
+            // S of 64 rows: N = 64
+            constexpr uint32_t kIdescS = (1u << 4) | (E::kFormat << 7) | (E::kFormat << 10) | ((kHalf >> 3) << 17) | ((kTileRows >> 4) << 24);
+            auto issue_s = [&](uint32_t qt, uint32_t ks, uint32_t h) {
+                const uint64_t da = umma_desc(base + L::kQ + qt * kTile), db = umma_desc(base + L::kK + ks * kTile + h * (kHalf * 128));
 #pragma unroll
                 for (int kk = 0; kk < D / 16; ++kk) {
                     const uint32_t off = ((uint32_t)(kk / 4) * kBoxBytes + (uint32_t)(kk % 4) * 32u) >> 4;
-                    umma_bf16(tmem_s(x), da + off, db + off, kIdescS, kk > 0 ? 1u : 0u);
+                    umma_bf16(tmem_s(x) + h * kHalf, da + off, db + off, kIdescS, kk > 0 ? 1u : 0u);
                 }
-                umma_commit(s_full(x));
-            };
-            // O += P V of team x: 16 rows an instruction, 8 columns of P; its halves follow the softmax's
-            auto issue_pv = [&](uint32_t x, uint32_t &np, uint32_t vs, int steps, bool first) {
-                const uint64_t dv = umma_desc_mn(base + L::kV + vs * kTile, kBoxBytes, 1024u);
-#pragma unroll
-                for (uint32_t half = 0; half < 2; ++half) {
-                    if (!wait(p_half(x, half), np)) return;
-                    tc_fence_after();
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int kk = 4 * (int)half + i;
-                        if (kk < steps) umma_ts(tmem_o(x), tmem_s(x) + 8u * kk, dv + kk * (2048u >> 4), kIdescO, first && kk == 0 ? 0u : 1u);
-                    }
-                }
-                ++np;
+                umma_commit(s_full(x, h));
             };
             for (uint32_t k = 0; alive; ++k) {
                 const uint32_t sl = k % kItems;
@@ -346,47 +407,62 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                 const int tiles = it.kt1 - it.kt0;
                 if (tiles <= 0) continue;
                 const bool pair = is_pair(it);
-                const int most0 = pair ? tiles_of_first(it) : tiles;
-                if (!wait(q_full, nq++)) break;
-                // the first tile of rows; with one query tile the second as well
-#pragma unroll 1
-                for (uint32_t t = 0; t < (pair || tiles == 1 ? 1u : 2u); ++t) {
-                    if (!wait(k_full((tg + t) % kKs), (tg + t) / kKs)) break;
+                const uint32_t qt = pair ? x : 0u;
+                const Part mine = part_of(it, x), others = part_of(it, x ^ 1u);
+                auto alone = [&](int t) { return !pair || t >= others.end; };
+                const bool all_mine = others.first >= others.end;          // the other team has nothing in this item
+                const uint32_t tg = tg0;
+                tg0 += (uint32_t)tiles;
+                ++nq;
+                if (mine.first >= mine.end) continue;
+                auto halves = [&](int t) { return mine.rows - (it.kt0 + t) * kTileRows > kHalf ? 2 : 1; };
+                if (!wait_count(q_asked, nq) || !wait(q_full, nq - 1u)) break;
+                {
+                    const uint32_t ks = (tg + mine.first) % kKs;
+                    if (!wait_count(k_asked, tg + mine.first + 1) || !wait(k_full(ks), (tg + mine.first) / kKs)) break;
                     tc_fence_after();
-                    if (pair ? most0 > 0 : t == 0) issue_s(0, 0, (tg + t) % kKs);
-                    if (pair || t == 1) issue_s(1, pair ? 1 : 0, (tg + t) % kKs);
-                    umma_commit(k_empty((tg + t) % kKs));
+                    issue_s(qt, ks, 0);
+                    if (halves(mine.first) > 1) issue_s(qt, ks, 1);
+                    release(k_empty(ks), alone(mine.first));
+                    if (mine.first + mine.step >= mine.end) release(q_empty, all_mine);
                 }
-                if (tiles <= (pair ? 1 : 2)) umma_commit(q_empty);
+                if (!wait(o_free(x), ni + 1u)) break;
+                ++ni;
 #pragma unroll 1
-                for (int t = 0; t < tiles && alive; ++t, ++tg) {
-                    // a team's S of its next tile follows its P V at once: both run under the other team's softmax
-                    const uint32_t vs = tg % kVs, ahead = pair ? 1u : 2u, ks = (tg + ahead) % kKs;
-                    const int steps = min(kTileRows / 16, (it.rows - (it.kt0 + t) * kTileRows + 15) / 16);
-                    const bool more = t + (int)ahead < tiles, mine = pair || (t & 1) == 0, other = pair || (t & 1) == 1;
-                    if (!wait(v_ready(vs), tg / kVs)) break;
-                    if (mine && t < most0) {
-                        if (t == 0 && !wait(o_free(0), ni0 + 1u)) break;
-                        issue_pv(0, np0, vs, steps, t == 0);
-                        if (!alive) break;
-                        if (pair ? t + 1 == most0 : t + 2 >= tiles) { umma_commit(pv_done(0)); ++ni0; }
-                    }
-                    if (more) {
-                        if (!wait(k_full(ks), (tg + ahead) / kKs)) break;
+                for (int t = mine.first; t < mine.end && alive; t += mine.step) {
+                    const int then = t + mine.step;
+                    const uint32_t vs = (tg + t) % kVs, ks = (tg + then) % kKs;
+                    const int many = halves(t), steps = min(kTileRows / 16, (mine.rows - (it.kt0 + t) * kTileRows + 15) / 16);
+                    const int ahead = then < mine.end ? halves(then) : 0;
+                    if (!wait_count(v_checked, tg + t + 1)) break;
+                    const uint64_t dv = umma_desc_mn(base + L::kV + vs * kTile, kBoxBytes, 1024u);
+#pragma unroll
+                    for (uint32_t h = 0; h < 2; ++h) {
+                        if ((int)h >= many) continue;
+                        // O += P V of 64 rows, 16 an instruction; then at once S of as many rows of the next tile, over this P
+                        if (!wait(p_full(x, h), nh[h])) break;
+                        ++nh[h];
                         tc_fence_after();
-                        if (mine && t + (int)ahead < most0) issue_s(0, 0, ks);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int kk = 4 * (int)h + i;
+                            if (kk < steps) umma_ts(tmem_o(x), tmem_s(x) + h * kHalf + 8u * i, dv + kk * (2048u >> 4), kIdescO, t == mine.first && kk == 0 ? 0u : 1u);
+                        }
+                        umma_commit(pv(x));
+                        ++np;
+                        if ((int)h < ahead) {
+                            if (h == 0) {
+                                if (!wait_count(k_asked, tg + then + 1) || !wait(k_full(ks), (tg + then) / kKs)) break;
+                                tc_fence_after();
+                            }
+                            issue_s(qt, ks, h);
+                        }
                     }
-                    if (other) {
-                        if (t == (pair ? 0 : 1) && !wait(o_free(1), ni1 + 1u)) break;
-                        issue_pv(1, np1, vs, steps, t == (pair ? 0 : 1));
-                        if (!alive) break;
-                        if (pair ? t + 1 == tiles : t + 2 >= tiles) { umma_commit(pv_done(1)); ++ni1; }
-                        if (more) issue_s(1, pair ? 1 : 0, ks);
-                    }
-                    umma_commit(v_empty(vs));
-                    if (more) {
-                        umma_commit(k_empty(ks));
-                        if (t + (int)ahead + 1 == tiles) umma_commit(q_empty);
+                    if (!alive) break;
+                    release(v_empty(vs), alone(t));
+                    if (ahead > 0) {
+                        release(k_empty(ks), alone(then));
+                        if (then + mine.step >= mine.end) release(q_empty, all_mine);
                     }
                 }
             }
@@ -410,8 +486,8 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                 const uint32_t s = tg % kVs;
                 if (!mbar_wait(v_full(s), (tg / kVs) & 1u, abort_flag, status, kWaitLimitNs, kPollBackoffNs)) { alive = false; break; }
                 const int row0 = t * kTileRows, rows = min(kTileRows, it.rows - row0);
-                const uint4 absent = infos[tg % kInfos];
-                const bool any_absent = (absent.x | absent.y | absent.z | absent.w) != 0u;
+                const uint2 gone0 = infos[2 * (tg % kInfos)], gone1 = infos[2 * (tg % kInfos) + 1];
+                const bool any_absent = (gone0.x | gone0.y | gone1.x | gone1.y) != 0u;
                 const int check = any_absent ? 0 : max(0, it.limit + 1 - row0);           // rows before are seen by every token
                 const int end = (rows + 15) & ~15;
                 if (check < end) {
@@ -420,7 +496,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                     for (int i = check * kChunks + lane; i < end * kChunks; i += 32) {
                         const int r = i / kChunks, c = i % kChunks;
                         uint4 *at = reinterpret_cast<uint4 *>(tile + (c >> 3) * kBoxBytes + r * 128 + (((c & 7) ^ (r & 7)) << 4));
-                        const uint32_t word = r < 64 ? (r < 32 ? absent.x : absent.y) : (r < 96 ? absent.z : absent.w);
+                        const uint32_t word = r < 64 ? (r < 32 ? gone0.x : gone0.y) : (r < 96 ? gone1.x : gone1.y);
                         if (r >= rows || (word >> (r & 31)) & 1u) {
                             *at = make_uint4(0u, 0u, 0u, 0u);
                             continue;
@@ -448,7 +524,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                     fence_to_async();
                 }
                 __syncwarp();
-                if (lane == 0) mbar_arrive(v_ready(s));
+                if (lane == 0) publish(v_checked, (int)tg + 1);
             }
             if (lane == 0) mbar_arrive(item_empty(sl));
         }
@@ -461,7 +537,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
         const float c = a.scale_log2e;
         const float2 c2 = make_float2(c, c), top2 = make_float2(E::kTop, E::kTop);
         const int my_token = r / a.G, my_head = r - my_token * a.G;
-        uint32_t n = 0, ni = 0, tg0 = 0, nr = 0, no = 0;  // the team's tiles and items; the CTA's tiles; rendezvous; results taken over
+        uint32_t n = 0, n0 = 0, n1 = 0, tg0 = 0, nr = 0, no = 0;   // the team's halves; the CTA's tiles; rendezvous; results taken over
         auto meet = [&]() {
             __syncwarp();
             if (lane == 0) mbar_arrive(rdv(x));
@@ -480,139 +556,105 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
             const int ntok = min(a.tile_tokens, it.ntok - skip);
             const int limit = it.limit + skip + my_token;                                   // last row that this row sees
             const bool valid = my_token < ntok, live = q4 * 32 < ntok * a.G;                // live: some row of the warp counts
-            const int t0 = pair ? 0 : (int)x, step = pair ? 1 : 2, most = pair && x == 0 ? tiles_of_first(it) : tiles;
+            const Part part = part_of(it, x);
             float m = -INFINITY, l = 0.f;                 // running maximum (not scaled), sum
 #pragma unroll 1
-            for (int t = t0; t < most; t += step, ++n) {
-                if (!mbar_wait(s_full(x), n & 1u, abort_flag, status)) { alive = false; break; }
-                if (!live) {
-                    if (lane == 0) {
-                        mbar_arrive(p_half(x, 0));
-                        mbar_arrive(p_half(x, 1));
-                    }
-                    continue;
-                }
-                tc_fence_after();
-                const int row0 = (it.kt0 + t) * kTileRows;
-                const uint4 absent = infos[(tg0 + (uint32_t)t) % kInfos];
-                const int lim = min(limit, it.rows - 1) - row0;
-                const bool masked = __any_sync(0xFFFFFFFFu, lim < kTileRows - 1) || (absent.x | absent.y | absent.z | absent.w) != 0u;
-                auto seen = [&](int ch) {                 // columns of 32 that the row sees, as bits
-                    const int last = lim - 32 * ch;
-                    const uint32_t gone = ch == 0 ? absent.x : ch == 1 ? absent.y : ch == 2 ? absent.z : absent.w;
-                    return (last >= 31 ? 0xFFFFFFFFu : last < 0 ? 0u : (2u << last) - 1u) & ~gone;
-                };
-                float mx;
-                if (masked) {
-                    mx = -INFINITY;
+            for (int t = part.first; t < part.end && alive; t += part.step) {
+                const int tile0 = (it.kt0 + t) * kTileRows;
 #pragma unroll 1
-                    for (int ch = 0; ch < 4; ++ch) {
-                        uint32_t ra[32];
-                        tmem_ld32_async(s_addr + 32 * ch, ra);
-                        const uint32_t bits = seen(ch);
-                        tmem_ld_wait(ra);
-#pragma unroll
-                        for (int i = 0; i < 32; i += 2)
-                            mx = max3(mx, bits >> i & 1u ? __uint_as_float(ra[i]) : -INFINITY, bits >> (i + 1) & 1u ? __uint_as_float(ra[i + 1]) : -INFINITY);
+                for (int h = 0, many = part.rows - tile0 > kHalf ? 2 : 1; h < many; ++h, ++n) {
+                    const bool ends = h + 1 == many && t + part.step >= part.end;
+                    if (!mbar_wait(s_full(x, h), (h ? n1 : n0) & 1u, abort_flag, status)) { alive = false; break; }
+                    if (h) ++n1; else ++n0;
+                    if (!live) {
+                        if (ends && !mbar_wait(pv(x), (n - 1u) & 1u, abort_flag, status)) { alive = false; break; }
+                        if (lane == 0) mbar_arrive(p_full(x, h));
+                        continue;
                     }
-                } else {
-                    uint32_t ra[32], rb[32], rc[32], rd[32];
-                    tmem_ld32_async(s_addr, ra);
-                    tmem_ld32_async(s_addr + 32, rb);
-                    tmem_ld32_async(s_addr + 64, rc);
-                    tmem_ld32_async(s_addr + 96, rd);
-                    tmem_ld_wait(ra);
-                    tmem_ld_wait(rb);
-                    tmem_ld_wait(rc);
-                    tmem_ld_wait(rd);
-                    float ma = __uint_as_float(ra[0]), mb = __uint_as_float(rb[0]), mc = __uint_as_float(rc[0]), md = __uint_as_float(rd[0]);
-#pragma unroll
-                    for (int i = 0; i < 32; i += 2) {
-                        ma = max3(ma, __uint_as_float(ra[i]), __uint_as_float(ra[i + 1]));
-                        mb = max3(mb, __uint_as_float(rb[i]), __uint_as_float(rb[i + 1]));
-                        mc = max3(mc, __uint_as_float(rc[i]), __uint_as_float(rc[i + 1]));
-                        md = max3(md, __uint_as_float(rd[i]), __uint_as_float(rd[i + 1]));
-                    }
-                    mx = max3(max3(ma, mb, mc), md, md);
-                }
-                float factor = 1.f;
-                bool raise = false;
-                if (m == -INFINITY) {
-                    m = mx;                               // what was added before (rows of -inf alone) is nothing
-                    if (m != -INFINITY) l = 0.f;
-                } else if ((mx - m) * c > E::kRaise) {
-                    raise = true;
-                    factor = fast_exp2((m - mx) * c);
-                    m = mx;
-                    l *= factor;
-                } else if (mx != mx) {
-                    l = mx;
-                }
-                const float m_use = m == -INFINITY ? 0.f : m;
-                // S was issued behind the previous tile's P V, and the tensor cores complete in issue order: O is at
-                // rest. TMEM accesses are warp-wide: the other rows multiply by one.
-                if (__any_sync(0xFFFFFFFFu, raise)) {
-#pragma unroll 1
-                    for (int j = 0; j < D / 32; ++j) {
-                        uint32_t ro[32];
-                        tmem_ld32_async(o_addr + 32 * j, ro);
-                        tmem_ld_wait(ro);
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) ro[i] = __float_as_uint(__uint_as_float(ro[i]) * factor);
-                        tmem_st32(o_addr + 32 * j, ro);
-                    }
-                }
-                const float2 nm = make_float2(-m_use, -m_use);
-                float2 sum = make_float2(0.f, 0.f);
-                // 32 columns: P lands on columns of S that were read before
-                auto chunk = [&](const uint32_t (&raw)[32], int ch) {
-                    float2 e[16];
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        // the difference of two scores that are near each other is exact, at any scale
-                        const float2 d = __fadd2_rn(make_float2(__uint_as_float(raw[2 * i]), __uint_as_float(raw[2 * i + 1])), nm);
-                        e[i] = exp2_pair(__ffma2_rn(d, c2, top2), i);
-                    }
+                    tc_fence_after();
+                    const uint32_t addr = s_addr + kHalf * h;
+                    const uint2 gone = infos[2 * ((tg0 + (uint32_t)t) % kInfos) + h];   // absent rows; written before S was asked for
+                    uint32_t v[64];
+                    tmem_load(addr, v);
+                    // columns of the first and the last 32 that the row sees, as bits
+                    const int last = min(limit, it.rows - 1) - tile0 - kHalf * h;
+                    const bool masked = __any_sync(0xFFFFFFFFu, last < kHalf - 1) || (gone.x | gone.y) != 0u;
+                    const uint32_t see0 = (last >= 31 ? 0xFFFFFFFFu : last < 0 ? 0u : (2u << last) - 1u) & ~gone.x;
+                    const uint32_t see1 = (last >= 63 ? 0xFFFFFFFFu : last < 32 ? 0u : (2u << (last - 32)) - 1u) & ~gone.y;
                     if (masked) {
-                        const uint32_t bits = seen(ch);
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            if (!(bits >> (2 * i) & 1u)) e[i].x = 0.f;
-                            if (!(bits >> (2 * i + 1) & 1u)) e[i].y = 0.f;
+                        for (int i = 0; i < 32; ++i) {
+                            if (!(see0 >> i & 1u)) v[i] = 0xFF800000u;
+                            if (!(see1 >> i & 1u)) v[32 + i] = 0xFF800000u;
                         }
                     }
-                    uint32_t pk[16];
+                    float mx4[4];
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        sum = __fadd2_rn(sum, e[i]);
-                        pk[i] = E::pack(e[i].x, e[i].y);
+                    for (int j = 0; j < 4; ++j) {
+                        mx4[j] = __uint_as_float(v[16 * j]);
+#pragma unroll
+                        for (int i = 0; i < 16; i += 2) mx4[j] = max3(mx4[j], __uint_as_float(v[16 * j + i]), __uint_as_float(v[16 * j + i + 1]));
                     }
-                    tmem_st16(s_addr + 16 * ch, pk);
-                };
-                uint32_t ra[32], rb[32];
-                tmem_ld32_async(s_addr, ra);
+                    const float mx = max3(max3(mx4[0], mx4[1], mx4[2]), mx4[3], mx4[3]);
+                    float factor = 1.f;
+                    bool raise = false;
+                    if (m == -INFINITY) {
+                        m = mx;                           // what was added before (rows of -inf alone) is nothing
+                        if (m != -INFINITY) l = 0.f;
+                    } else if ((mx - m) * c > E::kRaise) {
+                        raise = true;
+                        factor = fast_exp2((m - mx) * c);
+                        m = mx;
+                        l *= factor;
+                    } else if (mx != mx) {
+                        l = mx;
+                    }
+                    // TMEM accesses are warp-wide: the other rows multiply by one
+                    if (__any_sync(0xFFFFFFFFu, raise)) {
+                        if (!mbar_wait(pv(x), (n - 1u) & 1u, abort_flag, status)) { alive = false; break; }   // O is at rest then
+                        tc_fence_after();
 #pragma unroll 1
-                for (uint32_t half = 0; half < 2; ++half) {
-                    tmem_ld_wait(ra);
-                    tmem_ld32_async(s_addr + 64 * half + 32, rb);
-                    chunk(ra, 2 * half);
-                    tmem_ld_wait(rb);
-                    if (half == 0) tmem_ld32_async(s_addr + 64, ra);
-                    chunk(rb, 2 * half + 1);
+                        for (int j = 0; j < D / 32; ++j) {
+                            uint32_t ro[32];
+                            tmem_load(o_addr + 32 * j, ro);
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) ro[i] = __float_as_uint(__uint_as_float(ro[i]) * factor);
+                            tmem_st32(o_addr + 32 * j, ro);
+                        }
+                    }
+                    const float m_use = m == -INFINITY ? 0.f : m;
+                    const float2 nm = make_float2(-m_use, -m_use);
+                    float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+                    uint32_t pk[32];
+                    auto exps = [&](auto mask_tag) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) {
+                            // the difference of two scores that are near each other is exact, at any scale
+                            const float2 d = __fadd2_rn(make_float2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])), nm);
+                            const float2 y = __ffma2_rn(d, c2, top2);
+                            const float2 e = decltype(mask_tag)::value ? make_float2(fast_exp2(y.x), fast_exp2(y.y)) : exp2_pair(y, i);
+                            sum[i & 1] = __fadd2_rn(sum[i & 1], e);
+                            pk[i] = E::pack(e.x, e.y);
+                        }
+                    };
+                    if (masked) exps(std::true_type{});   // the special-function unit gives an exact zero for -inf
+                    else exps(std::false_type{});
+                    tmem_st32(addr, pk);
+                    l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
                     tmem_st_wait();
+                    // before the item's last product: the one in front of it is done, so that the wait below is for that one phase
+                    if (ends && !mbar_wait(pv(x), (n - 1u) & 1u, abort_flag, status)) { alive = false; break; }
                     tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(p_half(x, half));
+                    if (lane == 0) mbar_arrive(p_full(x, h));
                 }
-                l += sum.x + sum.y;
             }
             if (!alive) break;
             tg0 += (uint32_t)tiles;
-            bool some = most > t0;                        // the team's O holds something
+            const bool some = part.first < part.end;      // the team's O holds something
             if (some) {
-                if (!mbar_wait(pv_done(x), ni & 1u, abort_flag, status)) { alive = false; break; }
+                if (!mbar_wait(pv(x), (n - 1u) & 1u, abort_flag, status)) { alive = false; break; }
                 tc_fence_after();
-                ++ni;
             }
             bool some1 = false;                           // the second team's O of a single query tile does
             float m1 = -INFINITY, f0 = 1.f, f1 = 0.f;
@@ -661,15 +703,13 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                         for (int i = 0; i < 32; ++i) f[i] = 0.f;
                         if (some) {
                             uint32_t ro[32];
-                            tmem_ld32_async(o_addr + 32 * j, ro);
-                            tmem_ld_wait(ro);
+                            tmem_load(o_addr + 32 * j, ro);
 #pragma unroll
                             for (int i = 0; i < 32; ++i) f[i] = none ? 0.f : __uint_as_float(ro[i]) * f0;
                         }
                         if (some1) {
                             uint32_t ro[32];
-                            tmem_ld32_async(tmem_o(1) + lane_sel + 32 * j, ro);
-                            tmem_ld_wait(ro);
+                            tmem_load(tmem_o(1) + lane_sel + 32 * j, ro);
 #pragma unroll
                             for (int i = 0; i < 32; ++i)
                                 if (m1 != -INFINITY) f[i] = fmaf(__uint_as_float(ro[i]), f1, f[i]);
