@@ -3,8 +3,6 @@
 //   x[j] = scale * <q, k_j>,   out = sum_j softmax(x)_j v_j,   lse = log sum_j exp(x_j)
 #include "ec_chunk.cuh"
 
-#include <type_traits>
-
 namespace ec {
 
 namespace {
@@ -16,6 +14,8 @@ constexpr int kInfos = 8;                        // absent rows of the tiles in 
 constexpr int kTmemCols = 512;                   // S of both teams (2 x 128 columns), O of both teams (2 x up to 128)
 constexpr int kUnitRows = 256;                   // cost of a unit beside its rows
 constexpr int kLeastRows = 768;                  // smallest share of a CTA
+constexpr float kLowest = -3.402823466e38f;      // a running maximum that has seen nothing: below every score, and -inf less it is still -inf
+constexpr float kLarge = 16777216.f;
 
 template <int DTYPE> struct Elem;
 template <> struct Elem<EC_BF16> {
@@ -62,7 +62,7 @@ struct Item {
 
 struct Parts {                                   // workspace
     float4 *o;                                   // [2 CTAs][2 teams][D / 4][128]
-    float2 *ml;                                  // [2 CTAs][2 teams][128] running maximum (not scaled), sum
+    float2 *ml;                                  // [2 CTAs][2 teams][128] running maximum (scaled), sum
 };
 
 __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32])
@@ -535,7 +535,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
         const uint32_t lane_sel = (uint32_t)(q4 * 32) << 16;
         const uint32_t s_addr = tmem_s(x) + lane_sel, o_addr = tmem_o(x) + lane_sel;
         const float c = a.scale_log2e;
-        const float2 c2 = make_float2(c, c), top2 = make_float2(E::kTop, E::kTop);
+        const float2 c2 = make_float2(c, c);
         const int my_token = r / a.G, my_head = r - my_token * a.G;
         uint32_t n = 0, n0 = 0, n1 = 0, tg0 = 0, nr = 0, no = 0;   // the team's halves; the CTA's tiles; rendezvous; results taken over
         auto meet = [&]() {
@@ -557,7 +557,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
             const int limit = it.limit + skip + my_token;                                   // last row that this row sees
             const bool valid = my_token < ntok, live = q4 * 32 < ntok * a.G;                // live: some row of the warp counts
             const Part part = part_of(it, x);
-            float m = -INFINITY, l = 0.f;                 // running maximum (not scaled), sum
+            float m = -INFINITY, m2 = kLowest, l = 0.f;   // running maximum (not scaled; scaled), sum
 #pragma unroll 1
             for (int t = part.first; t < part.end && alive; t += part.step) {
                 const int tile0 = (it.kt0 + t) * kTileRows;
@@ -596,18 +596,20 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                         for (int i = 0; i < 16; i += 2) mx4[j] = max3(mx4[j], __uint_as_float(v[16 * j + i]), __uint_as_float(v[16 * j + i + 1]));
                     }
                     const float mx = max3(max3(mx4[0], mx4[1], mx4[2]), mx4[3], mx4[3]);
+                    // The running maximum is m; exponents are counted from m2 = m * c, rounded: a rounding that all of the row shares
                     float factor = 1.f;
                     bool raise = false;
-                    if (m == -INFINITY) {
-                        m = mx;                           // what was added before (rows of -inf alone) is nothing
-                        if (m != -INFINITY) l = 0.f;
-                    } else if ((mx - m) * c > E::kRaise) {
-                        raise = true;
-                        factor = fast_exp2((m - mx) * c);
+                    if (!(fmaf(mx, c, -m2) <= E::kRaise)) {               // also the first rows that are not all hidden, and NaN
+                        const float to = mx * c;
+                        if (m == -INFINITY) {
+                            l = 0.f;                      // what was added before (rows of -inf alone) is nothing
+                        } else {
+                            raise = true;
+                            factor = fast_exp2(m2 - to);
+                            l *= factor;
+                        }
                         m = mx;
-                        l *= factor;
-                    } else if (mx != mx) {
-                        l = mx;
+                        m2 = to;
                     }
                     // TMEM accesses are warp-wide: the other rows multiply by one
                     if (__any_sync(0xFFFFFFFFu, raise)) {
@@ -622,23 +624,32 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                             tmem_st32(o_addr + 32 * j, ro);
                         }
                     }
-                    const float m_use = m == -INFINITY ? 0.f : m;
-                    const float2 nm = make_float2(-m_use, -m_use);
+                    const float from = E::kTop - m2;
+                    const float2 from2 = make_float2(from, from);
                     float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
                     uint32_t pk[32];
-                    auto exps = [&](auto mask_tag) {
+                    // Scores so large that m2's rounding would show in the exponent (half a step of 2^24 and more): the
+                    // difference of two scores that are near each other is exact before the scale.
+                    const bool large = __any_sync(0xFFFFFFFFu, fabsf(m2) > kLarge && m2 != kLowest);
+                    if (!large) {
 #pragma unroll
                         for (int i = 0; i < 32; ++i) {
-                            // the difference of two scores that are near each other is exact, at any scale
-                            const float2 d = __fadd2_rn(make_float2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])), nm);
-                            const float2 y = __ffma2_rn(d, c2, top2);
-                            const float2 e = decltype(mask_tag)::value ? make_float2(fast_exp2(y.x), fast_exp2(y.y)) : exp2_pair(y, i);
+                            const float2 y = __ffma2_rn(make_float2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])), c2, from2);
+                            const float2 e = make_float2(fast_exp2(y.x), fast_exp2(y.y));
                             sum[i & 1] = __fadd2_rn(sum[i & 1], e);
                             pk[i] = E::pack(e.x, e.y);
                         }
-                    };
-                    if (masked) exps(std::true_type{});   // the special-function unit gives an exact zero for -inf
-                    else exps(std::false_type{});
+                    } else {
+                        const bool far = fabsf(m2) > kLarge;
+                        const float rest = E::kTop + (far ? 0.f : fmaf(m, c, -m2)), use = m == -INFINITY ? 0.f : m;
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) {
+                            const float2 e = make_float2(fast_exp2(fmaf(__uint_as_float(v[2 * i]) - use, c, rest)),
+                                                         fast_exp2(fmaf(__uint_as_float(v[2 * i + 1]) - use, c, rest)));
+                            sum[i & 1] = __fadd2_rn(sum[i & 1], e);
+                            pk[i] = E::pack(e.x, e.y);
+                        }
+                    }
                     tmem_st32(addr, pk);
                     l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
                     tmem_st_wait();
@@ -657,10 +668,10 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                 tc_fence_after();
             }
             bool some1 = false;                           // the second team's O of a single query tile does
-            float m1 = -INFINITY, f0 = 1.f, f1 = 0.f;
+            float f0 = 1.f, f1 = 0.f;
             if (!pair && tiles > 1) {
                 if (x == 1) {
-                    other_s[r] = make_float2(m, l);
+                    other_s[r] = make_float2(m2, l);
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(other_done);
@@ -670,12 +681,11 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                     const float2 ml = other_s[r];
                     ++no;
                     some1 = true;
-                    m1 = ml.x;
-                    const float top = max3(m, m1, m1), use = top == -INFINITY ? 0.f : top;
-                    f0 = fast_exp2((m - use) * c);
-                    f1 = fast_exp2((m1 - use) * c);
+                    const float top = max3(m2, ml.x, ml.x);
+                    f0 = fast_exp2(m2 - top);
+                    f1 = fast_exp2(ml.x - top);
                     l = l * f0 + ml.y * f1;
-                    m = top;
+                    m2 = top;
                 }
             }
             if (pair || x == 0) {
@@ -691,9 +701,9 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                                            E::pack(g[4] * inv, g[5] * inv), E::pack(g[6] * inv, g[7] * inv));
                     }
                 };
-                auto log_sum = [&](float mt, float lt) { return mt == -INFINITY && lt == lt ? -INFINITY : fmaf(mt, c, log2f(lt) - E::kTop) * kLn2; };
+                auto log_sum = [&](float mt, float lt) { return mt == kLowest && lt == lt ? -INFINITY : (mt + (log2f(lt) - E::kTop)) * kLn2; };
                 const size_t at = (size_t)it.slot * 2 + x;
-                const bool none = m == -INFINITY && l == l;               // the row sees nothing, or scores of -inf alone
+                const bool none = m2 == kLowest && l == l;               // the row sees nothing, or scores of -inf alone
                 const float inv = none ? 0.f : 1.f / l;
                 if (live) {
 #pragma unroll 1
@@ -711,8 +721,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                             uint32_t ro[32];
                             tmem_load(tmem_o(1) + lane_sel + 32 * j, ro);
 #pragma unroll
-                            for (int i = 0; i < 32; ++i)
-                                if (m1 != -INFINITY) f[i] = fmaf(__uint_as_float(ro[i]), f1, f[i]);
+                            for (int i = 0; i < 32; ++i) f[i] = none ? 0.f : fmaf(__uint_as_float(ro[i]), f1, f[i]);
                         }
                         if (dirty) {
 #pragma unroll
@@ -728,8 +737,8 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                                 __stcg(parts.o + (at * (D / 4) + 8 * j + i) * kTileRows + r, make_float4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]));
                         }
                     }
-                    if (valid && it.parts == 0 && lse) lse[token * a.Hq + head] = log_sum(m, l);
-                    if (valid && it.parts > 0) __stcg(parts.ml + at * kTileRows + r, make_float2(m, some ? l : 0.f));
+                    if (valid && it.parts == 0 && lse) lse[token * a.Hq + head] = log_sum(m2, l);
+                    if (valid && it.parts > 0) __stcg(parts.ml + at * kTileRows + r, make_float2(m2, some ? l : 0.f));
                 }
                 tc_fence_before();
                 __syncwarp();
@@ -754,10 +763,9 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                         for (int row = lane; row < (ntok * a.G + 31) / 32 * 32; row += 32) {
                             const int in = row / a.G;
                             if (in >= ntok) continue;
-                            float M = -INFINITY;
+                            float M = kLowest;
 #pragma unroll 4
                             for (int p = 0; p < it.parts; ++p) M = fmaxf(M, __ldcg(parts.ml + part_at(p) * kTileRows + row).x);
-                            const float mu = M == -INFINITY ? 0.f : M;
                             float sum = 0.f, f[32] = {};
 #pragma unroll 2
                             for (int p = 0; p < it.parts; ++p) {
@@ -765,9 +773,9 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                                 float4 o[D / 16];
 #pragma unroll
                                 for (int i = 0; i < D / 16; ++i) o[i] = __ldcg(parts.o + (part_at(p) * (D / 4) + q4 * (D / 16) + i) * kTileRows + row);
-                                const float g = fast_exp2((ml.x - mu) * c);
+                                const float g = fast_exp2(ml.x - M);
                                 sum = fmaf(ml.y, g, sum);
-                                if (ml.x == -INFINITY) continue;          // nothing was seen: its sums are none
+                                if (ml.x == kLowest) continue;          // nothing was seen: its sums are none
 #pragma unroll
                                 for (int i = 0; i < D / 16; ++i) {
                                     f[4 * i] = fmaf(o[i].x, g, f[4 * i]);
@@ -776,7 +784,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                                     f[4 * i + 3] = fmaf(o[i].w, g, f[4 * i + 3]);
                                 }
                             }
-                            const float scale = M == -INFINITY && sum == sum ? 0.f : 1.f / sum;
+                            const float scale = M == kLowest && sum == sum ? 0.f : 1.f / sum;
                             const size_t tk = (size_t)it.token + skip + in, hd = (size_t)it.h * a.G + (row - in * a.G);
                             uint4 *to = reinterpret_cast<uint4 *>(out + (int64_t)tk * out_token + (int64_t)hd * out_head + q4 * (D / 4));
 #pragma unroll
