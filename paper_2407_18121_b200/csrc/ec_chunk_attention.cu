@@ -8,7 +8,7 @@ namespace ec {
 namespace {
 
 constexpr int kThreads = 384;                    // warps: copies, products of a team, value check, products of the other, 4 + 4 softmax
-constexpr int kHalf = 64;                        // rows whose S a team works on at a time; the next 64 are under way
+constexpr int kHalf = 64;                        // columns of S that a thread holds at a time; P V of the first runs under the second
 constexpr int kItems = 4;                        // descriptions of work ahead
 constexpr int kInfos = 8;                        // absent rows of the tiles in flight (the rings hold 4 at most)
 constexpr int kTmemCols = 512;                   // S of both teams (2 x 128 columns), O of both teams (2 x up to 128)
@@ -135,6 +135,27 @@ __device__ __forceinline__ float max3(float a, float b, float c)
     return d;
 }
 
+// Of 32 columns from `col` on, as bits, those in which one of the rows begin .. end - 1 has a value that is not finite. A slow way
+// that healthy values never take.
+template <uint32_t EXPONENT>
+__device__ __forceinline__ uint32_t spoilt(const ChunkArgs &a, int n, int h, int begin, int end, int col)
+{
+    uint32_t bits = 0u;
+#pragma unroll 1
+    for (int row = begin; row < end; ++row) {
+        const Slot s = look_up_slot(a.c, n, row);
+        if (!valid_page(a.c, s)) continue;
+        const uint32_t *v = reinterpret_cast<const uint32_t *>(a.c.V + row_offset(a.c, s) + (size_t)h * a.c.head_step) + col / 2;
+#pragma unroll 1
+        for (int j = 0; j < 16; ++j) {
+            const uint32_t e = v[j] & EXPONENT;
+            if ((e & 0xFFFFu) == (EXPONENT & 0xFFFFu)) bits |= 1u << (2 * j);
+            if (e >> 16 == EXPONENT >> 16) bits |= 2u << (2 * j);
+        }
+    }
+    return bits;
+}
+
 template <int D>
 struct Smem {
     static constexpr int kTile = kTileRows * D * 2;
@@ -143,17 +164,16 @@ struct Smem {
     static constexpr int kK = 2 * kTile;
     static constexpr int kV = kK + kKs * kTile;
     static constexpr int kOther = kV + kVs * kTile;                       // [128] maximum and sum of the second team
-    static constexpr int kBad = kOther + kTileRows * 8;                   // [items][D] 16 bits, see the value check
-    static constexpr int kBadAny = kBad + kItems * D * 2;                 // [items]
+    static constexpr int kBadAny = kOther + kTileRows * 8;                    // [items] whether a value that is not finite became zero
     static constexpr int kItem = kBadAny + kItems * 4;
     static constexpr int kInfo = kItem + kItems * (int)sizeof(Item);
     static constexpr int kBars = kInfo + kInfos * 16;
-    // q_full, q_empty, k_full[], k_empty[], v_full[], v_empty[], per team: s_full[2], p_full[2], pv, o_free, rdv; other_done; item_full, item_empty
+    // q_full, q_empty, k_full[], k_empty[], v_full[], v_empty[], per team: s_full, p_full[2], pv, o_free, rdv, pv_half; other_done; item_full, item_empty
     static constexpr int kNumBars = 2 + 2 * kKs + 2 * kVs + 2 * 7 + 1 + 2 * kItems;
     static constexpr int kTmemSlot = kBars + kNumBars * 8;
     static constexpr int kAbort = kTmemSlot + 4;
     static constexpr int kLast = kAbort + 4;                              // [2] whether this CTA joins the unit's parts
-    static constexpr int kCount = kLast + 8;                              // [3] see Counts
+    static constexpr int kCount = kLast + 8;                              // [3], see where they are used
     static constexpr int kTotal = kCount + 12;
     static_assert(kTotal <= 232448, "shared memory of a block");
 };
@@ -186,13 +206,14 @@ __device__ __forceinline__ bool reached(const int *count, int least, volatile in
 template <int D, int DTYPE>
 __global__ void __launch_bounds__(kThreads, 1)
 chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
-                       const __grid_constant__ CUtensorMap map_v, const ChunkArgs a, uint16_t *__restrict__ out, int64_t out_token,
+                       const __grid_constant__ CUtensorMap map_v, const __grid_constant__ ChunkArgs a, uint16_t *__restrict__ out, int64_t out_token,
                        int64_t out_head, float *__restrict__ lse, const Parts parts)
 {
     using L = Smem<D>;
     using E = Elem<DTYPE>;
     constexpr int kTile = L::kTile, kKs = L::kKs, kVs = L::kVs;
     constexpr int kBoxBytes = kTileRows * 128;
+    constexpr uint32_t kIdescS = (1u << 4) | (E::kFormat << 7) | (E::kFormat << 10) | ((kTileRows >> 3) << 17) | ((kTileRows >> 4) << 24);
     constexpr uint32_t kIdescO = (1u << 4) | (E::kFormat << 7) | (E::kFormat << 10) | (1u << 16) | ((D >> 3) << 17) | ((kTileRows >> 4) << 24);
 
     extern __shared__ __align__(1024) uint8_t smem[];
@@ -204,18 +225,18 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
     auto v_full = [&](uint32_t s) { return bar(2 + 2 * kKs + s); };
     auto v_empty = [&](uint32_t s) { return bar(2 + 2 * kKs + kVs + s); };
     constexpr int kT0 = 2 + 2 * kKs + 2 * kVs;
-    auto s_full = [&](uint32_t x, uint32_t h) { return bar(kT0 + 7 * x + h); };
-    auto p_full = [&](uint32_t x, uint32_t h) { return bar(kT0 + 7 * x + 2 + h); };
-    auto pv = [&](uint32_t x) { return bar(kT0 + 7 * x + 4); };
-    auto o_free = [&](uint32_t x) { return bar(kT0 + 7 * x + 5); };
-    auto rdv = [&](uint32_t x) { return bar(kT0 + 7 * x + 6); };
+    auto s_full = [&](uint32_t x) { return bar(kT0 + 7 * x); };
+    auto p_full = [&](uint32_t x, uint32_t h) { return bar(kT0 + 7 * x + 1 + h); };
+    auto pv = [&](uint32_t x) { return bar(kT0 + 7 * x + 3); };
+    auto o_free = [&](uint32_t x) { return bar(kT0 + 7 * x + 4); };
+    auto rdv = [&](uint32_t x) { return bar(kT0 + 7 * x + 5); };
+    auto pv_half = [&](uint32_t x) { return bar(kT0 + 7 * x + 6); };
     const uint32_t other_done = bar(kT0 + 14);
     auto item_full = [&](uint32_t k) { return bar(kT0 + 15 + k); };
     auto item_empty = [&](uint32_t k) { return bar(kT0 + 15 + kItems + k); };
     Item *items = reinterpret_cast<Item *>(smem + L::kItem);
-    uint2 *infos = reinterpret_cast<uint2 *>(smem + L::kInfo);           // [kInfos][2 halves]
     float2 *other_s = reinterpret_cast<float2 *>(smem + L::kOther);
-    uint32_t *bad = reinterpret_cast<uint32_t *>(smem + L::kBad);
+    uint2 *infos = reinterpret_cast<uint2 *>(smem + L::kInfo);           // [kInfos][2 halves]
     volatile int *bad_any = reinterpret_cast<volatile int *>(smem + L::kBadAny);
     volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(smem + L::kTmemSlot);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + L::kAbort);
@@ -235,18 +256,17 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
         for (uint32_t s = 0; s < (uint32_t)kKs; ++s) { mbar_init(k_full(s), 1); mbar_init(k_empty(s), 2); }
         for (uint32_t s = 0; s < (uint32_t)kVs; ++s) { mbar_init(v_full(s), 1); mbar_init(v_empty(s), 2); }
         for (uint32_t x = 0; x < 2; ++x) {
-            for (uint32_t h = 0; h < 2; ++h) {
-                mbar_init(s_full(x, h), 1);
-                mbar_init(p_full(x, h), 4);
-            }
+            mbar_init(s_full(x), 1);
+            for (uint32_t h = 0; h < 2; ++h) mbar_init(p_full(x, h), 4);
             mbar_init(pv(x), 1);
+            mbar_init(pv_half(x), 1);
             mbar_init(o_free(x), 4);
             mbar_init(rdv(x), 4);
         }
         mbar_init(other_done, 4);
         for (uint32_t k = 0; k < (uint32_t)kItems; ++k) {
             mbar_init(item_full(k), 1);
-            mbar_init(item_empty(k), 2 + 1 + 8);                         // the products' threads, the value check, the softmax warps
+            mbar_init(item_empty(k), 2 + 1 + 8);                         // the products' thread, the value check, the softmax warps
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_to_async();
@@ -372,8 +392,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
         // ------------------------------------------------------------ products of a team
         if (lane == 0) {
             const uint32_t x = (uint32_t)warp >> 1;
-            uint32_t tg0 = 0, nq = 0, np = 0, ni = 0;     // the CTA's tiles and query loads; the team's halves and items so far
-            uint32_t nh[2] = {0, 0};
+            uint32_t tg0 = 0, nq = 0, np = 0, ni = 0;     // the CTA's tiles and query loads, the team's tiles and items so far
             auto wait = [&](uint32_t b, uint32_t phase) {
                 if (!mbar_wait(b, phase & 1u, abort_flag, status, kWaitLimitNs, kPollBackoffNs)) alive = false;
                 return alive;
@@ -387,16 +406,14 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                 umma_commit(b);
                 if (alone) umma_commit(b);
             };
-            // S of 64 rows: N = 64
-            constexpr uint32_t kIdescS = (1u << 4) | (E::kFormat << 7) | (E::kFormat << 10) | ((kHalf >> 3) << 17) | ((kTileRows >> 4) << 24);
-            auto issue_s = [&](uint32_t qt, uint32_t ks, uint32_t h) {
-                const uint64_t da = umma_desc(base + L::kQ + qt * kTile), db = umma_desc(base + L::kK + ks * kTile + h * (kHalf * 128));
+            auto issue_s = [&](uint32_t qt, uint32_t ks) {
+                const uint64_t da = umma_desc(base + L::kQ + qt * kTile), db = umma_desc(base + L::kK + ks * kTile);
 #pragma unroll
                 for (int kk = 0; kk < D / 16; ++kk) {
                     const uint32_t off = ((uint32_t)(kk / 4) * kBoxBytes + (uint32_t)(kk % 4) * 32u) >> 4;
-                    umma_bf16(tmem_s(x) + h * kHalf, da + off, db + off, kIdescS, kk > 0 ? 1u : 0u);
+                    umma_bf16(tmem_s(x), da + off, db + off, kIdescS, kk > 0 ? 1u : 0u);
                 }
-                umma_commit(s_full(x, h));
+                umma_commit(s_full(x));
             };
             for (uint32_t k = 0; alive; ++k) {
                 const uint32_t sl = k % kItems;
@@ -415,14 +432,12 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                 tg0 += (uint32_t)tiles;
                 ++nq;
                 if (mine.first >= mine.end) continue;
-                auto halves = [&](int t) { return mine.rows - (it.kt0 + t) * kTileRows > kHalf ? 2 : 1; };
                 if (!wait_count(q_asked, nq) || !wait(q_full, nq - 1u)) break;
                 {
                     const uint32_t ks = (tg + mine.first) % kKs;
                     if (!wait_count(k_asked, tg + mine.first + 1) || !wait(k_full(ks), (tg + mine.first) / kKs)) break;
                     tc_fence_after();
-                    issue_s(qt, ks, 0);
-                    if (halves(mine.first) > 1) issue_s(qt, ks, 1);
+                    issue_s(qt, ks);
                     release(k_empty(ks), alone(mine.first));
                     if (mine.first + mine.step >= mine.end) release(q_empty, all_mine);
                 }
@@ -432,53 +447,45 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                 for (int t = mine.first; t < mine.end && alive; t += mine.step) {
                     const int then = t + mine.step;
                     const uint32_t vs = (tg + t) % kVs, ks = (tg + then) % kKs;
-                    const int many = halves(t), steps = min(kTileRows / 16, (mine.rows - (it.kt0 + t) * kTileRows + 15) / 16);
-                    const int ahead = then < mine.end ? halves(then) : 0;
+                    const int steps = min(kTileRows / 16, (mine.rows - (it.kt0 + t) * kTileRows + 15) / 16);
                     if (!wait_count(v_checked, tg + t + 1)) break;
                     const uint64_t dv = umma_desc_mn(base + L::kV + vs * kTile, kBoxBytes, 1024u);
 #pragma unroll
                     for (uint32_t h = 0; h < 2; ++h) {
-                        if ((int)h >= many) continue;
-                        // O += P V of 64 rows, 16 an instruction; then at once S of as many rows of the next tile, over this P
-                        if (!wait(p_full(x, h), nh[h])) break;
-                        ++nh[h];
+                        // O += P V of 64 rows, 16 an instruction
+                        if (!wait(p_full(x, h), np)) break;
                         tc_fence_after();
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
                             const int kk = 4 * (int)h + i;
                             if (kk < steps) umma_ts(tmem_o(x), tmem_s(x) + h * kHalf + 8u * i, dv + kk * (2048u >> 4), kIdescO, t == mine.first && kk == 0 ? 0u : 1u);
                         }
-                        umma_commit(pv(x));
-                        ++np;
-                        if ((int)h < ahead) {
-                            if (h == 0) {
-                                if (!wait_count(k_asked, tg + then + 1) || !wait(k_full(ks), (tg + then) / kKs)) break;
-                                tc_fence_after();
-                            }
-                            issue_s(qt, ks, h);
-                        }
+                        if (h == 0) umma_commit(pv_half(x));
                     }
                     if (!alive) break;
-                    release(v_empty(vs), alone(t));
-                    if (ahead > 0) {
+                    ++np;
+                    if (then >= mine.end) umma_commit(pv(x));
+                    if (then < mine.end) {                // S of the next tile, over this P
+                        if (!wait_count(k_asked, tg + then + 1) || !wait(k_full(ks), (tg + then) / kKs)) break;
+                        tc_fence_after();
+                        issue_s(qt, ks);
                         release(k_empty(ks), alone(then));
                         if (then + mine.step >= mine.end) release(q_empty, all_mine);
                     }
+                    release(v_empty(vs), alone(t));
                 }
             }
         }
     } else if (warp == 2) {
         // ------------------------------------------------------------ value check
         // A product with P = 0 does not hide a value that is not finite, so tiles whose rows some token must not see are
-        // looked over: such values become zeros, and the first row that has one is noted for every column (16 bits, counted from
-        // the last row that the first token sees), for the tokens that do see it. Rows behind the last one (memory that holds anything) and absent rows become zeros too.
+        // looked over: such values become zeros, and the item is marked, for the tokens that do see them. Rows behind the last one
+        // (memory that holds anything) and absent rows become zeros too.
         uint32_t tg = 0;
         for (uint32_t k = 0; alive; ++k) {
             const uint32_t sl = k % kItems;
             if (!mbar_wait(item_full(sl), (k / kItems) & 1u, abort_flag, status, kWaitLimitNs, kPollBackoffNs)) { alive = false; break; }
             const Item it = items[sl];
-            uint32_t *mine = bad + sl * (D / 2);
-            for (int d = lane; d < D / 2; d += 32) mine[d] = 0xFFFFFFFFu;
             if (lane == 0) bad_any[sl] = 0;
             __syncwarp();
             if (it.n < 0) break;
@@ -488,7 +495,8 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                 const int row0 = t * kTileRows, rows = min(kTileRows, it.rows - row0);
                 const uint2 gone0 = infos[2 * (tg % kInfos)], gone1 = infos[2 * (tg % kInfos) + 1];
                 const bool any_absent = (gone0.x | gone0.y | gone1.x | gone1.y) != 0u;
-                const int check = any_absent ? 0 : max(0, it.limit + 1 - row0);           // rows before are seen by every token
+                const int hidden = max(0, it.limit + 1 - row0);                            // rows before are seen by every token
+                const int check = any_absent ? 0 : hidden;
                 const int end = (rows + 15) & ~15;
                 if (check < end) {
                     uint8_t *tile = smem + L::kV + s * kTile;
@@ -501,6 +509,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                             *at = make_uint4(0u, 0u, 0u, 0u);
                             continue;
                         }
+                        if (r < hidden) continue;
                         uint4 v = *at;
                         uint32_t w[4] = {v.x, v.y, v.z, v.w};
                         bool found = false;
@@ -508,12 +517,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                         for (int j = 0; j < 4; ++j) {
                             const uint32_t e = w[j] & E::kExponent;
                             const bool lo = (e & 0xFFFFu) == (E::kExponent & 0xFFFFu), hi = (e >> 16) == (E::kExponent >> 16);
-                            if (lo || hi) {
-                                const uint32_t row = (uint32_t)max(row0 + r - it.limit, 0), note = (lo ? row : 0xFFFFu) | (hi ? row : 0xFFFFu) << 16;
-                                uint32_t was = mine[c * 4 + j], got;
-                                while ((got = atomicCAS(mine + c * 4 + j, was, __vminu2(was, note))) != was) was = got;
-                                w[j] &= (lo ? 0u : 0xFFFFu) | (hi ? 0u : 0xFFFF0000u);
-                            }
+                            w[j] &= (lo ? 0u : 0xFFFFu) | (hi ? 0u : 0xFFFF0000u);
                             found |= lo || hi;
                         }
                         if (found) {
@@ -533,11 +537,11 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
         const uint32_t x = (uint32_t)(warp - 4) >> 2;
         const int q4 = warp & 3, r = q4 * 32 + lane;
         const uint32_t lane_sel = (uint32_t)(q4 * 32) << 16;
-        const uint32_t s_addr = tmem_s(x) + lane_sel, o_addr = tmem_o(x) + lane_sel;
+        const uint32_t s_addr = tmem_s(x) + lane_sel;
         const float c = a.scale_log2e;
         const float2 c2 = make_float2(c, c);
         const int my_token = r / a.G, my_head = r - my_token * a.G;
-        uint32_t n = 0, n0 = 0, n1 = 0, tg0 = 0, nr = 0, no = 0;   // the team's halves; the CTA's tiles; rendezvous; results taken over
+        uint32_t ns = 0, ni = 0, tg0 = 0, nr = 0, no = 0;  // the team's tiles and items; the CTA's tiles; meetings; results taken over
         auto meet = [&]() {
             __syncwarp();
             if (lane == 0) mbar_arrive(rdv(x));
@@ -558,120 +562,120 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
             const bool valid = my_token < ntok, live = q4 * 32 < ntok * a.G;                // live: some row of the warp counts
             const Part part = part_of(it, x);
             float m = -INFINITY, m2 = kLowest, l = 0.f;   // running maximum (not scaled; scaled), sum
+            const int plain_to = min(__shfl_sync(0xFFFFFFFFu, limit, 0), it.rows - 1);       // of a warp's rows the first one sees the least
 #pragma unroll 1
-            for (int t = part.first; t < part.end && alive; t += part.step) {
-                const int tile0 = (it.kt0 + t) * kTileRows;
-#pragma unroll 1
-                for (int h = 0, many = part.rows - tile0 > kHalf ? 2 : 1; h < many; ++h, ++n) {
-                    const bool ends = h + 1 == many && t + part.step >= part.end;
-                    if (!mbar_wait(s_full(x, h), (h ? n1 : n0) & 1u, abort_flag, status)) { alive = false; break; }
-                    if (h) ++n1; else ++n0;
-                    if (!live) {
-                        if (ends && !mbar_wait(pv(x), (n - 1u) & 1u, abort_flag, status)) { alive = false; break; }
-                        if (lane == 0) mbar_arrive(p_full(x, h));
-                        continue;
-                    }
+            for (int i = 2 * part.first; i < 2 * part.end; i += (i & 1) ? 2 * part.step - 1 : 1) {
+                const int h = i & 1, t = i >> 1;          // a half of tile t
+                if (h == 0) {
+                    if (!mbar_wait(s_full(x), ns & 1u, abort_flag, status)) { alive = false; break; }
+                    ++ns;
                     tc_fence_after();
-                    const uint32_t addr = s_addr + kHalf * h;
-                    const uint2 gone = infos[2 * ((tg0 + (uint32_t)t) % kInfos) + h];   // absent rows; written before S was asked for
-                    uint32_t v[64];
+                }
+                const uint32_t addr = s_addr + kHalf * h;
+                const int col0 = (it.kt0 + t) * kTileRows + h * kHalf;
+                uint32_t pk[32];
+                float2 sum = make_float2(0.f, 0.f);
+                if (live) {
+                    uint32_t v[kHalf];
                     tmem_load(addr, v);
-                    // columns of the first and the last 32 that the row sees, as bits
-                    const int last = min(limit, it.rows - 1) - tile0 - kHalf * h;
-                    const bool masked = __any_sync(0xFFFFFFFFu, last < kHalf - 1) || (gone.x | gone.y) != 0u;
-                    const uint32_t see0 = (last >= 31 ? 0xFFFFFFFFu : last < 0 ? 0u : (2u << last) - 1u) & ~gone.x;
-                    const uint32_t see1 = (last >= 63 ? 0xFFFFFFFFu : last < 32 ? 0u : (2u << (last - 32)) - 1u) & ~gone.y;
-                    if (masked) {
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) {
-                            if (!(see0 >> i & 1u)) v[i] = 0xFF800000u;
-                            if (!(see1 >> i & 1u)) v[32 + i] = 0xFF800000u;
-                        }
-                    }
+                    // The running maximum is m; exponents are counted from m2 = m * c, rounded: a rounding that all of the row shares.
+                    // Hidden columns make this one too large at most.
                     float mx4[4];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         mx4[j] = __uint_as_float(v[16 * j]);
 #pragma unroll
-                        for (int i = 0; i < 16; i += 2) mx4[j] = max3(mx4[j], __uint_as_float(v[16 * j + i]), __uint_as_float(v[16 * j + i + 1]));
+                        for (int k2 = 0; k2 < 16; k2 += 2) mx4[j] = max3(mx4[j], __uint_as_float(v[16 * j + k2]), __uint_as_float(v[16 * j + k2 + 1]));
                     }
                     const float mx = max3(max3(mx4[0], mx4[1], mx4[2]), mx4[3], mx4[3]);
-                    // The running maximum is m; exponents are counted from m2 = m * c, rounded: a rounding that all of the row shares
-                    float factor = 1.f;
-                    bool raise = false;
-                    if (!(fmaf(mx, c, -m2) <= E::kRaise)) {               // also the first rows that are not all hidden, and NaN
-                        const float to = mx * c;
-                        if (m == -INFINITY) {
-                            l = 0.f;                      // what was added before (rows of -inf alone) is nothing
-                        } else {
-                            raise = true;
-                            factor = fast_exp2(m2 - to);
-                            l *= factor;
-                        }
-                        m = mx;
-                        m2 = to;
-                    }
-                    // TMEM accesses are warp-wide: the other rows multiply by one
-                    if (__any_sync(0xFFFFFFFFu, raise)) {
-                        if (!mbar_wait(pv(x), (n - 1u) & 1u, abort_flag, status)) { alive = false; break; }   // O is at rest then
-                        tc_fence_after();
-#pragma unroll 1
-                        for (int j = 0; j < D / 32; ++j) {
-                            uint32_t ro[32];
-                            tmem_load(o_addr + 32 * j, ro);
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) ro[i] = __float_as_uint(__uint_as_float(ro[i]) * factor);
-                            tmem_st32(o_addr + 32 * j, ro);
-                        }
-                    }
+                    const uint2 gone = infos[2 * ((tg0 + (uint32_t)t) % kInfos) + h];      // absent rows
+                    const bool plain = plain_to >= col0 + kHalf - 1 && (gone.x | gone.y) == 0u;
                     const float from = E::kTop - m2;
                     const float2 from2 = make_float2(from, from);
-                    float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-                    uint32_t pk[32];
-                    // Scores so large that m2's rounding would show in the exponent (half a step of 2^24 and more): the
-                    // difference of two scores that are near each other is exact before the scale.
-                    const bool large = __any_sync(0xFFFFFFFFu, fabsf(m2) > kLarge && m2 != kLowest);
-                    if (!large) {
+                    if (plain && __all_sync(0xFFFFFFFFu, fmaf(mx, c, -m2) <= E::kRaise && fabsf(m2) <= kLarge)) {
+                        // almost always: nothing hidden, no new maximum
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) {
-                            const float2 y = __ffma2_rn(make_float2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])), c2, from2);
-                            const float2 e = make_float2(fast_exp2(y.x), fast_exp2(y.y));
-                            sum[i & 1] = __fadd2_rn(sum[i & 1], e);
-                            pk[i] = E::pack(e.x, e.y);
+                        for (int k2 = 0; k2 < 32; ++k2) {
+                            const float2 e = exp2_pair(__ffma2_rn(make_float2(__uint_as_float(v[2 * k2]), __uint_as_float(v[2 * k2 + 1])), c2, from2), k2);
+                            sum = __fadd2_rn(sum, e);
+                            pk[k2] = E::pack(e.x, e.y);
                         }
                     } else {
+                        // columns of the first and the last 32 that the row sees, as bits
+                        const int last = min(limit, it.rows - 1) - col0;
+                        const uint32_t see[2] = {(last >= 31 ? 0xFFFFFFFFu : last < 0 ? 0u : (2u << last) - 1u) & ~gone.x,
+                                                 (last >= 63 ? 0xFFFFFFFFu : last < 32 ? 0u : (2u << (last - 32)) - 1u) & ~gone.y};
+                        float top = -INFINITY;
+#pragma unroll
+                        for (int k2 = 0; k2 < 32; ++k2) {
+                            if (!(see[0] >> k2 & 1u)) v[k2] = 0xFF800000u;
+                            if (!(see[1] >> k2 & 1u)) v[32 + k2] = 0xFF800000u;
+                            top = max3(top, __uint_as_float(v[k2]), __uint_as_float(v[32 + k2]));
+                        }
+                        float factor = 1.f;
+                        bool raise = false;
+                        if (!(fmaf(top, c, -m2) <= E::kRaise)) {          // also the first rows that are not all hidden, and NaN
+                            const float to = top * c;
+                            if (m == -INFINITY) {
+                                l = 0.f;                  // what was added before (rows of -inf alone) is nothing
+                            } else {
+                                raise = true;
+                                factor = fast_exp2(m2 - to);
+                                l *= factor;
+                            }
+                            m = top;
+                            m2 = to;
+                        }
+                        // TMEM accesses are warp-wide: the other rows multiply by one
+                        if (__any_sync(0xFFFFFFFFu, raise)) {
+                            // S was issued behind the previous tile's P V, and the tensor cores complete in issue order: O is at
+                            // rest, but for the product with the tile's own first half
+                            if (h == 1) {
+                                if (!mbar_wait(pv_half(x), (ns & 1u) ^ 1u, abort_flag, status)) { alive = false; break; }
+                                tc_fence_after();
+                            }
+#pragma unroll 1
+                            for (int j = 0; j < D / 32; ++j) {
+                                tmem_load(tmem_o(x) + lane_sel + 32 * j, pk);
+#pragma unroll
+                                for (int k2 = 0; k2 < 32; ++k2) pk[k2] = __float_as_uint(__uint_as_float(pk[k2]) * factor);
+                                tmem_st32(tmem_o(x) + lane_sel + 32 * j, pk);
+                            }
+                            tmem_st_wait();
+                        }
+                        // Scores so large that m2's rounding would show in the exponent (half a step of 2^24 and more): the
+                        // difference of two scores that are near each other is exact before the scale.
                         const bool far = fabsf(m2) > kLarge;
                         const float rest = E::kTop + (far ? 0.f : fmaf(m, c, -m2)), use = m == -INFINITY ? 0.f : m;
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) {
-                            const float2 e = make_float2(fast_exp2(fmaf(__uint_as_float(v[2 * i]) - use, c, rest)),
-                                                         fast_exp2(fmaf(__uint_as_float(v[2 * i + 1]) - use, c, rest)));
-                            sum[i & 1] = __fadd2_rn(sum[i & 1], e);
-                            pk[i] = E::pack(e.x, e.y);
+                        for (int k2 = 0; k2 < 32; ++k2) { // an exact zero for -inf
+                            const float2 e = make_float2(fast_exp2(fmaf(__uint_as_float(v[2 * k2]) - use, c, rest)),
+                                                         fast_exp2(fmaf(__uint_as_float(v[2 * k2 + 1]) - use, c, rest)));
+                            sum = __fadd2_rn(sum, e);
+                            pk[k2] = E::pack(e.x, e.y);
                         }
                     }
                     tmem_st32(addr, pk);
-                    l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+                    l += sum.x + sum.y;
                     tmem_st_wait();
-                    // before the item's last product: the one in front of it is done, so that the wait below is for that one phase
-                    if (ends && !mbar_wait(pv(x), (n - 1u) & 1u, abort_flag, status)) { alive = false; break; }
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(p_full(x, h));
                 }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(p_full(x, h));
             }
             if (!alive) break;
             tg0 += (uint32_t)tiles;
             const bool some = part.first < part.end;      // the team's O holds something
             if (some) {
-                if (!mbar_wait(pv(x), (n - 1u) & 1u, abort_flag, status)) { alive = false; break; }
+                if (!mbar_wait(pv(x), ni & 1u, abort_flag, status)) { alive = false; break; }
+                ++ni;
                 tc_fence_after();
             }
             bool some1 = false;                           // the second team's O of a single query tile does
             float f0 = 1.f, f1 = 0.f;
             if (!pair && tiles > 1) {
                 if (x == 1) {
-                    other_s[r] = make_float2(m2, l);
+                    other_s[r] = make_float2(m2, l);      // read before o_free(1) lets the team's next product go ahead
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(other_done);
@@ -690,10 +694,9 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
             }
             if (pair || x == 0) {
                 const bool dirty = bad_any[sl] != 0;
-                const uint16_t *mine = reinterpret_cast<const uint16_t *>(bad + sl * (D / 2));
                 const size_t token = (size_t)it.token + skip + my_token, head = (size_t)it.h * a.G + my_head;
-                auto store = [&](uint16_t *row, const float (&f)[32], int j, float inv) {
-                    uint4 *to = reinterpret_cast<uint4 *>(row + 32 * j);
+                auto store = [&](uint16_t *row, const float (&f)[32], float inv) {
+                    uint4 *to = reinterpret_cast<uint4 *>(row);
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
                         const float *g = f + 8 * q;
@@ -708,33 +711,36 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                 if (live) {
 #pragma unroll 1
                     for (int j = 0; j < D / 32; ++j) {
+                        const int col = 32 * j;
                         float f[32];
 #pragma unroll
                         for (int i = 0; i < 32; ++i) f[i] = 0.f;
                         if (some) {
                             uint32_t ro[32];
-                            tmem_load(o_addr + 32 * j, ro);
+                            tmem_load(tmem_o(x) + lane_sel + col, ro);
 #pragma unroll
                             for (int i = 0; i < 32; ++i) f[i] = none ? 0.f : __uint_as_float(ro[i]) * f0;
                         }
                         if (some1) {
                             uint32_t ro[32];
-                            tmem_load(tmem_o(1) + lane_sel + 32 * j, ro);
+                            tmem_load(tmem_o(1) + lane_sel + col, ro);
 #pragma unroll
                             for (int i = 0; i < 32; ++i) f[i] = none ? 0.f : fmaf(__uint_as_float(ro[i]), f1, f[i]);
                         }
-                        if (dirty) {
+                        if (dirty && valid) {             // rows of this CTA that not every token of the item sees
+                            const uint32_t bits = spoilt<E::kExponent>(a, it.n, it.h, max(max(it.limit + 1, 0), it.kt0 * kTileRows),
+                                                                       min(min(limit + 1, it.rows), it.kt1 * kTileRows), col);
 #pragma unroll
                             for (int i = 0; i < 32; ++i)
-                                if (mine[32 * j + i] <= skip + my_token) f[i] = __int_as_float(0x7FFFFFFF);
+                                if (bits >> i & 1u) f[i] = __int_as_float(0x7FFFFFFF);
                         }
                         if (!valid) continue;
                         if (it.parts == 0) {
-                            store(out + (int64_t)token * out_token + (int64_t)head * out_head, f, j, inv);
+                            store(out + (int64_t)token * out_token + (int64_t)head * out_head + col, f, inv);
                         } else {
 #pragma unroll
                             for (int i = 0; i < 8; ++i)
-                                __stcg(parts.o + (at * (D / 4) + 8 * j + i) * kTileRows + r, make_float4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]));
+                                __stcg(parts.o + (at * (D / 4) + col / 4 + i) * kTileRows + r, make_float4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]));
                         }
                     }
                     if (valid && it.parts == 0 && lse) lse[token * a.Hq + head] = log_sum(m2, l);
@@ -764,9 +770,9 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                             const int in = row / a.G;
                             if (in >= ntok) continue;
                             float M = kLowest;
-#pragma unroll 4
+#pragma unroll 8
                             for (int p = 0; p < it.parts; ++p) M = fmaxf(M, __ldcg(parts.ml + part_at(p) * kTileRows + row).x);
-                            float sum = 0.f, f[32] = {};
+                            float sum = 0.f, f[D / 4] = {};
 #pragma unroll 2
                             for (int p = 0; p < it.parts; ++p) {
                                 const float2 ml = __ldcg(parts.ml + part_at(p) * kTileRows + row);
@@ -775,7 +781,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                                 for (int i = 0; i < D / 16; ++i) o[i] = __ldcg(parts.o + (part_at(p) * (D / 4) + q4 * (D / 16) + i) * kTileRows + row);
                                 const float g = fast_exp2(ml.x - M);
                                 sum = fmaf(ml.y, g, sum);
-                                if (ml.x == kLowest) continue;          // nothing was seen: its sums are none
+                                if (ml.x == kLowest) continue;            // nothing was seen: its sums are none
 #pragma unroll
                                 for (int i = 0; i < D / 16; ++i) {
                                     f[4 * i] = fmaf(o[i].x, g, f[4 * i]);
