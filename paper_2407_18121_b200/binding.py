@@ -637,16 +637,14 @@ def ec_rotary_frequencies(rot: int, base: float = 10000.0, scaling: int = EC_ROT
 
 
 def _rows(t: torch.Tensor, name: str, dtype: torch.dtype, shape: tuple, device: int):
-    """Pointer and strides (all but the last) of rows that are contiguous along D; a stride along an axis of extent 1 is never used,
-    a dense one stands in for it."""
-    if t.dtype is not dtype or t.shape != shape or t.get_device() != device or t.stride(-1) != 1:
+    """Pointer, token and head stride of packed rows [tokens, heads, D] that are contiguous along D. A stride along an axis of extent 1
+    is never used, a dense one stands in for it."""
+    s = t.stride()
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != device or s[2] != 1:
         raise ValueError(f"{name} must be a {dtype} tensor {list(shape)} with contiguous rows on device {device}, "
-                         f"got {t.dtype} {list(t.shape)}, strides {list(t.stride())}, on {t.device}")
-    strides, dense = [], shape[-1]
-    for extent, stride in zip(reversed(shape[:-1]), reversed(t.stride()[:-1])):
-        strides.append(stride if extent > 1 else dense)
-        dense = max(dense, strides[-1]) * max(extent, 1)
-    return (t.data_ptr(), *reversed(strides))
+                         f"got {t.dtype} {list(t.shape)}, strides {list(s)}, on {t.device}")
+    tokens, heads, D = shape
+    return t.data_ptr(), s[0] if tokens > 1 else heads * D, s[1] if heads > 1 else D
 
 
 def ec_rotary(x: torch.Tensor, out: torch.Tensor, positions: torch.Tensor, freqs: Optional[torch.Tensor], rot: int, interleaved: bool,
@@ -660,13 +658,17 @@ def ec_rotary(x: torch.Tensor, out: torch.Tensor, positions: torch.Tensor, freqs
     if dev < 0:
         raise ValueError("x must lie on a CUDA device")
     stream = _paged_stream(dev)
-    px = _rows(x, "x", x.dtype, tuple(x.shape), dev)
-    po = _rows(out, "out", x.dtype, tuple(x.shape), dev)
+    if out.dtype is not x.dtype or out.shape != x.shape or out.get_device() != dev or x.stride(3) != 1 or out.stride(3) != 1:
+        raise ValueError("out must be like x, rows of both contiguous along D")
+
+    def strides(t):                              # of axes of extent 1, never used: dense ones
+        n, tk, h, _ = t.stride()
+        return n if N > 1 else 0, tk if T > 1 else heads * D, h if heads > 1 else D
     if positions.dtype is not torch.int32 or positions.get_device() != dev or positions.shape not in ((N, T), (T,)) or \
             (T > 1 and positions.stride(-1) != 1):
         raise ValueError("positions must be int32 [N, T] or [T] on x's device")
     pos_n = positions.stride(0) if positions.dim() == 2 and N > 1 else 0
-    st = lib().ec_rotary(*px, *po, positions.data_ptr(), pos_n, _want(freqs, "freqs", torch.float64, (int(rot) // 2,), dev), N, T, heads, D,
+    st = lib().ec_rotary(x.data_ptr(), *strides(x), out.data_ptr(), *strides(out), positions.data_ptr(), pos_n, _want(freqs, "freqs", torch.float64, (int(rot) // 2,), dev), N, T, heads, D,
                          _ELEM[x.dtype], int(rot), int(bool(interleaved)), factor, int(bool(inverse)), stream)
     _check(st, "ec_rotary")
 

@@ -23,6 +23,7 @@ struct ChunkArgs {
     int tile_tokens;                             // tokens of a 128-row query tile: 128 / G
     int box_rows;                                // rows of a copy of cached rows
     float scale_log2e;
+    double inv_ctas;                             // 1 / CTAs of the launch
 };
 
 // Counters behind the state block's other ones: of the CTAs that share a unit, the first one's are counted up.
@@ -68,12 +69,23 @@ __device__ __forceinline__ Problem read_problem(const Args &a, int n)
 // A place in the batch's work. Work is counted in 64 bits (rows for the attention, tokens for the weights); every unit of
 // it (a pair of query tiles of a head, a block of cached rows of a head) costs its contraction and a constant for what
 // surrounds it. Costs have a closed form, so that no CTA has to walk over the units in front of its own:
-//   U::units(a, p)          units of a head of problem p
-//   U::before(a, p, i)      cost of its units 0 .. i - 1
+//   U::units(a, p)             units of a head of problem p
+//   U::before(a, p, units, i)  cost of its units 0 .. i - 1
 template <typename U, typename Args>
 __device__ __forceinline__ long long head_cost(const Args &a, const Problem &p)
 {
-    return p.count > 0 ? U::before(a, p, U::units(a, p)) : 0;
+    if (p.count == 0) return 0;
+    const int units = U::units(a, p);
+    return U::before(a, p, units, units);
+}
+
+// a / b for a quotient of less than 2^20: an estimate, put right (a division of 64 bits takes ten times as long).
+__device__ __forceinline__ int quotient(long long a, long long b)
+{
+    int q = (int)__fdividef((float)a, (float)b);
+    while ((q + 1) * b <= a) ++q;
+    while (q * b > a) --q;
+    return q;
 }
 
 struct Share {
@@ -99,7 +111,8 @@ __device__ __forceinline__ Share make_share(const Args &a, long long least)
     }
     const long long total = __shfl_sync(0xFFFFFFFFu, incl, 31);
     Share s;
-    s.per = max(least, (total + gridDim.x - 1) / gridDim.x);
+    // any share that covers the work will do: no exact division
+    s.per = max(least, (long long)((double)total * a.inv_ctas) + (total >> 50) + 1);
     s.first = s.per * blockIdx.x;
     s.last = min(total, s.first + s.per);
     s.n = 0;
@@ -137,17 +150,17 @@ struct Walk {
         n = s.n;
         p = read_problem(a, n);
         units = U::units(a, p);
-        const long long head = head_cost<U>(a, p), in = s.first - s.before;
-        h = (int)(in / head);
+        const long long head = U::before(a, p, units, units), in = s.first - s.before;
+        h = quotient(in, head);
         const long long rest = in - h * head;
         int lo = 0, hi = units - 1;              // the last unit that does not begin behind `rest`
         while (lo < hi) {
             const int mid = (lo + hi + 1) >> 1;
-            if (U::before(a, p, mid) <= rest) lo = mid;
+            if (U::before(a, p, units, mid) <= rest) lo = mid;
             else hi = mid - 1;
         }
         i = lo;
-        at = s.before + h * head + U::before(a, p, i);
+        at = s.before + h * head + U::before(a, p, units, i);
         return true;
     }
 

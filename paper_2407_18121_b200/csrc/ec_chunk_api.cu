@@ -78,6 +78,7 @@ ec::ChunkArgs chunk(const ec_paged *c, const int32_t *starts, const int32_t *cou
     a.tile_tokens = ec::kTileRows / a.G;
     a.box_rows = ec::box_rows_of(c->page_size);
     a.scale_log2e = scale * 1.4426950408889634f;
+    a.inv_ctas = 1.0 / ec::chunk_grid();
     return a;
 }
 

@@ -39,10 +39,10 @@ template <> struct Elem<EC_FP16> {
 
 struct PairUnits {                               // a unit: two adjacent query tiles of a head
     static __device__ __forceinline__ int units(const ChunkArgs &a, const Problem &p) { return (p.count + 2 * a.tile_tokens - 1) / (2 * a.tile_tokens); }
-    static __device__ __forceinline__ long long before(const ChunkArgs &a, const Problem &p, int i)
+    static __device__ __forceinline__ long long before(const ChunkArgs &a, const Problem &p, int units, int i)
     {
         const long long base = max(p.len - p.count, 0), step = 2 * a.tile_tokens;
-        const int full = units(a, p) - 1;
+        const int full = units - 1;
         const long long k = i <= full ? i : full;
         long long cost = k * (base + kUnitRows) + step * (k * (k + 1) / 2);
         if (i > full) cost += base + p.count + kUnitRows;
@@ -203,6 +203,67 @@ __device__ __forceinline__ bool reached(const int *count, int least, volatile in
     }
 }
 
+// Natural log-sum-exp from the maximum (log2) and the sum.
+template <typename E>
+__device__ __forceinline__ float log_sum(float m2, float l)
+{
+    return m2 == kLowest && l == l ? -INFINITY : (m2 + (log2f(l) - E::kTop)) * kLn2;
+}
+
+// Joins the parts of a unit's query tile, in the order of the rows: a warp of the team takes 32 rows at a time and a quarter of their
+// columns, and has two parts in flight.
+template <int D, int DTYPE>
+__device__ __forceinline__ void join_parts(const Parts parts, int first, int many, int x, int ntok, int G, uint16_t *out, int64_t out_token,
+                                        int64_t out_head, float *lse, int Hq)
+{
+    using E = Elem<DTYPE>;
+    const int lane = threadIdx.x & 31, q4 = (threadIdx.x >> 5) & 3;
+#pragma unroll 1
+    for (int row = lane; row < ntok * G; row += 32) {
+        float M = kLowest, sum = 0.f, f[D / 4] = {};
+#pragma unroll 1
+        for (int p = 0; p < many; p += 2) {
+            float2 ml[2] = {make_float2(kLowest, 0.f), make_float2(kLowest, 0.f)};
+            float4 o[2][D / 16];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                if (p + u >= many) continue;
+                const size_t from = (size_t)(2 * (first + p + u) + (p + u == 0)) * 2 + x;
+                ml[u] = __ldcg(parts.ml + from * kTileRows + row);
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i) o[u][i] = __ldcg(parts.o + (from * (D / 4) + q4 * (D / 16) + i) * kTileRows + row);
+            }
+            const float top = max3(M, ml[0].x, ml[1].x), old = fast_exp2(M - top);
+            const float g[2] = {fast_exp2(ml[0].x - top), fast_exp2(ml[1].x - top)};
+            M = top;
+            sum = fmaf(ml[1].y, g[1], fmaf(ml[0].y, g[0], sum * old));
+#pragma unroll
+            for (int i = 0; i < D / 4; ++i) f[i] *= old;
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                if (ml[u].x == kLowest) continue;         // nothing was seen, or no such part
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i) {
+                    f[4 * i] = fmaf(o[u][i].x, g[u], f[4 * i]);
+                    f[4 * i + 1] = fmaf(o[u][i].y, g[u], f[4 * i + 1]);
+                    f[4 * i + 2] = fmaf(o[u][i].z, g[u], f[4 * i + 2]);
+                    f[4 * i + 3] = fmaf(o[u][i].w, g[u], f[4 * i + 3]);
+                }
+            }
+        }
+        const float scale = M == kLowest && sum == sum ? 0.f : 1.f / sum;
+        const int in = row / G, head = row - in * G;
+        uint4 *to = reinterpret_cast<uint4 *>(out + in * out_token + head * out_head + q4 * (D / 4));
+#pragma unroll
+        for (int q = 0; q < D / 32; ++q) {
+            const float *g = f + 8 * q;
+            to[q] = make_uint4(E::pack(g[0] * scale, g[1] * scale), E::pack(g[2] * scale, g[3] * scale), E::pack(g[4] * scale, g[5] * scale),
+                               E::pack(g[6] * scale, g[7] * scale));
+        }
+        if (q4 == 0 && lse) lse[(int64_t)in * Hq + head] = log_sum<E>(M, sum);
+    }
+}
+
 template <int D, int DTYPE>
 __global__ void __launch_bounds__(kThreads, 1)
 chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
@@ -304,8 +365,12 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
     };
     bool alive = true;
 
+    // A thread of the softmax holds 64 scores and as many addresses as the epilogue needs: 4 warps x 88 + 8 x 208 registers are the
+    // 12 x 168 of the launch.
+    auto fewer_registers = [] { asm volatile("setmaxnreg.dec.sync.aligned.u32 88;"); };
     if (warp == 0) {
         // ------------------------------------------------------------ plan and copies
+        fewer_registers();
         Walk<PairUnits> w;
         bool more = w.begin(a, kLeastRows);
         uint32_t tg = 0, nk = 0, nv = 0, nq = 0;           // tiles; copies of K, V and queries started
@@ -324,14 +389,14 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                 it.limit = w.p.len - w.p.count + w.i * step;
                 it.rows = max(0, min(w.p.len, it.limit + it.ntok));
                 const int tiles = (it.rows + kTileRows - 1) / kTileRows;
-                cost = PairUnits::before(a, w.p, w.i + 1) - PairUnits::before(a, w.p, w.i);
+                cost = PairUnits::before(a, w.p, w.units, w.i + 1) - PairUnits::before(a, w.p, w.units, w.i);
                 const long long from = max(w.s.first - w.at, 0ll), to = min(w.s.last - w.at, cost);
                 auto tile_at = [&](long long x) { return (int)min(max((x - kUnitRows) / kTileRows, 0ll), (long long)tiles); };
                 it.kt0 = from == 0 ? 0 : tile_at(from);
                 it.kt1 = to >= cost ? tiles : tile_at(to);
                 if (from > 0 || to < cost) {
-                    it.first = (int)(w.at / w.s.per);
-                    it.parts = (int)((w.at + cost - 1) / w.s.per) - it.first + 1;
+                    it.first = quotient(w.at, w.s.per);
+                    it.parts = quotient(w.at + cost - 1, w.s.per) - it.first + 1;
                     it.slot = 2 * (int)blockIdx.x + (from == 0);
                 }
             }
@@ -390,6 +455,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
         }
     } else if (warp == 1 || warp == 3) {
         // ------------------------------------------------------------ products of a team
+        fewer_registers();
         if (lane == 0) {
             const uint32_t x = (uint32_t)warp >> 1;
             uint32_t tg0 = 0, nq = 0, np = 0, ni = 0;     // the CTA's tiles and query loads, the team's tiles and items so far
@@ -478,6 +544,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
         }
     } else if (warp == 2) {
         // ------------------------------------------------------------ value check
+        fewer_registers();
         // A product with P = 0 does not hide a value that is not finite, so tiles whose rows some token must not see are
         // looked over: such values become zeros, and the item is marked, for the tokens that do see them. Rows behind the last one
         // (memory that holds anything) and absent rows become zeros too.
@@ -534,6 +601,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
         }
     } else if (warp >= 4) {
         // ------------------------------------------------------------ softmax: a thread owns a query row
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
         const uint32_t x = (uint32_t)(warp - 4) >> 2;
         const int q4 = warp & 3, r = q4 * 32 + lane;
         const uint32_t lane_sel = (uint32_t)(q4 * 32) << 16;
@@ -704,7 +772,6 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                                            E::pack(g[4] * inv, g[5] * inv), E::pack(g[6] * inv, g[7] * inv));
                     }
                 };
-                auto log_sum = [&](float mt, float lt) { return mt == kLowest && lt == lt ? -INFINITY : (mt + (log2f(lt) - E::kTop)) * kLn2; };
                 const size_t at = (size_t)it.slot * 2 + x;
                 const bool none = m2 == kLowest && l == l;               // the row sees nothing, or scores of -inf alone
                 const float inv = none ? 0.f : 1.f / l;
@@ -743,7 +810,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                                 __stcg(parts.o + (at * (D / 4) + col / 4 + i) * kTileRows + r, make_float4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]));
                         }
                     }
-                    if (valid && it.parts == 0 && lse) lse[token * a.Hq + head] = log_sum(m2, l);
+                    if (valid && it.parts == 0 && lse) lse[token * a.Hq + head] = log_sum<E>(m2, l);
                     if (valid && it.parts > 0) __stcg(parts.ml + at * kTileRows + r, make_float2(m2, some ? l : 0.f));
                 }
                 tc_fence_before();
@@ -763,44 +830,9 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                     }
                     if (!meet()) { alive = false; break; }
                     if (last_s[x]) {
-                        // a warp takes 32 rows at a time and a quarter of their columns
-                        auto part_at = [&](int p) { return (size_t)(2 * (it.first + p) + (p == 0)) * 2 + x; };
-#pragma unroll 1
-                        for (int row = lane; row < (ntok * a.G + 31) / 32 * 32; row += 32) {
-                            const int in = row / a.G;
-                            if (in >= ntok) continue;
-                            float M = kLowest;
-#pragma unroll 8
-                            for (int p = 0; p < it.parts; ++p) M = fmaxf(M, __ldcg(parts.ml + part_at(p) * kTileRows + row).x);
-                            float sum = 0.f, f[D / 4] = {};
-#pragma unroll 2
-                            for (int p = 0; p < it.parts; ++p) {
-                                const float2 ml = __ldcg(parts.ml + part_at(p) * kTileRows + row);
-                                float4 o[D / 16];
-#pragma unroll
-                                for (int i = 0; i < D / 16; ++i) o[i] = __ldcg(parts.o + (part_at(p) * (D / 4) + q4 * (D / 16) + i) * kTileRows + row);
-                                const float g = fast_exp2(ml.x - M);
-                                sum = fmaf(ml.y, g, sum);
-                                if (ml.x == kLowest) continue;            // nothing was seen: its sums are none
-#pragma unroll
-                                for (int i = 0; i < D / 16; ++i) {
-                                    f[4 * i] = fmaf(o[i].x, g, f[4 * i]);
-                                    f[4 * i + 1] = fmaf(o[i].y, g, f[4 * i + 1]);
-                                    f[4 * i + 2] = fmaf(o[i].z, g, f[4 * i + 2]);
-                                    f[4 * i + 3] = fmaf(o[i].w, g, f[4 * i + 3]);
-                                }
-                            }
-                            const float scale = M == kLowest && sum == sum ? 0.f : 1.f / sum;
-                            const size_t tk = (size_t)it.token + skip + in, hd = (size_t)it.h * a.G + (row - in * a.G);
-                            uint4 *to = reinterpret_cast<uint4 *>(out + (int64_t)tk * out_token + (int64_t)hd * out_head + q4 * (D / 4));
-#pragma unroll
-                            for (int q = 0; q < D / 32; ++q) {
-                                const float *g = f + 8 * q;
-                                to[q] = make_uint4(E::pack(g[0] * scale, g[1] * scale), E::pack(g[2] * scale, g[3] * scale),
-                                                   E::pack(g[4] * scale, g[5] * scale), E::pack(g[6] * scale, g[7] * scale));
-                            }
-                            if (q4 == 0 && lse) lse[tk * a.Hq + hd] = log_sum(M, sum);
-                        }
+                        join_parts<D, DTYPE>(parts, it.first, it.parts, (int)x, ntok, a.G,
+                                             out + ((int64_t)it.token + skip) * out_token + (int64_t)it.h * a.G * out_head, out_token, out_head,
+                                             lse ? lse + ((int64_t)it.token + skip) * a.Hq + (int64_t)it.h * a.G : nullptr, a.Hq);
                     }
                 }
             }

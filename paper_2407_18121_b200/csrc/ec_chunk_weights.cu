@@ -25,7 +25,7 @@ struct WeightArgs : ChunkArgs {
 
 struct BlockUnits {                              // a unit: kBlockRows cached rows of a head; its cost is counted in tokens
     static __device__ __forceinline__ int units(const WeightArgs &, const Problem &p) { return (p.len + kBlockRows - 1) / kBlockRows; }
-    static __device__ __forceinline__ long long before(const WeightArgs &a, const Problem &p, int i)
+    static __device__ __forceinline__ long long before(const WeightArgs &a, const Problem &p, int, int i)
     {
         // block j is first seen by token max(0, kBlockRows j - base)
         const long long base = p.len - p.count, fixed = (long long)kUnitTiles * a.tile_tokens;
@@ -160,7 +160,7 @@ chunk_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 it.start = w.p.start;
                 it.count = w.p.count;
                 const int begin = max(0, it.row0 - (it.len - it.count)) / a.tile_tokens, end = (it.count + a.tile_tokens - 1) / a.tile_tokens;
-                cost = BlockUnits::before(a, w.p, w.i + 1) - BlockUnits::before(a, w.p, w.i);
+                cost = BlockUnits::before(a, w.p, w.units, w.i + 1) - BlockUnits::before(a, w.p, w.units, w.i);
                 const long long from = max(w.s.first - w.at, 0ll), to = min(w.s.last - w.at, cost);
                 auto tile_at = [&](long long x) {
                     return (int)min(max(x / a.tile_tokens - kUnitTiles, 0ll) + begin, (long long)end);
@@ -168,8 +168,8 @@ chunk_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 it.qt0 = from == 0 ? begin : tile_at(from);
                 it.qt1 = to >= cost ? end : tile_at(to);
                 if (from > 0 || to < cost) {
-                    it.first = (int)(w.at / w.s.per);
-                    it.parts = (int)((w.at + cost - 1) / w.s.per) - it.first + 1;
+                    it.first = quotient(w.at, w.s.per);
+                    it.parts = quotient(w.at + cost - 1, w.s.per) - it.first + 1;
                     it.slot = 2 * (int)blockIdx.x + (from == 0);
                 }
             }
@@ -178,11 +178,14 @@ chunk_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             if (lane == 0) mbar_arrive(item_full(sl));
             if (!more) break;
             if (it.qt0 < it.qt1) {
+                TilePages all[kTeams];                    // read side by side
+#pragma unroll
+                for (int x = 0; x < kTeams; ++x) all[x] = tile_pages(a, it.n, it.row0 + x * kTileRows, it.len);
 #pragma unroll
                 for (uint32_t x = 0; x < (uint32_t)kTeams; ++x) {
                     const int row0 = it.row0 + (int)x * kTileRows;
                     if (row0 >= it.len) continue;
-                    TilePages pages = tile_pages(a, it.n, row0, it.len);
+                    TilePages &pages = all[x];
                     const uint32_t bytes = (uint32_t)check_pages(a, pages) * (uint32_t)a.box_rows * D * 2u;
                     if (!mbar_wait(k_empty(x), (nk[x] & 1u) ^ 1u, abort_flag, status, kWaitLimitNs, kPollBackoffNs)) { alive = false; break; }
                     if (lane == 0) mbar_expect_tx(k_full(x), bytes);
