@@ -183,6 +183,42 @@ struct Walk {
     }
 };
 
+// What this CTA has of a unit: its tiles t0 .. t1 - 1 (the unit's are 0 .. tiles - 1), and, where the unit is shared, with whom.
+struct Cut {
+    bool mine;                                   // false: nothing, another CTA sees to it
+    int t0, t1;
+    int first, parts;                            // parts > 0: CTAs first .. first + parts - 1 share it
+};
+
+// The unit lies at `at` in the work, costs `fixed` and `grain` a tile. Short units are not shared (handing parts over takes as long as
+// some tiles do): the CTA that holds their middle has them. Of the others every CTA that takes part has a tile at least.
+constexpr int kWholeTiles = 3;
+
+__device__ __forceinline__ Cut cut_unit(const Share &s, long long at, long long cost, int fixed, int grain, int tiles)
+{
+    const int me = (int)blockIdx.x;
+    Cut cut;
+    cut.t0 = 0;
+    cut.t1 = tiles;
+    cut.parts = 0;
+    if (tiles <= kWholeTiles) {
+        cut.first = quotient(at + min(cost, (long long)fixed + tiles * grain / 2) - 1, s.per);
+        cut.mine = cut.first == me;
+        return cut;
+    }
+    cut.first = quotient(at + fixed + grain - 1, s.per);
+    const int last = quotient(at + min(cost, fixed + (long long)grain * tiles) - 1, s.per);
+    auto tile_at = [&](int cta) {                // the first tile that begins behind the CTA's first place
+        const long long x = cta * s.per - at - fixed;
+        return x <= 0 ? 0 : min((int)((unsigned)x / (unsigned)grain), tiles);
+    };
+    cut.mine = me >= cut.first && me <= last;
+    if (me > cut.first) cut.t0 = tile_at(me);
+    if (me < last) cut.t1 = tile_at(me + 1);
+    if (last > cut.first) cut.parts = last - cut.first + 1;
+    return cut;
+}
+
 inline int box_rows_of(int page_size)
 {
     int b = 1;

@@ -12,8 +12,8 @@ constexpr int kHalf = 64;                        // columns of S that a thread h
 constexpr int kItems = 4;                        // descriptions of work ahead
 constexpr int kInfos = 8;                        // absent rows of the tiles in flight (the rings hold 4 at most)
 constexpr int kTmemCols = 512;                   // S of both teams (2 x 128 columns), O of both teams (2 x up to 128)
-constexpr int kUnitRows = 256;                   // cost of a unit beside its rows
-constexpr int kLeastRows = 768;                  // smallest share of a CTA
+constexpr int kUnitRows = 384;                   // cost of a unit beside its rows
+constexpr int kLeastRows = 640;                  // smallest share of a CTA
 constexpr float kLowest = -3.402823466e38f;      // a running maximum that has seen nothing: below every score, and -inf less it is still -inf
 constexpr float kLarge = 16777216.f;
 
@@ -376,34 +376,50 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
         uint32_t tg = 0, nk = 0, nv = 0, nq = 0;           // tiles; copies of K, V and queries started
         for (uint32_t k = 0; alive; ++k) {
             const uint32_t sl = k % kItems;
-            if (!mbar_wait(item_empty(sl), ((k / kItems) & 1u) ^ 1u, abort_flag, status, kWaitLimitNs, kPollBackoffNs)) { alive = false; break; }
             Item it = {};
             it.n = -1;
             long long cost = 0;
-            if (more) {
+            while (more) {                                // the next unit that this CTA has something of
                 const int step = 2 * a.tile_tokens;
-                it.n = w.n;
-                it.h = w.h;
-                it.token = w.p.start + w.i * step;
                 it.ntok = min(step, w.p.count - w.i * step);
                 it.limit = w.p.len - w.p.count + w.i * step;
                 it.rows = max(0, min(w.p.len, it.limit + it.ntok));
-                const int tiles = (it.rows + kTileRows - 1) / kTileRows;
                 cost = PairUnits::before(a, w.p, w.units, w.i + 1) - PairUnits::before(a, w.p, w.units, w.i);
-                const long long from = max(w.s.first - w.at, 0ll), to = min(w.s.last - w.at, cost);
-                auto tile_at = [&](long long x) { return (int)min(max((x - kUnitRows) / kTileRows, 0ll), (long long)tiles); };
-                it.kt0 = from == 0 ? 0 : tile_at(from);
-                it.kt1 = to >= cost ? tiles : tile_at(to);
-                if (from > 0 || to < cost) {
-                    it.first = quotient(w.at, w.s.per);
-                    it.parts = quotient(w.at + cost - 1, w.s.per) - it.first + 1;
-                    it.slot = 2 * (int)blockIdx.x + (from == 0);
+                const Cut cut = cut_unit(w.s, w.at, cost, kUnitRows, kTileRows, (it.rows + kTileRows - 1) / kTileRows);
+                if (cut.mine) {
+                    it.n = w.n;
+                    it.h = w.h;
+                    it.token = w.p.start + w.i * step;
+                    it.kt0 = cut.t0;
+                    it.kt1 = cut.t1;
+                    it.first = cut.first;
+                    it.parts = cut.parts;
+                    it.slot = 2 * (int)blockIdx.x + (cut.first == (int)blockIdx.x);
+                    break;
                 }
+                more = w.next(a, cost);
             }
+            if (!mbar_wait(item_empty(sl), ((k / kItems) & 1u) ^ 1u, abort_flag, status, kWaitLimitNs, kPollBackoffNs)) { alive = false; break; }
             if (lane == 0) items[sl] = it;
             __syncwarp();
             if (lane == 0) mbar_arrive(item_full(sl));
             if (!more) break;
+            auto copy_queries = [&] {
+                if (lane == 0) {
+                    const int tiles = it.ntok > a.tile_tokens ? 2 : 1;
+                    mbar_expect_tx(q_full, (uint32_t)(tiles * a.tile_tokens * a.G * D * 2));
+                    publish(q_asked, (int)nq + 1);
+                    for (int x = 0; x < tiles; ++x)
+#pragma unroll
+                        for (int half = 0; half < D / 64; ++half)
+                            tma_load_3d(base + L::kQ + x * kTile + half * kBoxBytes, &map_q, half * 64, it.h * a.G,
+                                        it.token + x * a.tile_tokens, q_full);
+                }
+                ++nq;
+            };
+            // the queries first when their place is free, else behind the first tile's rows
+            bool asked = it.kt0 >= it.kt1 || __all_sync(0xFFFFFFFFu, mbar_try(q_empty, (nq & 1u) ^ 1u));
+            if (asked && it.kt0 < it.kt1) copy_queries();
             TilePages next = tile_pages(a, it.n, it.kt0 * kTileRows, it.kt0 < it.kt1 ? it.rows : 0);
             for (int t = it.kt0; t < it.kt1 && alive; ++t, ++tg) {
                 TilePages now = next;
@@ -421,19 +437,10 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                 __syncwarp();
                 copy_boxes<D>(a, &map_k, now, it.h, row0, base + L::kK + ks * kTile, k_full(ks));
                 ++nk;
-                if (t == it.kt0) {
+                if (!asked) {
                     if (!mbar_wait(q_empty, (nq & 1u) ^ 1u, abort_flag, status, kWaitLimitNs, kPollBackoffNs)) { alive = false; break; }
-                    if (lane == 0) {
-                        const int tiles = it.ntok > a.tile_tokens ? 2 : 1;
-                        mbar_expect_tx(q_full, (uint32_t)(tiles * a.tile_tokens * a.G * D * 2));
-                        publish(q_asked, (int)nq + 1);
-                        for (int x = 0; x < tiles; ++x)
-#pragma unroll
-                            for (int half = 0; half < D / 64; ++half)
-                                tma_load_3d(base + L::kQ + x * kTile + half * kBoxBytes, &map_q, half * 64, it.h * a.G,
-                                            it.token + x * a.tile_tokens, q_full);
-                    }
-                    ++nq;
+                    copy_queries();
+                    asked = true;
                 }
                 next = tile_pages(a, it.n, row0 + kTileRows, t + 1 < it.kt1 ? it.rows : 0);
                 if (!mbar_wait(v_empty(vs), ((tg / kVs) & 1u) ^ 1u, abort_flag, status, kWaitLimitNs, kPollBackoffNs)) { alive = false; break; }

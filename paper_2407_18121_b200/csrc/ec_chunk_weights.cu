@@ -148,31 +148,30 @@ chunk_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         uint32_t nk[kTeams] = {0, 0, 0, 0}, nq = 0;
         for (uint32_t k = 0; alive; ++k) {
             const uint32_t sl = k % kItems;
-            if (!mbar_wait(item_empty(sl), ((k / kItems) & 1u) ^ 1u, abort_flag, status, kWaitLimitNs, kPollBackoffNs)) { alive = false; break; }
             Item it = {};
             it.n = -1;
             long long cost = 0;
-            if (more) {
-                it.n = w.n;
-                it.h = w.h;
+            while (more) {                                // the next unit that this CTA has something of
                 it.row0 = w.i * kBlockRows;
                 it.len = w.p.len;
                 it.start = w.p.start;
                 it.count = w.p.count;
                 const int begin = max(0, it.row0 - (it.len - it.count)) / a.tile_tokens, end = (it.count + a.tile_tokens - 1) / a.tile_tokens;
                 cost = BlockUnits::before(a, w.p, w.units, w.i + 1) - BlockUnits::before(a, w.p, w.units, w.i);
-                const long long from = max(w.s.first - w.at, 0ll), to = min(w.s.last - w.at, cost);
-                auto tile_at = [&](long long x) {
-                    return (int)min(max(x / a.tile_tokens - kUnitTiles, 0ll) + begin, (long long)end);
-                };
-                it.qt0 = from == 0 ? begin : tile_at(from);
-                it.qt1 = to >= cost ? end : tile_at(to);
-                if (from > 0 || to < cost) {
-                    it.first = quotient(w.at, w.s.per);
-                    it.parts = quotient(w.at + cost - 1, w.s.per) - it.first + 1;
-                    it.slot = 2 * (int)blockIdx.x + (from == 0);
+                const Cut cut = cut_unit(w.s, w.at, cost, kUnitTiles * a.tile_tokens, a.tile_tokens, end - begin);
+                if (cut.mine) {
+                    it.n = w.n;
+                    it.h = w.h;
+                    it.qt0 = begin + cut.t0;
+                    it.qt1 = begin + cut.t1;
+                    it.first = cut.first;
+                    it.parts = cut.parts;
+                    it.slot = 2 * (int)blockIdx.x + (cut.first == (int)blockIdx.x);
+                    break;
                 }
+                more = w.next(a, cost);
             }
+            if (!mbar_wait(item_empty(sl), ((k / kItems) & 1u) ^ 1u, abort_flag, status, kWaitLimitNs, kPollBackoffNs)) { alive = false; break; }
             if (lane == 0) items[sl] = it;
             __syncwarp();
             if (lane == 0) mbar_arrive(item_full(sl));
