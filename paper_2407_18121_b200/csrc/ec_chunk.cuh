@@ -262,77 +262,27 @@ inline int chunk_grid()
     return n < kChunkMaxCtas ? n : kChunkMaxCtas;
 }
 
-// Page numbers of a tile's boxes, four lanes' worth at most: box lane + 32 k of the tile. -2: behind the last row that is
-// needed, -1: the table has no valid page.
-struct TilePages {
-    int page[4];
-};
+// The page of a box of rows: -1 behind the last row that is needed. A box of page -1 is copied like any other: it lies outside of the
+// pool, and what arrives is zeros, so that every tile brings the same number of bytes.
+__device__ __forceinline__ int box_page(const ChunkArgs &a, int n, int row, int rows) { return row < rows ? look_up_slot(a.c, n, row).page : -1; }
 
-__device__ __forceinline__ TilePages tile_pages(const ChunkArgs &a, int n, int row0, int rows)
+// Turns an entry outside the pool into -1 and reports it. True when there was one.
+__device__ __forceinline__ bool bad_page(const ChunkArgs &a, int row, int rows, int &page)
 {
-    TilePages t;
-    const int lane = threadIdx.x & 31, boxes = kTileRows / a.box_rows;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const int box = lane + 32 * k, row = row0 + box * a.box_rows;
-        t.page[k] = -2;
-        if (box < boxes && row < rows) t.page[k] = look_up_slot(a.c, n, row).page;
-    }
-    return t;
+    if (row >= rows || (unsigned)page < (unsigned)a.c.n_pages) return false;
+    page = -1;
+    report_page(a.c);
+    return true;
 }
 
-// Turns entries outside the pool into -1, reports them and counts the boxes that will be copied (all lanes get the sum).
-__device__ __forceinline__ int check_pages(const ChunkArgs &a, TilePages &t)
-{
-    int mine = 0;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        if (t.page[k] == -2) continue;
-        if ((unsigned)t.page[k] < (unsigned)a.c.n_pages) {
-            ++mine;
-        } else {
-            t.page[k] = -1;
-            report_page(a.c);
-        }
-    }
-    return __reduce_add_sync(0xFFFFFFFFu, mine);
-}
-
-// Starts the copies of a tile's boxes (whole warp; the barrier has been told their bytes).
+// Starts the copies of one box to row `at` of the tile at dst.
 template <int D>
-__device__ __forceinline__ void copy_boxes(const ChunkArgs &a, const CUtensorMap *map, const TilePages &t, int h, int row0, uint32_t dst, uint32_t bar)
+__device__ __forceinline__ void copy_box(const ChunkArgs &a, const CUtensorMap *map, int page, int h, int row, int at, uint32_t dst, uint32_t bar)
 {
-    const int lane = threadIdx.x & 31;
+    const int slot = row - page_of(a.c, row) * a.c.page_size;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        if (t.page[k] < 0) continue;
-        const int at = (lane + 32 * k) * a.box_rows, row = row0 + at;
-        const int slot = row - page_of(a.c, row) * a.c.page_size;
-#pragma unroll
-        for (int half = 0; half < D / 64; ++half)
-            tma_load_4d(dst + half * (kTileRows * 128) + at * 128, map, half * 64, slot, h, t.page[k], bar);
-    }
-}
-
-// Rows of the tile whose page the table does not have, as 128 bits (every lane gets them).
-__device__ __forceinline__ uint4 absent_rows(const ChunkArgs &a, const TilePages &t)
-{
-    uint32_t w[4] = {0u, 0u, 0u, 0u};
-    const int lane = threadIdx.x & 31;
-    bool any = false;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) any |= t.page[k] == -1;
-    if (__any_sync(0xFFFFFFFFu, any)) {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            if (t.page[k] != -1) continue;
-            const int at = (lane + 32 * k) * a.box_rows;
-            for (int r = at; r < at + a.box_rows; ++r) w[r >> 5] |= 1u << (r & 31);
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = __reduce_or_sync(0xFFFFFFFFu, w[i]);
-    }
-    return make_uint4(w[0], w[1], w[2], w[3]);
+    for (int half = 0; half < D / 64; ++half)
+        tma_load_4d(dst + half * (kTileRows * 128) + at * 128, map, half * 64, slot, h, page, bar);
 }
 
 // Plain shared-memory stores seen by the tensor cores' reads that a later arrival lets go ahead.

@@ -349,7 +349,6 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
     auto tmem_s = [&](uint32_t x) { return tmem + x * (uint32_t)kTileRows; };                 // S, and P over its first half
     auto tmem_o = [&](uint32_t x) { return tmem + 2u * kTileRows + x * (uint32_t)kTileRows; };
     grid_wait();
-    grid_release();
 
     // A unit of two query tiles: a team per tile, every tile of rows serves both. A unit of one: both teams work on it and
     // take its tiles of rows in turn; the first team puts the two results together.
@@ -420,33 +419,67 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
             // the queries first when their place is free, else behind the first tile's rows
             bool asked = it.kt0 >= it.kt1 || __all_sync(0xFFFFFFFFu, mbar_try(q_empty, (nq & 1u) ^ 1u));
             if (asked && it.kt0 < it.kt1) copy_queries();
-            TilePages next = tile_pages(a, it.n, it.kt0 * kTileRows, it.kt0 < it.kt1 ? it.rows : 0);
-            for (int t = it.kt0; t < it.kt1 && alive; ++t, ++tg) {
-                TilePages now = next;
-                const int row0 = t * kTileRows;
-                const uint32_t bytes = (uint32_t)check_pages(a, now) * (uint32_t)a.box_rows * D * 2u;
-                const uint4 absent = absent_rows(a, now);
+            // page numbers of a lane's first box are read a tile ahead; pages of fewer than 4 rows have more boxes than lanes
+            const int boxes = kTileRows / a.box_rows;
+            int row = it.kt0 * kTileRows + lane * a.box_rows, next = it.kt0 < it.kt1 ? box_page(a, it.n, row, it.rows) : -1;
+            for (int t = it.kt0; t < it.kt1 && alive; ++t, ++tg, row += kTileRows) {
+                int page = next;
                 const uint32_t ks = tg % kKs, vs = tg % kVs;
                 if (!mbar_wait(k_empty(ks), ((tg / kKs) & 1u) ^ 1u, abort_flag, status, kWaitLimitNs, kPollBackoffNs)) { alive = false; break; }
+                uint32_t gone[4] = {0u, 0u, 0u, 0u};      // absent rows
+                auto lost = [&](int at) {
+                    for (int r = at; r < at + a.box_rows; ++r) {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            if (r >> 5 == j) gone[j] |= 1u << (r & 31);
+                    }
+                };
+                bool any = lane < boxes && bad_page(a, row, it.rows, page);
+                if (any) lost(lane * a.box_rows);
                 if (lane == 0) {
-                    infos[2 * (tg % kInfos)] = make_uint2(absent.x, absent.y);
-                    infos[2 * (tg % kInfos) + 1] = make_uint2(absent.z, absent.w);
-                    mbar_expect_tx(k_full(ks), bytes);
-                    publish(k_asked, (int)tg + 1);
+                    mbar_expect_tx(k_full(ks), kTile);
                 }
                 __syncwarp();
-                copy_boxes<D>(a, &map_k, now, it.h, row0, base + L::kK + ks * kTile, k_full(ks));
+                const uint32_t k_to = base + L::kK + ks * kTile, v_to = base + L::kV + vs * kTile;
+                if (lane < boxes) copy_box<D>(a, &map_k, page, it.h, row, lane * a.box_rows, k_to, k_full(ks));
+#pragma unroll 1
+                for (int box = lane + 32; box < boxes; box += 32) {
+                    const int r = t * kTileRows + box * a.box_rows;
+                    int p = box_page(a, it.n, r, it.rows);
+                    if (bad_page(a, r, it.rows, p)) {
+                        any = true;
+                        lost(box * a.box_rows);
+                    }
+                    copy_box<D>(a, &map_k, p, it.h, r, box * a.box_rows, k_to, k_full(ks));
+                }
+                any = __any_sync(0xFFFFFFFFu, any);
+                if (any) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) gone[j] = __reduce_or_sync(0xFFFFFFFFu, gone[j]);
+                }
+                if (lane == 0) {
+                    infos[2 * (tg % kInfos)] = make_uint2(gone[0], gone[1]);
+                    infos[2 * (tg % kInfos) + 1] = make_uint2(gone[2], gone[3]);
+                    publish(k_asked, (int)tg + 1);        // S is asked for behind this
+                }
                 ++nk;
                 if (!asked) {
                     if (!mbar_wait(q_empty, (nq & 1u) ^ 1u, abort_flag, status, kWaitLimitNs, kPollBackoffNs)) { alive = false; break; }
                     copy_queries();
                     asked = true;
                 }
-                next = tile_pages(a, it.n, row0 + kTileRows, t + 1 < it.kt1 ? it.rows : 0);
+                next = t + 1 < it.kt1 ? box_page(a, it.n, row + kTileRows, it.rows) : -1;
                 if (!mbar_wait(v_empty(vs), ((tg / kVs) & 1u) ^ 1u, abort_flag, status, kWaitLimitNs, kPollBackoffNs)) { alive = false; break; }
-                if (lane == 0) mbar_expect_tx(v_full(vs), bytes);
+                if (lane == 0) mbar_expect_tx(v_full(vs), kTile);
                 __syncwarp();
-                copy_boxes<D>(a, &map_v, now, it.h, row0, base + L::kV + vs * kTile, v_full(vs));
+                if (lane < boxes) copy_box<D>(a, &map_v, page, it.h, row, lane * a.box_rows, v_to, v_full(vs));
+#pragma unroll 1
+                for (int box = lane + 32; box < boxes; box += 32) {
+                    const int r = t * kTileRows + box * a.box_rows;
+                    int p = box_page(a, it.n, r, it.rows);
+                    bad_page(a, r, it.rows, p);
+                    copy_box<D>(a, &map_v, p, it.h, r, box * a.box_rows, v_to, v_full(vs));
+                }
                 ++nv;
             }
             if (!alive) break;
@@ -554,7 +587,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
         fewer_registers();
         // A product with P = 0 does not hide a value that is not finite, so tiles whose rows some token must not see are
         // looked over: such values become zeros, and the item is marked, for the tokens that do see them. Rows behind the last one
-        // (memory that holds anything) and absent rows become zeros too.
+        // (memory that holds anything) become zeros too; absent ones are.
         uint32_t tg = 0;
         for (uint32_t k = 0; alive; ++k) {
             const uint32_t sl = k % kItems;
@@ -567,10 +600,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                 const uint32_t s = tg % kVs;
                 if (!mbar_wait(v_full(s), (tg / kVs) & 1u, abort_flag, status, kWaitLimitNs, kPollBackoffNs)) { alive = false; break; }
                 const int row0 = t * kTileRows, rows = min(kTileRows, it.rows - row0);
-                const uint2 gone0 = infos[2 * (tg % kInfos)], gone1 = infos[2 * (tg % kInfos) + 1];
-                const bool any_absent = (gone0.x | gone0.y | gone1.x | gone1.y) != 0u;
-                const int hidden = max(0, it.limit + 1 - row0);                            // rows before are seen by every token
-                const int check = any_absent ? 0 : hidden;
+                const int check = max(0, it.limit + 1 - row0);                             // rows before are seen by every token
                 const int end = (rows + 15) & ~15;
                 if (check < end) {
                     uint8_t *tile = smem + L::kV + s * kTile;
@@ -578,12 +608,10 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                     for (int i = check * kChunks + lane; i < end * kChunks; i += 32) {
                         const int r = i / kChunks, c = i % kChunks;
                         uint4 *at = reinterpret_cast<uint4 *>(tile + (c >> 3) * kBoxBytes + r * 128 + (((c & 7) ^ (r & 7)) << 4));
-                        const uint32_t word = r < 64 ? (r < 32 ? gone0.x : gone0.y) : (r < 96 ? gone1.x : gone1.y);
-                        if (r >= rows || (word >> (r & 31)) & 1u) {
+                        if (r >= rows) {
                             *at = make_uint4(0u, 0u, 0u, 0u);
                             continue;
                         }
-                        if (r < hidden) continue;
                         uint4 v = *at;
                         uint32_t w[4] = {v.x, v.y, v.z, v.w};
                         bool found = false;

@@ -118,6 +118,12 @@ chunk_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_to_async();
     }
+    // Rows of a query tile that no copy fills: zeros, so that their scores are finite and the normaliser of -inf hides them.
+    for (int i = threadIdx.x; i < kStages * (D / 64) * (kTileRows - a.tile_tokens * a.G) * 8; i += kThreads) {
+        const int row = a.tile_tokens * a.G + (i >> 3) % (kTileRows - a.tile_tokens * a.G), tile = (i >> 3) / (kTileRows - a.tile_tokens * a.G);
+        *reinterpret_cast<uint4 *>(smem + L::kQ + tile * kBoxBytes + row * 128 + (i & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+    }
+    fence_to_async();
     if (threadIdx.x == 32) {
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map_q) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map_k) : "memory");
@@ -132,7 +138,6 @@ chunk_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
     grid_wait();
-    grid_release();
 
     // Whether any token of query tile q sees a row of team x's tile.
     auto meets = [&](const Item &it, uint32_t x, int q) {
@@ -145,7 +150,7 @@ chunk_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         // ------------------------------------------------------------ plan and copies
         Walk<BlockUnits> w;
         bool more = w.begin(a, (long long)kLeastTiles * a.tile_tokens);
-        uint32_t nk[kTeams] = {0, 0, 0, 0}, nq = 0;
+        uint32_t nk = 0, asked = 0, nq = 0;       // per team one bit: the parity of its copies, whether there were any; query tiles
         for (uint32_t k = 0; alive; ++k) {
             const uint32_t sl = k % kItems;
             Item it = {};
@@ -177,21 +182,26 @@ chunk_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             if (lane == 0) mbar_arrive(item_full(sl));
             if (!more) break;
             if (it.qt0 < it.qt1) {
-                TilePages all[kTeams];                    // read side by side
-#pragma unroll
-                for (int x = 0; x < kTeams; ++x) all[x] = tile_pages(a, it.n, it.row0 + x * kTileRows, it.len);
-#pragma unroll
-                for (uint32_t x = 0; x < (uint32_t)kTeams; ++x) {
-                    const int row0 = it.row0 + (int)x * kTileRows;
-                    if (row0 >= it.len) continue;
-                    TilePages &pages = all[x];
-                    const uint32_t bytes = (uint32_t)check_pages(a, pages) * (uint32_t)a.box_rows * D * 2u;
-                    if (!mbar_wait(k_empty(x), (nk[x] & 1u) ^ 1u, abort_flag, status, kWaitLimitNs, kPollBackoffNs)) { alive = false; break; }
-                    if (lane == 0) mbar_expect_tx(k_full(x), bytes);
-                    __syncwarp();
-                    copy_boxes<D>(a, &map_k, pages, it.h, row0, base + L::kK + x * kTile, k_full(x));
-                    ++nk[x];
+                // the block's boxes, a lane's first one read ahead
+                const int teams = min(kTeams, (it.len - it.row0 + kTileRows - 1) / kTileRows), boxes = teams * (kTileRows / a.box_rows);
+                int page = lane < boxes ? box_page(a, it.n, it.row0 + lane * a.box_rows, it.len) : -1;
+#pragma unroll 1
+                for (int x = 0; x < teams; ++x) {
+                    if (!mbar_wait(k_empty(x), (nk >> x & 1u) ^ 1u, abort_flag, status, kWaitLimitNs, kPollBackoffNs)) { alive = false; break; }
+                    if (lane == 0) mbar_expect_tx(k_full(x), kTile);
+                    nk ^= 1u << x;
+                    asked |= 1u << x;
                 }
+                if (!alive) break;
+                __syncwarp();
+#pragma unroll 1
+                for (int box = lane; box < boxes; box += 32) {
+                    const int at = box * a.box_rows, row = it.row0 + at, x = at / kTileRows;
+                    if (box >= 32) page = box_page(a, it.n, row, it.len);
+                    bad_page(a, row, it.len, page);
+                    copy_box<D>(a, &map_k, page, it.h, row, at % kTileRows, base + L::kK + x * kTile, k_full(x));
+                }
+                __syncwarp();
             }
             for (int q = it.qt0; q < it.qt1 && alive; ++q, ++nq) {
                 const uint32_t s = nq % kStages;
@@ -221,7 +231,7 @@ chunk_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         if (*abort_flag) {
             // let copies that are still in flight land before the CTA gives its memory back
             for (uint32_t x = 0; x < (uint32_t)kTeams; ++x)
-                if (nk[x] > 0) mbar_wait(k_full(x), (nk[x] - 1u) & 1u, abort_flag, status, 200000ull);
+                if (asked >> x & 1u) mbar_wait(k_full(x), (nk >> x & 1u) ^ 1u, abort_flag, status, 200000ull);
             for (uint32_t t = nq > (uint32_t)kStages ? nq - kStages : 0; t < nq; ++t)
                 mbar_wait(q_full(t % kStages), (t / kStages) & 1u, abort_flag, status, 200000ull);
         }
@@ -312,7 +322,7 @@ chunk_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     ++ns;
                     tc_fence_after();
                     const int token0 = q * a.tile_tokens;
-                    const int columns = min(a.tile_tokens, it.count - token0) * a.G;
+                    const int tokens = min(a.tile_tokens, it.count - token0), columns = tokens * a.G;
                     // columns of tokens that see the row: from here on (rows behind the last one: none that matter)
                     const int lo = (row - (it.len - it.count) - token0) * a.G;
                     const int lo_warp = __shfl_sync(0xFFFFFFFFu, lo, 0);
@@ -344,7 +354,7 @@ chunk_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                         __syncwarp();
                         if (lane == 0) mbar_arrive(s_empty(x));
                     };
-                    const bool masked = columns < kTileRows || __any_sync(0xFFFFFFFFu, lo > 0);
+                    const bool masked = tokens < a.tile_tokens || __any_sync(0xFFFFFFFFu, lo > 0);
                     if (masked) {
                         // chunks that no row of the warp takes part in are left out
                         const int ch0 = max(lo_warp, 0) / 32, ch1 = (columns + 31) / 32;
