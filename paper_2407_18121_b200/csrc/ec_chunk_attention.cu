@@ -693,6 +693,10 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                     const float mx = max3(max3(mx4[0], mx4[1], mx4[2]), mx4[3], mx4[3]);
                     const uint2 gone = infos[2 * ((tg0 + (uint32_t)t) % kInfos) + h];      // absent rows
                     const bool plain = plain_to >= col0 + kHalf - 1 && (gone.x | gone.y) == 0u;
+                    if (plain && i == 2 * part.first && fabsf(mx) < INFINITY) {            // the first maximum: nothing to rescale
+                        m = mx;
+                        m2 = mx * c;
+                    }
                     const float from = E::kTop - m2;
                     const float2 from2 = make_float2(from, from);
                     if (plain && __all_sync(0xFFFFFFFFu, fmaf(mx, c, -m2) <= E::kRaise && fabsf(m2) <= kLarge)) {

@@ -369,18 +369,16 @@ chunk_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     } else {
                         uint32_t ra[32], rb[32];
                         tmem_ld32_async(s_addr, ra);
-                        tmem_ld_wait(ra);
-                        tmem_ld32_async(s_addr + 32, rb);
-                        chunk(ra, 0, std::false_type{});
-                        tmem_ld_wait(rb);
-                        tmem_ld32_async(s_addr + 64, ra);
-                        chunk(rb, 1, std::false_type{});
-                        tmem_ld_wait(ra);
-                        tmem_ld32_async(s_addr + 96, rb);
-                        chunk(ra, 2, std::false_type{});
-                        tmem_ld_wait(rb);
-                        release();
-                        chunk(rb, 3, std::false_type{});
+#pragma unroll 1
+                        for (int ch = 0; ch < 4; ch += 2) {               // a chunk is under way while the one before is worked on
+                            tmem_ld_wait(ra);
+                            tmem_ld32_async(s_addr + 32 * ch + 32, rb);
+                            chunk(ra, ch, std::false_type{});
+                            tmem_ld_wait(rb);
+                            if (ch == 0) tmem_ld32_async(s_addr + 64, ra);
+                            else release();
+                            chunk(rb, ch + 1, std::false_type{});
+                        }
                     }
                     total += (accA.x + accA.y) + (accB.x + accB.y);
                 }
