@@ -13,8 +13,7 @@ namespace ec {
 
 namespace {
 
-constexpr int kRotThreads = 256;
-constexpr int kFlight = 4;                       // items of a thread in flight
+constexpr int kRotThreads = 128;
 
 template <int DTYPE> __device__ __forceinline__ void widen(const uint4 &v, float (&f)[8])
 {
@@ -58,72 +57,99 @@ __device__ __forceinline__ float2 turn_of(double freq, int position, float facto
     return make_float2(c * factor, (inverse ? -s : s) * factor);
 }
 
+// Not the read-only path: the output may be the input.
+__device__ __forceinline__ uint4 load_once(const uint4 *p)
+{
+    uint4 v;
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
+    return v;
+}
+
 // What one head row of a token becomes: its place in the input and in the output, nullptr: nothing.
 struct RowPlace {
     const uint4 *from;
     uint4 *to;
 };
 
-// A thread keeps its place in the head (piece `v`) and walks over the rows (token, head) of the CTA, kFlight at a time.
-// Places(row, token) gives the row's pointers.
+// A thread keeps its place in the head (piece `v`) and walks over the rows (token, head) of the CTA. Places(token, head) gives a row's
+// pointers. One row a thread in flight, and as many CTAs as fit: 8192 tokens of 32 + 8 + 8 heads in 32 us, two rows 37, four 40.
 template <int DTYPE, bool HALF, typename Places>
-__device__ __forceinline__ void turn_rows(const RotaryTurn &r, int D, const float2 *table, int tokens, int heads, Places places)
-{
-    const int turning = r.rot / (HALF ? 16 : 8), pieces = turning + (D - r.rot) / 8;
-    const int step = kRotThreads / pieces, v = threadIdx.x % pieces, first = threadIdx.x / pieces;
-    if (first >= step) return;
-    const int rows = tokens * heads, half = r.rot / 2;
-    // offsets in pieces of 16 bytes
-    const bool turns = v < turning;
-    const int lo = turns ? v : v - turning + r.rot / 8, hi = HALF && turns ? v + half / 8 : -1;
-    for (int row0 = first; row0 < rows; row0 += kFlight * step) {
-        RowPlace at[kFlight];
-        uint4 a[kFlight], b[kFlight];
-        int token[kFlight];
+struct RowTurner {
+    const RotaryTurn &r;
+    Places places;
+    int step, v, lo, hi, row, rows, heads;       // lo, hi: pieces of a row, of 16 bytes; hi < 0: there is none
+    bool turns;
+    RowPlace at;
+    uint4 a, b;
+    int token;
+
+    __device__ __forceinline__ RowTurner(const RotaryTurn &turn, int D, int tokens, int heads_, Places p) : r(turn), places(p), heads(heads_)
+    {
+        const int turning = r.rot / (HALF ? 16 : 8), pieces = turning + (D - r.rot) / 8;
+        step = kRotThreads / pieces;
+        v = threadIdx.x % pieces;
+        row = threadIdx.x / pieces;
+        rows = row < step ? tokens * heads : 0;
+        turns = v < turning;
+        lo = turns ? v : v - turning + r.rot / 8;
+        hi = HALF && turns ? v + r.rot / 16 : -1;
+    }
+
+    __device__ __forceinline__ void load()
+    {
+        token = row / heads;
+        at = places(token, row - token * heads);
+        if (at.to == nullptr) return;
+        a = load_once(at.from + lo);
+        if (hi >= 0) b = load_once(at.from + hi);
+    }
+
+    __device__ __forceinline__ void store(const float2 *table)
+    {
+        if (at.to == nullptr) return;
+        if (turns) {
+            const float2 *cs = table + token * (r.rot / 2);
+            float x[8];
+            widen<DTYPE>(a, x);
+            if (HALF) {
+                float y[8];
+                widen<DTYPE>(b, y);
 #pragma unroll
-        for (int u = 0; u < kFlight; ++u) {
-            const int row = row0 + u * step;
-            at[u].to = nullptr;
-            if (row >= rows) continue;
-            token[u] = row / heads;
-            at[u] = places(token[u], row - token[u] * heads);
-            if (at[u].to == nullptr) continue;
-            a[u] = at[u].from[lo];
-            if (hi >= 0) b[u] = at[u].from[hi];
-        }
-#pragma unroll
-        for (int u = 0; u < kFlight; ++u) {
-            if (at[u].to == nullptr) continue;
-            if (turns) {
-                const float2 *cs = table + token[u] * half;
-                float x[8];
-                widen<DTYPE>(a[u], x);
-                if (HALF) {
-                    float y[8];
-                    widen<DTYPE>(b[u], y);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float2 t = cs[8 * v + i];
-                        const float p = x[i] * t.x - y[i] * t.y, q = x[i] * t.y + y[i] * t.x;
-                        x[i] = p;
-                        y[i] = q;
-                    }
-                    at[u].to[hi] = narrow<DTYPE>(y);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float2 t = cs[4 * v + i];
-                        const float p = x[2 * i] * t.x - x[2 * i + 1] * t.y, q = x[2 * i] * t.y + x[2 * i + 1] * t.x;
-                        x[2 * i] = p;
-                        x[2 * i + 1] = q;
-                    }
+                for (int i = 0; i < 8; ++i) {
+                    const float2 t = cs[8 * v + i];
+                    const float p = x[i] * t.x - y[i] * t.y, q = x[i] * t.y + y[i] * t.x;
+                    x[i] = p;
+                    y[i] = q;
                 }
-                a[u] = narrow<DTYPE>(x);
+                at.to[hi] = narrow<DTYPE>(y);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float2 t = cs[4 * v + i];
+                    const float p = x[2 * i] * t.x - x[2 * i + 1] * t.y, q = x[2 * i] * t.y + x[2 * i + 1] * t.x;
+                    x[2 * i] = p;
+                    x[2 * i + 1] = q;
+                }
             }
-            at[u].to[lo] = a[u];
+            a = narrow<DTYPE>(x);
+        }
+        at.to[lo] = a;
+    }
+
+    // The first rows are under way while `make_table` works out the angles.
+    template <typename Table>
+    __device__ __forceinline__ void run(const float2 *table, Table make_table)
+    {
+        if (row < rows) load();
+        make_table();
+        __syncthreads();
+        while (row < rows) {
+            store(table);
+            row += step;
+            if (row < rows) load();
         }
     }
-}
+};
 
 template <int DTYPE, bool HALF>
 __global__ void __launch_bounds__(kRotThreads)
@@ -133,15 +159,17 @@ rotary_kernel(const RotaryTurn r, const RotaryRows x, int D, int per)
     const int first = blockIdx.x * per, tokens = min(per, x.N * x.T - first);
     grid_wait();
     grid_release();
-    const int half = r.rot / 2;
-    for (int i = threadIdx.x; i < tokens * half; i += kRotThreads) {
-        const int t = i / half, token = first + t, n = token / x.T;
-        table[i] = turn_of(r.freqs[i - t * half], x.positions[n * x.pos_n + (token - n * x.T)], r.factor, r.inverse);
-    }
-    __syncthreads();
-    turn_rows<DTYPE, HALF>(r, D, table, tokens, x.heads, [&](int t, int h) {
+    auto place = [&](int t, int h) {
         const int token = first + t, n = token / x.T, at = token - n * x.T;
         return RowPlace{x.x + n * x.x_n + at * x.x_t + h * x.x_h, x.out + n * x.out_n + at * x.out_t + h * x.out_h};
+    };
+    RowTurner<DTYPE, HALF, decltype(place)> turner(r, D, tokens, x.heads, place);
+    turner.run(table, [&] {
+        const int half = r.rot / 2;
+        for (int i = threadIdx.x; i < tokens * half; i += kRotThreads) {
+            const int t = i / half, token = first + t, n = token / x.T;
+            table[i] = turn_of(r.freqs[i - t * half], x.positions[n * x.pos_n + (token - n * x.T)], r.factor, r.inverse);
+        }
     });
 }
 
@@ -163,11 +191,6 @@ join_kernel(const RotaryTurn r, const PagedView c, const JoinArgs j, int D, int 
         slot_s[threadIdx.x] = slot;
         pos_s[threadIdx.x] = j.positions[first + threadIdx.x];
     }
-    const int half = r.rot / 2;
-    for (int i = threadIdx.x; i < tokens * half; i += kRotThreads) {
-        const int t = i / half;
-        table[i] = turn_of(r.freqs[i - t * half], j.positions[first + t], r.factor, false);
-    }
     __syncthreads();
     auto place = [&](int t) {
         Slot s;
@@ -175,29 +198,24 @@ join_kernel(const RotaryTurn r, const PagedView c, const JoinArgs j, int D, int 
         s.slot = slot_s[t] - s.page * c.page_size;
         return s;
     };
-    turn_rows<DTYPE, HALF>(r, D, table, tokens, j.Hq + c.H, [&](int t, int h) {
+    auto row_place = [&](int t, int h) {
         if (slot_s[t] < 0) return RowPlace{nullptr, nullptr};
         if (h < j.Hq) return RowPlace{j.q + (first + t) * j.q_t + h * j.q_h, j.q_out + (first + t) * j.qo_t + h * j.qo_h};
         h -= j.Hq;
         return RowPlace{j.k + (first + t) * j.k_t + h * j.k_h, c.K + row_offset(c, place(t)) + (size_t)h * c.head_step};
+    };
+    RowTurner<DTYPE, HALF, decltype(row_place)> turner(r, D, tokens, j.Hq + c.H, row_place);
+    turner.run(table, [&] {
+        const int half = r.rot / 2;
+        for (int i = threadIdx.x; i < tokens * half; i += kRotThreads) {
+            const int t = i / half;
+            table[i] = turn_of(r.freqs[i - t * half], pos_s[t], r.factor, false);
+        }
     });
     const int pieces = D / 8, v = threadIdx.x % pieces, step = kRotThreads / pieces, rows = tokens * c.H;
-    for (int row0 = threadIdx.x / pieces; row0 < rows; row0 += kFlight * step) {
-        uint4 x[kFlight];
-        uint4 *to[kFlight];
-#pragma unroll
-        for (int u = 0; u < kFlight; ++u) {
-            const int row = row0 + u * step;
-            to[u] = nullptr;
-            if (row >= rows) continue;
-            const int t = row / c.H, h = row - t * c.H;
-            if (slot_s[t] < 0) continue;
-            to[u] = c.V + row_offset(c, place(t)) + (size_t)h * c.head_step + v;
-            x[u] = j.v[(first + t) * j.v_t + h * j.v_h + v];
-        }
-#pragma unroll
-        for (int u = 0; u < kFlight; ++u)
-            if (to[u]) *to[u] = x[u];
+    for (int row = threadIdx.x / pieces; row < rows; row += step) {
+        const int t = row / c.H, h = row - t * c.H;
+        if (slot_s[t] >= 0) c.V[row_offset(c, place(t)) + (size_t)h * c.head_step + v] = load_once(j.v + (first + t) * j.v_t + h * j.v_h + v);
     }
     for (int row = threadIdx.x; row < rows; row += kRotThreads) {
         const int t = row / c.H, h = row - t * c.H;
