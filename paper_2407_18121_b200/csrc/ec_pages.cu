@@ -86,7 +86,7 @@ __device__ __forceinline__ long long rows_wanted(const ReserveArgs &a, int len, 
 
 __device__ __forceinline__ int pages_for(const PagedView &c, long long rows) { return (int)((rows + c.page_size - 1) / c.page_size); }
 
-__global__ void __launch_bounds__kThreads
+__global__ void __launch_bounds__(kThreads)
 reserve_kernel(const PagedView c, const PagePool p, const ReserveArgs a)
 {
     __shared__ Sums warps[32];
@@ -184,7 +184,7 @@ reserve_kernel(const PagedView c, const PagePool p, const ReserveArgs a)
     if (tid == 0) *p.n_free = height - total.b;
 }
 
-__global__ void __launch_bounds__kThreads
+__global__ void __launch_bounds__(kThreads)
 release_kernel(const PagedView c, const PagePool p)
 {
     __shared__ Sums warps[32];

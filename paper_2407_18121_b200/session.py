@@ -239,3 +239,94 @@ class PagedCacheSession:
     def status(self) -> int:
         """Synchronises; EC_OK, or EC_ERR_PAGE once a length or a table entry was out of range."""
         return ec.ec_device_status(self.state)
+
+
+class PagedPoolSession(PagedCacheSession):
+    """A paged cache whose problems share one pool of pages and take several new tokens at once.
+
+        s = PagedPoolSession(N, H, D, budget=2048, recent=64, sinks=4, scale=1/sqrt(D), pool_rows=N * 1024, chunk=512)
+        s.chunk(q, k, v, counts, out)        # packed tokens [tokens, Hq or H, D] of all problems, counts int32 [N]: a piece of a
+                                             # prompt, a whole prompt, drafted tokens; positions follow on, rotary included
+        s.decode(q, k_new, v_new, out)       # one token per problem, as before (q and k_new turned by the caller: s.turn)
+
+    A chunk takes pages for its rows from the pool, attends, leaves its attention as weights and evicts down to `budget` rows
+    per problem; the pages that eviction or s.end(n) left behind go back with the next call. Where the pool holds too few, problems are
+    refused in the order of their numbers: `granted` [N] is 0 for them, nothing of them changes and their part of `out` stays as it
+    was. rot elements of every head turn (0: none) by frequencies of ec_rotary_frequencies.
+    """
+
+    def __init__(self, N: int, H: int, D: int, budget: int, recent: int, sinks: int, scale: float, pool_rows: int, chunk: int,
+                 Hq: Optional[int] = None, page_size: int = 64, dtype: torch.dtype = torch.bfloat16, decay: float = 1.0, rot: int = 0,
+                 interleaved: bool = False, freqs: Optional[torch.Tensor] = None, factor: float = 1.0,
+                 device: Optional[torch.device] = None):
+        self.N, self.H, self.D, self.Hq = N, H, D, Hq or H
+        self.budget, self.recent, self.sinks = int(budget), int(recent), int(sinks)
+        self.scale, self.decay = float(scale), float(decay)
+        dev = device or torch.device("cuda", torch.cuda.current_device())
+        self.device = dev
+        n_pages, max_pages = -(-int(pool_rows) // page_size), -(-(self.budget + int(chunk)) // page_size)
+        i32 = dict(dtype=torch.int32, device=dev)
+        self.Kp = torch.empty((n_pages, H, page_size, D), dtype=dtype, device=dev)
+        self.Vp = torch.empty_like(self.Kp)
+        self.weight = torch.zeros((n_pages, H, page_size), dtype=torch.float32, device=dev)
+        self.pos = torch.full((n_pages, H, page_size), -1, **i32)
+        self.table = torch.full((N, max_pages), -1, **i32)
+        self.lens, self.seen = torch.zeros(N, **i32), torch.zeros(N, **i32)
+        self.state = torch.empty(ec.ec_paged_state_bytes(N), dtype=torch.uint8, device=dev)
+        self.cache = ec.ec_paged_init(self.Kp, self.Vp, self.weight, self.pos, self.table, self.lens, self.seen, self.state)
+        self.pages = ec.ec_pages(torch.arange(n_pages, **i32).flip(0).contiguous(), torch.full((1,), n_pages, **i32), torch.zeros(N, **i32))
+        self.granted, self.starts = torch.zeros(N, **i32), torch.zeros(N + 1, **i32)
+        self.rot, self.interleaved, self.factor = int(rot), bool(interleaved), float(factor)
+        self.freqs = None if freqs is None else freqs.to(device=dev, dtype=torch.float64)
+        self.ws_step = torch.empty(ec.ec_paged_step_workspace(self.cache, self.Hq, self.budget), dtype=torch.uint8, device=dev)
+
+    def turn(self, x: torch.Tensor, out: torch.Tensor) -> None:
+        """Rotary positions of the problems' next tokens on x [N, heads, D], for decode()."""
+        ec.ec_rotary(x[:, None], out[:, None], self.seen.clamp(min=0)[:, None], self.freqs, self.rot, self.interleaved, self.factor)
+
+    def chunk(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, counts: torch.Tensor, out: torch.Tensor,
+              lse: Optional[torch.Tensor] = None) -> None:
+        """counts[n] tokens of every problem, packed in order of the problems. Can be captured and replayed with other counts."""
+        tokens = q.shape[0]
+        i32 = dict(dtype=torch.int32, device=self.device)
+        slots, positions = torch.empty(tokens, **i32), torch.empty(tokens, **i32)
+        turned = torch.empty((tokens, self.Hq, self.D), dtype=self.Kp.dtype, device=self.device)
+        if lse is None:
+            lse = torch.empty((tokens, self.Hq), dtype=torch.float32, device=self.device)
+        ws = self._scratch(ec.ec_paged_chunk_workspace(self.cache, self.Hq))
+        ws_app = self._scratch(ec.ec_paged_append_workspace(self.cache, 0, self.budget))
+        ec.ec_paged_release(self.cache, self.pages)
+        ec.ec_paged_reserve(self.cache, self.pages, counts, self.starts, self.granted, slots, positions)
+        ec.ec_paged_join(q, turned, k, v, None, slots, positions, self.cache, self.freqs, self.rot, self.interleaved, self.factor)
+        ec.ec_paged_chunk_attention(turned, self.starts, self.granted, self.cache, self.scale, out, lse, ws)
+        ec.ec_paged_chunk_weights(turned, lse, self.starts, self.granted, self.cache, self.scale, self.decay, ws)
+        ec.ec_paged_append(None, None, None, None, None, self.cache, False, self.budget, self.recent, self.sinks, ws_app)
+
+    def _rows_for(self, counts: torch.Tensor) -> torch.Tensor:
+        """Pages for rows that the next call adds; returns the lengths, with problems that got none marked as empty places."""
+        ec.ec_paged_release(self.cache, self.pages)
+        ec.ec_paged_reserve(self.cache, self.pages, counts, None, self.granted, advance=False, limit=self.budget)
+        kept = self.lens.clone()
+        self.lens.masked_fill_((self.granted == 0) & (counts > 0), -1)
+        return kept
+
+    def append(self, K: torch.Tensor, V: torch.Tensor, scores: Optional[torch.Tensor], counts: Optional[torch.Tensor] = None,
+               fresh: bool = False) -> None:
+        if fresh:
+            raise ValueError("problems begin with begin(n)")
+        if counts is None:
+            counts = torch.full((self.N,), K.shape[2], dtype=torch.int32, device=self.device)
+        kept = self._rows_for(counts)
+        super().append(K, V, scores, counts)
+        self.lens.copy_(torch.where((self.granted == 0) & (counts > 0), kept, self.lens))
+
+    def prompt(self, *args, **kwargs) -> None:
+        raise ValueError("a prompt is a chunk here: chunk()")
+
+    def decode(self, q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor, out: torch.Tensor,
+               lse: Optional[torch.Tensor] = None) -> None:
+        """One generation step. Problems that get no page are left out: `granted` is 0, their output zero."""
+        ones = torch.ones(self.N, dtype=torch.int32, device=self.device)
+        kept = self._rows_for(ones)
+        super().decode(q, k_new, v_new, out, lse)
+        self.lens.copy_(torch.where(self.granted == 0, kept, self.lens))
