@@ -711,7 +711,7 @@ int ec_paged_join(const void *q_dev, int64_t q_t, int64_t q_h, void *q_out_dev, 
  * for Hq query heads; query head i reads key / value head i / (Hq / H). Nothing of the cache changes.
  *   q_dev, out_dev    [tokens, Hq, D] by strides in elements, multiples of 8                               (in, out)
  *   starts_dev        int32 [N] (or more) first token of every problem                                     (in)
- *   counts_dev        int32 [N] its tokens; 0: none. Rows of tokens that no problem has are left as they are (in)
+ *   counts_dev        int32 [N] its tokens; 0 or less: none. Rows of tokens that no problem has stay as they are (in)
  *   out               fp32 accumulation; probabilities are rounded once to the element type before they meet V (fp16: rows that lie
  *                     more than 2^-35 below the leading one count as nothing), the result once. Zero where a token sees nothing (an
  *                     empty place, absent pages, all scores -inf)

@@ -59,7 +59,8 @@ __device__ __forceinline__ Problem read_problem(const Args &a, int n)
     p.start = a.starts[n];
     p.count = a.counts[n];
     p.len = max(read_len(a.c, n), 0);
-    if (p.count < 0 || (p.count > 0 && (p.start < 0 || p.count > a.tokens - p.start))) {
+    p.count = max(p.count, 0);
+    if (p.count > 0 && (p.start < 0 || p.count > a.tokens - p.start)) {
         report_page(a.c);
         p.count = 0;
     }
