@@ -619,6 +619,8 @@ def ec_paged_reserve(cache: ec_paged, pages: ec_pages, counts: torch.Tensor, sta
     `limit` rows per problem at most (0: no limit), and slots and positions are None."""
     N, dev, i32 = cache._dims[0], cache._dims[4], torch.int32
     given = slots if slots is not None else positions
+    if advance and given is None:
+        raise ValueError("rows that join have slots: slots or positions say how many packed tokens there are")
     tokens = 0 if given is None else given.shape[0]
     st = lib().ec_paged_reserve(C.byref(cache), C.byref(pages._c(cache)), _want(counts, "counts", i32, (N,), dev), tokens, int(bool(advance)),
                                 int(limit), _want(starts, "starts", i32, (N + 1,), dev), _want(granted, "granted", i32, (N,), dev),

@@ -124,6 +124,14 @@ def test_pool_counts_out_of_range_are_reported():
         assert 0 <= int(p.n_free) <= p.cache.n_pages or int(p.n_free) in (-3, 1 << 20)
 
 
+def test_rows_that_join_need_slots():
+    p = Pool(6, 4, 50, seed=4)
+    with pytest.raises(ValueError):
+        ec.ec_paged_reserve(p.cache, p.pages, i32([1] * 6), None, i32([0] * 6))
+    with pytest.raises(ValueError):
+        ec.ec_paged_reserve(p.cache, p.pages, i32([1] * 6), None, i32([0] * 6), i32([0] * 6), i32([0] * 5))
+
+
 def test_a_captured_reserve_replayed():
     p = Pool(20, 8, 600, seed=5)
     counts, tokens = [n % 5 for n in range(20)], 40
