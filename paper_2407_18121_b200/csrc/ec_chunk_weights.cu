@@ -57,7 +57,8 @@ struct Smem {
     static constexpr int kTmemSlot = kBars + kNumBars * 8;
     static constexpr int kAbort = kTmemSlot + 4;
     static constexpr int kLast = kAbort + 4;
-    static constexpr int kTotal = kLast + 4 * kTeams;
+    static constexpr int kOdd = kLast + 4 * kTeams;                       // [stages] whether a normaliser of the tile is not finite
+    static constexpr int kTotal = kOdd + 4 * kStages;
     static_assert(kTotal <= 232448, "shared memory of a block");
 };
 
@@ -98,6 +99,7 @@ chunk_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
     volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(smem + L::kTmemSlot);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + L::kAbort);
     volatile int *last_s = reinterpret_cast<volatile int *>(smem + L::kLast);
+    volatile int *odd_s = reinterpret_cast<volatile int *>(smem + L::kOdd);
     int *status = a.c.state;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -206,6 +208,7 @@ chunk_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             for (int q = it.qt0; q < it.qt1 && alive; ++q, ++nq) {
                 const uint32_t s = nq % kStages;
                 float nl[4];
+                bool odd = false;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int r = lane + 32 * i, in = r / a.G, t = q * a.tile_tokens + in;
@@ -213,10 +216,13 @@ chunk_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     if (in >= a.tile_tokens || t >= it.count) continue;
                     const float z = a.lse[(size_t)(it.start + t) * a.Hq + (size_t)it.h * a.G + (r - in * a.G)];
                     if (z != -INFINITY) nl[i] = fmaf(-z, kLog2e, (float)(a.log2_decay * (double)(it.count - 1 - t)));
+                    odd |= !(fabsf(nl[i]) < INFINITY);
                 }
                 if (!mbar_wait(q_empty(s), ((nq / kStages) & 1u) ^ 1u, abort_flag, status, kWaitLimitNs, kPollBackoffNs)) { alive = false; break; }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) lse_s[s * kTileRows + lane + 32 * i] = nl[i];
+                odd = __any_sync(0xFFFFFFFFu, odd);
+                if (lane == 0) odd_s[s] = odd;
                 __syncwarp();
                 if (lane == 0) {
                     mbar_expect_tx(q_full(s), (uint32_t)(a.tile_tokens * a.G * D * 2));
@@ -354,7 +360,9 @@ chunk_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                         __syncwarp();
                         if (lane == 0) mbar_arrive(s_empty(x));
                     };
-                    const bool masked = tokens < a.tile_tokens || __any_sync(0xFFFFFFFFu, lo > 0);
+                    // The polynomial that takes part in the exponentials knows neither NaN nor an exact zero: normalisers like that go the
+                    // careful way too.
+                    const bool masked = tokens < a.tile_tokens || odd_s[s] != 0 || __any_sync(0xFFFFFFFFu, lo > 0);
                     if (masked) {
                         // chunks that no row of the warp takes part in are left out
                         const int ch0 = max(lo_warp, 0) / 32, ch1 = (columns + 31) / 32;

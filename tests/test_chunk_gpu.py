@@ -233,6 +233,27 @@ def test_a_key_or_query_that_is_not_a_number_stays_where_it_belongs():
     assert torch.isfinite(out.cpu()[~bad]).all()
 
 
+@pytest.mark.parametrize("token", [0, 1, 2, 8, 77, 255])
+def test_a_query_that_is_not_a_number_reaches_every_row_that_it_sees(token):
+    """Its normaliser is not a number, and so is the weight of each row that it sees; the others keep theirs."""
+    length, count = 700, 256
+    m = mirror([length, 90], 1, 64, 16)
+    q = rand((count + 90, 1, 64), BF, 2)
+    q[token] = float("nan")
+    starts, counts = torch.tensor([0, count], dtype=torch.int32), torch.tensor([count, 90], dtype=torch.int32)
+    cache = m.cache(ec)
+    ws = scratch(ec.ec_paged_chunk_workspace(cache, 1))
+    out, lse = torch.empty(count + 90, 1, 64, dtype=BF, device="cuda"), torch.empty(count + 90, 1, device="cuda")
+    ec.ec_paged_chunk_attention(q.cuda(), starts.cuda(), counts.cuda(), cache, 0.125, out, lse, ws)
+    ec.ec_paged_chunk_weights(q.cuda(), lse, starts.cuda(), counts.cuda(), cache, 0.125, 1.0, ws)
+    weight = m.dev["weight"].cpu()
+    for n, rows in ((0, length), (1, 90)):
+        page, slot = m.where(n, rows)
+        bad = torch.isnan(weight[page, 0, slot])
+        sees = torch.arange(rows) <= length - count + token if n == 0 else torch.zeros(rows, dtype=torch.bool)
+        assert torch.equal(bad, sees)
+
+
 @pytest.mark.parametrize("dt", [BF, HF])
 def test_scores_of_minus_infinity(dt):
     """Keys that give -inf: rows that nothing is left of are zero, the others do without them."""
