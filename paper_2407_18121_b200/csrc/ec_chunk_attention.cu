@@ -1,6 +1,35 @@
 // Attention of a chunk of new tokens over a paged cache (grouped query heads, ragged batch), with each row's normaliser.
 //   token t of problem n sees rows j <= lens[n] - counts[n] + t:
 //   x[j] = scale * <q, k_j>,   out = sum_j softmax(x)_j v_j,   lse = log sum_j exp(x_j)
+//
+// One pass over the rows, 128 at a time, for a tile of 128 query rows (tokens with the heads that share the key head):
+//   S = Q K^T      tcgen05.mma from tiles that TMA brought page by page, S in TMEM
+//   P = 2^(c S - m2 + top)   a thread owns a query row; P goes over S, as the type of the rows: one rounding of half a step, the
+//                  tensor cores take nothing wider. Sums and maxima are fp32 and taken before that rounding.
+//   O += P V       P from TMEM, V as it lies in shared memory
+// The running maximum is raised when a half of a tile exceeds it by 2^8 (bf16) or 2^4 (fp16), so O is rescaled rarely.
+//
+// What bounds it. Long prompts: each of two teams of four warps waits for its own S (issued behind its own P V: 512 columns of
+// TMEM hold S of both and O of both, with P over S) while the other computes. Per tile and team about 3200 clocks of softmax
+// (1800 of them exponentials, where the special functions' rate for both teams is 1540) and 2000 of waiting for S. 8192 tokens of
+// 32 heads on 8, D = 128: 670 us, 0.82 PFLOP/s at the 1.5 GHz that the power limit leaves (610 us in a short run); the products alone
+// take 336 us at the rate of a large library product. Few tokens on long caches (32 problems of up to 8 on up to 8192 rows): 37 us,
+// of which 15.5 are the rows' bytes; starting (8 thousand clocks to the first S) and joining the parts are the rest. Many short problems: a unit of one to
+// three tiles keeps the softmax warps busy for 6 to 7 us whatever it holds; for one token a problem the single-token call is the
+// one to use.
+//
+// Why so.
+//  - Two query tiles of a head to a CTA, a team each: rows are fetched once for both. A unit of one query tile has both teams take its
+//    tiles in turn and is put together in the CTA: few tokens meet long caches with twice the warps.
+//  - The batch's work is cut evenly over one resident CTA per SM by a closed form of its cost, and what a cut leaves of a unit goes
+//    through the workspace in fp32, joined in the order of the rows by whoever arrives last: the same bits in every run.
+//  - A lazy maximum per half of a tile lets P V of the first half run under the exponentials of the second.
+//  - Values of masked rows: a warp looks over the tiles that not every token sees and turns what is not finite into zeros (a
+//    product with P = 0 would not hide it); who does see such a row reads it again.
+// Tried and slower, 8192 tokens (670 us) and a mixed batch (79 us): sixteen softmax warps with two threads a row 1083 and 145 (they
+// spill); a whole row of 128 columns a thread 747 and 94 (spills); the maximum looked at behind the exponentials 686 and 90; teams that
+// take turns on a scheduler 705 and 94; S in halves of 64 columns (a product of 64 columns takes as long as one of 128); an item per
+// team for short units (no change); the next launch let in early (mixed 100 against 89 before other steps).
 #include "ec_chunk.cuh"
 
 namespace ec {
@@ -327,7 +356,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
         mbar_init(other_done, 4);
         for (uint32_t k = 0; k < (uint32_t)kItems; ++k) {
             mbar_init(item_full(k), 1);
-            mbar_init(item_empty(k), 2 + 1 + 8);                         // the products' thread, the value check, the softmax warps
+            mbar_init(item_empty(k), 2 + 1 + 8);                         // the products' threads, the value check, the softmax warps
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_to_async();
