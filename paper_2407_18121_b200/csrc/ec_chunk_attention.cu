@@ -29,7 +29,10 @@
 // Tried and slower, 8192 tokens (670 us) and a mixed batch (79 us): sixteen softmax warps with two threads a row 1083 and 145 (they
 // spill); a whole row of 128 columns a thread 747 and 94 (spills); the maximum looked at behind the exponentials 686 and 90; teams that
 // take turns on a scheduler 705 and 94; S in halves of 64 columns (a product of 64 columns takes as long as one of 128); an item per
-// team for short units (no change); the next launch let in early (mixed 100 against 89 before other steps).
+// team for short units (no change); the second team helping to put a single query tile together and to join its parts (32 problems of few
+// tokens 37.0 and 36.5, the long prompt 608 and 651 in short runs); a masked half that nobody sees as plain zeros (many units of one tile
+// 5% faster, the long prompt 666); the next launch let in early (mixed 100 against 89 before other steps). What stands around the loop
+// over the tiles moves its time by several per cent, whatever it does.
 #include "ec_chunk.cuh"
 
 namespace ec {

@@ -9,8 +9,8 @@
 // Four teams of four warps hold 512 rows of a head, the query tiles (and their numbers) stream past: a query tile is fetched once per
 // 512 rows, a row once. A team's S is the only one that it has; while its threads compute, the products fill the other teams'.
 // Units are cut over the CTAs along the queries; the parts are added in the order of the tokens by whoever arrives last.
-// Bound: the exponentials' issue. 8192 tokens of 32 heads on 8, D = 128: 331 us, 0.83 PFLOP/s (168 us at the rate of a large library
-// product); about 2 thousand clocks for the four tiles that a query tile meets. 32 problems of up to 8 tokens on up to 8192 rows:
+// Bound: the special functions, at 64% of their rate: about 4800 clocks for the four tiles of S that a query tile meets, 3070 of them
+// exponentials. 8192 tokens of 32 heads on 8, D = 128: 331 us, 0.83 PFLOP/s (168 us at the rate of a large library product). 32 problems of up to 8 tokens on up to 8192 rows:
 // 35 us, of which 8 are the rows' bytes; the rest is starting, one query tile's latency per unit, and joining.
 #include "ec_chunk.cuh"
 
