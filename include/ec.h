@@ -607,7 +607,7 @@ int ec_paged_decode_step(const void *q_dev, const void *k_new_dev, const void *v
 /*
  * Several new tokens of every problem at once: a piece of a prompt, a whole prompt, drafted tokens to be verified. The tokens
  * of all problems are packed one after the other: problem n has counts[n] of them from starts[n] on (device arrays, so that a
- * captured run can be replayed on other lengths). A step:
+ * captured run can be replayed on other lengths). With no tokens at all the calls do nothing, and the packed tensors may be NULL. A step:
  *
  *   ec_paged_release          pages that no row needs any more go back to the pool
  *   ec_paged_reserve          the chunk's rows get pages; every token learns its slot and its position; lens and seen grow
@@ -683,7 +683,7 @@ int ec_rotary_frequencies(double *freqs_host, float *factor_host, int rot, doubl
  *   positions_dev   int32 [N, T], rows pos_n apart (0: one row of positions for all)
  *   freqs_dev       fp64 [rot / 2] (NULL when rot = 0)
  *   rot             0 .. D, a multiple of 16 (interleaved: of 8)
- * Limits: N * T < 2^31.
+ * Limits: N * T < 2^31, heads <= 65536.
  */
 int ec_rotary(const void *x_dev, int64_t x_n, int64_t x_t, int64_t x_h, void *out_dev, int64_t out_n, int64_t out_t, int64_t out_h,
               const int32_t *positions_dev, int64_t pos_n, const double *freqs_dev, int N, int T, int heads, int D, int dtype, int rot,
@@ -698,7 +698,8 @@ int ec_rotary(const void *x_dev, int64_t x_n, int64_t x_t, int64_t x_h, void *ou
  *   k_dev, v_dev      [tokens, H, D] by strides                                                            (in)
  *   w_new_dev         fp32 [tokens, H] weights of the rows; NULL: zero                                     (in)
  *   slots_dev, positions_dev  int32 [tokens]; slots that are not negative differ from each other           (in)
- * A slot behind the pool is left out and the status word says EC_ERR_PAGE. Inputs must not overlap the pool.
+ * A slot behind the pool is left out and the status word says EC_ERR_PAGE. Inputs must not overlap the pool. Limits: Hq + H <= 65536,
+ * tokens * (Hq + H) < 2^31.
  */
 int ec_paged_join(const void *q_dev, int64_t q_t, int64_t q_h, void *q_out_dev, int64_t qo_t, int64_t qo_h, const void *k_dev,
                   int64_t k_t, int64_t k_h, const void *v_dev, int64_t v_t, int64_t v_h, const float *w_new_dev, const int32_t *slots_dev,
@@ -732,8 +733,9 @@ int ec_paged_chunk_attention(const void *q_dev, int64_t q_t, int64_t q_h, const 
  *   weight_j <- decay^count * weight_j + sum_t decay^(count - 1 - t) * sum_g p[t, g, j]
  * over the group's query heads: what counts[n] calls of ec_paged_attention for one token each would have left.
  *   lse_dev           fp32 [tokens, Hq] as ec_paged_chunk_attention gives it, same q, scale and cache; -inf: the row takes no part (in)
- * Other arguments, limits and workspace as there; 0 < decay <= 1, in double: its powers over a long chunk would show a rounding. NaN in q, lse or a key that is seen leaves the weights of the rows that
- * meet it undefined. Deterministic.
+ * Other arguments, limits and workspace as there; 0 < decay <= 1, in double: its powers over a long chunk would show a rounding.
+ * An lse that is not a number (NaN in q, or in a key that is seen) makes the weights of the rows that its token sees not a number.
+ * Deterministic.
  */
 int ec_paged_chunk_weights(const void *q_dev, int64_t q_t, int64_t q_h, const float *lse_dev, const int32_t *starts_dev,
                            const int32_t *counts_dev, const ec_paged *c, int Hq, int tokens, float scale, double decay, void *ws_dev,

@@ -594,8 +594,12 @@ class ec_pages:
     held int32 [N], how many every problem holds. At the start free_pages holds all page numbers and held is zero."""
 
     def __init__(self, free_pages: torch.Tensor, n_free: torch.Tensor, held: torch.Tensor):
-        self.free_pages, self.n_free, self.held = free_pages, n_free, held
+        self._arrays = free_pages, n_free, held
         self._for = None
+
+    free_pages = property(lambda self: self._arrays[0])          # the library keeps their addresses: they stay what they are
+    n_free = property(lambda self: self._arrays[1])
+    held = property(lambda self: self._arrays[2])
 
     def _c(self, cache: ec_paged) -> _ec_pages:
         if self._for is None or self._for[0] is not cache:

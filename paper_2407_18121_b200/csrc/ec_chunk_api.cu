@@ -162,13 +162,13 @@ int ec_rotary(const void *x, int64_t x_n, int64_t x_t, int64_t x_h, void *out, i
     if (dtype != EC_BF16 && dtype != EC_FP16) return EC_ERR_ARG;
     if ((long long)N * T >= (1LL << 31) || heads > 65536) return EC_ERR_SHAPE;
     int st = check_turn(freqs, rot, interleaved, factor, D);
-    if (st == EC_OK) st = check_rows(x, x_t, x_h, D);
+    if (st != EC_OK || N == 0 || T == 0) return st;                      // of no rows nothing is looked at
+    st = check_rows(x, x_t, x_h, D);
     if (st == EC_OK) st = check_rows(out, out_t, out_h, D);
     if (st != EC_OK) return st;
     if (!positions) return EC_ERR_NULL;
     if (!aligned(positions, 4)) return EC_ERR_ALIGN;
     if (x_n < 0 || out_n < 0 || x_n % 8 || out_n % 8 || pos_n < 0) return EC_ERR_ARG;
-    if (N == 0 || T == 0) return EC_OK;
     ec::RotaryRows r;
     r.x = static_cast<const uint4 *>(x);
     r.out = static_cast<uint4 *>(out);
@@ -194,16 +194,16 @@ int ec_paged_join(const void *q, int64_t q_t, int64_t q_h, void *q_out, int64_t 
     int st = ec::check_paged(c);
     if (st != EC_OK) return st;
     if (tokens < 0 || Hq < 0 || (long long)tokens * (Hq + c->H) >= (1LL << 31) || Hq + c->H > 65536) return EC_ERR_SHAPE;
-    if ((Hq > 0) != (q != nullptr) || (Hq > 0) != (q_out != nullptr)) return EC_ERR_NULL;
     st = check_turn(freqs, rot, interleaved, factor, c->D);
-    if (st == EC_OK && Hq > 0) st = check_rows(q, q_t, q_h, c->D);
+    if (st != EC_OK || tokens == 0) return st;
+    if ((Hq > 0) != (q != nullptr) || (Hq > 0) != (q_out != nullptr)) return EC_ERR_NULL;
+    if (Hq > 0) st = check_rows(q, q_t, q_h, c->D);
     if (st == EC_OK && Hq > 0) st = check_rows(q_out, qo_t, qo_h, c->D);
     if (st == EC_OK) st = check_rows(k, k_t, k_h, c->D);
     if (st == EC_OK) st = check_rows(v, v_t, v_h, c->D);
     if (st != EC_OK) return st;
     if (!slots || !positions) return EC_ERR_NULL;
     if (!aligned(slots, 4) || !aligned(positions, 4) || !aligned(w_new, 4)) return EC_ERR_ALIGN;
-    if (tokens == 0) return EC_OK;
     ec::JoinArgs j;
     j.q = static_cast<const uint4 *>(q);
     j.k = static_cast<const uint4 *>(k);
@@ -238,8 +238,8 @@ int ec_paged_chunk_attention(const void *q, int64_t q_t, int64_t q_h, const int3
 {
     ec::NvtxRange nvtx_range("ec_paged_chunk_attention");
     int st = check_chunk(c, starts, counts, tokens, Hq, scale);
-    if (st == EC_OK) st = check_rows(q, q_t, q_h, c->D);
-    if (st == EC_OK) st = check_rows(out, out_t, out_h, c->D);
+    if (st == EC_OK && tokens > 0) st = check_rows(q, q_t, q_h, c->D);
+    if (st == EC_OK && tokens > 0) st = check_rows(out, out_t, out_h, c->D);
     if (st != EC_OK) return st;
     if (!aligned(lse, 4)) return EC_ERR_ALIGN;
     st = ec::check_ws(ws, ws_bytes, ec_paged_chunk_workspace(c, Hq));
@@ -253,9 +253,9 @@ int ec_paged_chunk_weights(const void *q, int64_t q_t, int64_t q_h, const float 
 {
     ec::NvtxRange nvtx_range("ec_paged_chunk_weights");
     int st = check_chunk(c, starts, counts, tokens, Hq, scale);
-    if (st == EC_OK) st = check_rows(q, q_t, q_h, c->D);
+    if (st == EC_OK && tokens > 0) st = check_rows(q, q_t, q_h, c->D);
     if (st != EC_OK) return st;
-    if (!lse) return EC_ERR_NULL;
+    if (!lse && tokens > 0) return EC_ERR_NULL;
     if (!(decay > 0.0 && decay <= 1.0)) return EC_ERR_ARG;
     if (!aligned(lse, 4)) return EC_ERR_ALIGN;
     st = ec::check_ws(ws, ws_bytes, ec_paged_chunk_workspace(c, Hq));

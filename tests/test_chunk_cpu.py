@@ -91,6 +91,26 @@ def test_rotary_refusals(L):  # noqa: F811
     assert f(N=0) == 0 and f(T=0) == 0
 
 
+def test_no_tokens_are_nothing_to_do(L):  # noqa: F811
+    """Tensors without elements have no address."""
+    r = C.byref(paged())
+    size = L.ec_paged_chunk_workspace(r, 6)
+    assert L.ec_paged_chunk_attention(None, 384, 64, P, P, r, 6, 0, 1.0, None, 384, 64, None, P, size, None) == 0
+    assert L.ec_paged_chunk_weights(None, 384, 64, None, P, P, r, 6, 0, 1.0, 1.0, P, size, None) == 0
+    assert L.ec_paged_join(None, 384, 64, None, 384, 64, None, 128, 64, None, 128, 64, None, None, None, r, 6, 0, P, 32, 0, 1.0, None) == 0
+    assert L.ec_rotary(None, 0, 256, 64, None, 0, 256, 64, None, 0, P, 2, 0, 4, 64, 0, 64, 0, 1.0, 0, None) == 0
+    assert L.ec_paged_join(None, 384, 64, None, 384, 64, None, 128, 64, None, 128, 64, None, None, None, r, 6, 0, P, 24, 0, 1.0, None) == 4
+
+
+def test_the_arrays_of_a_pool_stay():
+    t = torch.zeros(3, dtype=torch.int32)
+    pages = ec.ec_pages(t, t, t)
+    for name in ("free_pages", "n_free", "held"):
+        assert getattr(pages, name) is t
+        with pytest.raises(AttributeError):
+            setattr(pages, name, t.clone())
+
+
 def test_frequencies(L):  # noqa: F811
     f, factor = ec.ec_rotary_frequencies(64)
     assert factor == 1.0 and torch.allclose(f, 10000.0 ** (-torch.arange(32, dtype=torch.float64) / 32), rtol=1e-15, atol=0)
