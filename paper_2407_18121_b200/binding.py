@@ -703,6 +703,22 @@ def ec_paged_chunk_workspace(cache: ec_paged, Hq: int) -> int:
     return int(lib().ec_paged_chunk_workspace(C.byref(cache), int(Hq)))
 
 
+def check_chunk_args(cache: ec_paged, Hq: int, counts: torch.Tensor, lse: Optional[torch.Tensor], q: torch.Tensor, k: torch.Tensor,
+                     v: torch.Tensor, out: torch.Tensor) -> None:
+    """ValueError unless a chunk of these tensors would be taken by all of its calls."""
+    N, H, D, dt, dev = cache._dims
+    tokens = q.shape[0]
+    _paged_stream(dev)
+    for name, t, heads in (("q", q, Hq), ("k", k, H), ("v", v, H), ("out", out, Hq)):
+        p, token, head = _rows(t, name, dt, (tokens, heads, D), dev)
+        if tokens > 0 and (p % 16 or token < 1 or token % 8 or head < D or head % 8):
+            raise ValueError(f"rows of {name} must begin at multiples of 16 bytes and not overlap, got strides {t.stride()}")
+    _want(lse, "lse", torch.float32, (tokens, Hq), dev)
+    _want(counts, "counts", torch.int32, (N,), dev)
+    if tokens * (Hq + H) >= 1 << 31:
+        raise ValueError(f"too many tokens: {tokens}")
+
+
 def _first(starts: torch.Tensor, N: int, device: int) -> int:
     if starts.shape not in ((N,), (N + 1,)):
         raise ValueError(f"starts must be int32 [{N}] or [{N + 1}], got {list(starts.shape)}")

@@ -262,6 +262,10 @@ class PagedPoolSession(PagedCacheSession):
         self.N, self.H, self.D, self.Hq = N, H, D, Hq or H
         self.budget, self.recent, self.sinks = int(budget), int(recent), int(sinks)
         self.scale, self.decay = float(scale), float(decay)
+        if not 0.0 < self.scale < 1e38 or not 0.0 < self.decay <= 1.0:
+            raise ValueError(f"scale must be positive and decay in (0, 1], got {scale} and {decay}")
+        if not 0 <= rot <= D or rot % (8 if interleaved else 16) or (rot and (freqs is None or tuple(freqs.shape) != (rot // 2,))):
+            raise ValueError(f"rot = {rot} must be a multiple of 16 (interleaved: of 8) up to {D}, with {rot // 2} frequencies")
         dev = device or torch.device("cuda", torch.cuda.current_device())
         self.device = dev
         n_pages, max_pages = -(-int(pool_rows) // page_size), -(-(self.budget + int(chunk)) // page_size)
@@ -287,6 +291,7 @@ class PagedPoolSession(PagedCacheSession):
     def chunk(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, counts: torch.Tensor, out: torch.Tensor,
               lse: Optional[torch.Tensor] = None) -> None:
         """counts[n] tokens of every problem, packed in order of the problems. Can be captured and replayed with other counts."""
+        ec.check_chunk_args(self.cache, self.Hq, counts, lse, q, k, v, out)      # once the rows have joined it is too late
         tokens = q.shape[0]
         i32 = dict(dtype=torch.int32, device=self.device)
         slots, positions = torch.empty(tokens, **i32), torch.empty(tokens, **i32)
@@ -317,8 +322,10 @@ class PagedPoolSession(PagedCacheSession):
         if counts is None:
             counts = torch.full((self.N,), K.shape[2], dtype=torch.int32, device=self.device)
         kept = self._rows_for(counts)
-        super().append(K, V, scores, counts)
-        self.lens.copy_(torch.where((self.granted == 0) & (counts > 0), kept, self.lens))
+        try:
+            super().append(K, V, scores, counts)
+        finally:
+            self.lens.copy_(torch.where((self.granted == 0) & (counts > 0), kept, self.lens))
 
     def prompt(self, *args, **kwargs) -> None:
         raise ValueError("a prompt is a chunk here: chunk()")
@@ -328,5 +335,7 @@ class PagedPoolSession(PagedCacheSession):
         """One generation step. Problems that get no page are left out: `granted` is 0, their output zero."""
         ones = torch.ones(self.N, dtype=torch.int32, device=self.device)
         kept = self._rows_for(ones)
-        super().decode(q, k_new, v_new, out, lse)
-        self.lens.copy_(torch.where(self.granted == 0, kept, self.lens))
+        try:
+            super().decode(q, k_new, v_new, out, lse)
+        finally:
+            self.lens.copy_(torch.where(self.granted == 0, kept, self.lens))

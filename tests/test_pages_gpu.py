@@ -447,3 +447,41 @@ def test_the_session_refuses():
         s.chunk(q, q[:4], q, i32([5, 0]), torch.empty_like(q))
     with pytest.raises(ValueError):
         s.chunk(q, q, q, i32([5]), torch.empty_like(q))
+
+
+def test_a_refused_call_leaves_the_session_as_it_was():
+    """Wrong tensors are found before any row joins, and places that wait for pages keep their rows."""
+    s = PagedPoolSession(2, 2, 64, budget=64, recent=8, sinks=1, scale=0.125, pool_rows=32, chunk=40, page_size=16)
+    q = rand((32, 2, 64), BF, 1).cuda()
+    out = torch.empty_like(q)
+    s.chunk(q, q, q, i32([16, 16]), out)                   # the pool is empty now
+    wide = torch.zeros(32, 2, 68, dtype=BF, device="cuda")[:, :, :64]
+    for bad in (dict(k=q[:4]), dict(v=q.half()), dict(out=out[:, :1]), dict(q=wide), dict(out=wide), dict(counts=i32([16])),
+                dict(lse=torch.empty(32, 1, device="cuda")), dict(k=q.cpu())):
+        a = dict(q=q, k=q, v=q, counts=i32([16, 16]), out=out, lse=None)
+        a.update(bad)
+        with pytest.raises(ValueError):
+            s.chunk(**a)
+        assert s.lens.tolist() == [16, 16] and s.seen.tolist() == [16, 16] and s.pages.held.tolist() == [1, 1]
+    one = q[:2].clone()
+    with pytest.raises(ValueError):
+        s.decode(one, one, one[:1], torch.empty_like(one))
+    assert s.lens.tolist() == [16, 16]
+    with pytest.raises(ValueError):
+        s.append(torch.zeros(2, 2, 3, 32, dtype=BF, device="cuda"), torch.zeros(2, 2, 3, 64, dtype=BF, device="cuda"), None)
+    assert s.lens.tolist() == [16, 16] and s.status() == ec.EC_OK
+    for kw in (dict(scale=0.0), dict(decay=1.5), dict(rot=24), dict(rot=32), dict(rot=128), dict(rot=32, freqs=torch.ones(8))):
+        with pytest.raises(ValueError):
+            PagedPoolSession(**{**dict(N=2, H=2, D=64, budget=64, recent=8, sinks=1, scale=0.125, pool_rows=400, chunk=40), **kw})
+
+
+def test_a_chunk_of_no_tokens():
+    s = PagedPoolSession(2, 2, 64, budget=64, recent=8, sinks=1, scale=0.125, pool_rows=400, chunk=40)
+    q = rand((5, 2, 64), BF, 1).cuda()
+    s.chunk(q, q, q, i32([2, 3]), torch.empty_like(q))
+    weight = s.weight.clone()
+    s.chunk(q[:0], q[:0], q[:0], i32([0, 0]), torch.empty_like(q[:0]))
+    s.chunk(q[:0], q[:0], q[:0], i32([4, 0]), torch.empty_like(q[:0]))   # no packed rows for them: not granted
+    assert s.lens.tolist() == [2, 3] and s.granted.tolist() == [0, 0] and torch.equal(s.weight, weight) and s.status() == ec.EC_OK
+    x = torch.empty(2, 0, 4, 64, dtype=BF, device="cuda")
+    ec.ec_rotary(x, x, torch.empty(2, 0, dtype=torch.int32, device="cuda"), ec.ec_rotary_frequencies(64)[0].cuda(), 64, False)
