@@ -2,7 +2,7 @@
 //   pair i of a head turns by position * freq_i, scaled by `factor`: (a, b) -> (a cos - b sin, a sin + b cos); the inverse turns back
 //   (the transposed map, which is the gradient). Pairs are elements (2 i, 2 i + 1) or (i, i + rot / 2) of the first `rot`.
 // Bound by HBM: every element is read once and written once. 8192 tokens with 32 + 8 + 8 heads of 128 into their pages (151 MB):
-// 32.4 us, 4.7 TB/s (23.1 us at the copy rate); 67 MB turned back 29.7 us against 22.6 of a plain copy of the same tensors.
+// 29.4 us, 5.1 TB/s (23.1 us at the copy rate); 67 MB turned back 24.8 us against 22.4 of a plain copy of the same tensors.
 // What the angles cost is shared by the heads of a token: a CTA
 // works out the sines and cosines of its tokens once, in shared memory.
 //  - An angle is kept as a fraction of a turn in 64 bits of fixed point: freq / 2 pi from the frequency's 64-bit value, times the
@@ -16,6 +16,7 @@ namespace ec {
 namespace {
 
 constexpr int kRotThreads = 128;
+constexpr int kRotCtas = 12;                     // on an SM, by registers: 29.4 and 24.8 us below; 10 and 13 are slower
 
 template <int DTYPE> __device__ __forceinline__ void widen(const uint4 &v, float (&f)[8])
 {
@@ -67,6 +68,14 @@ __device__ __forceinline__ uint4 load_once(const uint4 *p)
     return v;
 }
 
+// Where pair i of `pairs` lies in a token's table. A thread takes the pairs of its piece, PER of them, two at a time: neighbouring pieces
+// lie next to each other, so that a read of a warp meets no bank twice (in the order of the pairs: 32.2 and 29.4 us against 30.5 and 27.6).
+template <int PER> __device__ __forceinline__ int table_place(int i, int pieces)
+{
+    const int j = i % PER;
+    return ((j >> 1) * pieces + i / PER) * 2 + (j & 1);
+}
+
 // What one head row of a token becomes: its place in the input and in the output, nullptr: nothing.
 struct RowPlace {
     const uint4 *from;
@@ -74,7 +83,8 @@ struct RowPlace {
 };
 
 // A thread keeps its place in the head (piece `v`) and walks over the rows (token, head) of the CTA. Places(token, head) gives a row's
-// pointers. One row a thread in flight, and as many CTAs as fit: 8192 tokens of 32 + 8 + 8 heads in 32 us, two rows 37, four 40.
+// pointers. One row a thread in flight, and as many CTAs as fit: two and four rows a thread are slower (32 -> 37 and 40 us before
+// the CTAs were as many).
 template <int DTYPE, bool HALF, typename Places>
 struct RowTurner {
     const RotaryTurn &r;
@@ -110,27 +120,32 @@ struct RowTurner {
     {
         if (at.to == nullptr) return;
         if (turns) {
-            const float2 *cs = table + token * (r.rot / 2);
+            const int pieces = r.rot / (HALF ? 16 : 8);
+            const float4 *cs = reinterpret_cast<const float4 *>(table + token * (r.rot / 2)) + v;
             float x[8];
             widen<DTYPE>(a, x);
             if (HALF) {
                 float y[8];
                 widen<DTYPE>(b, y);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float2 t = cs[8 * v + i];
-                    const float p = x[i] * t.x - y[i] * t.y, q = x[i] * t.y + y[i] * t.x;
+                for (int i = 0; i < 8; i += 2) {
+                    const float4 t = cs[i / 2 * pieces];
+                    const float p = x[i] * t.x - y[i] * t.y, q = x[i + 1] * t.z - y[i + 1] * t.w;
+                    y[i] = x[i] * t.y + y[i] * t.x;
+                    y[i + 1] = x[i + 1] * t.w + y[i + 1] * t.z;
                     x[i] = p;
-                    y[i] = q;
+                    x[i + 1] = q;
                 }
                 at.to[hi] = narrow<DTYPE>(y);
             } else {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float2 t = cs[4 * v + i];
-                    const float p = x[2 * i] * t.x - x[2 * i + 1] * t.y, q = x[2 * i] * t.y + x[2 * i + 1] * t.x;
-                    x[2 * i] = p;
-                    x[2 * i + 1] = q;
+                for (int i = 0; i < 8; i += 4) {
+                    const float4 t = cs[i / 4 * pieces];
+                    const float p = x[i] * t.x - x[i + 1] * t.y, q = x[i + 2] * t.z - x[i + 3] * t.w;
+                    x[i + 1] = x[i] * t.y + x[i + 1] * t.x;
+                    x[i + 3] = x[i + 2] * t.w + x[i + 3] * t.z;
+                    x[i] = p;
+                    x[i + 2] = q;
                 }
             }
             a = narrow<DTYPE>(x);
@@ -154,10 +169,10 @@ struct RowTurner {
 };
 
 template <int DTYPE, bool HALF>
-__global__ void __launch_bounds__(kRotThreads)
+__global__ void __launch_bounds__(kRotThreads, kRotCtas)
 rotary_kernel(const RotaryTurn r, const RotaryRows x, int D, int per)
 {
-    extern __shared__ float2 table[];
+    extern __shared__ __align__(16) float2 table[];
     const int first = blockIdx.x * per, tokens = min(per, x.N * x.T - first);
     grid_wait();
     grid_release();
@@ -170,16 +185,17 @@ rotary_kernel(const RotaryTurn r, const RotaryRows x, int D, int per)
         const int half = r.rot / 2;
         for (int i = threadIdx.x; i < tokens * half; i += kRotThreads) {
             const int t = i / half, token = first + t, n = token / x.T;
-            table[i] = turn_of(r.freqs[i - t * half], x.positions[n * x.pos_n + (token - n * x.T)], r.factor, r.inverse);
+            table[t * half + table_place<HALF ? 8 : 4>(i - t * half, r.rot / (HALF ? 16 : 8))] =
+                turn_of(r.freqs[i - t * half], x.positions[n * x.pos_n + (token - n * x.T)], r.factor, r.inverse);
         }
     });
 }
 
 template <int DTYPE, bool HALF>
-__global__ void __launch_bounds__(kRotThreads)
+__global__ void __launch_bounds__(kRotThreads, kRotCtas)
 join_kernel(const RotaryTurn r, const PagedView c, const JoinArgs j, int D, int per)
 {
-    extern __shared__ float2 table[];
+    extern __shared__ __align__(16) float2 table[];
     __shared__ int slot_s[kRotaryMostTokens], pos_s[kRotaryMostTokens];
     const int first = blockIdx.x * per, tokens = min(per, j.tokens - first);
     grid_wait();
@@ -211,7 +227,7 @@ join_kernel(const RotaryTurn r, const PagedView c, const JoinArgs j, int D, int 
         const int half = r.rot / 2;
         for (int i = threadIdx.x; i < tokens * half; i += kRotThreads) {
             const int t = i / half;
-            table[i] = turn_of(r.freqs[i - t * half], pos_s[t], r.factor, false);
+            table[t * half + table_place<HALF ? 8 : 4>(i - t * half, r.rot / (HALF ? 16 : 8))] = turn_of(r.freqs[i - t * half], pos_s[t], r.factor, false);
         }
     });
     const int pieces = D / 8, v = threadIdx.x % pieces, step = kRotThreads / pieces, rows = tokens * c.H;
@@ -228,7 +244,8 @@ join_kernel(const RotaryTurn r, const PagedView c, const JoinArgs j, int D, int 
     }
 }
 
-// Tokens of a CTA: their angles are worked out together. Few tokens spread over as many CTAs.
+// Tokens of a CTA: their angles are worked out together (one: 30.5 and 23.9 us, two: 29.4 and 24.8, four: 30.5 and 27.6). Few tokens spread
+// over as many CTAs.
 int tokens_per_cta(int tokens) { return tokens >= 2048 ? kRotaryMostTokens : 1; }
 
 }  // namespace
