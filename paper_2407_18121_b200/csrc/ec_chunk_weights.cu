@@ -9,8 +9,9 @@
 // Four teams of four warps hold 512 rows of a head, the query tiles (and their numbers) stream past: a query tile is fetched once per
 // 512 rows, a row once. A team's S is the only one that it has; while its threads compute, the products fill the other teams'.
 // Units are cut over the CTAs along the queries; the parts are added in the order of the tokens by whoever arrives last.
-// Bound: the special functions, at 64% of their rate: about 4800 clocks for the four tiles of S that a query tile meets, 3070 of them
-// exponentials. 8192 tokens of 32 heads on 8, D = 128: 331 us, 0.83 PFLOP/s (168 us at the rate of a large library product). 32 problems of up to 8 tokens on up to 8192 rows:
+// Bound: the special functions, at 65% of their rate: about 4700 clocks for the four tiles of S that a query tile meets, 3070 of them
+// exponentials. 8192 tokens of 32 heads on 8, D = 128: 333 us, 0.83 PFLOP/s (168 us at the rate of a large library product; 293 in a
+// short run, 301 with two warps more that did nothing; S handed back a chunk earlier 299 to 339, with its spills). 32 problems of up to 8 tokens on up to 8192 rows:
 // 35 us, of which 8 are the rows' bytes; the rest is starting, one query tile's latency per unit, and joining.
 #include "ec_chunk.cuh"
 
@@ -20,7 +21,7 @@ namespace {
 
 constexpr int kTeams = 4;                        // of four warps, with a tile of 128 cached rows each
 constexpr int kBlockRows = kTeams * kTileRows;   // cached rows of a unit: the query tiles stream past all of them at once
-constexpr int kThreads = 128 + kTeams * 128;     // warps: copies, products, (two none), teams
+constexpr int kThreads = 64 + kTeams * 128;      // warps: copies, products, teams
 constexpr int kItems = 4;
 constexpr int kStages = 3;                       // query tiles
 constexpr int kTmemCols = 512;                   // S of every team
@@ -298,9 +299,9 @@ chunk_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     }
             }
         }
-    } else if (warp >= 4) {
+    } else {
         // ------------------------------------------------------------ sums: a thread owns a cached row
-        const uint32_t x = (uint32_t)(warp - 4) >> 2;
+        const uint32_t x = (uint32_t)(warp - 2) >> 2;
         const int q4 = warp & 3, r = q4 * 32 + lane;
         const uint32_t s_addr = tmem + x * kTileRows + ((uint32_t)(q4 * 32) << 16);
         const float2 c2 = make_float2(a.scale_log2e, a.scale_log2e);
