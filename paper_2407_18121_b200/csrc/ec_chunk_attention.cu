@@ -26,8 +26,8 @@
 //  - A lazy maximum per half of a tile lets P V of the first half run under the exponentials of the second.
 //  - Values of masked rows: a warp looks over the tiles that not every token sees and turns what is not finite into zeros (a
 //    product with P = 0 would not hide it); who does see such a row reads it again.
-// Tried and slower, 8192 tokens (670 us) and a mixed batch (79 us): sixteen softmax warps with two threads a row 1083 and 145 (they
-// spill); a whole row of 128 columns a thread 747 and 94 (spills); the maximum looked at behind the exponentials 686 and 90; teams that
+// Tried and slower, 8192 tokens (670 us) and a mixed batch (79 us): sixteen softmax warps with two threads a row (they spill
+// and meet once a tile; 732 against 609 in short runs, 98 against 82); a whole row of 128 columns a thread 747 and 94 (spills); the maximum looked at behind the exponentials 686 and 90; teams that
 // take turns on a scheduler 705 and 94; S in halves of 64 columns (a product of 64 columns takes as long as one of 128); an item per
 // team for short units (no change); the second team helping to put a single query tile together and to join its parts (32 problems of few
 // tokens 37.0 and 36.5, the long prompt 608 and 651 in short runs); a masked half that nobody sees as plain zeros (many units of one tile
