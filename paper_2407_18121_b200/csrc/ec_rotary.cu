@@ -2,7 +2,8 @@
 //   pair i of a head turns by position * freq_i, scaled by `factor`: (a, b) -> (a cos - b sin, a sin + b cos); the inverse turns back
 //   (the transposed map, which is the gradient). Pairs are elements (2 i, 2 i + 1) or (i, i + rot / 2) of the first `rot`.
 // Bound by HBM: every element is read once and written once. 8192 tokens with 32 + 8 + 8 heads of 128 into their pages (151 MB):
-// 29.4 us, 5.1 TB/s (23.1 us at the copy rate); 67 MB turned back 24.8 us against 22.4 of a plain copy of the same tensors.
+// 29.2 us, 5.2 TB/s (23.1 us at the copy rate); 67 MB turned back 24.6 us against 22.4 of a plain copy of the same tensors. The issue
+// slots are as busy as the memory (75%): no division per row, two pairs an instruction (16384 tokens of 8 heads 19.1 -> 17.0 us).
 // What the angles cost is shared by the heads of a token: a CTA
 // works out the sines and cosines of its tokens once, in shared memory.
 //  - An angle is kept as a fraction of a turn in 64 bits of fixed point: freq / 2 pi from the frequency's 64-bit value, times the
@@ -18,33 +19,19 @@ namespace {
 constexpr int kRotThreads = 128;
 constexpr int kRotCtas = 12;                     // on an SM, by registers: 29.4 and 24.8 us below; 10 and 13 are slower
 
-template <int DTYPE> __device__ __forceinline__ void widen(const uint4 &v, float (&f)[8])
+template <int DTYPE> __device__ __forceinline__ float2 widen2(uint32_t v)
 {
-    if constexpr (DTYPE == EC_BF16) {
-        unpack8(v, f);
-    } else {
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float2 p = __half22float2(*reinterpret_cast<const __half2 *>(&w[i]));
-            f[2 * i] = p.x;
-            f[2 * i + 1] = p.y;
-        }
-    }
+    if constexpr (DTYPE == EC_BF16) return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xFFFF0000u));
+    else return __half22float2(*reinterpret_cast<const __half2 *>(&v));
 }
 
-template <int DTYPE> __device__ __forceinline__ uint4 narrow(const float (&f)[8])
+template <int DTYPE> __device__ __forceinline__ uint32_t narrow2(float2 f)
 {
     if constexpr (DTYPE == EC_BF16) {
-        return pack8(f);
+        return pack2(f.x, f.y);
     } else {
-        uint32_t w[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const __half2 h = __floats2half2_rn(f[2 * i], f[2 * i + 1]);
-            w[i] = *reinterpret_cast<const uint32_t *>(&h);
-        }
-        return make_uint4(w[0], w[1], w[2], w[3]);
+        const __half2 h = __floats2half2_rn(f.x, f.y);
+        return *reinterpret_cast<const uint32_t *>(&h);
     }
 }
 
@@ -68,12 +55,14 @@ __device__ __forceinline__ uint4 load_once(const uint4 *p)
     return v;
 }
 
-// Where pair i of `pairs` lies in a token's table. A thread takes the pairs of its piece, PER of them, two at a time: neighbouring pieces
-// lie next to each other, so that a read of a warp meets no bank twice (in the order of the pairs: 32.2 and 29.4 us against 30.5 and 27.6).
-template <int PER> __device__ __forceinline__ int table_place(int i, int pieces)
+// A token's table: for two neighbouring pairs (cos, cos, sin, sin), a piece of a row takes PER pairs. Neighbouring pieces lie next to
+// each other, so that a read of a warp meets no bank twice (in the order of the pairs: 32.2 and 29.4 us against 30.5 and 27.6).
+template <int PER> __device__ __forceinline__ void put_turn(float *table, int i, int pieces, float2 cs)
 {
     const int j = i % PER;
-    return ((j >> 1) * pieces + i / PER) * 2 + (j & 1);
+    float *to = table + ((j >> 1) * pieces + i / PER) * 4 + (j & 1);
+    to[0] = cs.x;
+    to[2] = cs.y;
 }
 
 // What one head row of a token becomes: its place in the input and in the output, nullptr: nothing.
@@ -89,19 +78,20 @@ template <int DTYPE, bool HALF, typename Places>
 struct RowTurner {
     const RotaryTurn &r;
     Places places;
-    int step, v, lo, hi, row, rows, heads;       // lo, hi: pieces of a row, of 16 bytes; hi < 0: there is none
+    int step, v, lo, hi;                         // lo, hi: pieces of a row, of 16 bytes; hi < 0: there is none
+    int token, head, tokens, heads;              // the row in flight, until token = tokens
     bool turns;
     RowPlace at;
     uint4 a, b;
-    int token;
 
-    __device__ __forceinline__ RowTurner(const RotaryTurn &turn, int D, int tokens, int heads_, Places p) : r(turn), places(p), heads(heads_)
+    __device__ __forceinline__ RowTurner(const RotaryTurn &turn, int D, int tokens_, int heads_, Places p) : r(turn), places(p), tokens(tokens_), heads(heads_)
     {
         const int turning = r.rot / (HALF ? 16 : 8), pieces = turning + (D - r.rot) / 8;
         step = kRotThreads / pieces;
         v = threadIdx.x % pieces;
-        row = threadIdx.x / pieces;
-        rows = row < step ? tokens * heads : 0;
+        head = threadIdx.x / pieces;
+        token = head < step ? 0 : tokens;        // threads without a piece of a row
+        settle();
         turns = v < turning;
         lo = turns ? v : v - turning + r.rot / 8;
         hi = HALF && turns ? v + r.rot / 16 : -1;
@@ -109,11 +99,18 @@ struct RowTurner {
 
     __device__ __forceinline__ void load()
     {
-        token = row / heads;
-        at = places(token, row - token * heads);
+        at = places(token, head);
         if (at.to == nullptr) return;
         a = load_once(at.from + lo);
         if (hi >= 0) b = load_once(at.from + hi);
+    }
+
+    __device__ __forceinline__ void settle()
+    {
+        while (head >= heads && token < tokens) {
+            head -= heads;
+            ++token;
+        }
     }
 
     __device__ __forceinline__ void store(const float2 *table)
@@ -122,33 +119,22 @@ struct RowTurner {
         if (turns) {
             const int pieces = r.rot / (HALF ? 16 : 8);
             const float4 *cs = reinterpret_cast<const float4 *>(table + token * (r.rot / 2)) + v;
-            float x[8];
-            widen<DTYPE>(a, x);
-            if (HALF) {
-                float y[8];
-                widen<DTYPE>(b, y);
+            uint32_t *xa = reinterpret_cast<uint32_t *>(&a), *xb = reinterpret_cast<uint32_t *>(&b);
 #pragma unroll
-                for (int i = 0; i < 8; i += 2) {
+            for (int i = 0; i < 4; ++i) {
+                const float2 u = widen2<DTYPE>(xa[i]);
+                if (HALF) {                      // two pairs an instruction
+                    const float4 t = cs[i * pieces];
+                    const float2 c = make_float2(t.x, t.y), s = make_float2(t.z, t.w), w = widen2<DTYPE>(xb[i]);
+                    xa[i] = narrow2<DTYPE>(__ffma2_rn(u, c, __fmul2_rn(make_float2(-w.x, -w.y), s)));
+                    xb[i] = narrow2<DTYPE>(__ffma2_rn(u, s, __fmul2_rn(w, c)));
+                } else {
                     const float4 t = cs[i / 2 * pieces];
-                    const float p = x[i] * t.x - y[i] * t.y, q = x[i + 1] * t.z - y[i + 1] * t.w;
-                    y[i] = x[i] * t.y + y[i] * t.x;
-                    y[i + 1] = x[i + 1] * t.w + y[i + 1] * t.z;
-                    x[i] = p;
-                    x[i + 1] = q;
-                }
-                at.to[hi] = narrow<DTYPE>(y);
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; i += 4) {
-                    const float4 t = cs[i / 4 * pieces];
-                    const float p = x[i] * t.x - x[i + 1] * t.y, q = x[i + 2] * t.z - x[i + 3] * t.w;
-                    x[i + 1] = x[i] * t.y + x[i + 1] * t.x;
-                    x[i + 3] = x[i + 2] * t.w + x[i + 3] * t.z;
-                    x[i] = p;
-                    x[i + 2] = q;
+                    const float c = i & 1 ? t.y : t.x, s = i & 1 ? t.w : t.z;
+                    xa[i] = narrow2<DTYPE>(make_float2(u.x * c - u.y * s, u.x * s + u.y * c));
                 }
             }
-            a = narrow<DTYPE>(x);
+            if (HALF) at.to[hi] = b;
         }
         at.to[lo] = a;
     }
@@ -157,13 +143,14 @@ struct RowTurner {
     template <typename Table>
     __device__ __forceinline__ void run(const float2 *table, Table make_table)
     {
-        if (row < rows) load();
+        if (token < tokens) load();
         make_table();
         __syncthreads();
-        while (row < rows) {
+        while (token < tokens) {
             store(table);
-            row += step;
-            if (row < rows) load();
+            head += step;
+            settle();
+            if (token < tokens) load();
         }
     }
 };
@@ -176,8 +163,13 @@ rotary_kernel(const RotaryTurn r, const RotaryRows x, int D, int per)
     const int first = blockIdx.x * per, tokens = min(per, x.N * x.T - first);
     grid_wait();
     grid_release();
+    const int n0 = first / x.T, at0 = first - n0 * x.T;
     auto place = [&](int t, int h) {
-        const int token = first + t, n = token / x.T, at = token - n * x.T;
+        int n = n0, at = at0 + t;
+        while (at >= x.T) {
+            at -= x.T;
+            ++n;
+        }
         return RowPlace{x.x + n * x.x_n + at * x.x_t + h * x.x_h, x.out + n * x.out_n + at * x.out_t + h * x.out_h};
     };
     RowTurner<DTYPE, HALF, decltype(place)> turner(r, D, tokens, x.heads, place);
@@ -185,8 +177,8 @@ rotary_kernel(const RotaryTurn r, const RotaryRows x, int D, int per)
         const int half = r.rot / 2;
         for (int i = threadIdx.x; i < tokens * half; i += kRotThreads) {
             const int t = i / half, token = first + t, n = token / x.T;
-            table[t * half + table_place<HALF ? 8 : 4>(i - t * half, r.rot / (HALF ? 16 : 8))] =
-                turn_of(r.freqs[i - t * half], x.positions[n * x.pos_n + (token - n * x.T)], r.factor, r.inverse);
+            put_turn<HALF ? 8 : 4>(reinterpret_cast<float *>(table + t * half), i - t * half, r.rot / (HALF ? 16 : 8),
+                                   turn_of(r.freqs[i - t * half], x.positions[n * x.pos_n + (token - n * x.T)], r.factor, r.inverse));
         }
     });
 }
@@ -197,6 +189,7 @@ join_kernel(const RotaryTurn r, const PagedView c, const JoinArgs j, int D, int 
 {
     extern __shared__ __align__(16) float2 table[];
     __shared__ int slot_s[kRotaryMostTokens], pos_s[kRotaryMostTokens];
+    __shared__ uint32_t offset_s[kRotaryMostTokens], meta_s[kRotaryMostTokens];    // of head 0, in the pools and in weight and pos
     const int first = blockIdx.x * per, tokens = min(per, j.tokens - first);
     grid_wait();
     grid_release();
@@ -208,37 +201,39 @@ join_kernel(const RotaryTurn r, const PagedView c, const JoinArgs j, int D, int 
         }
         slot_s[threadIdx.x] = slot;
         pos_s[threadIdx.x] = j.positions[first + threadIdx.x];
+        if (slot >= 0) {
+            Slot s;
+            s.page = page_of(c, slot);
+            s.slot = slot - s.page * c.page_size;
+            offset_s[threadIdx.x] = row_offset(c, s);
+            meta_s[threadIdx.x] = meta_index(c, 0, s);
+        }
     }
     __syncthreads();
-    auto place = [&](int t) {
-        Slot s;
-        s.page = page_of(c, slot_s[t]);
-        s.slot = slot_s[t] - s.page * c.page_size;
-        return s;
-    };
     auto row_place = [&](int t, int h) {
         if (slot_s[t] < 0) return RowPlace{nullptr, nullptr};
         if (h < j.Hq) return RowPlace{j.q + (first + t) * j.q_t + h * j.q_h, j.q_out + (first + t) * j.qo_t + h * j.qo_h};
         h -= j.Hq;
-        return RowPlace{j.k + (first + t) * j.k_t + h * j.k_h, c.K + row_offset(c, place(t)) + (size_t)h * c.head_step};
+        return RowPlace{j.k + (first + t) * j.k_t + h * j.k_h, c.K + offset_s[t] + (size_t)h * c.head_step};
     };
     RowTurner<DTYPE, HALF, decltype(row_place)> turner(r, D, tokens, j.Hq + c.H, row_place);
     turner.run(table, [&] {
         const int half = r.rot / 2;
         for (int i = threadIdx.x; i < tokens * half; i += kRotThreads) {
             const int t = i / half;
-            table[t * half + table_place<HALF ? 8 : 4>(i - t * half, r.rot / (HALF ? 16 : 8))] = turn_of(r.freqs[i - t * half], pos_s[t], r.factor, false);
+            put_turn<HALF ? 8 : 4>(reinterpret_cast<float *>(table + t * half), i - t * half, r.rot / (HALF ? 16 : 8),
+                                   turn_of(r.freqs[i - t * half], pos_s[t], r.factor, false));
         }
     });
     const int pieces = D / 8, v = threadIdx.x % pieces, step = kRotThreads / pieces, rows = tokens * c.H;
     for (int row = threadIdx.x / pieces; row < rows; row += step) {
         const int t = row / c.H, h = row - t * c.H;
-        if (slot_s[t] >= 0) c.V[row_offset(c, place(t)) + (size_t)h * c.head_step + v] = load_once(j.v + (first + t) * j.v_t + h * j.v_h + v);
+        if (slot_s[t] >= 0) c.V[offset_s[t] + (size_t)h * c.head_step + v] = load_once(j.v + (first + t) * j.v_t + h * j.v_h + v);
     }
     for (int row = threadIdx.x; row < rows; row += kRotThreads) {
         const int t = row / c.H, h = row - t * c.H;
         if (slot_s[t] < 0) continue;
-        const uint32_t at = meta_index(c, h, place(t));
+        const uint32_t at = meta_s[t] + (uint32_t)h * (uint32_t)c.page_size;
         c.weight[at] = j.w_new ? j.w_new[(size_t)(first + t) * c.H + h] : 0.f;
         c.pos[at] = pos_s[t];
     }
