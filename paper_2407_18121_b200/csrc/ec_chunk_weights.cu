@@ -12,7 +12,9 @@
 // Bound: the special functions, at 65% of their rate: about 4700 clocks for the four tiles of S that a query tile meets, 3070 of them
 // exponentials. 8192 tokens of 32 heads on 8, D = 128: 333 us, 0.83 PFLOP/s (168 us at the rate of a large library product; 293 in a
 // short run, 301 with two warps more that did nothing; S handed back a chunk earlier 299 to 339, with its spills). 32 problems of up to 8 tokens on up to 8192 rows:
-// 35 us, of which 8 are the rows' bytes; the rest is starting, one query tile's latency per unit, and joining.
+// 34 us, of which 8 are the rows' bytes; the rest is starting and one query tile's latency per unit: a unit's rows are asked for when the
+// products of the one before are done, its queries before that (behind the rows: 35). Each team's rows let go behind its own last product
+// gained nothing there and cost the long prompt 4%.
 #include "ec_chunk.cuh"
 
 namespace ec {
@@ -194,29 +196,7 @@ chunk_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             __syncwarp();
             if (lane == 0) mbar_arrive(item_full(sl));
             if (!more) break;
-            if (it.qt0 < it.qt1) {
-                // the block's boxes, a lane's first one read ahead
-                const int teams = min(kTeams, (it.len - it.row0 + kTileRows - 1) / kTileRows), boxes = teams * (kTileRows / a.box_rows);
-                int page = lane < boxes ? box_page(a, it.n, it.row0 + lane * a.box_rows, it.len) : -1;
-#pragma unroll 1
-                for (int x = 0; x < teams; ++x) {
-                    if (!mbar_wait(k_empty(x), (nk >> x & 1u) ^ 1u, abort_flag, status, kWaitLimitNs, kPollBackoffNs)) { alive = false; break; }
-                    if (lane == 0) mbar_expect_tx(k_full(x), kTile);
-                    nk ^= 1u << x;
-                    asked |= 1u << x;
-                }
-                if (!alive) break;
-                __syncwarp();
-#pragma unroll 1
-                for (int box = lane; box < boxes; box += 32) {
-                    const int at = box * a.box_rows, row = it.row0 + at, x = at / kTileRows;
-                    if (box >= 32) page = box_page(a, it.n, row, it.len);
-                    bad_page(a, row, it.len, page);
-                    copy_box<D>(a, &map_k, page, it.h, row, at % kTileRows, base + L::kK + x * kTile, k_full(x));
-                }
-                __syncwarp();
-            }
-            for (int q = it.qt0; q < it.qt1 && alive; ++q, ++nq) {
+            auto copy_queries = [&](int q) {
                 const uint32_t s = nq % kStages;
                 float nl[4];
                 bool odd = false;
@@ -229,7 +209,7 @@ chunk_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     if (z != -INFINITY) nl[i] = fmaf(-z, kLog2e, (float)(a.log2_decay * (double)(it.count - 1 - t)));
                     odd |= !(fabsf(nl[i]) < INFINITY);
                 }
-                if (!mbar_wait(q_empty(s), ((nq / kStages) & 1u) ^ 1u, abort_flag, status, kWaitLimitNs, kPollBackoffNs)) { alive = false; break; }
+                if (!mbar_wait(q_empty(s), ((nq / kStages) & 1u) ^ 1u, abort_flag, status, kWaitLimitNs, kPollBackoffNs)) { alive = false; return; }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) lse_s[s * kTileRows + lane + 32 * i] = nl[i];
                 odd = __any_sync(0xFFFFFFFFu, odd);
@@ -241,7 +221,35 @@ chunk_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     for (int half = 0; half < D / 64; ++half)
                         tma_load_3d(base + L::kQ + s * kTile + half * kBoxBytes, &map_q, half * 64, it.h * a.G, it.start + q * a.tile_tokens, q_full(s));
                 }
+                ++nq;
+            };
+            if (it.qt0 < it.qt1) copy_queries(it.qt0);    // ahead of the rows, which wait for more
+            if (!alive) break;
+            if (it.qt0 < it.qt1) {
+                // Tile by tile, behind the products of the unit before. Page numbers of all tiles are read at once where they fit a warp.
+                const int teams = min(kTeams, (it.len - it.row0 + kTileRows - 1) / kTileRows), per = kTileRows / a.box_rows;
+                const bool ahead = teams * per <= 32;
+                const int first = ahead && lane < teams * per ? box_page(a, it.n, it.row0 + lane * a.box_rows, it.len) : -1;
+#pragma unroll 1
+                for (int x = 0; x < teams; ++x) {
+                    int page = __shfl_sync(0xFFFFFFFFu, first, (x * per + lane) & 31);
+                    if (!mbar_wait(k_empty(x), (nk >> x & 1u) ^ 1u, abort_flag, status, kWaitLimitNs, kPollBackoffNs)) { alive = false; break; }
+                    if (lane == 0) mbar_expect_tx(k_full(x), kTile);
+                    nk ^= 1u << x;
+                    asked |= 1u << x;
+                    __syncwarp();
+#pragma unroll 1
+                    for (int box = lane; box < per; box += 32) {
+                        const int at = box * a.box_rows, row = it.row0 + x * kTileRows + at;
+                        if (!ahead) page = box_page(a, it.n, row, it.len);
+                        bad_page(a, row, it.len, page);
+                        copy_box<D>(a, &map_k, page, it.h, row, at, base + L::kK + x * kTile, k_full(x));
+                    }
+                }
+                if (!alive) break;
+                __syncwarp();
             }
+            for (int q = it.qt0 + 1; q < it.qt1 && alive; ++q) copy_queries(q);
             if (!alive) break;
             more = w.next(a, cost);
         }
