@@ -11,6 +11,9 @@
 //    rounding, 2^-53, is all (in fp32 an angle of 10^6 is off by 0.06).
 #include "ec_paged.cuh"
 #include "ec_rotary.cuh"
+#include "ec_tc.cuh"
+
+#include <algorithm>
 
 namespace ec {
 
@@ -71,8 +74,8 @@ struct RowPlace {
     uint4 *to;
 };
 
-// A thread keeps its place in the head (piece `v`) and walks over the rows (token, head) of the CTA. Places(token, head) gives a row's
-// pointers. One row a thread in flight, and as many CTAs as fit: two and four rows a thread are slower (32 -> 37 and 40 us before
+// A thread keeps its place in the head (piece `v`) and walks over the rows (token, head) of the CTA; gridDim.y parts of the heads have a
+// CTA each. Places(token, head) gives a row's pointers. One row a thread in flight, and as many CTAs as fit: two and four rows a thread are slower (32 -> 37 and 40 us before
 // the CTAs were as many).
 template <int DTYPE, bool HALF, typename Places>
 struct RowTurner {
@@ -107,9 +110,13 @@ struct RowTurner {
 
     __device__ __forceinline__ void settle()
     {
-        while (head >= heads && token < tokens) {
-            head -= heads;
-            ++token;
+        if (head < heads || token >= tokens) return;
+        head -= heads;
+        ++token;
+        if (head >= heads) {                     // fewer heads than rows at a time
+            const int n = head / heads;
+            head -= n * heads;
+            token += n;
         }
     }
 
@@ -163,16 +170,17 @@ rotary_kernel(const RotaryTurn r, const RotaryRows x, int D, int per)
     const int first = blockIdx.x * per, tokens = min(per, x.N * x.T - first);
     grid_wait();
     grid_release();
-    const int n0 = first / x.T, at0 = first - n0 * x.T;
+    const int n0 = first / x.T, at0 = first - n0 * x.T, share = (x.heads + gridDim.y - 1) / gridDim.y, h0 = blockIdx.y * share;
     auto place = [&](int t, int h) {
         int n = n0, at = at0 + t;
-        while (at >= x.T) {
-            at -= x.T;
-            ++n;
+        if (at >= x.T) {
+            n += at / x.T;
+            at %= x.T;
         }
+        h += h0;
         return RowPlace{x.x + n * x.x_n + at * x.x_t + h * x.x_h, x.out + n * x.out_n + at * x.out_t + h * x.out_h};
     };
-    RowTurner<DTYPE, HALF, decltype(place)> turner(r, D, tokens, x.heads, place);
+    RowTurner<DTYPE, HALF, decltype(place)> turner(r, D, h0 < x.heads ? tokens : 0, min(share, x.heads - h0), place);
     turner.run(table, [&] {
         const int half = r.rot / 2;
         for (int i = threadIdx.x; i < tokens * half; i += kRotThreads) {
@@ -210,13 +218,15 @@ join_kernel(const RotaryTurn r, const PagedView c, const JoinArgs j, int D, int 
         }
     }
     __syncthreads();
+    const int heads = j.Hq + c.H, share = (heads + gridDim.y - 1) / gridDim.y, h0 = blockIdx.y * share;
     auto row_place = [&](int t, int h) {
+        h += h0;
         if (slot_s[t] < 0) return RowPlace{nullptr, nullptr};
         if (h < j.Hq) return RowPlace{j.q + (first + t) * j.q_t + h * j.q_h, j.q_out + (first + t) * j.qo_t + h * j.qo_h};
         h -= j.Hq;
         return RowPlace{j.k + (first + t) * j.k_t + h * j.k_h, c.K + offset_s[t] + (size_t)h * c.head_step};
     };
-    RowTurner<DTYPE, HALF, decltype(row_place)> turner(r, D, tokens, j.Hq + c.H, row_place);
+    RowTurner<DTYPE, HALF, decltype(row_place)> turner(r, D, h0 < heads ? tokens : 0, min(share, heads - h0), row_place);
     turner.run(table, [&] {
         const int half = r.rot / 2;
         for (int i = threadIdx.x; i < tokens * half; i += kRotThreads) {
@@ -225,13 +235,16 @@ join_kernel(const RotaryTurn r, const PagedView c, const JoinArgs j, int D, int 
                                    turn_of(r.freqs[i - t * half], pos_s[t], r.factor, false));
         }
     });
-    const int pieces = D / 8, v = threadIdx.x % pieces, step = kRotThreads / pieces, rows = tokens * c.H;
+    // values, weights and positions of the part's share of the key heads
+    const int few = (c.H + gridDim.y - 1) / gridDim.y, v0 = blockIdx.y * few, H = min(few, c.H - v0);
+    if (H <= 0) return;
+    const int pieces = D / 8, v = threadIdx.x % pieces, step = kRotThreads / pieces, rows = tokens * H;
     for (int row = threadIdx.x / pieces; row < rows; row += step) {
-        const int t = row / c.H, h = row - t * c.H;
+        const int t = row / H, h = v0 + row - t * H;
         if (slot_s[t] >= 0) c.V[offset_s[t] + (size_t)h * c.head_step + v] = load_once(j.v + (first + t) * j.v_t + h * j.v_h + v);
     }
     for (int row = threadIdx.x; row < rows; row += kRotThreads) {
-        const int t = row / c.H, h = row - t * c.H;
+        const int t = row / H, h = v0 + row - t * H;
         if (slot_s[t] < 0) continue;
         const uint32_t at = meta_s[t] + (uint32_t)h * (uint32_t)c.page_size;
         c.weight[at] = j.w_new ? j.w_new[(size_t)(first + t) * c.H + h] : 0.f;
@@ -239,26 +252,42 @@ join_kernel(const RotaryTurn r, const PagedView c, const JoinArgs j, int D, int 
     }
 }
 
-// Tokens of a CTA: their angles are worked out together (one: 30.5 and 23.9 us, two: 29.4 and 24.8, four: 30.5 and 27.6). Few tokens spread
-// over as many CTAs.
-int tokens_per_cta(int tokens) { return tokens >= 2048 ? kRotaryMostTokens : 1; }
+// A CTA has about 72 rows of 256 bytes: tokens of few heads together (one token of 32 and 48 heads: 23.9 and 30.5 us, two 24.8 and 29.4, four
+// 27.6 and 30.5), as long as there are twelve CTAs an SM; where there are fewer, many heads of a
+// token are split (300 tokens of 288 head rows 29 -> 9 us, 24 of 48 4.6 -> 3.2; 512 of 48 would take 6.0 instead of 4.8). One head, 187
+// thousand tokens: 100 us with two tokens a CTA, 36 with sixteen.
+struct RotaryShape {
+    int per;                                     // tokens of a CTA
+    dim3 grid;
+};
+
+RotaryShape rotary_shape(int tokens, int heads, int D)
+{
+    RotaryShape s;
+    const int rows = 72 * 128 / D;
+    s.per = std::max(1, std::min({(rows + heads / 2) / heads, tokens / (kRotCtas * sm_count()), kRotaryMostTokens}));
+    const int ctas = (tokens + s.per - 1) / s.per;
+    const int least = ctas < sm_count() ? kRotThreads / (D / 8) : rows;   // rows at once, where there are hardly any
+    s.grid = dim3(ctas, std::max(1, std::min(kRotCtas * sm_count() / ctas, (heads + least - 1) / least)));
+    return s;
+}
 
 }  // namespace
 
 cudaError_t launch_rotary(const RotaryTurn &r, const RotaryRows &x, int D, int dtype, bool half, cudaStream_t stream)
 {
-    const int per = tokens_per_cta(x.N * x.T);
-    const dim3 grid((x.N * x.T + per - 1) / per);
-    auto go = [&](auto kernel) { return launch_chained(kernel, grid, kRotThreads, (size_t)per * (r.rot / 2) * sizeof(float2), stream, r, x, D, per); };
+    const RotaryShape shape = rotary_shape(x.N * x.T, x.heads, D);
+    const int per = shape.per;
+    auto go = [&](auto kernel) { return launch_chained(kernel, shape.grid, kRotThreads, (size_t)per * (r.rot / 2) * sizeof(float2), stream, r, x, D, per); };
     if (dtype == EC_BF16) return half ? go(rotary_kernel<EC_BF16, true>) : go(rotary_kernel<EC_BF16, false>);
     return half ? go(rotary_kernel<EC_FP16, true>) : go(rotary_kernel<EC_FP16, false>);
 }
 
 cudaError_t launch_join(const RotaryTurn &r, const PagedView &c, const JoinArgs &j, int D, int dtype, bool half, cudaStream_t stream)
 {
-    const int per = tokens_per_cta(j.tokens);
-    const dim3 grid((j.tokens + per - 1) / per);
-    auto go = [&](auto kernel) { return launch_chained(kernel, grid, kRotThreads, (size_t)per * (r.rot / 2) * sizeof(float2), stream, r, c, j, D, per); };
+    const RotaryShape shape = rotary_shape(j.tokens, j.Hq + c.H, D);
+    const int per = shape.per;
+    auto go = [&](auto kernel) { return launch_chained(kernel, shape.grid, kRotThreads, (size_t)per * (r.rot / 2) * sizeof(float2), stream, r, c, j, D, per); };
     if (dtype == EC_BF16) return half ? go(join_kernel<EC_BF16, true>) : go(join_kernel<EC_BF16, false>);
     return half ? go(join_kernel<EC_FP16, true>) : go(join_kernel<EC_FP16, false>);
 }

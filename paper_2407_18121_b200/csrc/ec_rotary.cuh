@@ -5,7 +5,7 @@
 
 namespace ec {
 
-constexpr int kRotaryMostTokens = 2;             // of a CTA
+constexpr int kRotaryMostTokens = 16;            // of a CTA
 
 struct RotaryTurn {
     const double *freqs;                         // [rot / 2], radians per position

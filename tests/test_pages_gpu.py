@@ -178,6 +178,20 @@ def test_rotary_both_ways(D, rot, interleaved, dt):
             assert torch.equal(out.cpu()[..., rot:].view(torch.int16), x[..., rot:].view(torch.int16))     # the rest as it was, bit for bit
 
 
+@pytest.mark.parametrize("N,T,heads,D,rot,interleaved", [(4300, 7, 1, 64, 64, False), (30011, 1, 1, 64, 48, False), (2, 14000, 3, 128, 24, True),
+                                                         (1, 100, 300, 64, 32, True), (3, 11, 97, 128, 128, False), (1, 1, 2049, 64, 16, False)])
+def test_rotary_many_tokens_of_few_heads_and_the_other_way_round(N, T, heads, D, rot, interleaved):
+    """Tokens that share a CTA across problems, and heads of a token that several CTAs share."""
+    freqs, factor = ec.ec_rotary_frequencies(rot)
+    x = rand((N, T, heads, D), BF, 3)
+    pos = torch.randint(0, 5000, (N, T), generator=torch.Generator().manual_seed(2), dtype=torch.int32)
+    out = torch.full_like(x, 7.0, device="cuda")
+    ec.ec_rotary(x.cuda(), out, pos.cuda(), freqs.cuda(), rot, interleaved, 1.25)
+    want = rotary(x, pos, freqs, 1.25, rot, interleaved)
+    assert ((out.cpu().double() - want).abs() <= turn_tolerance(x, want, 1.25)).all()
+    assert torch.equal(out.cpu()[..., rot:].view(torch.int16), x[..., rot:].view(torch.int16))
+
+
 @pytest.mark.parametrize("interleaved", [False, True])
 def test_rotary_far_and_negative_positions(interleaved):
     freqs, _ = ec.ec_rotary_frequencies(64)
@@ -264,6 +278,38 @@ def test_join(dt, D, rot, page, tokens, rows):
     K, want_k = m.dev["K"].cpu(), turn(both[:, Hq:Hq + H])
     assert ((K[p, :, s].double() - want_k[into]).abs() <= turn_tolerance(both[:, Hq:Hq + H], want_k, factor)[into]).all()
     m.K[p, :, s] = K[p, :, s]                          # the rest of the pool has to be as it was, bit for bit
+    m.V[p, :, s] = both[into][:, Hq + H:]
+    m.weight[p, :, s] = w[into].double()
+    m.pos[p, :, s] = pos[into][:, None].expand(-1, H)
+    m.assert_same_rows(0.0, "join")
+
+
+@pytest.mark.parametrize("H,Hq,tokens", [(1, 0, 30000), (1, 2, 20000), (5, 200, 37), (3, 150, 300), (40, 7, 2)])
+def test_join_many_tokens_of_few_heads_and_the_other_way_round(H, Hq, tokens):
+    """Tokens that share a CTA, and heads of a token that several CTAs share: every row, weight and position is written once."""
+    D, page = 64, 16
+    m = PagedMirror([tokens + 3], H, D, page, tokens + 3, BF, "heads")
+    cache = m.cache(ec)
+    freqs, _ = ec.ec_rotary_frequencies(64)
+    both = rand((tokens, Hq + 2 * H, D), BF, 1)
+    g = torch.Generator().manual_seed(2)
+    row = torch.randperm(tokens + 3, generator=g)[:tokens]
+    slots = (m.table[0].long()[row // page] * page + row % page).to(torch.int32)
+    slots[::5] = -1
+    pos = torch.randint(0, 5000, (tokens,), generator=g, dtype=torch.int32)
+    w = torch.rand(tokens, H, generator=g)
+    dev, into = both.cuda(), slots >= 0
+    q_out = torch.full((tokens, Hq, D), 7.0, dtype=BF, device="cuda") if Hq else None
+    ec.ec_paged_join(dev[:, :Hq] if Hq else None, q_out, dev[:, Hq:Hq + H], dev[:, Hq + H:], w.cuda(), slots.cuda(), pos.cuda(), cache,
+                     freqs.cuda(), 64, False)
+    want = rotary(both[:, :Hq + H], pos, freqs, 1.0, 64, False)
+    allowed = turn_tolerance(both[:, :Hq + H], want, 1.0)
+    if Hq:
+        assert ((q_out.cpu().double() - want[:, :Hq]).abs() <= allowed[:, :Hq])[into].all() and (q_out.cpu()[~into] == 7.0).all()
+    p, s = slots.long()[into] // page, slots.long()[into] % page
+    K = m.dev["K"].cpu()
+    assert ((K[p, :, s].double() - want[into][:, Hq:]).abs() <= allowed[into][:, Hq:]).all()
+    m.K[p, :, s] = K[p, :, s]
     m.V[p, :, s] = both[into][:, Hq + H:]
     m.weight[p, :, s] = w[into].double()
     m.pos[p, :, s] = pos[into][:, None].expand(-1, H)
