@@ -397,276 +397,275 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
     bool alive = true;
 
     // A thread of the softmax holds 64 scores and as many addresses as the epilogue needs: 4 warps x 88 + 8 x 208 registers are the
-    // 12 x 168 of the launch.
-    auto fewer_registers = [] { asm volatile("setmaxnreg.dec.sync.aligned.u32 88;"); };
-    if (warp == 0) {
-        // ------------------------------------------------------------ plan and copies
-        fewer_registers();
-        Walk<PairUnits> w;
-        bool more = w.begin(a, kLeastRows);
-        uint32_t tg = 0, nk = 0, nv = 0, nq = 0;           // tiles; copies of K, V and queries started
-        for (uint32_t k = 0; alive; ++k) {
-            const uint32_t sl = k % kItems;
-            Item it = {};
-            it.n = -1;
-            long long cost = 0;
-            while (more) {                                // the next unit that this CTA has something of
-                const int step = 2 * a.tile_tokens;
-                it.ntok = min(step, w.p.count - w.i * step);
-                it.limit = w.p.len - w.p.count + w.i * step;
-                it.rows = max(0, min(w.p.len, it.limit + it.ntok));
-                cost = PairUnits::before(a, w.p, w.units, w.i + 1) - PairUnits::before(a, w.p, w.units, w.i);
-                const Cut cut = cut_unit(w.s, w.at, cost, kUnitRows, kTileRows, (it.rows + kTileRows - 1) / kTileRows);
-                if (cut.mine) {
-                    it.n = w.n;
-                    it.h = w.h;
-                    it.token = w.p.start + w.i * step;
-                    it.kt0 = cut.t0;
-                    it.kt1 = cut.t1;
-                    it.first = cut.first;
-                    it.parts = cut.parts;
-                    it.slot = 2 * (int)blockIdx.x + (cut.first == (int)blockIdx.x);
-                    break;
-                }
-                more = w.next(a, cost);
-            }
-            if (!mbar_wait(item_empty(sl), ((k / kItems) & 1u) ^ 1u, abort_flag, status, kWaitLimitNs, kPollBackoffNs)) { alive = false; break; }
-            if (lane == 0) items[sl] = it;
-            __syncwarp();
-            if (lane == 0) mbar_arrive(item_full(sl));
-            if (!more) break;
-            auto copy_queries = [&] {
-                if (lane == 0) {
-                    const int tiles = it.ntok > a.tile_tokens ? 2 : 1;
-                    mbar_expect_tx(q_full, (uint32_t)(tiles * a.tile_tokens * a.G * D * 2));
-                    publish(q_asked, (int)nq + 1);
-                    for (int x = 0; x < tiles; ++x)
-#pragma unroll
-                        for (int half = 0; half < D / 64; ++half)
-                            tma_load_3d(base + L::kQ + x * kTile + half * kBoxBytes, &map_q, half * 64, it.h * a.G,
-                                        it.token + x * a.tile_tokens, q_full);
-                }
-                ++nq;
-            };
-            // the queries first when their place is free, else behind the first tile's rows
-            bool asked = it.kt0 >= it.kt1 || __all_sync(0xFFFFFFFFu, mbar_try(q_empty, (nq & 1u) ^ 1u));
-            if (asked && it.kt0 < it.kt1) copy_queries();
-            // page numbers of a lane's first box are read a tile ahead; pages of fewer than 4 rows have more boxes than lanes
-            const int boxes = kTileRows / a.box_rows;
-            int row = it.kt0 * kTileRows + lane * a.box_rows, next = it.kt0 < it.kt1 ? box_page(a, it.n, row, it.rows) : -1;
-            for (int t = it.kt0; t < it.kt1 && alive; ++t, ++tg, row += kTileRows) {
-                int page = next;
-                const uint32_t ks = tg % kKs, vs = tg % kVs;
-                if (!mbar_wait(k_empty(ks), ((tg / kKs) & 1u) ^ 1u, abort_flag, status, kWaitLimitNs, kPollBackoffNs)) { alive = false; break; }
-                uint32_t gone[4] = {0u, 0u, 0u, 0u};      // absent rows
-                auto lost = [&](int at) {
-                    for (int r = at; r < at + a.box_rows; ++r) {
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            if (r >> 5 == j) gone[j] |= 1u << (r & 31);
-                    }
-                };
-                bool any = lane < boxes && bad_page(a, row, it.rows, page);
-                if (any) lost(lane * a.box_rows);
-                if (lane == 0) {
-                    mbar_expect_tx(k_full(ks), kTile);
-                }
-                __syncwarp();
-                const uint32_t k_to = base + L::kK + ks * kTile, v_to = base + L::kV + vs * kTile;
-                if (lane < boxes) copy_box<D>(a, &map_k, page, it.h, row, lane * a.box_rows, k_to, k_full(ks));
-#pragma unroll 1
-                for (int box = lane + 32; box < boxes; box += 32) {
-                    const int r = t * kTileRows + box * a.box_rows;
-                    int p = box_page(a, it.n, r, it.rows);
-                    if (bad_page(a, r, it.rows, p)) {
-                        any = true;
-                        lost(box * a.box_rows);
-                    }
-                    copy_box<D>(a, &map_k, p, it.h, r, box * a.box_rows, k_to, k_full(ks));
-                }
-                any = __any_sync(0xFFFFFFFFu, any);
-                if (any) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) gone[j] = __reduce_or_sync(0xFFFFFFFFu, gone[j]);
-                }
-                if (lane == 0) {
-                    infos[2 * (tg % kInfos)] = make_uint2(gone[0], gone[1]);
-                    infos[2 * (tg % kInfos) + 1] = make_uint2(gone[2], gone[3]);
-                    publish(k_asked, (int)tg + 1);        // S is asked for behind this
-                }
-                ++nk;
-                if (!asked) {
-                    if (!mbar_wait(q_empty, (nq & 1u) ^ 1u, abort_flag, status, kWaitLimitNs, kPollBackoffNs)) { alive = false; break; }
-                    copy_queries();
-                    asked = true;
-                }
-                next = t + 1 < it.kt1 ? box_page(a, it.n, row + kTileRows, it.rows) : -1;
-                if (!mbar_wait(v_empty(vs), ((tg / kVs) & 1u) ^ 1u, abort_flag, status, kWaitLimitNs, kPollBackoffNs)) { alive = false; break; }
-                if (lane == 0) mbar_expect_tx(v_full(vs), kTile);
-                __syncwarp();
-                if (lane < boxes) copy_box<D>(a, &map_v, page, it.h, row, lane * a.box_rows, v_to, v_full(vs));
-#pragma unroll 1
-                for (int box = lane + 32; box < boxes; box += 32) {
-                    const int r = t * kTileRows + box * a.box_rows;
-                    int p = box_page(a, it.n, r, it.rows);
-                    bad_page(a, r, it.rows, p);
-                    copy_box<D>(a, &map_v, p, it.h, r, box * a.box_rows, v_to, v_full(vs));
-                }
-                ++nv;
-            }
-            if (!alive) break;
-            more = w.next(a, cost);
-        }
-        if (*abort_flag) {
-            // let copies that are still in flight land before the CTA gives its memory back
-            if (nq > 0) mbar_wait(q_full, (nq - 1u) & 1u, abort_flag, status, 200000ull);
-            for (uint32_t t = nk > (uint32_t)kKs ? nk - kKs : 0; t < nk; ++t)
-                mbar_wait(k_full(t % kKs), (t / kKs) & 1u, abort_flag, status, 200000ull);
-            for (uint32_t t = nv > (uint32_t)kVs ? nv - kVs : 0; t < nv; ++t)
-                mbar_wait(v_full(t % kVs), (t / kVs) & 1u, abort_flag, status, 200000ull);
-        }
-    } else if (warp == 1 || warp == 3) {
-        // ------------------------------------------------------------ products of a team
-        fewer_registers();
-        if (lane == 0) {
-            const uint32_t x = (uint32_t)warp >> 1;
-            uint32_t tg0 = 0, nq = 0, np = 0, ni = 0;     // the CTA's tiles and query loads, the team's tiles and items so far
-            auto wait = [&](uint32_t b, uint32_t phase) {
-                if (!mbar_wait(b, phase & 1u, abort_flag, status, kWaitLimitNs, kPollBackoffNs)) alive = false;
-                return alive;
-            };
-            auto wait_count = [&](const int *count, uint32_t least) {
-                if (!reached(count, (int)least, abort_flag, status)) alive = false;
-                return alive;
-            };
-            // released by both teams: who works alone on it does so twice
-            auto release = [&](uint32_t b, bool alone) {
-                umma_commit(b);
-                if (alone) umma_commit(b);
-            };
-            auto issue_s = [&](uint32_t qt, uint32_t ks) {
-                const uint64_t da = umma_desc(base + L::kQ + qt * kTile), db = umma_desc(base + L::kK + ks * kTile);
-#pragma unroll
-                for (int kk = 0; kk < D / 16; ++kk) {
-                    const uint32_t off = ((uint32_t)(kk / 4) * kBoxBytes + (uint32_t)(kk % 4) * 32u) >> 4;
-                    umma_bf16(tmem_s(x), da + off, db + off, kIdescS, kk > 0 ? 1u : 0u);
-                }
-                umma_commit(s_full(x));
-            };
+    // 12 x 168 of the launch. The four warps of a group change their share by the same instruction, in front of their roles.
+    if (warp < 4) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+        if (warp == 0) {
+            // ------------------------------------------------------------ plan and copies
+            Walk<PairUnits> w;
+            bool more = w.begin(a, kLeastRows);
+            uint32_t tg = 0, nk = 0, nv = 0, nq = 0;           // tiles; copies of K, V and queries started
             for (uint32_t k = 0; alive; ++k) {
                 const uint32_t sl = k % kItems;
-                if (!wait(item_full(sl), k / kItems)) break;
-                const Item it = items[sl];
-                mbar_arrive(item_empty(sl));
-                if (it.n < 0) break;
-                const int tiles = it.kt1 - it.kt0;
-                if (tiles <= 0) continue;
-                const bool pair = is_pair(it);
-                const uint32_t qt = pair ? x : 0u;
-                const Part mine = part_of(it, x), others = part_of(it, x ^ 1u);
-                auto alone = [&](int t) { return !pair || t >= others.end; };
-                const bool all_mine = others.first >= others.end;          // the other team has nothing in this item
-                const uint32_t tg = tg0;
-                tg0 += (uint32_t)tiles;
-                ++nq;
-                if (mine.first >= mine.end) continue;
-                if (!wait_count(q_asked, nq) || !wait(q_full, nq - 1u)) break;
-                {
-                    const uint32_t ks = (tg + mine.first) % kKs;
-                    if (!wait_count(k_asked, tg + mine.first + 1) || !wait(k_full(ks), (tg + mine.first) / kKs)) break;
-                    tc_fence_after();
-                    issue_s(qt, ks);
-                    release(k_empty(ks), alone(mine.first));
-                    if (mine.first + mine.step >= mine.end) release(q_empty, all_mine);
-                }
-                if (!wait(o_free(x), ni + 1u)) break;
-                ++ni;
-#pragma unroll 1
-                for (int t = mine.first; t < mine.end && alive; t += mine.step) {
-                    const int then = t + mine.step;
-                    const uint32_t vs = (tg + t) % kVs, ks = (tg + then) % kKs;
-                    const int steps = min(kTileRows / 16, (mine.rows - (it.kt0 + t) * kTileRows + 15) / 16);
-                    if (!wait_count(v_checked, tg + t + 1)) break;
-                    const uint64_t dv = umma_desc_mn(base + L::kV + vs * kTile, kBoxBytes, 1024u);
-#pragma unroll
-                    for (uint32_t h = 0; h < 2; ++h) {
-                        // O += P V of 64 rows, 16 an instruction
-                        if (!wait(p_full(x, h), np)) break;
-                        tc_fence_after();
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int kk = 4 * (int)h + i;
-                            if (kk < steps) umma_ts(tmem_o(x), tmem_s(x) + h * kHalf + 8u * i, dv + kk * (2048u >> 4), kIdescO, t == mine.first && kk == 0 ? 0u : 1u);
-                        }
-                        if (h == 0) umma_commit(pv_half(x));
+                Item it = {};
+                it.n = -1;
+                long long cost = 0;
+                while (more) {                                // the next unit that this CTA has something of
+                    const int step = 2 * a.tile_tokens;
+                    it.ntok = min(step, w.p.count - w.i * step);
+                    it.limit = w.p.len - w.p.count + w.i * step;
+                    it.rows = max(0, min(w.p.len, it.limit + it.ntok));
+                    cost = PairUnits::before(a, w.p, w.units, w.i + 1) - PairUnits::before(a, w.p, w.units, w.i);
+                    const Cut cut = cut_unit(w.s, w.at, cost, kUnitRows, kTileRows, (it.rows + kTileRows - 1) / kTileRows);
+                    if (cut.mine) {
+                        it.n = w.n;
+                        it.h = w.h;
+                        it.token = w.p.start + w.i * step;
+                        it.kt0 = cut.t0;
+                        it.kt1 = cut.t1;
+                        it.first = cut.first;
+                        it.parts = cut.parts;
+                        it.slot = 2 * (int)blockIdx.x + (cut.first == (int)blockIdx.x);
+                        break;
                     }
-                    if (!alive) break;
-                    ++np;
-                    if (then >= mine.end) umma_commit(pv(x));
-                    if (then < mine.end) {                // S of the next tile, over this P
-                        if (!wait_count(k_asked, tg + then + 1) || !wait(k_full(ks), (tg + then) / kKs)) break;
+                    more = w.next(a, cost);
+                }
+                if (!mbar_wait(item_empty(sl), ((k / kItems) & 1u) ^ 1u, abort_flag, status, kWaitLimitNs, kPollBackoffNs)) { alive = false; break; }
+                if (lane == 0) items[sl] = it;
+                __syncwarp();
+                if (lane == 0) mbar_arrive(item_full(sl));
+                if (!more) break;
+                auto copy_queries = [&] {
+                    if (lane == 0) {
+                        const int tiles = it.ntok > a.tile_tokens ? 2 : 1;
+                        mbar_expect_tx(q_full, (uint32_t)(tiles * a.tile_tokens * a.G * D * 2));
+                        publish(q_asked, (int)nq + 1);
+                        for (int x = 0; x < tiles; ++x)
+    #pragma unroll
+                            for (int half = 0; half < D / 64; ++half)
+                                tma_load_3d(base + L::kQ + x * kTile + half * kBoxBytes, &map_q, half * 64, it.h * a.G,
+                                            it.token + x * a.tile_tokens, q_full);
+                    }
+                    ++nq;
+                };
+                // the queries first when their place is free, else behind the first tile's rows
+                bool asked = it.kt0 >= it.kt1 || __all_sync(0xFFFFFFFFu, mbar_try(q_empty, (nq & 1u) ^ 1u));
+                if (asked && it.kt0 < it.kt1) copy_queries();
+                // page numbers of a lane's first box are read a tile ahead; pages of fewer than 4 rows have more boxes than lanes
+                const int boxes = kTileRows / a.box_rows;
+                int row = it.kt0 * kTileRows + lane * a.box_rows, next = it.kt0 < it.kt1 ? box_page(a, it.n, row, it.rows) : -1;
+                for (int t = it.kt0; t < it.kt1 && alive; ++t, ++tg, row += kTileRows) {
+                    int page = next;
+                    const uint32_t ks = tg % kKs, vs = tg % kVs;
+                    if (!mbar_wait(k_empty(ks), ((tg / kKs) & 1u) ^ 1u, abort_flag, status, kWaitLimitNs, kPollBackoffNs)) { alive = false; break; }
+                    uint32_t gone[4] = {0u, 0u, 0u, 0u};      // absent rows
+                    auto lost = [&](int at) {
+                        for (int r = at; r < at + a.box_rows; ++r) {
+    #pragma unroll
+                            for (int j = 0; j < 4; ++j)
+                                if (r >> 5 == j) gone[j] |= 1u << (r & 31);
+                        }
+                    };
+                    bool any = lane < boxes && bad_page(a, row, it.rows, page);
+                    if (any) lost(lane * a.box_rows);
+                    if (lane == 0) {
+                        mbar_expect_tx(k_full(ks), kTile);
+                    }
+                    __syncwarp();
+                    const uint32_t k_to = base + L::kK + ks * kTile, v_to = base + L::kV + vs * kTile;
+                    if (lane < boxes) copy_box<D>(a, &map_k, page, it.h, row, lane * a.box_rows, k_to, k_full(ks));
+    #pragma unroll 1
+                    for (int box = lane + 32; box < boxes; box += 32) {
+                        const int r = t * kTileRows + box * a.box_rows;
+                        int p = box_page(a, it.n, r, it.rows);
+                        if (bad_page(a, r, it.rows, p)) {
+                            any = true;
+                            lost(box * a.box_rows);
+                        }
+                        copy_box<D>(a, &map_k, p, it.h, r, box * a.box_rows, k_to, k_full(ks));
+                    }
+                    any = __any_sync(0xFFFFFFFFu, any);
+                    if (any) {
+    #pragma unroll
+                        for (int j = 0; j < 4; ++j) gone[j] = __reduce_or_sync(0xFFFFFFFFu, gone[j]);
+                    }
+                    if (lane == 0) {
+                        infos[2 * (tg % kInfos)] = make_uint2(gone[0], gone[1]);
+                        infos[2 * (tg % kInfos) + 1] = make_uint2(gone[2], gone[3]);
+                        publish(k_asked, (int)tg + 1);        // S is asked for behind this
+                    }
+                    ++nk;
+                    if (!asked) {
+                        if (!mbar_wait(q_empty, (nq & 1u) ^ 1u, abort_flag, status, kWaitLimitNs, kPollBackoffNs)) { alive = false; break; }
+                        copy_queries();
+                        asked = true;
+                    }
+                    next = t + 1 < it.kt1 ? box_page(a, it.n, row + kTileRows, it.rows) : -1;
+                    if (!mbar_wait(v_empty(vs), ((tg / kVs) & 1u) ^ 1u, abort_flag, status, kWaitLimitNs, kPollBackoffNs)) { alive = false; break; }
+                    if (lane == 0) mbar_expect_tx(v_full(vs), kTile);
+                    __syncwarp();
+                    if (lane < boxes) copy_box<D>(a, &map_v, page, it.h, row, lane * a.box_rows, v_to, v_full(vs));
+    #pragma unroll 1
+                    for (int box = lane + 32; box < boxes; box += 32) {
+                        const int r = t * kTileRows + box * a.box_rows;
+                        int p = box_page(a, it.n, r, it.rows);
+                        bad_page(a, r, it.rows, p);
+                        copy_box<D>(a, &map_v, p, it.h, r, box * a.box_rows, v_to, v_full(vs));
+                    }
+                    ++nv;
+                }
+                if (!alive) break;
+                more = w.next(a, cost);
+            }
+            if (*abort_flag) {
+                // let copies that are still in flight land before the CTA gives its memory back
+                if (nq > 0) mbar_wait(q_full, (nq - 1u) & 1u, abort_flag, status, 200000ull);
+                for (uint32_t t = nk > (uint32_t)kKs ? nk - kKs : 0; t < nk; ++t)
+                    mbar_wait(k_full(t % kKs), (t / kKs) & 1u, abort_flag, status, 200000ull);
+                for (uint32_t t = nv > (uint32_t)kVs ? nv - kVs : 0; t < nv; ++t)
+                    mbar_wait(v_full(t % kVs), (t / kVs) & 1u, abort_flag, status, 200000ull);
+            }
+        } else if (warp == 1 || warp == 3) {
+            // ------------------------------------------------------------ products of a team
+            if (lane == 0) {
+                const uint32_t x = (uint32_t)warp >> 1;
+                uint32_t tg0 = 0, nq = 0, np = 0, ni = 0;     // the CTA's tiles and query loads, the team's tiles and items so far
+                auto wait = [&](uint32_t b, uint32_t phase) {
+                    if (!mbar_wait(b, phase & 1u, abort_flag, status, kWaitLimitNs, kPollBackoffNs)) alive = false;
+                    return alive;
+                };
+                auto wait_count = [&](const int *count, uint32_t least) {
+                    if (!reached(count, (int)least, abort_flag, status)) alive = false;
+                    return alive;
+                };
+                // released by both teams: who works alone on it does so twice
+                auto release = [&](uint32_t b, bool alone) {
+                    umma_commit(b);
+                    if (alone) umma_commit(b);
+                };
+                auto issue_s = [&](uint32_t qt, uint32_t ks) {
+                    const uint64_t da = umma_desc(base + L::kQ + qt * kTile), db = umma_desc(base + L::kK + ks * kTile);
+    #pragma unroll
+                    for (int kk = 0; kk < D / 16; ++kk) {
+                        const uint32_t off = ((uint32_t)(kk / 4) * kBoxBytes + (uint32_t)(kk % 4) * 32u) >> 4;
+                        umma_bf16(tmem_s(x), da + off, db + off, kIdescS, kk > 0 ? 1u : 0u);
+                    }
+                    umma_commit(s_full(x));
+                };
+                for (uint32_t k = 0; alive; ++k) {
+                    const uint32_t sl = k % kItems;
+                    if (!wait(item_full(sl), k / kItems)) break;
+                    const Item it = items[sl];
+                    mbar_arrive(item_empty(sl));
+                    if (it.n < 0) break;
+                    const int tiles = it.kt1 - it.kt0;
+                    if (tiles <= 0) continue;
+                    const bool pair = is_pair(it);
+                    const uint32_t qt = pair ? x : 0u;
+                    const Part mine = part_of(it, x), others = part_of(it, x ^ 1u);
+                    auto alone = [&](int t) { return !pair || t >= others.end; };
+                    const bool all_mine = others.first >= others.end;          // the other team has nothing in this item
+                    const uint32_t tg = tg0;
+                    tg0 += (uint32_t)tiles;
+                    ++nq;
+                    if (mine.first >= mine.end) continue;
+                    if (!wait_count(q_asked, nq) || !wait(q_full, nq - 1u)) break;
+                    {
+                        const uint32_t ks = (tg + mine.first) % kKs;
+                        if (!wait_count(k_asked, tg + mine.first + 1) || !wait(k_full(ks), (tg + mine.first) / kKs)) break;
                         tc_fence_after();
                         issue_s(qt, ks);
-                        release(k_empty(ks), alone(then));
-                        if (then + mine.step >= mine.end) release(q_empty, all_mine);
+                        release(k_empty(ks), alone(mine.first));
+                        if (mine.first + mine.step >= mine.end) release(q_empty, all_mine);
                     }
-                    release(v_empty(vs), alone(t));
+                    if (!wait(o_free(x), ni + 1u)) break;
+                    ++ni;
+    #pragma unroll 1
+                    for (int t = mine.first; t < mine.end && alive; t += mine.step) {
+                        const int then = t + mine.step;
+                        const uint32_t vs = (tg + t) % kVs, ks = (tg + then) % kKs;
+                        const int steps = min(kTileRows / 16, (mine.rows - (it.kt0 + t) * kTileRows + 15) / 16);
+                        if (!wait_count(v_checked, tg + t + 1)) break;
+                        const uint64_t dv = umma_desc_mn(base + L::kV + vs * kTile, kBoxBytes, 1024u);
+    #pragma unroll
+                        for (uint32_t h = 0; h < 2; ++h) {
+                            // O += P V of 64 rows, 16 an instruction
+                            if (!wait(p_full(x, h), np)) break;
+                            tc_fence_after();
+    #pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const int kk = 4 * (int)h + i;
+                                if (kk < steps) umma_ts(tmem_o(x), tmem_s(x) + h * kHalf + 8u * i, dv + kk * (2048u >> 4), kIdescO, t == mine.first && kk == 0 ? 0u : 1u);
+                            }
+                            if (h == 0) umma_commit(pv_half(x));
+                        }
+                        if (!alive) break;
+                        ++np;
+                        if (then >= mine.end) umma_commit(pv(x));
+                        if (then < mine.end) {                // S of the next tile, over this P
+                            if (!wait_count(k_asked, tg + then + 1) || !wait(k_full(ks), (tg + then) / kKs)) break;
+                            tc_fence_after();
+                            issue_s(qt, ks);
+                            release(k_empty(ks), alone(then));
+                            if (then + mine.step >= mine.end) release(q_empty, all_mine);
+                        }
+                        release(v_empty(vs), alone(t));
+                    }
                 }
             }
-        }
-    } else if (warp == 2) {
-        // ------------------------------------------------------------ value check
-        fewer_registers();
-        // A product with P = 0 does not hide a value that is not finite, so tiles whose rows some token must not see are
-        // looked over: such values become zeros, and the item is marked, for the tokens that do see them. Rows behind the last one
-        // (memory that holds anything) become zeros too; absent ones are.
-        uint32_t tg = 0;
-        for (uint32_t k = 0; alive; ++k) {
-            const uint32_t sl = k % kItems;
-            if (!mbar_wait(item_full(sl), (k / kItems) & 1u, abort_flag, status, kWaitLimitNs, kPollBackoffNs)) { alive = false; break; }
-            const Item it = items[sl];
-            if (lane == 0) bad_any[sl] = 0;
-            __syncwarp();
-            if (it.n < 0) break;
-            for (int t = it.kt0; t < it.kt1; ++t, ++tg) {
-                const uint32_t s = tg % kVs;
-                if (!mbar_wait(v_full(s), (tg / kVs) & 1u, abort_flag, status, kWaitLimitNs, kPollBackoffNs)) { alive = false; break; }
-                const int row0 = t * kTileRows, rows = min(kTileRows, it.rows - row0);
-                const int check = max(0, it.limit + 1 - row0);                             // rows before are seen by every token
-                const int end = (rows + 15) & ~15;
-                if (check < end) {
-                    uint8_t *tile = smem + L::kV + s * kTile;
-                    constexpr int kChunks = D / 8;                                         // 16-byte pieces of a row
-                    for (int i = check * kChunks + lane; i < end * kChunks; i += 32) {
-                        const int r = i / kChunks, c = i % kChunks;
-                        uint4 *at = reinterpret_cast<uint4 *>(tile + (c >> 3) * kBoxBytes + r * 128 + (((c & 7) ^ (r & 7)) << 4));
-                        if (r >= rows) {
-                            *at = make_uint4(0u, 0u, 0u, 0u);
-                            continue;
-                        }
-                        uint4 v = *at;
-                        uint32_t w[4] = {v.x, v.y, v.z, v.w};
-                        bool found = false;
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const uint32_t e = w[j] & E::kExponent;
-                            const bool lo = (e & 0xFFFFu) == (E::kExponent & 0xFFFFu), hi = (e >> 16) == (E::kExponent >> 16);
-                            w[j] &= (lo ? 0u : 0xFFFFu) | (hi ? 0u : 0xFFFF0000u);
-                            found |= lo || hi;
-                        }
-                        if (found) {
-                            *at = make_uint4(w[0], w[1], w[2], w[3]);
-                            bad_any[sl] = 1;
-                        }
-                    }
-                    fence_to_async();
-                }
+        } else if (warp == 2) {
+            // ------------------------------------------------------------ value check
+            // A product with P = 0 does not hide a value that is not finite, so tiles whose rows some token must not see are
+            // looked over: such values become zeros, and the item is marked, for the tokens that do see them. Rows behind the last one
+            // (memory that holds anything) become zeros too; absent ones are.
+            uint32_t tg = 0;
+            for (uint32_t k = 0; alive; ++k) {
+                const uint32_t sl = k % kItems;
+                if (!mbar_wait(item_full(sl), (k / kItems) & 1u, abort_flag, status, kWaitLimitNs, kPollBackoffNs)) { alive = false; break; }
+                const Item it = items[sl];
+                if (lane == 0) bad_any[sl] = 0;
                 __syncwarp();
-                if (lane == 0) publish(v_checked, (int)tg + 1);
+                if (it.n < 0) break;
+                for (int t = it.kt0; t < it.kt1; ++t, ++tg) {
+                    const uint32_t s = tg % kVs;
+                    if (!mbar_wait(v_full(s), (tg / kVs) & 1u, abort_flag, status, kWaitLimitNs, kPollBackoffNs)) { alive = false; break; }
+                    const int row0 = t * kTileRows, rows = min(kTileRows, it.rows - row0);
+                    const int check = max(0, it.limit + 1 - row0);                             // rows before are seen by every token
+                    const int end = (rows + 15) & ~15;
+                    if (check < end) {
+                        uint8_t *tile = smem + L::kV + s * kTile;
+                        constexpr int kChunks = D / 8;                                         // 16-byte pieces of a row
+                        for (int i = check * kChunks + lane; i < end * kChunks; i += 32) {
+                            const int r = i / kChunks, c = i % kChunks;
+                            uint4 *at = reinterpret_cast<uint4 *>(tile + (c >> 3) * kBoxBytes + r * 128 + (((c & 7) ^ (r & 7)) << 4));
+                            if (r >= rows) {
+                                *at = make_uint4(0u, 0u, 0u, 0u);
+                                continue;
+                            }
+                            uint4 v = *at;
+                            uint32_t w[4] = {v.x, v.y, v.z, v.w};
+                            bool found = false;
+    #pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                const uint32_t e = w[j] & E::kExponent;
+                                const bool lo = (e & 0xFFFFu) == (E::kExponent & 0xFFFFu), hi = (e >> 16) == (E::kExponent >> 16);
+                                w[j] &= (lo ? 0u : 0xFFFFu) | (hi ? 0u : 0xFFFF0000u);
+                                found |= lo || hi;
+                            }
+                            if (found) {
+                                *at = make_uint4(w[0], w[1], w[2], w[3]);
+                                bad_any[sl] = 1;
+                            }
+                        }
+                        fence_to_async();
+                    }
+                    __syncwarp();
+                    if (lane == 0) publish(v_checked, (int)tg + 1);
+                }
+                if (lane == 0) mbar_arrive(item_empty(sl));
             }
-            if (lane == 0) mbar_arrive(item_empty(sl));
         }
-    } else if (warp >= 4) {
+    } else {
         // ------------------------------------------------------------ softmax: a thread owns a query row
         asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
         const uint32_t x = (uint32_t)(warp - 4) >> 2;
