@@ -348,8 +348,9 @@ chunk_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     tc_fence_after();
                     const int token0 = q * a.tile_tokens;
                     const int tokens = min(a.tile_tokens, it.count - token0), columns = tokens * a.G;
-                    // columns of tokens that see the row: from here on (rows behind the last one: none that matter)
-                    const int lo = (row - (it.len - it.count) - token0) * a.G;
+                    // columns of tokens that see the row: from here on (rows behind the last one: none). Cut before the product: the
+                    // distance to a row of long ago, times the group, passes 32 bits.
+                    const int lo = min(max(row - (it.len - it.count) - token0, 0), a.tile_tokens) * a.G;
                     const int lo_warp = __shfl_sync(0xFFFFFFFFu, lo, 0);
                     float2 accA = make_float2(0.f, 0.f), accB = accA;
                     auto chunk = [&](const uint32_t (&raw)[32], int ch, auto mask_tag) {
@@ -384,7 +385,7 @@ chunk_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     const bool masked = tokens < a.tile_tokens || odd_s[s] != 0 || __any_sync(0xFFFFFFFFu, lo > 0);
                     if (masked) {
                         // chunks that no row of the warp takes part in are left out
-                        const int ch0 = max(lo_warp, 0) / 32, ch1 = (columns + 31) / 32;
+                        const int ch0 = lo_warp / 32, ch1 = (columns + 31) / 32;
                         for (int ch = ch0; ch < ch1; ++ch) {
                             uint32_t raw[32];
                             tmem_ld32_async(s_addr + 32 * ch, raw);
