@@ -730,7 +730,9 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                     }
                     const float from = E::kTop - m2;
                     const float2 from2 = make_float2(from, from);
-                    if (plain && __all_sync(0xFFFFFFFFu, fmaf(mx, c, -m2) <= E::kRaise && fabsf(m2) <= kLarge)) {
+                    // Rows that are nobody's (the next problem's queries, or what a kernel before left there) have no say: the two ways
+                    // differ in the last bits, and a result's bits are its own problem's.
+                    if (plain && __all_sync(0xFFFFFFFFu, !valid || (fmaf(mx, c, -m2) <= E::kRaise && fabsf(m2) <= kLarge))) {
                         // almost always: nothing hidden, no new maximum
 #pragma unroll
                         for (int k2 = 0; k2 < 32; ++k2) {
@@ -752,7 +754,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                         }
                         float factor = 1.f;
                         bool raise = false;
-                        if (!(fmaf(top, c, -m2) <= E::kRaise)) {          // also the first rows that are not all hidden, and NaN
+                        if (valid && !(fmaf(top, c, -m2) <= E::kRaise)) { // also the first rows that are not all hidden, and NaN
                             const float to = top * c;
                             if (m == -INFINITY) {
                                 l = 0.f;                  // what was added before (rows of -inf alone) is nothing
