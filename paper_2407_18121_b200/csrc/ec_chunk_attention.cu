@@ -866,7 +866,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
 #pragma unroll
                             for (int i = 0; i < 32; ++i) f[i] = none ? 0.f : fmaf(__uint_as_float(ro[i]), f1, f[i]);
                         }
-                        if (dirty && valid) {             // rows of this CTA that not every token of the item sees
+                        if (dirty && valid && !none) {    // rows of this CTA that not every token of the item sees
                             const uint32_t bits = spoilt<E::kExponent>(a, it.n, it.h, max(max(it.limit + 1, 0), it.kt0 * kTileRows),
                                                                        min(min(limit + 1, it.rows), it.kt1 * kTileRows), col);
 #pragma unroll
