@@ -363,10 +363,11 @@ chunk_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                             float2 e1 = __ffma2_rn(make_float2(__uint_as_float(raw[4 * i + 2]), __uint_as_float(raw[4 * i + 3])), c2, make_float2(nl.z, nl.w));
                             if (MASKED) {
                                 const int c = ch * 32 + 4 * i;
-                                e0.x = c >= lo && c < columns ? fast_exp2(e0.x) : 0.f;
-                                e0.y = c + 1 >= lo && c + 1 < columns ? fast_exp2(e0.y) : 0.f;
-                                e1.x = c + 2 >= lo && c + 2 < columns ? fast_exp2(e1.x) : 0.f;
-                                e1.y = c + 3 >= lo && c + 3 < columns ? fast_exp2(e1.y) : 0.f;
+                                // a token without a normaliser takes no part, whatever its query makes of the score
+                                e0.x = c >= lo && c < columns && nl.x != -INFINITY ? fast_exp2(e0.x) : 0.f;
+                                e0.y = c + 1 >= lo && c + 1 < columns && nl.y != -INFINITY ? fast_exp2(e0.y) : 0.f;
+                                e1.x = c + 2 >= lo && c + 2 < columns && nl.z != -INFINITY ? fast_exp2(e1.x) : 0.f;
+                                e1.y = c + 3 >= lo && c + 3 < columns && nl.w != -INFINITY ? fast_exp2(e1.y) : 0.f;
                             } else {
                                 e0 = exp2_pair(e0, 2 * i);
                                 e1 = exp2_pair(e1, 2 * i + 1);
