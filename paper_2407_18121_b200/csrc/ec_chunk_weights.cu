@@ -4,7 +4,8 @@
 // which is what `count` steps of one token each would have left.
 //
 // One contraction, K Q^T with a cached row to a TMEM lane and the queries as columns, so that a thread adds up its row's
-// probabilities and nothing has to be exchanged. The decay and the normaliser are one number a column, worked out in 64 bits:
+// probabilities and nothing has to be exchanged. The decay and the normaliser are one number a column, worked out in 64 bits and
+// rounded once to fp32:
 //   2^(c S + n),  n = -lse log2(e) + (count - 1 - t) log2(decay)
 // Four teams of four warps hold 512 rows of a head, the query tiles (and their numbers) stream past: a query tile is fetched once per
 // 512 rows, a row once. A team's S is the only one that it has; while its threads compute, the products fill the other teams'.
@@ -29,6 +30,7 @@ constexpr int kStages = 3;                       // query tiles
 constexpr int kTmemCols = 512;                   // S of every team
 constexpr int kUnitTiles = 2;                    // cost of a unit beside its query tiles
 constexpr int kLeastTiles = 6;                   // smallest share of a CTA
+constexpr double kLog2eWide = 1.4426950408889634074;
 
 struct WeightArgs : ChunkArgs {
     const float *lse;                            // [tokens, Hq]
@@ -206,7 +208,7 @@ chunk_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     nl[i] = -INFINITY;
                     if (in >= a.tile_tokens || t >= it.count) continue;
                     const float z = a.lse[(size_t)(it.start + t) * a.Hq + (size_t)it.h * a.G + (r - in * a.G)];
-                    if (z != -INFINITY) nl[i] = fmaf(-z, kLog2e, (float)(a.log2_decay * (double)(it.count - 1 - t)));
+                    if (z != -INFINITY) nl[i] = (float)fma(-(double)z, kLog2eWide, a.log2_decay * (double)(it.count - 1 - t));
                     odd |= !(fabsf(nl[i]) < INFINITY);
                 }
                 if (!mbar_wait(q_empty(s), ((nq / kStages) & 1u) ^ 1u, abort_flag, status, kWaitLimitNs, kPollBackoffNs)) { alive = false; return; }

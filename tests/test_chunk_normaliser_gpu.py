@@ -1,4 +1,6 @@
 """The weights of a chunk go by the normaliser that they are given, and by nothing else of a token that takes no part."""
+import math
+
 import pytest
 import torch
 
@@ -15,6 +17,21 @@ def gather(m, q, lse, starts, counts, decay=1.0, scale=0.125):
     ec.ec_paged_chunk_weights(q.cuda(), lse.cuda(), starts.cuda(), torch.tensor(counts, dtype=torch.int32).cuda(), cache, scale, decay, ws)
     assert ec.ec_device_status(state_of(cache)) == ec.EC_OK
     return m.dev["weight"].clone()
+
+
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_the_exponent_is_rounded_once(sign):
+    """One row a head and a score of zero: the gain is exp(-lse). The exponent, -lse log2(e), lies between 2^5 and 2^7 and is rounded by
+    half a step, 2^-18 at most; the exponential is off by 2^-22 and the weight's sum rounded once."""
+    H = 256
+    m = mirror([1], H, 64, 16)
+    m.dev["weight"].zero_()
+    lse = sign * torch.linspace(40.0, 85.0, H)[None]
+    weight = gather(m, torch.zeros(1, H, 64, dtype=BF), lse, torch.tensor([0], dtype=torch.int32), [1])
+    page, slot = m.where(0, 1)
+    got = weight.cpu()[page[0], :, slot[0]].double()
+    off = (got / torch.exp(-lse[0].double()) - 1).abs()
+    assert (off <= math.log(2.0) * 2.0 ** -18 + 2.0 ** -21).all(), float(off.max())
 
 
 @pytest.mark.parametrize("dt", [BF, HF])
