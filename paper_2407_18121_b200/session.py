@@ -11,6 +11,7 @@ copies (on the current stream), for callers whose data starts on the host.
 """
 from __future__ import annotations
 
+import math
 from typing import Optional
 
 import torch
@@ -261,9 +262,21 @@ class PagedPoolSession(PagedCacheSession):
                  device: Optional[torch.device] = None):
         self.N, self.H, self.D, self.Hq = N, H, D, Hq or H
         self.budget, self.recent, self.sinks = int(budget), int(recent), int(sinks)
-        self.scale, self.decay = float(scale), float(decay)
-        if not 0.0 < self.scale < 1e38 or not 0.0 < self.decay <= 1.0:
+        self.scale, self.decay, self.rot, self.factor = float(scale), float(decay), int(rot), float(factor)
+        # what one of a chunk's calls would refuse is refused here: by then the rows have joined
+        if min(N, H, self.budget, int(pool_rows), int(chunk), int(page_size)) < 1 or N > 65536:
+            raise ValueError(f"N (up to 65536), H, budget, pool_rows, chunk and page_size must be positive, got {N}, {H}, {budget}, {pool_rows}, "
+                             f"{chunk}, {page_size}")
+        if self.Hq < 1 or self.Hq % H or self.Hq // H > 128 or self.Hq + H > 65536:
+            raise ValueError(f"Hq must be a multiple of H = {H}, 128 times it at most, and the heads together 65536 at most, got {self.Hq}")
+        if min(self.recent, self.sinks) < 0 or self.recent + self.sinks > self.budget:
+            raise ValueError(f"recent and sinks must not be negative nor exceed the budget of {budget} together, got {recent} and {sinks}")
+        # the calls take fp32, where a small number may be none and a large one infinite
+        scale32, decay32, factor32 = (torch.tensor(x, dtype=torch.float64).float().item() for x in (self.scale, self.decay, self.factor))
+        if not 0.0 < scale32 < 1e38 or not 0.0 < decay32 <= 1.0 or self.decay > 1.0:
             raise ValueError(f"scale must be positive and decay in (0, 1], got {scale} and {decay}")
+        if not math.isfinite(factor32):
+            raise ValueError(f"factor must be finite, got {factor}")
         if not 0 <= rot <= D or rot % (8 if interleaved else 16) or (rot and (freqs is None or tuple(freqs.shape) != (rot // 2,))):
             raise ValueError(f"rot = {rot} must be a multiple of 16 (interleaved: of 8) up to {D}, with {rot // 2} frequencies")
         dev = device or torch.device("cuda", torch.cuda.current_device())
@@ -280,9 +293,13 @@ class PagedPoolSession(PagedCacheSession):
         self.cache = ec.ec_paged_init(self.Kp, self.Vp, self.weight, self.pos, self.table, self.lens, self.seen, self.state)
         self.pages = ec.ec_pages(torch.arange(n_pages, **i32).flip(0).contiguous(), torch.full((1,), n_pages, **i32), torch.zeros(N, **i32))
         self.granted, self.starts = torch.zeros(N, **i32), torch.zeros(N + 1, **i32)
-        self.rot, self.interleaved, self.factor = int(rot), bool(interleaved), float(factor)
-        self.freqs = None if freqs is None else freqs.to(device=dev, dtype=torch.float64)
-        self.ws_step = torch.empty(ec.ec_paged_step_workspace(self.cache, self.Hq, self.budget), dtype=torch.uint8, device=dev)
+        self.interleaved = bool(interleaved)
+        self.freqs = freqs.to(device=dev, dtype=torch.float64).contiguous() if self.rot else None
+        sizes = (ec.ec_paged_step_workspace(self.cache, self.Hq, self.budget), ec.ec_paged_chunk_workspace(self.cache, self.Hq),
+                 ec.ec_paged_append_workspace(self.cache, 0, self.budget))
+        if 0 in sizes:
+            raise ValueError("a step, a chunk or an eviction of these sizes would be refused")
+        self.ws_step = torch.empty(sizes[0], dtype=torch.uint8, device=dev)
 
     def turn(self, x: torch.Tensor, out: torch.Tensor) -> None:
         """Rotary positions of the problems' next tokens on x [N, heads, D], for decode()."""
