@@ -132,18 +132,20 @@ int ec_rotary_frequencies(double *freqs, float *factor, int rot, double base, in
     if (scaling == EC_ROTARY_BASE && rot < 4) return EC_ERR_SHAPE;
     if (scaling == EC_ROTARY_BASE) base *= pow(stretch, (double)rot / (rot - 2));
     double lo = 0.0, hi = 0.0;
+    bool all_slow = false;                       // even the fastest pair turns less than `slow` times
     if (scaling == EC_ROTARY_BY_PARTS) {
         // the (fractional) pair that turns x times over the trained length
         auto pair_of = [&](double x) { return rot * log(trained / (x * 2.0 * M_PI)) / (2.0 * log(base)); };
         lo = fmax(floor(pair_of(fast)), 0.0);
         hi = fmin(ceil(pair_of(slow)), rot - 1.0);
+        all_slow = pair_of(slow) < 0.0;
     }
     for (int i = 0; i < rot / 2; ++i) {
         const double f = pow(base, -2.0 * i / rot);
         if (scaling == EC_ROTARY_LINEAR) {
             freqs[i] = f / stretch;
         } else if (scaling == EC_ROTARY_BY_PARTS) {
-            const double ramp = fmin(fmax((i - lo) / fmax(hi - lo, 1e-3), 0.0), 1.0);
+            const double ramp = all_slow ? 1.0 : fmin(fmax((i - lo) / fmax(hi - lo, 1e-3), 0.0), 1.0);
             freqs[i] = f / stretch * ramp + f * (1.0 - ramp);
         } else {
             freqs[i] = f;
