@@ -654,7 +654,7 @@ int ec_paged_release(const ec_paged *c, const ec_pages *p, void *stream);
  *   slots_dev       int32 [tokens] page * page_size + place in the page of every token's row; -1: not granted, or behind the
  *                   last problem; nullable                                                                    (out)
  *   positions_dev   int32 [tokens] seen[n] + t, -1 likewise; nullable                                         (out)
- * Limits: N <= 65536. Deterministic. A count of the stack or of held pages out of range is cut, or the problem not granted, and the status word
+ * Limits: N <= 65536. counts must not overlap an output. Deterministic. A count of the stack or of held pages out of range is cut, or the problem not granted, and the status word
  * says EC_ERR_PAGE; so for a page number out of range, whose rows have no slot.
  */
 int ec_paged_reserve(const ec_paged *c, const ec_pages *p, const int32_t *counts_dev, int tokens, int advance, int limit,

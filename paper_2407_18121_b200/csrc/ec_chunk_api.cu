@@ -106,6 +106,8 @@ int ec_paged_reserve(const ec_paged *c, const ec_pages *p, const int32_t *counts
     if (tokens < 0 || limit < 0 || (!advance && (slots || positions))) return EC_ERR_ARG;
     if (c->N > 65536) return EC_ERR_SHAPE;
     if (!aligned(counts, 4) || !aligned(starts, 4) || !aligned(granted, 4) || !aligned(slots, 4) || !aligned(positions, 4)) return EC_ERR_ALIGN;
+    // several CTAs read the counts while one of them writes the answers
+    if (counts == granted || counts == starts || counts == slots || counts == positions) return EC_ERR_ARG;
     ec::ReserveArgs a;
     a.counts = counts;
     a.starts = starts;
