@@ -178,11 +178,12 @@ int ec_prefill_attention(const void *Q_dev, const void *K_dev, const void *V_dev
 int ec_device_status(void *ws_dev, void *stream);
 
 /*
- * Self-test of the failure path (no counterpart in the paper). The importance kernels wait
- * on hardware barriers with a time limit so that a lost signal can never hang the GPU. This
- * call enqueues a one-CTA kernel that waits, with that same routine, on a barrier nothing
- * completes; after `limit_us` microseconds (1 .. 1 000 000) the wait gives up, sets the status
- * word of `ws_dev` (any 256-byte-aligned device buffer of >= 256 bytes) and the kernel ends
+ * Self-test of the failure path (no counterpart in the paper). The tensor-core kernels wait
+ * on hardware barriers, and on counts in shared memory, with a time limit so that a lost signal
+ * can never hang the GPU. This call enqueues a one-CTA kernel that waits, with those same
+ * routines, on a barrier nothing completes and then for a count nothing raises; each wait gives up
+ * after `limit_us` microseconds (1 .. 1 000 000). When both did, the status
+ * word of `ws_dev` (any 256-byte-aligned device buffer of >= 256 bytes) is set; the kernel ends
  * normally. ec_device_status(ws_dev) then reports EC_ERR_TIMEOUT; the context stays usable.
  */
 int ec_selftest_wait_timeout(void *ws_dev, unsigned limit_us, void *stream);

@@ -210,31 +210,6 @@ struct Smem {
     static_assert(kTotal <= 232448, "shared memory of a block");
 };
 
-// A count in shared memory that one thread raises and others wait for, as the barriers are waited for.
-__device__ __forceinline__ void publish(int *count, int value)
-{
-    asm volatile("st.release.cta.shared::cta.s32 [%0], %1;" ::"r"(smem_u32(count)), "r"(value) : "memory");
-}
-__device__ __forceinline__ bool reached(const int *count, int least, volatile int *abort_flag, int *status)
-{
-    unsigned long long t0 = 0;
-    for (uint32_t spin = 0;; ++spin) {
-        int now;
-        asm volatile("ld.acquire.cta.shared::cta.s32 %0, [%1];" : "=r"(now) : "r"(smem_u32(count)) : "memory");
-        if (now - least >= 0) return true;
-        if (spin == 0) t0 = global_ns();
-        __nanosleep(kPollBackoffNs);
-        if ((spin & 63u) == 63u) {
-            if (*abort_flag) return false;
-            if (global_ns() - t0 > kWaitLimitNs) {
-                *abort_flag = 1;
-                atomicExch(status, 1);
-                return false;
-            }
-        }
-    }
-}
-
 // Natural log-sum-exp from the maximum (log2) and the sum.
 template <typename E>
 __device__ __forceinline__ float log_sum(float m2, float l)

@@ -466,19 +466,20 @@ __global__ void lse_import_kernel(const float *__restrict__ lse_nat, float *__re
     lse2[(size_t)unit * Tpad + m] = (m < T) ? lse_nat[(size_t)unit * T + m] * kLog2e : INFINITY;
 }
 
-// One CTA waits, with the same bounded wait the importance kernels use, on a barrier that
-// nothing ever completes: the wait has to expire, flag the status word and let the kernel end.
+// One thread waits, with the same bounded waits the kernels use, on a barrier that nothing ever completes and then for a count that
+// nothing raises: both have to expire and say so for the status word to be set, and the kernel ends.
 __global__ void wait_selftest_kernel(int *status, unsigned long long limit_ns)
 {
     __shared__ __align__(8) unsigned long long bar;
-    __shared__ int abort_flag;
-    if (threadIdx.x == 0) {
-        abort_flag = 0;
-        mbar_init(smem_u32(&bar), 1);
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    }
-    __syncthreads();
-    if (threadIdx.x == 0) mbar_wait(smem_u32(&bar), 0, &abort_flag, status, limit_ns);
+    __shared__ int abort_flag[2], expired[2], count;
+    if (threadIdx.x != 0) return;
+    for (int i = 0; i < 2; ++i) abort_flag[i] = expired[i] = 0;
+    count = 0;
+    mbar_init(smem_u32(&bar), 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    const bool completed = mbar_wait(smem_u32(&bar), 0, &abort_flag[0], &expired[0], limit_ns);
+    const bool raised = reached(&count, 1, &abort_flag[1], &expired[1], limit_ns);
+    if (!completed && !raised && atomicAdd(&expired[0], 0) == 1 && atomicAdd(&expired[1], 0) == 1) atomicExch(status, 1);
 }
 
 template <int D, int STAGES>
