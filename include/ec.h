@@ -641,10 +641,11 @@ int ec_paged_release(const ec_paged *c, const ec_pages *p, void *stream);
 /*
  * Pages are handed out for counts[n] new rows per problem, in order of the problems: the pages that problem n needs beyond held[n] come
  * off the top of the stack. A problem is granted its rows whole or not at all: not when it is an empty place, its rows would not fit the
- * table, its tokens end behind `tokens`, or the stack does not hold what this problem and those before it ask for (a problem that needs no page is
+ * table, its tokens end behind `tokens` (advance != 0), or the stack does not hold what this problem and those before it ask for (a problem that needs no page is
  * not held up by that). Negative counts count as 0.
  *   counts_dev      int32 [N]                                                                                 (in)
- *   tokens          rows of the packed tensors: length of slots and positions
+ *   tokens          rows of the packed tensors: length of slots and positions. With advance = 0 there are none, and `tokens` holds
+ *                   nobody back
  *   advance         != 0: the new rows join: lens[n] and seen[n] grow by what is granted, and slots and positions are
  *                   written. 0: only pages are handed out (for rows that ec_paged_append or ec_paged_decode_step will add), and
  *                   slots and positions have to be NULL

@@ -30,7 +30,6 @@ struct ChunkArgs {
 constexpr int kChunkMaxCtas = kPagedMaxCtas / 2;
 constexpr int kChunkCounters = 4;                // teams of a CTA that finish on their own
 
-size_t chunk_workspace_bytes(const ec_paged *c, int Hq);
 cudaError_t launch_chunk_attention(const ChunkArgs &a, int D, int dtype, const void *q, int64_t q_token, int64_t q_head, void *out,
                                    int64_t out_token, int64_t out_head, float *lse, void *ws, cudaStream_t stream);
 cudaError_t launch_chunk_weights(const ChunkArgs &a, int D, int dtype, const void *q, int64_t q_token, int64_t q_head, const float *lse,
@@ -209,7 +208,7 @@ __device__ __forceinline__ Cut cut_unit(const Share &s, long long at, long long 
     }
     cut.first = quotient(at + fixed + grain - 1, s.per);
     const int last = quotient(at + min(cost, fixed + (long long)grain * tiles) - 1, s.per);
-    auto tile_at = [&](int cta) {                // the first tile that begins behind the CTA's first place
+    auto tile_at = [&](int cta) {                // the tile that holds the CTA's first place, which is the CTA's own
         const long long x = cta * s.per - at - fixed;
         return x <= 0 ? 0 : min((int)((unsigned)x / (unsigned)grain), tiles);
     };
@@ -288,8 +287,6 @@ __device__ __forceinline__ void copy_box(const ChunkArgs &a, const CUtensorMap *
 
 // Plain shared-memory stores seen by the tensor cores' reads that a later arrival lets go ahead.
 __device__ __forceinline__ void fence_to_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-
-__device__ __forceinline__ void team_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 
 }  // namespace
 

@@ -104,7 +104,7 @@ reserve_kernel(const PagedView c, const PagePool p, const ReserveArgs a)
         const int n = n0 + tid, many = min(kThreads, c.N - n0);
         int cnt = 0, len = -1, held = -1, seen = 0;
         if (n < c.N) {
-            cnt = a.counts ? max(a.counts[n], 0) : 0;
+            cnt = max(a.counts[n], 0);
             len = c.lens[n];
             held = held_of(c, p, n);
             seen = c.seen[n];
@@ -127,7 +127,7 @@ reserve_kernel(const PagedView c, const PagePool p, const ReserveArgs a)
         s_base[tid] = upto - need;
         if (blockIdx.x == 0 && n < c.N) {
             if (a.starts) a.starts[n] = s_start[tid];
-            if (a.granted) a.granted[n] = ok ? cnt : 0;
+            a.granted[n] = ok ? cnt : 0;
             if (a.starts && n == c.N - 1) a.starts[c.N] = (int)min(end, (long long)a.tokens);
         }
         __syncthreads();
