@@ -679,7 +679,8 @@ int ec_rotary_frequencies(double *freqs_host, float *factor_host, int rot, doubl
  * Rotary positions: pair i of every head turns by the angle positions * freqs[i], scaled by `factor`:
  *   (a, b) -> factor * (a cos - b sin, a sin + b cos);   inverse != 0: the transposed map (a cos + b sin, b cos - a sin), which is
  * its gradient. Pairs are elements (2 i, 2 i + 1) (interleaved != 0) or (i, i + rot / 2) of the first `rot`; the others are
- * copied. fp32 arithmetic, one rounding of the result; angles are exact to 2^-24 of a half turn at any position (negative ones too).
+ * copied. fp32 arithmetic, one rounding of the result; at any position (negative ones too) an angle is off by
+ * 2^-24 of a half turn and by 2^-52 of itself, as if the last bit of its frequency were another.
  *   x_dev, out_dev  elements of `dtype` [N, T, heads, D] by strides in elements, multiples of 8; rows are contiguous and do not overlap
  *                   (head stride >= D); out may be x with the same strides, else they must not overlap
  *   positions_dev   int32 [N, T], rows pos_n apart (0: one row of positions for all)
