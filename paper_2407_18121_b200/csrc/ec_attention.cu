@@ -257,11 +257,11 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             }
             if (*abort_flag) {
                 // let copies that are still in flight land before the CTA gives its memory back
-                if (q_armed > 0) mbar_wait(bar_q_full, (q_armed - 1u) & 1u, abort_flag, status, 200000ull);
+                if (q_armed > 0) mbar_drain(bar_q_full, (q_armed - 1u) & 1u);
                 for (uint32_t t = k_armed > 2u ? k_armed - 2u : 0; t < k_armed; ++t)
-                    mbar_wait(bar_k_full(t & 1u), (t >> 1) & 1u, abort_flag, status, 200000ull);
+                    mbar_drain(bar_k_full(t & 1u), (t >> 1) & 1u);
                 for (uint32_t t = v_armed > 2u ? v_armed - 2u : 0; t < v_armed; ++t)
-                    mbar_wait(bar_v_full(t & 1u), (t >> 1) & 1u, abort_flag, status, 200000ull);
+                    mbar_drain(bar_v_full(t & 1u), (t >> 1) & 1u);
             }
         }
     } else if (warp == 1) {

@@ -494,11 +494,11 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
             }
             if (*abort_flag) {
                 // let copies that are still in flight land before the CTA gives its memory back
-                if (nq > 0) mbar_wait(q_full, (nq - 1u) & 1u, abort_flag, status, 200000ull);
+                if (nq > 0) mbar_drain(q_full, (nq - 1u) & 1u);
                 for (uint32_t t = nk > (uint32_t)kKs ? nk - kKs : 0; t < nk; ++t)
-                    mbar_wait(k_full(t % kKs), (t / kKs) & 1u, abort_flag, status, 200000ull);
+                    mbar_drain(k_full(t % kKs), (t / kKs) & 1u);
                 for (uint32_t t = nv > (uint32_t)kVs ? nv - kVs : 0; t < nv; ++t)
-                    mbar_wait(v_full(t % kVs), (t / kVs) & 1u, abort_flag, status, 200000ull);
+                    mbar_drain(v_full(t % kVs), (t / kVs) & 1u);
             }
         } else if (warp == 1 || warp == 3) {
             // ------------------------------------------------------------ products of a team

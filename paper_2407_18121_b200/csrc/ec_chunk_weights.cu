@@ -258,9 +258,9 @@ chunk_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         if (*abort_flag) {
             // let copies that are still in flight land before the CTA gives its memory back
             for (uint32_t x = 0; x < (uint32_t)kTeams; ++x)
-                if (asked >> x & 1u) mbar_wait(k_full(x), (nk >> x & 1u) ^ 1u, abort_flag, status, 200000ull);
+                if (asked >> x & 1u) mbar_drain(k_full(x), (nk >> x & 1u) ^ 1u);
             for (uint32_t t = nq > (uint32_t)kStages ? nq - kStages : 0; t < nq; ++t)
-                mbar_wait(q_full(t % kStages), (t / kStages) & 1u, abort_flag, status, 200000ull);
+                mbar_drain(q_full(t % kStages), (t / kStages) & 1u);
         }
     } else if (warp == 1) {
         // ------------------------------------------------------------ products

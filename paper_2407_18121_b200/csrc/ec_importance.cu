@@ -221,9 +221,9 @@ importance_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
             }
             if (*abort_flag) {
                 // let copies that are still in flight land before the CTA gives its memory back
-                if (stat_armed > 0) mbar_wait(bar_stat_full, (stat_armed - 1u) & 1u, abort_flag, status, 200000ull);
+                if (stat_armed > 0) mbar_drain(bar_stat_full, (stat_armed - 1u) & 1u);
                 for (uint32_t t = armed > (uint32_t)STAGES ? armed - STAGES : 0; t < armed; ++t)
-                    mbar_wait(bar_full(t % STAGES), (t / STAGES) & 1u, abort_flag, status, 200000ull);
+                    mbar_drain(bar_full(t % STAGES), (t / STAGES) & 1u);
             }
         }
     } else if (warp == 1) {

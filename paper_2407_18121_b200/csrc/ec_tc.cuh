@@ -75,6 +75,17 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
     }
 }
 
+// For copies that are still in flight when the CTA gives up: waits for them whatever the abort flag says, but no longer than a copy
+// can take.
+constexpr unsigned long long kDrainLimitNs = 200000ull;
+
+__device__ __forceinline__ void mbar_drain(uint32_t bar, uint32_t parity)
+{
+    const unsigned long long t0 = global_ns();
+    while (!mbar_try(bar, parity))
+        if (global_ns() - t0 > kDrainLimitNs) return;
+}
+
 // A count in shared memory that one thread raises and others wait for, as the barriers are waited for.
 __device__ __forceinline__ void publish(int *count, int value)
 {
