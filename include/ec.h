@@ -718,12 +718,13 @@ int ec_paged_join(const void *q_dev, int64_t q_t, int64_t q_h, void *q_out_dev, 
  *   counts_dev        int32 [N] its tokens; 0 or less: none. Rows of tokens that no problem has stay as they are (in)
  *   out               fp32 accumulation; probabilities are rounded once to the element type before they meet V (fp16: rows that lie
  *                     more than 2^-35 below the leading one count as nothing), the result once. Zero where a token sees nothing (an
- *                     empty place, absent pages, all scores -inf)
+ *                     empty place, absent pages, all scores -inf), whatever the values are
  *   lse_dev           fp32 [tokens, Hq]; -inf where a token sees nothing; nullable                         (out)
  * What a token does not see has no effect on it, values that are not finite included; an infinity in a value row that it does see comes
  * out as NaN or as an infinity. A problem whose tokens lie outside 0 .. tokens is left out, and the status word says EC_ERR_PAGE.
  * Limits: Hq / H <= 128, tokens * Hq < 2^31. Workspace: ec_paged_chunk_workspace bytes, which need not survive
- * between calls; calls that may run at once need one each. q must not overlap out. Deterministic.
+ * between calls; calls that may run at once need one each. q must not overlap out. Deterministic: packed
+ * rows of nobody and other problems' queries do not reach a token's bits (the lengths and counts of the batch, by which the work is cut, do).
  */
 size_t ec_paged_chunk_workspace(const ec_paged *c, int Hq);
 int ec_paged_chunk_attention(const void *q_dev, int64_t q_t, int64_t q_h, const int32_t *starts_dev, const int32_t *counts_dev,
@@ -734,8 +735,9 @@ int ec_paged_chunk_attention(const void *q_dev, int64_t q_t, int64_t q_h, const 
  * The weights that the chunk leaves behind, from its normaliser: with p[t, g, j] = exp(scale * <q, k_j> - lse[t, g]) for the rows that
  * token t sees, every row of a problem with counts[n] > 0 gets
  *   weight_j <- decay^count * weight_j + sum_t decay^(count - 1 - t) * sum_g p[t, g, j]
- * over the group's query heads: what counts[n] calls of ec_paged_attention for one token each would have left.
- *   lse_dev           fp32 [tokens, Hq] as ec_paged_chunk_attention gives it, same q, scale and cache; -inf: the row takes no part (in)
+ * over the group's query heads: what counts[n] calls of ec_paged_attention for one token each would have left, but for the rounding of
+ * the normaliser, which is given in fp32: a probability is off by a factor of exp(2^-22 |lse|) at most (2% at scores of 10^5).
+ *   lse_dev           fp32 [tokens, Hq] as ec_paged_chunk_attention gives it, same q, scale and cache; -inf: the row takes no part, whatever its query holds (in)
  * Other arguments, limits and workspace as there; 0 < decay <= 1, in double: its powers over a long chunk would show a rounding.
  * An lse that is not a number (NaN in q, or in a key that is seen) makes the weights of the rows that its token sees not a number.
  * Deterministic.

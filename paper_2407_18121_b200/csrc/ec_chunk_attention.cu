@@ -5,15 +5,16 @@
 // One pass over the rows, 128 at a time, for a tile of 128 query rows (tokens with the heads that share the key head):
 //   S = Q K^T      tcgen05.mma from tiles that TMA brought page by page, S in TMEM
 //   P = 2^(c S - m2 + top)   a thread owns a query row; P goes over S, as the type of the rows: one rounding of half a step, the
-//                  tensor cores take nothing wider. Sums and maxima are fp32 and taken before that rounding.
+//                  tensor cores take nothing wider. Sums and maxima are fp32 and taken before that rounding. Of the exponentials one
+//                  pair in four is a polynomial, 6e-6 off: a hundredth of that rounding, but the normaliser has it too
 //   O += P V       P from TMEM, V as it lies in shared memory
 // The running maximum is raised when a half of a tile exceeds it by 2^8 (bf16) or 2^4 (fp16), so O is rescaled rarely.
 //
 // What bounds it. Long prompts: each of two teams of four warps waits for its own S (issued behind its own P V: 512 columns of
 // TMEM hold S of both and O of both, with P over S) while the other computes. Per tile and team about 3200 clocks of softmax
 // (1800 of them exponentials, where the special functions' rate for both teams is 1540) and 2000 of waiting for S. 8192 tokens of
-// 32 heads on 8, D = 128: 670 us, 0.82 PFLOP/s at the 1.5 GHz that the power limit leaves (610 us in a short run); the products alone
-// take 336 us at the rate of a large library product. Few tokens on long caches (32 problems of up to 8 on up to 8192 rows): 37 us,
+// 32 heads on 8, D = 128: 680 to 694 us by the box, 0.80 PFLOP/s at the 1.5 GHz that the power limit leaves (610 us in a short run); the
+// products alone take 336 us at the rate of a large library product. Few tokens on long caches (32 problems of up to 8 on up to 8192 rows): 37 us,
 // of which 15.5 are the rows' bytes; starting (8 thousand clocks to the first S) and joining the parts are the rest. Many short problems: a unit of one to
 // three tiles keeps the softmax warps busy for 6 to 7 us whatever it holds; for one token a problem the single-token call is the
 // one to use.
@@ -22,11 +23,13 @@
 //  - Two query tiles of a head to a CTA, a team each: rows are fetched once for both. A unit of one query tile has both teams take its
 //    tiles in turn and is put together in the CTA: few tokens meet long caches with twice the warps.
 //  - The batch's work is cut evenly over one resident CTA per SM by a closed form of its cost, and what a cut leaves of a unit goes
-//    through the workspace in fp32, joined in the order of the rows by whoever arrives last: the same bits in every run.
+//    through the workspace in fp32, joined in the order of the rows by whoever arrives last. A warp's rows choose together between two
+//    ways of computing them, which differ in the last bits; rows that are nobody's have no say. So the bits are the same in every run.
 //  - A lazy maximum per half of a tile lets P V of the first half run under the exponentials of the second.
 //  - Values of masked rows: a warp looks over the tiles that not every token sees and turns what is not finite into zeros (a
 //    product with P = 0 would not hide it); who does see such a row reads it again.
-// Tried and slower, 8192 tokens (670 us) and a mixed batch (79 us): sixteen softmax warps with two threads a row (they spill
+// Registers: at D = 128 nothing is spilt, at D = 64 40 bytes a thread.
+// Tried and slower, 8192 tokens (670 us then) and a mixed batch (79 us): sixteen softmax warps with two threads a row (they spill
 // and meet once a tile; 732 against 609 in short runs, 98 against 82); a whole row of 128 columns a thread 747 and 94 (spills); the maximum looked at behind the exponentials 686 and 90; teams that
 // take turns on a scheduler 705 and 94; S in halves of 64 columns (a product of 64 columns takes as long as one of 128); an item per
 // team for short units (no change); the second team helping to put a single query tile together and to join its parts (32 problems of few
@@ -44,8 +47,11 @@ constexpr int kHalf = 64;                        // columns of S that a thread h
 constexpr int kItems = 4;                        // descriptions of work ahead
 constexpr int kInfos = 8;                        // absent rows of the tiles in flight (the rings hold 4 at most)
 constexpr int kTmemCols = 512;                   // S of both teams (2 x 128 columns), O of both teams (2 x up to 128)
-constexpr int kUnitRows = 384;                   // cost of a unit beside its rows
-constexpr int kLeastRows = 640;                  // smallest share of a CTA
+// Cost of a unit beside its rows, and the smallest share of a CTA. 128, 384 and 768 rows a unit: 32 problems of few tokens 57.0, 36.6 and
+// 38.3 us, 16 pieces 113.6, 81.8 and 93.8, the odd batch 35.2, 37.1 and 39.6, 8192 tokens 714, 693 and 710. 256, 640 and 1280 rows a share:
+// the odd batch 37.2, 37.1 and 44.9, the others within 1%.
+constexpr int kUnitRows = 384;
+constexpr int kLeastRows = 640;
 constexpr float kLowest = -3.402823466e38f;      // a running maximum that has seen nothing: below every score, and -inf less it is still -inf
 constexpr float kLarge = 16777216.f;
 

@@ -9,13 +9,14 @@
 //   2^(c S + n),  n = -lse log2(e) + (count - 1 - t) log2(decay)
 // Four teams of four warps hold 512 rows of a head, the query tiles (and their numbers) stream past: a query tile is fetched once per
 // 512 rows, a row once. A team's S is the only one that it has; while its threads compute, the products fill the other teams'.
+// One pair of exponentials in four is a polynomial, 6e-6 off, where a warp's rows are seen by all tokens of a query tile.
 // Units are cut over the CTAs along the queries; the parts are added in the order of the tokens by whoever arrives last.
 // Bound: the special functions, at 65% of their rate: about 4700 clocks for the four tiles of S that a query tile meets, 3070 of them
-// exponentials. 8192 tokens of 32 heads on 8, D = 128: 333 us, 0.83 PFLOP/s (168 us at the rate of a large library product; 293 in a
+// exponentials. 8192 tokens of 32 heads on 8, D = 128: 333 to 339 us by the box, 0.82 PFLOP/s (168 us at the rate of a large library product; 293 in a
 // short run, 301 with two warps more that did nothing; S handed back a chunk earlier 299 to 339, with its spills). 32 problems of up to 8 tokens on up to 8192 rows:
 // 34 us, of which 8 are the rows' bytes; the rest is starting and one query tile's latency per unit: a unit's rows are asked for when the
 // products of the one before are done, its queries before that (behind the rows: 35). Each team's rows let go behind its own last product
-// gained nothing there and cost the long prompt 4%.
+// gained nothing there and cost the long prompt 4%. A thread spills 40 bytes.
 #include "ec_chunk.cuh"
 
 namespace ec {
@@ -28,8 +29,11 @@ constexpr int kThreads = 64 + kTeams * 128;      // warps: copies, products, tea
 constexpr int kItems = 4;
 constexpr int kStages = 3;                       // query tiles
 constexpr int kTmemCols = 512;                   // S of every team
-constexpr int kUnitTiles = 2;                    // cost of a unit beside its query tiles
-constexpr int kLeastTiles = 6;                   // smallest share of a CTA
+// Cost of a unit beside its query tiles, and the smallest share of a CTA, in query tiles. 1, 2 and 4 a unit: 32 problems of few tokens 43.2,
+// 39.6 and 36.9 us, the odd batch 32.8, 30.7 and 30.7, 8192 tokens 333.1, 334.6 and 336.6. 3, 6 and 12 a share: few tokens 39.7, 39.6 and
+// 43.9, the odd batch 26.6, 30.7 and 43.6, 8192 tokens within 0.2%.
+constexpr int kUnitTiles = 2;
+constexpr int kLeastTiles = 6;
 constexpr double kLog2eWide = 1.4426950408889634074;
 
 struct WeightArgs : ChunkArgs {
